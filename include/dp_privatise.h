@@ -409,6 +409,93 @@ dp_status dp_add_noise_finalize_flat(const float *acc, float *out, float *theta,
                                      int n_seg, float sigma, float clip_total, uint64_t total_batch, uint64_t seed,
                                      uint64_t step, const uint64_t *step_dev, float lr, float momentum, dp_stream stream);
 
+/* ---- Activations kept in 8 bits from the forward to the privatising backward pass ------------------------------------
+ * A checkpoint of activations x [rows, features] (a row is a token) holds a byte for each value and one for each block of 32
+ * consecutive features of a row:
+ *   a     = largest finite |x| of the block,   s = 2^e the smallest power of two with a <= 448 s, -100 <= e <= 119 (e = -100 for zeros)
+ *   code  = the e4m3 number nearest to x / s, ties to even, at most +-448 (relative error at most 2^-4; 2^-10 s in absolute terms
+ *           where x / s is below 2^-6); infinities and NaN become NaN (0x7f)
+ *   value = code * s, a bf16 number exactly
+ *   codes  [device] [rows, pitch] bytes, pitch = dp_checkpoint_pitch(features): features rounded up to a multiple of 32; the codes
+ *          after the last feature are zeros.  16-byte aligned.
+ *   scales [device] [rows, pitch / 32] bytes, e + 127.  Any alignment.
+ * A row depends on nothing but its own values: rows may be written a few at a time.
+ * The calls that read a checkpoint take its scales as they are: bytes outside 27 .. 246 are not checked and give unspecified values. */
+int dp_checkpoint_pitch(int features);      /* 0 on a bad argument.  Pure host. */
+
+/* x [device] in_dtype, row r at x + r * row_stride elements (row_stride = 0: features; at least features), aligned to its element.
+ * rows = 0: nothing to do.  features at most 2^20.                                                                              */
+dp_status dp_checkpoint_write(const void *x, int in_dtype, size_t rows, int features, size_t row_stride, uint8_t *codes,
+                              uint8_t *scales, dp_stream stream);
+/* The values of a checkpoint: x [device] out_dtype, rows as above, overwritten (what lies between rows is left alone).           */
+dp_status dp_checkpoint_read(const uint8_t *codes, const uint8_t *scales, size_t rows, int features, void *x, int out_dtype,
+                             size_t row_stride, dp_stream stream);
+
+/* H1 and the layer's share of H2 of a dense layer whose input activations are a checkpoint: dp_per_example_grad with X_i the values of rows
+ * i * tokens .. of the checkpoint and, where `lengths` says so, fewer tokens:
+ *   dW_i[o,k] = sum_{t < len_i} dY_i[t,o] * X_i[t,k];   db_i[o] = sum_{t < len_i} dY_i[t,o]
+ * desc       a dense layer (else DP_ERR_UNSUPPORTED); in_dtype is dY's.  Rows of the checkpoint: n * tokens, features: cin.
+ * lengths    [device] [n] int32 tokens of each example (taken as 0 .. tokens), or NULL: all of them.  What lies in later tokens of
+ *            either operand is not used, whatever it is.  An example of no token has zero gradients and norm 0.
+ * Products of bf16 dY are those of bf16 matrix instructions with fp32 sums and nothing is rounded in between; fp32 dY is split into three
+ * bf16 numbers that add up to it (magnitudes below 2^127).  Norms alone of bf16 layers with few tokens go by way of Gram matrices,
+ *   |dW_i|^2 = sum_{t,u} (X_t . X_u)(dY_t . dY_u),
+ * which lose digits where the sum over the tokens cancels (a norm below 2^-20 of what its terms add up to is not resolved, and can come out
+ * negative: such an example is left out, dp_clip_factors); stored gradients give sums of squares always.
+ * Other arguments, errors: as dp_per_example_grad.  ws: dp_checkpoint_workspace_bytes(desc, DP_WS_PER_EXAMPLE_GRAD).               */
+size_t dp_checkpoint_workspace_bytes(const dp_layer_desc *desc /*[host]*/, int use /*dp_ws_use*/);
+dp_status dp_checkpoint_example_grad(const dp_layer_desc *desc /*[host]*/, const uint8_t *codes, const uint8_t *scales, const void *dy,
+                                     const int32_t *lengths, float *g_w, float *g_b, size_t g_stride, float *sqnorm, void *ws,
+                                     size_t ws_bytes, dp_stream stream);
+/* H4, recomputing form, from a checkpoint: acc_w += sum_i f_i dW_i, acc_b += sum_i f_i db_i (dp_clip_accumulate_recompute).  The factors meet
+ * fp32 values; an example of factor 0 is not read.  ws: dp_checkpoint_workspace_bytes(desc, DP_WS_RECOMPUTE), which may be 0.     */
+dp_status dp_checkpoint_clip_accumulate(const dp_layer_desc *desc /*[host]*/, const uint8_t *codes, const uint8_t *scales, const void *dy,
+                                        const int32_t *lengths, const float *sqnorm, float clip_c, float *acc_w, float *acc_b, void *ws,
+                                        size_t ws_bytes, dp_stream stream);
+
+/* ---- Attention probabilities under a learned relative position bias, and its per-example gradient ---------------------
+ * The parameter is a table [buckets, heads]; a place (query q, key k) gets the entry of the bucket of its distance
+ * d = (position of q) - (position of k).  Key k has position k, query q of example i position first_i + q.
+ *   nb = buckets / 2 (bidirectional) or buckets;  near = nb / 2
+ *   mag(d) = d for d < near, else min(nb - 1, near + floor((nb - near) log(d / near) / log(max_distance / near))), borders exact
+ *   bucket = mag(d) for d >= 0;  nb + mag(-d) (bidirectional) or 0 for keys after the query                               */
+#define DP_QUERIES_AT_END (-1)
+typedef struct dp_bias_desc {
+    int in_dtype;            /* dp_dtype of scores, probabilities and their gradients */
+    int n, heads, queries, keys;     /* tensors are [n, heads, queries] rows of `keys` values; each >= 1, below 2^30 */
+    int buckets;             /* entries of the table for each head: 2 .. 256 a side; even if bidirectional */
+    int max_distance;        /* near < max_distance <= 4096 */
+    int bidirectional;
+    int causal;              /* keys after the query do not count */
+    int query_offset;        /* first_i, 0 .. 2^30; DP_QUERIES_AT_END: key_length_i - query_length_i, an example's queries are its last
+                                keys (decoding from a cache) */
+    float scale;             /* of the scores; finite */
+    size_t row_stride;       /* elements from one row to the next, of every tensor of the call; 0: keys */
+} dp_bias_desc;
+
+/* Bucket of a distance; -1 on a bad descriptor.  Pure host. */
+int dp_bias_bucket(const dp_bias_desc *desc /*[host]*/, int distance);
+
+/* probs[i,h,q,k] = exp(z_k) / sum_k' exp(z_k'),  z_k = scale * scores[i,h,q,k] + table[bucket(first_i + q - k), h], over the keys that count:
+ * k < key_length_i, and not after the query if causal.  Zero for the others; a query at or beyond query_length_i, one with no key that
+ * counts, and one whose z are all -inf have zeros throughout.  What lies in places that do not count is not used, whatever it is.
+ * scores, probs [device] in_dtype, aligned to their element; probs may be scores.  table [device] fp32.
+ * query_lengths, key_lengths [device] [n] int32 (taken as 0 .. queries, 0 .. keys), or NULL: all.                                 */
+dp_status dp_bias_softmax(const dp_bias_desc *desc /*[host]*/, const void *scores, const float *table, const int32_t *query_lengths,
+                          const int32_t *key_lengths, void *probs, dp_stream stream);
+
+/* Its backward pass, with H1 and H2 of the table:
+ *   dz = probs * (dprobs - sum_k probs * dprobs)        (zero at places that do not count, dprobs not used there)
+ *   dscores = scale * dz;   g_table[i][b, h] = sum of dz over the places of bucket b of example i;   sqnorm[i] = |g_table[i]|^2
+ * dscores [device] in_dtype, may be probs or dprobs.  g_table [device] fp32, example i's [buckets, heads] at g_table + i * g_stride, overwritten
+ * (g_stride 0: packed; else a multiple of 4, at least buckets * heads), ready for dp_clip_accumulate.  The table's gradient is that of
+ * dz before it is rounded to in_dtype.  sqnorm [device] [n] or NULL.  ws: dp_bias_workspace_bytes(desc).
+ * Sums run in a fixed order: the same inputs give the same bits on every call.                                                  */
+size_t dp_bias_workspace_bytes(const dp_bias_desc *desc /*[host]*/);
+dp_status dp_bias_softmax_backward(const dp_bias_desc *desc /*[host]*/, const void *probs, const void *dprobs, const int32_t *query_lengths,
+                                   const int32_t *key_lengths, void *dscores, float *g_table, size_t g_stride, float *sqnorm, void *ws,
+                                   size_t ws_bytes, dp_stream stream);
+
 /* The raw 32-bit Philox word behind each element of the stream above (diagnostic; lets a
  * test compare the integer stream bit for bit).  raw [device] [p] uint32.                      */
 dp_status dp_philox_raw(uint32_t *raw, size_t p, uint64_t seed, uint64_t step, uint32_t tensor_id,

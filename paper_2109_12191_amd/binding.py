@@ -13,6 +13,7 @@ DP_WS_PER_EXAMPLE_GRAD, DP_WS_RECOMPUTE = 0, 1
 DP_VARIANT_SHARED = 2
 DP_VARIANT_MATERIALISE = 4
 DP_RECOMPUTE_BLOCKS = 8
+DP_QUERIES_AT_END = -1
 
 _STATUS_NAMES = {1: "DP_ERR_INVALID_ARG", 2: "DP_ERR_UNSUPPORTED", 3: "DP_ERR_WORKSPACE", 4: "DP_ERR_DEVICE"}
 _KINDS = {"dense": DP_DENSE, "conv": DP_CONV2D, "gn": DP_GN_AFFINE}
@@ -36,6 +37,13 @@ class LayerDesc(C.Structure):
                 ("has_bias", C.c_int), ("gn_groups", C.c_int), ("gn_eps", C.c_float)]
 
 
+class BiasDesc(C.Structure):
+    """Mirror of dp_bias_desc."""
+    _fields_ = [("in_dtype", C.c_int), ("n", C.c_int), ("heads", C.c_int), ("queries", C.c_int), ("keys", C.c_int),
+                ("buckets", C.c_int), ("max_distance", C.c_int), ("bidirectional", C.c_int), ("causal", C.c_int),
+                ("query_offset", C.c_int), ("scale", C.c_float), ("row_stride", C.c_size_t)]
+
+
 def lib_path() -> str:
     return _LIB_PATH
 
@@ -50,7 +58,7 @@ def load_library():
                            "(or __graft_entry__.build()); there is no CPU fallback")
     lib = C.CDLL(_LIB_PATH)
     vp, sz, u64, u32, fl, it = C.c_void_p, C.c_size_t, C.c_uint64, C.c_uint32, C.c_float, C.c_int
-    dpp = C.POINTER(LayerDesc)
+    dpp, dbp = C.POINTER(LayerDesc), C.POINTER(BiasDesc)
     sigs = {
         "dp_group_clip_bounds": (it, [fl, it, vp, vp]),
         "dp_weight_count": (sz, [dpp]),
@@ -87,6 +95,16 @@ def load_library():
         "dp_add_noise_finalize_update": (it, [vp, vp, vp, vp, sz, fl, fl, u64, u64, u64, u32, fl, fl, vp]),
         "dp_add_noise_finalize_flat": (it, [vp, vp, vp, vp, vp, vp, vp, it, fl, fl, u64, u64, u64, vp, fl, fl, vp]),
         "dp_philox_raw": (it, [vp, sz, u64, u64, u32, vp]),
+        "dp_checkpoint_pitch": (it, [it]),
+        "dp_checkpoint_write": (it, [vp, it, sz, it, sz, vp, vp, vp]),
+        "dp_checkpoint_read": (it, [vp, vp, sz, it, vp, it, sz, vp]),
+        "dp_checkpoint_workspace_bytes": (sz, [dpp, it]),
+        "dp_checkpoint_example_grad": (it, [dpp, vp, vp, vp, vp, vp, vp, sz, vp, vp, sz, vp]),
+        "dp_checkpoint_clip_accumulate": (it, [dpp, vp, vp, vp, vp, vp, fl, vp, vp, vp, sz, vp]),
+        "dp_bias_bucket": (it, [dbp, it]),
+        "dp_bias_softmax": (it, [dbp, vp, vp, vp, vp, vp, vp]),
+        "dp_bias_workspace_bytes": (sz, [dbp]),
+        "dp_bias_softmax_backward": (it, [dbp, vp, vp, vp, vp, vp, vp, sz, vp, vp, sz, vp]),
         "dp_profile_next_contraction": (it, [vp, vp]),
         "dp_last_error": (C.c_char_p, []),
         "dp_version": (C.c_char_p, []),
@@ -107,6 +125,8 @@ EXPORTED = ("dp_group_clip_bounds", "dp_weight_count", "dp_bias_count", "dp_work
             "dp_example_addresses", "dp_per_example_grad_batch_at", "dp_per_example_grad_blocks_batch_at", "dp_clip_accumulate_recompute_batch_at", "dp_clip_accumulate_recompute_blocks_batch_at", "dp_unit_grad_batch_at",
             "dp_clip_accumulate_columns",
             "dp_clip_factors", "dp_clip_accumulate", "dp_clip_accumulate_segments", "dp_clip_accumulate_recompute", "dp_add_noise_finalize", "dp_add_noise_finalize_update", "dp_add_example_noise",
+            "dp_checkpoint_pitch", "dp_checkpoint_write", "dp_checkpoint_read", "dp_checkpoint_workspace_bytes", "dp_checkpoint_example_grad",
+            "dp_checkpoint_clip_accumulate", "dp_bias_bucket", "dp_bias_softmax", "dp_bias_workspace_bytes", "dp_bias_softmax_backward",
             "dp_add_noise_finalize_flat", "dp_philox_raw", "dp_profile_next_contraction", "dp_last_error", "dp_version")
 
 
@@ -407,3 +427,97 @@ def dp_profile_next_contraction(start_event, stop_event):
 
 def dp_philox_raw(raw, p: int, seed: int, step: int, tensor_id: int, stream=None):
     _check(load_library().dp_philox_raw(_ptr(raw), p, seed, step, tensor_id, _stream(stream)))
+
+
+# ---- 8-bit activation checkpoints ---------------------------------------------------------------------------------
+
+def _rows_of(t):
+    """(dtype code, rows, features, elements from row to row) of a tensor whose leading dimensions are evenly spaced rows."""
+    import torch
+    if t.dtype not in (torch.float32, torch.bfloat16):
+        raise DpError(DP_ERR_UNSUPPORTED, f"activations are float32 or bfloat16, not {t.dtype}")
+    features = t.shape[-1] if t.dim() else 0
+    spacing = t.stride(-2) if t.dim() > 1 else features
+    even = features > 0 and (features == 1 or t.stride(-1) == 1)
+    for d in range(t.dim() - 2):
+        even = even and (t.shape[d] == 1 or t.stride(d) == t.shape[d + 1] * t.stride(d + 1))
+    rows = t.numel() // features if features else 0
+    if not even or (rows > 1 and spacing < features):
+        raise DpError(DP_ERR_INVALID_ARG, f"not rows of consecutive values: shape {tuple(t.shape)}, strides {t.stride()}")
+    return (DP_BF16 if t.dtype == torch.bfloat16 else DP_F32), rows, features, max(spacing, features)
+
+
+def _check_checkpoint(codes, scales, rows: int, features: int):
+    pitch = dp_checkpoint_pitch(features)
+    for t, need, what in ((codes, rows * pitch, "codes"), (scales, rows * (pitch // 32), "scales")):
+        if t.element_size() != 1 or not t.is_contiguous() or t.numel() < need:
+            raise DpError(DP_ERR_INVALID_ARG, f"{what} must be at least {need} contiguous bytes for {rows} rows of {features} features")
+
+
+def dp_checkpoint_pitch(features: int) -> int:
+    """Bytes of codes of a row: features rounded up to a multiple of 32."""
+    pitch = int(load_library().dp_checkpoint_pitch(features))
+    if not pitch:
+        raise DpError(DP_ERR_INVALID_ARG, dp_last_error())
+    return pitch
+
+
+def dp_checkpoint_write(x, codes, scales, stream=None):
+    """x [..., features] (rows evenly spaced, float32 or bfloat16) into codes [rows, pitch] and scales [rows, pitch / 32] (bytes)."""
+    dtype, rows, features, stride = _rows_of(x)
+    _check_checkpoint(codes, scales, rows, features)
+    _check(load_library().dp_checkpoint_write(_ptr(x), dtype, rows, features, stride, _ptr(codes), _ptr(scales), _stream(stream)))
+
+
+def dp_checkpoint_read(codes, scales, x, stream=None):
+    """The values of a checkpoint into x [..., features] (rows evenly spaced, float32 or bfloat16)."""
+    dtype, rows, features, stride = _rows_of(x)
+    _check_checkpoint(codes, scales, rows, features)
+    _check(load_library().dp_checkpoint_read(_ptr(codes), _ptr(scales), rows, features, _ptr(x), dtype, stride, _stream(stream)))
+
+
+def dp_checkpoint_workspace_bytes(desc: LayerDesc, use: int = DP_WS_PER_EXAMPLE_GRAD) -> int:
+    return int(load_library().dp_checkpoint_workspace_bytes(C.byref(desc), use))
+
+
+def dp_checkpoint_example_grad(desc: LayerDesc, codes, scales, dy, g_w, g_b, sqnorm, ws, lengths=None, g_stride: int = 0,
+                               ws_bytes: Optional[int] = None, stream=None):
+    """dp_per_example_grad of a dense layer with its input activations from a checkpoint; lengths: int32 tokens of each example."""
+    _check(load_library().dp_checkpoint_example_grad(C.byref(desc), _ptr(codes), _ptr(scales), _ptr(dy), _ptr(lengths), _ptr(g_w), _ptr(g_b),
+                                                     g_stride, _ptr(sqnorm), _ptr(ws), _nbytes(ws) if ws_bytes is None else ws_bytes,
+                                                     _stream(stream)))
+
+
+def dp_checkpoint_clip_accumulate(desc: LayerDesc, codes, scales, dy, sqnorm, clip_c: float, acc_w, acc_b, ws, lengths=None,
+                                  ws_bytes: Optional[int] = None, stream=None):
+    """dp_clip_accumulate_recompute of a dense layer with its input activations from a checkpoint."""
+    _check(load_library().dp_checkpoint_clip_accumulate(C.byref(desc), _ptr(codes), _ptr(scales), _ptr(dy), _ptr(lengths), _ptr(sqnorm), clip_c,
+                                                        _ptr(acc_w), _ptr(acc_b), _ptr(ws), _nbytes(ws) if ws_bytes is None else ws_bytes,
+                                                        _stream(stream)))
+
+
+# ---- attention probabilities under a relative position bias ---------------------------------------------------------
+
+def dp_bias_bucket(desc: BiasDesc, distance: int) -> int:
+    """Row of the bias table that a distance (query position - key position) uses."""
+    bucket = int(load_library().dp_bias_bucket(C.byref(desc), distance))
+    if bucket < 0:
+        raise DpError(DP_ERR_INVALID_ARG, dp_last_error())
+    return bucket
+
+
+def dp_bias_softmax(desc: BiasDesc, scores, table, probs, query_lengths=None, key_lengths=None, stream=None):
+    _check(load_library().dp_bias_softmax(C.byref(desc), _ptr(scores), _ptr(table), _ptr(query_lengths), _ptr(key_lengths), _ptr(probs),
+                                          _stream(stream)))
+
+
+def dp_bias_workspace_bytes(desc: BiasDesc) -> int:
+    return int(load_library().dp_bias_workspace_bytes(C.byref(desc)))
+
+
+def dp_bias_softmax_backward(desc: BiasDesc, probs, dprobs, dscores, g_table, sqnorm, ws, query_lengths=None, key_lengths=None,
+                             g_stride: int = 0, ws_bytes: Optional[int] = None, stream=None):
+    """Gradient of the scores, and per example the gradient of the bias table and its squared norm."""
+    _check(load_library().dp_bias_softmax_backward(C.byref(desc), _ptr(probs), _ptr(dprobs), _ptr(query_lengths), _ptr(key_lengths), _ptr(dscores),
+                                                   _ptr(g_table), g_stride, _ptr(sqnorm), _ptr(ws),
+                                                   _nbytes(ws) if ws_bytes is None else ws_bytes, _stream(stream)))

@@ -1,6 +1,7 @@
 // C ABI of libdp_privatise: argument validation (all on the host, before any launch) and
 // dispatch to the kernels.  See include/dp_privatise.h for the contract of every call.
 #include "internal.h"
+#include "checkpoint.h"
 #include "group.h"
 
 #include <cmath>
@@ -1011,6 +1012,226 @@ dp_status dp_philox_raw(uint32_t *raw, size_t p, uint64_t seed, uint64_t step, u
     if (p >= ((size_t)1 << 40)) return fail(DP_ERR_UNSUPPORTED, "p too large");
     g_err[0] = 0;
     return launch_philox_raw(raw, p, seed, step, tensor_id, static_cast<hipStream_t>(stream));
+}
+
+// ---- 8-bit activation checkpoints -----------------------------------------------------------
+
+int dp_checkpoint_pitch(int features)
+{
+    if (features < 1 || features > (1 << 20)) {
+        fail(DP_ERR_INVALID_ARG, "features = %d (need 1 .. 2^20)", features);
+        return 0;
+    }
+    return ck_pitch(features);
+}
+
+// Tensors whose kernels take rows from any element on.
+static dp_status check_rows(const void *p, const char *name, int dtype, bool required = true)
+{
+    if (dtype != DP_F32 && dtype != DP_BF16) return fail(DP_ERR_INVALID_ARG, "unknown dtype %d", dtype);
+    return check_ptr(p, name, required, dtype == DP_BF16 ? 2 : 4);
+}
+
+static dp_status check_checkpoint(size_t rows, int features, size_t &row_stride)
+{
+    if (dp_checkpoint_pitch(features) == 0) return DP_ERR_INVALID_ARG;
+    if (row_stride == 0) row_stride = (size_t)features;
+    if (row_stride < (size_t)features) return fail(DP_ERR_INVALID_ARG, "row_stride %zu is smaller than the %d features", row_stride, features);
+    if (rows >= ((size_t)1 << 31)) return fail(DP_ERR_UNSUPPORTED, "2^31 rows or more");
+    return DP_OK;
+}
+
+dp_status dp_checkpoint_write(const void *x, int in_dtype, size_t rows, int features, size_t row_stride, uint8_t *codes, uint8_t *scales,
+                              dp_stream stream)
+{
+    DP_TRY(check_checkpoint(rows, features, row_stride));
+    DP_TRY(check_rows(x, "x", in_dtype, rows != 0));
+    DP_TRY(check_ptr(codes, "codes", rows != 0));
+    DP_TRY(check_ptr(scales, "scales", rows != 0, 1));
+    g_err[0] = 0;
+    if (rows == 0) return DP_OK;                     // (an empty tensor's address is NULL)
+    return launch_checkpoint_write(x, in_dtype == DP_BF16, rows, features, row_stride, codes, scales, static_cast<hipStream_t>(stream));
+}
+
+dp_status dp_checkpoint_read(const uint8_t *codes, const uint8_t *scales, size_t rows, int features, void *x, int out_dtype, size_t row_stride,
+                             dp_stream stream)
+{
+    DP_TRY(check_checkpoint(rows, features, row_stride));
+    DP_TRY(check_rows(x, "x", out_dtype, rows != 0));
+    DP_TRY(check_ptr(codes, "codes", rows != 0));
+    DP_TRY(check_ptr(scales, "scales", rows != 0, 1));
+    g_err[0] = 0;
+    if (rows == 0) return DP_OK;                     // (an empty tensor's address is NULL)
+    return launch_checkpoint_read(codes, scales, out_dtype == DP_BF16, rows, features, x, row_stride, static_cast<hipStream_t>(stream));
+}
+
+static dp_status make_checkpoint_geo(const dp_layer_desc *desc, Geo &g)
+{
+    DP_TRY(make_geo(desc, g));
+    if (g.kind != DP_DENSE) return fail(DP_ERR_UNSUPPORTED, "a checkpoint is read for dense layers only");
+    if (g.cin > (1 << 20) || g.cout > (1 << 20)) return fail(DP_ERR_UNSUPPORTED, "more than 2^20 features");
+    const size_t lim = (size_t)1 << 31, wide = (size_t)ck_pitch(g.cin);
+    if ((size_t)g.n * ((size_t)(g.h + 31) / 32) >= lim || (size_t)g.h * wide >= lim ||
+        (size_t)g.n * ((wide + 127) / 128 + 1) * (((size_t)g.cout + 127) / 128) >= lim)
+        return fail(DP_ERR_UNSUPPORTED, "layer too large for one call");
+    return DP_OK;
+}
+
+size_t dp_checkpoint_workspace_bytes(const dp_layer_desc *desc, int use)
+{
+    Geo g;
+    if (make_checkpoint_geo(desc, g) != DP_OK) return 0;
+    if (use != DP_WS_PER_EXAMPLE_GRAD && use != DP_WS_RECOMPUTE) {
+        fail(DP_ERR_INVALID_ARG, "unknown workspace use %d", use);
+        return 0;
+    }
+    return checkpoint_ws_bytes(g, use == DP_WS_RECOMPUTE ? MODE_WEIGHTED : MODE_NORM);
+}
+
+dp_status dp_checkpoint_example_grad(const dp_layer_desc *desc, const uint8_t *codes, const uint8_t *scales, const void *dy,
+                                     const int32_t *lengths, float *g_w, float *g_b, size_t g_stride, float *sqnorm, void *ws, size_t ws_bytes,
+                                     dp_stream stream)
+{
+    Geo g;
+    DP_TRY(make_checkpoint_geo(desc, g));
+    DP_TRY(check_ptr(codes, "codes", true));
+    DP_TRY(check_ptr(scales, "scales", true, 1));
+    DP_TRY(check_ptr(dy, "dy", true));
+    DP_TRY(check_ptr(lengths, "lengths", false, 4));
+    DP_TRY(check_ptr(g_w, "g_w", false));
+    DP_TRY(check_ptr(g_b, "g_b", false));
+    DP_TRY(check_ptr(sqnorm, "sqnorm", false, 4));
+    if (!g_w && !sqnorm) return fail(DP_ERR_INVALID_ARG, "nothing to compute: g_w and sqnorm are both NULL");
+    if (g_w && g.pb && !g_b) return fail(DP_ERR_INVALID_ARG, "g_w given but g_b is NULL for a layer with a bias");
+    if (g_b && (!g_w || !g.pb)) return fail(DP_ERR_INVALID_ARG, "g_b given without g_w, or for a layer without bias");
+    if (g_stride) {
+        if (g_stride % 4) return fail(DP_ERR_INVALID_ARG, "g_stride must be a multiple of 4");
+        if (g_stride < g.pw || g_stride < g.pb) return fail(DP_ERR_INVALID_ARG, "g_stride smaller than the tensor");
+    }
+    DP_TRY(check_room(checkpoint_ws_bytes(g, MODE_NORM), ws, ws_bytes));
+    g_err[0] = 0;
+    return launch_checkpoint_dense(g, g_w ? MODE_MATERIALISE : MODE_NORM, codes, scales, dy, lengths, g_w, g_b, g_stride, sqnorm, nullptr, 0.0f, ws,
+                                   static_cast<hipStream_t>(stream));
+}
+
+dp_status dp_checkpoint_clip_accumulate(const dp_layer_desc *desc, const uint8_t *codes, const uint8_t *scales, const void *dy,
+                                        const int32_t *lengths, const float *sqnorm, float clip_c, float *acc_w, float *acc_b, void *ws,
+                                        size_t ws_bytes, dp_stream stream)
+{
+    Geo g;
+    DP_TRY(make_checkpoint_geo(desc, g));
+    DP_TRY(check_ptr(codes, "codes", true));
+    DP_TRY(check_ptr(scales, "scales", true, 1));
+    DP_TRY(check_ptr(dy, "dy", true));
+    DP_TRY(check_ptr(lengths, "lengths", false, 4));
+    DP_TRY(check_ptr(sqnorm, "sqnorm", true, 4));
+    DP_TRY(check_ptr(acc_w, "acc_w", true));
+    DP_TRY(check_ptr(acc_b, "acc_b", g.pb != 0));
+    if (!g.pb && acc_b) return fail(DP_ERR_INVALID_ARG, "acc_b given for a layer without bias");
+    DP_TRY(check_clip(clip_c));
+    DP_TRY(check_room(checkpoint_ws_bytes(g, MODE_WEIGHTED), ws, ws_bytes));
+    g_err[0] = 0;
+    return launch_checkpoint_dense(g, MODE_WEIGHTED, codes, scales, dy, lengths, acc_w, acc_b, 0, nullptr, sqnorm, clip_c, ws,
+                                   static_cast<hipStream_t>(stream));
+}
+
+// ---- attention probabilities under a relative position bias ---------------------------------
+
+// Validates a descriptor and finds where its buckets begin: bucket near + k at the smallest whole d with
+// (d / near)^(nb - near) >= (max_distance / near)^k.  80-bit floats tell whether that is a whole number itself: distances are below 2^12, and an
+// irrational border nearer than 1e-15 to one of them does not occur among powers this small.
+static dp_status make_bias_geo(const dp_bias_desc *d, BiasGeo &g)
+{
+    if (!d) return fail(DP_ERR_INVALID_ARG, "descriptor is NULL");
+    if (d->in_dtype != DP_F32 && d->in_dtype != DP_BF16) return fail(DP_ERR_INVALID_ARG, "unknown input dtype %d", d->in_dtype);
+    const int lim = 1 << 30;
+    if (d->n < 1 || d->heads < 1 || d->queries < 1 || d->keys < 1)
+        return fail(DP_ERR_INVALID_ARG, "non-positive dimension (n %d heads %d queries %d keys %d)", d->n, d->heads, d->queries, d->keys);
+    if (d->queries >= lim || d->keys >= lim || d->query_offset > lim || d->n > 65535 || d->heads > 65535)
+        return fail(DP_ERR_UNSUPPORTED, "dimension beyond kernel limits");
+    if (d->query_offset < 0 && d->query_offset != DP_QUERIES_AT_END)
+        return fail(DP_ERR_INVALID_ARG, "query_offset = %d (need >= 0 or DP_QUERIES_AT_END)", d->query_offset);
+    if (!std::isfinite(d->scale)) return fail(DP_ERR_INVALID_ARG, "scale must be finite");
+    if (d->bidirectional && d->buckets % 2) return fail(DP_ERR_INVALID_ARG, "%d buckets cannot be shared by two directions", d->buckets);
+    const int nb = d->bidirectional ? d->buckets / 2 : d->buckets;
+    if (d->buckets < 2 || nb < 2) return fail(DP_ERR_INVALID_ARG, "buckets = %d (need 2 a side)", d->buckets);
+    if (nb > 256) return fail(DP_ERR_UNSUPPORTED, "more than 256 buckets a side");
+    const int near = nb / 2, span = nb - near;
+    if (d->max_distance <= near) return fail(DP_ERR_INVALID_ARG, "max_distance = %d (need more than %d)", d->max_distance, near);
+    if (d->max_distance > 4096) return fail(DP_ERR_UNSUPPORTED, "max_distance beyond 4096");
+    if (d->row_stride && d->row_stride < (size_t)d->keys) return fail(DP_ERR_INVALID_ARG, "row_stride smaller than the keys");
+    memset(&g, 0, sizeof(g));
+    g.bf16 = d->in_dtype == DP_BF16; g.n = d->n; g.heads = d->heads; g.queries = d->queries; g.keys = d->keys;
+    g.buckets = d->buckets; g.bidirectional = d->bidirectional ? 1 : 0; g.causal = d->causal ? 1 : 0;
+    g.query_offset = d->query_offset; g.scale = d->scale;
+    g.row_stride = d->row_stride ? d->row_stride : (size_t)d->keys;
+    if (g.row_stride >= ((size_t)1 << 40) || (size_t)g.n * g.heads * g.queries >= ((size_t)1 << 31))
+        return fail(DP_ERR_UNSUPPORTED, "2^31 rows or more");
+    g.near = near;
+    const long double step = logl((long double)d->max_distance / near) / span;
+    for (int k = 1; k < span; ++k) {
+        const long double at = near * expl(step * k), whole = rintl(at);
+        g.borders[g.border_count++] = (int)(fabsl(at - whole) < 1e-15L * at ? whole : ceill(at));
+    }
+    g.far = g.border_count ? g.borders[g.border_count - 1] : near;
+    return DP_OK;
+}
+
+int dp_bias_bucket(const dp_bias_desc *desc, int distance)
+{
+    BiasGeo g;
+    if (make_bias_geo(desc, g) != DP_OK) return -1;
+    long long d = distance;
+    int side = 0;
+    if (g.bidirectional && d < 0) { side = g.buckets / 2; d = -d; }
+    if (d < 0) d = 0;
+    int b = d < g.near ? (int)d : g.near;
+    for (int k = 0; k < g.border_count; ++k) b += d >= g.borders[k];
+    return side + b;
+}
+
+dp_status dp_bias_softmax(const dp_bias_desc *desc, const void *scores, const float *table, const int32_t *query_lengths,
+                          const int32_t *key_lengths, void *probs, dp_stream stream)
+{
+    BiasGeo g;
+    DP_TRY(make_bias_geo(desc, g));
+    DP_TRY(check_rows(scores, "scores", desc->in_dtype));
+    DP_TRY(check_rows(probs, "probs", desc->in_dtype));
+    DP_TRY(check_ptr(table, "table", true, 4));
+    DP_TRY(check_ptr(query_lengths, "query_lengths", false, 4));
+    DP_TRY(check_ptr(key_lengths, "key_lengths", false, 4));
+    g_err[0] = 0;
+    return launch_bias_softmax(g, scores, table, query_lengths, key_lengths, probs, static_cast<hipStream_t>(stream));
+}
+
+size_t dp_bias_workspace_bytes(const dp_bias_desc *desc)
+{
+    BiasGeo g;
+    return make_bias_geo(desc, g) == DP_OK ? bias_ws_bytes(g) : 0;
+}
+
+dp_status dp_bias_softmax_backward(const dp_bias_desc *desc, const void *probs, const void *dprobs, const int32_t *query_lengths,
+                                   const int32_t *key_lengths, void *dscores, float *g_table, size_t g_stride, float *sqnorm, void *ws,
+                                   size_t ws_bytes, dp_stream stream)
+{
+    BiasGeo g;
+    DP_TRY(make_bias_geo(desc, g));
+    DP_TRY(check_rows(probs, "probs", desc->in_dtype));
+    DP_TRY(check_rows(dprobs, "dprobs", desc->in_dtype));
+    DP_TRY(check_rows(dscores, "dscores", desc->in_dtype));
+    DP_TRY(check_ptr(query_lengths, "query_lengths", false, 4));
+    DP_TRY(check_ptr(key_lengths, "key_lengths", false, 4));
+    DP_TRY(check_ptr(g_table, "g_table", true));
+    DP_TRY(check_ptr(sqnorm, "sqnorm", false, 4));
+    const size_t entries = (size_t)g.buckets * g.heads;
+    if (g_stride) {
+        if (g_stride % 4) return fail(DP_ERR_INVALID_ARG, "g_stride must be a multiple of 4");
+        if (g_stride < entries) return fail(DP_ERR_INVALID_ARG, "g_stride smaller than the table");
+    }
+    DP_TRY(check_room(bias_ws_bytes(g), ws, ws_bytes));
+    g_err[0] = 0;
+    return launch_bias_softmax_backward(g, probs, dprobs, query_lengths, key_lengths, dscores, g_table, g_stride ? g_stride : entries, sqnorm, ws,
+                                        static_cast<hipStream_t>(stream));
 }
 
 }  // extern "C"

@@ -1,6 +1,7 @@
 // Internal declarations shared by the translation units of libdp_privatise (gfx950 only).
 #pragma once
 
+#include <atomic>
 #include <type_traits>
 #include <hip/hip_runtime.h>
 #include <stddef.h>
@@ -18,6 +19,26 @@ dp_status check_launch(const char *what);
 // launcher calls profile_begin(s) right before and profile_end(s) right after its main kernel.
 void profile_begin(hipStream_t s);
 void profile_end(hipStream_t s);
+
+// Launch of a kernel with `lds` bytes of dynamic LDS; the runtime is told once for a kernel and device that it may pass 64 KB (telling it
+// twice is harmless).
+template <auto Kernel, typename... Args>
+dp_status launch_lds(dim3 grid, unsigned threads, unsigned lds, hipStream_t s, const Args &...args)
+{
+    static std::atomic<uint64_t> told{0};                // a bit for each device
+    if (lds > 32768u) {
+        int dev = 0;
+        if (hipGetDevice(&dev) != hipSuccess) return fail(DP_ERR_DEVICE, "hipGetDevice failed");
+        const uint64_t bit = 1ull << (dev & 63);
+        if (!(told.load() & bit)) {
+            if (hipFuncSetAttribute(reinterpret_cast<const void *>(Kernel), hipFuncAttributeMaxDynamicSharedMemorySize, 152 * 1024) != hipSuccess)
+                return fail(DP_ERR_DEVICE, "cannot reserve %u bytes of LDS", lds);
+            told.fetch_or(bit);
+        }
+    }
+    hipLaunchKernelGGL(Kernel, grid, dim3(threads), lds, s, args...);
+    return check_launch("kernel");
+}
 
 // ---- geometry of a validated descriptor ------------------------------------------------
 struct Geo {
@@ -172,6 +193,34 @@ dp_status launch_noise_finalize_flat(const float *acc, float *out, float *theta,
                                      const uint64_t *step_dev, float lr, float momentum, hipStream_t s);
 dp_status launch_philox_raw(uint32_t *raw, size_t p, uint64_t seed, uint64_t step, uint32_t tensor_id,
                             hipStream_t s);
+
+// 8-bit activation checkpoints (checkpoint.hip) and the dense layers that are contracted from them (checkpoint_dense.hip); g.bf16: of dY
+dp_status launch_checkpoint_write(const void *x, bool bf16, size_t rows, int features, size_t stride, uint8_t *codes, uint8_t *scales,
+                                  hipStream_t s);
+dp_status launch_checkpoint_read(const uint8_t *codes, const uint8_t *scales, bool bf16, size_t rows, int features, void *x, size_t stride,
+                                 hipStream_t s);
+size_t checkpoint_ws_bytes(const Geo &g, int mode);
+dp_status launch_checkpoint_dense(const Geo &g, int mode, const uint8_t *codes, const uint8_t *scales, const void *dy, const int32_t *lengths,
+                                  float *out_w, float *out_b, size_t out_stride, float *sqnorm, const float *group_sqnorm, float clip_c,
+                                  void *ws, hipStream_t s);
+
+// softmax of scores under a learned relative position bias (bias_softmax.hip)
+constexpr int BIAS_BORDERS = 128;      // buckets of a side, at most twice as many
+struct BiasGeo {
+    int bf16, n, heads, queries, keys;
+    int buckets, bidirectional, causal, query_offset;     // query_offset < 0: the queries are an example's last keys
+    float scale;
+    size_t row_stride;
+    int near, border_count;      // distances below `near` have buckets of their own; borders[k]: where bucket near + 1 + k begins
+    int far;                     // from here on every distance of a side is in its last bucket
+    int borders[BIAS_BORDERS];
+};
+size_t bias_ws_bytes(const BiasGeo &g);
+dp_status launch_bias_softmax(const BiasGeo &g, const void *scores, const float *table, const int32_t *query_lengths,
+                              const int32_t *key_lengths, void *probs, hipStream_t s);
+dp_status launch_bias_softmax_backward(const BiasGeo &g, const void *probs, const void *dprobs, const int32_t *query_lengths,
+                                       const int32_t *key_lengths, void *dscores, float *g_table, size_t g_stride, float *sqnorm, void *ws,
+                                       hipStream_t s);
 
 // ---- device helpers --------------------------------------------------------------------
 #if defined(__HIP_DEVICE_COMPILE__) || defined(__HIPCC__)

@@ -1,0 +1,360 @@
+"""8-bit activation checkpoints on the GPU: the format bit by bit, and the per-example gradients, norms and clipped sums that are
+contracted from them, against plain 64-bit forms.
+
+Tolerances.  A checkpoint is exact: codes, scales and values are compared bit by bit.  A gradient is a sum of exact products, `planes` of
+them for a token (three where dY is fp32), with partial sums held in fp32: each of K = planes * tokens additions is off by at most 2^-23 of the
+sum of the magnitudes M = sum |dY||X| (a matrix instruction may cut where it does not round, hence 2^-23 and not 2^-24).  The bounds below are
+sums of those."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2109_12191_amd as dp
+
+pytestmark = pytest.mark.gpu
+U = 2.0 ** -23
+
+
+# ---- the format, in 64 bits -----------------------------------------------------------------------------------------
+
+def decode_table():
+    v = np.empty(256)
+    for c in range(256):
+        e, m = (c >> 3) & 15, c & 7
+        x = (1 + m / 8) * 2.0 ** (e - 7) if e else m / 8 * 2.0 ** -6
+        v[c] = math.nan if c & 127 == 127 else -x if c & 128 else x
+    return v
+
+
+TABLE = decode_table()
+POSITIVE = TABLE[:127]
+
+
+def encode(x):
+    """codes [rows, pitch], scales [rows, pitch / 32] of float64 x [rows, features]."""
+    rows, features = x.shape
+    pitch = (features + 31) // 32 * 32
+    v = np.zeros((rows, pitch))
+    v[:, :features] = x
+    v = v.reshape(rows, -1, 32)
+    finite = np.isfinite(v)
+    a = np.where(finite, np.abs(v), 0.0).max(2)
+    e = np.full(a.shape, -100)
+    for i in np.ndindex(a.shape):
+        while e[i] < 119 and a[i] > 448.0 * 2.0 ** int(e[i]):
+            e[i] += 1
+    y = np.where(finite, v, 0.0) / 2.0 ** e[:, :, None].astype(np.float64)
+    mag = np.minimum(np.abs(y), 448.0)
+    hi = np.searchsorted(POSITIVE, mag)                     # smallest number not below
+    lo = np.maximum(hi - 1, 0)
+    up, down = POSITIVE[hi] - mag, mag - POSITIVE[lo]
+    code = np.where((up < down) | ((up == down) & (hi % 2 == 0)), hi, lo)
+    code = np.where(np.signbit(y), code | 128, code)
+    code = np.where(finite, code, 127).astype(np.uint8)
+    return code.reshape(rows, pitch), (e + 127).astype(np.uint8)
+
+
+def decode(codes, scales, features):
+    rows = codes.shape[0]
+    v = TABLE[codes].reshape(rows, -1, 32) * 2.0 ** (scales.astype(np.float64) - 127)[:, :, None]
+    return v.reshape(rows, -1)[:, :features]
+
+
+def values(rng, rows, features, dtype):
+    """float32 [rows, features] on the dtype's grid, over many magnitudes."""
+    x = rng.standard_normal((rows, features)) * 2.0 ** rng.integers(-12, 12, (rows, 1)) * 2.0 ** rng.integers(-3, 3, (1, features))
+    return torch.from_numpy(x).to(dtype)
+
+
+def write(x):
+    pitch, rows = dp.dp_checkpoint_pitch(x.shape[-1]), x.shape[0]
+    codes = torch.full((rows + 1, pitch), 0xA5, dtype=torch.uint8, device="cuda:0")
+    scales = torch.full((rows + 1, pitch // 32), 0xA5, dtype=torch.uint8, device="cuda:0")
+    dp.dp_checkpoint_write(x, codes, scales)
+    torch.cuda.synchronize()
+    assert (codes[rows] == 0xA5).all() and (scales[rows] == 0xA5).all()
+    return codes[:rows].cpu().numpy(), scales[:rows].cpu().numpy()
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("features", [1, 15, 16, 17, 31, 32, 33, 48, 63, 70, 768, 1003])
+def test_write_and_read_bit_by_bit(dtype, features):
+    rng = np.random.default_rng(features)
+    for rows, start, gap in ((1, 0, 0), (5, 0, 0), (7, 1, 5), (300, 3, 2)):
+        x = values(rng, rows, features, dtype)
+        wide = torch.full((rows, start + features + gap), 3.0, dtype=dtype, device="cuda:0")
+        wide[:, start:start + features] = x.to("cuda:0")
+        view = wide[:, start:start + features]
+        codes, scales = write(view)
+        want_c, want_s = encode(x.double().numpy())
+        assert np.array_equal(scales, want_s) and np.array_equal(codes, want_c)
+        for out_dtype in (torch.bfloat16, torch.float32):
+            back = torch.full((rows, start + features + gap), 7.0, dtype=out_dtype, device="cuda:0")
+            dp.dp_checkpoint_read(torch.from_numpy(codes).cuda(), torch.from_numpy(scales).cuda(), back[:, start:start + features])
+            torch.cuda.synchronize()
+            got = back.double().cpu().numpy()
+            assert np.array_equal(got[:, start:start + features], decode(codes, scales, features))
+            assert (got[:, :start] == 7.0).all() and (got[:, start + features:] == 7.0).all()
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_every_code_ties_and_ends_of_the_range(dtype):
+    rows = []
+    ties = np.sort(np.concatenate([POSITIVE, (POSITIVE[1:] + POSITIVE[:-1]) / 2]))     # every number, and halfway between two
+    for e in (-100, -50, -3, 0, 40, 110):
+        scaled = np.concatenate([ties, -ties]) * 2.0 ** e
+        for i in range(0, len(scaled), 31):
+            block = np.zeros(32)
+            block[0] = 448.0 * 2.0 ** e                    # fixes the scale
+            part = scaled[i:i + 31]
+            block[1:1 + len(part)] = part
+            rows.append(block)
+    big = float(torch.finfo(dtype).max)
+    tiny = float(torch.finfo(dtype).tiny)
+    for special in ([big, -big, 1.0], [tiny, tiny * 2], [0.0, -0.0], [448.0 * 2.0 ** 119, big], [2.0 ** -100, 2.0 ** -109, 2.0 ** -110, 2.0 ** -111],
+                    [448.0, 449.0 if dtype == torch.float32 else 450.0], [1.75, 1.7578125], [math.inf, 1.0], [-math.inf, math.nan, 5.0], [math.nan],
+                    [math.inf] * 32, [math.nan] * 31 + [-3.0]):
+        block = np.zeros(32)
+        block[:len(special)] = special
+        rows.append(block)
+    x = torch.from_numpy(np.array(rows)).to(dtype)
+    codes, scales = write(x.cuda())
+    want_c, want_s = encode(x.double().numpy())
+    assert np.array_equal(scales, want_s)
+    assert np.array_equal(codes, want_c)
+    back = torch.empty(x.shape, dtype=dtype, device="cuda:0")
+    dp.dp_checkpoint_read(torch.from_numpy(codes).cuda(), torch.from_numpy(scales).cuda(), back)
+    assert np.array_equal(back.double().cpu().numpy(), decode(codes, scales, 32), equal_nan=True)
+    every = np.arange(256, dtype=np.uint8).reshape(8, 32)                  # and every code is read
+    for s in (27, 100, 127, 240):
+        sc = np.full((8, 1), s, dtype=np.uint8)
+        back = torch.empty((8, 32), dtype=dtype, device="cuda:0")
+        dp.dp_checkpoint_read(torch.from_numpy(every).cuda(), torch.from_numpy(sc).cuda(), back)
+        assert np.array_equal(back.double().cpu().numpy(), decode(every, sc, 32), equal_nan=True)
+
+
+def test_rows_written_a_few_at_a_time_are_those_written_together():
+    rng = np.random.default_rng(5)
+    x = values(rng, 40, 100, torch.bfloat16).cuda()
+    codes, scales = write(x)
+    pitch = dp.dp_checkpoint_pitch(100)
+    c = torch.zeros((40, pitch), dtype=torch.uint8, device="cuda:0")
+    s = torch.zeros((40, pitch // 32), dtype=torch.uint8, device="cuda:0")
+    for a, b in ((0, 1), (1, 2), (2, 9), (9, 40)):
+        dp.dp_checkpoint_write(x[a:b], c[a:b], s[a:b])
+    assert np.array_equal(c.cpu().numpy(), codes) and np.array_equal(s.cpu().numpy(), scales)
+    dp.dp_checkpoint_write(x[:0].reshape(0, 100), c, s)                    # no row
+
+
+# ---- gradients ------------------------------------------------------------------------------------------------------
+
+CASES = [
+    # n, tokens, cin, cout, bias, ragged
+    (1, 1, 1, 1, True, False),
+    (3, 1, 40, 24, True, True),
+    (5, 3, 33, 65, True, True),
+    (2, 5, 129, 7, False, False),
+    (9, 16, 48, 130, True, True),
+    (4, 17, 31, 16, False, True),
+    (3, 32, 128, 128, True, False),
+    (3, 33, 129, 127, True, True),
+    (6, 64, 96, 200, True, True),
+    (2, 65, 160, 264, False, True),
+    (2, 100, 250, 131, True, True),
+    (1, 300, 64, 72, True, False),
+    (2, 257, 300, 256, True, True),
+    (40, 20, 256, 300, True, True),
+]
+
+
+def problem(case, dtype, seed=0, broken=()):
+    """Inputs on the device and in 64 bits.  Later tokens hold NaN in both operands; examples of `broken` hold one everywhere."""
+    n, tokens, cin, cout, bias, ragged = case
+    rng = np.random.default_rng([seed, n, tokens, cin, cout])
+    x = np.abs(rng.standard_normal((n * tokens, cin))) * 2.0 ** rng.integers(-6, 6, (n * tokens, 1))
+    codes, scales = encode(torch.from_numpy(x).bfloat16().double().numpy())
+    dy = torch.from_numpy(rng.standard_normal((n, tokens, cout)) * 0.01 * 2.0 ** rng.integers(-4, 4, (n, tokens, 1))).to(dtype)
+    lengths = np.full(n, tokens)
+    if ragged:
+        lengths = rng.integers(0, tokens + 1, n)
+        lengths[n - 1] = tokens
+        if n > 1:
+            lengths[0] = 0
+    xv = decode(codes, scales, cin).reshape(n, tokens, cin)
+    dyv = dy.double().numpy().copy()
+    for i in range(n):
+        xv[i, lengths[i]:] = 0.0
+        dyv[i, lengths[i]:] = 0.0
+        dy[i, lengths[i]:] = math.nan
+        codes.reshape(n, tokens, -1)[i, lengths[i]:] = 127
+    for i in broken:
+        dy[i] = math.nan
+    desc = dp.LayerDesc(kind=dp.DP_DENSE, in_dtype=dp.DP_BF16 if dtype == torch.bfloat16 else dp.DP_F32, n=n, cin=cin, cout=cout, h=tokens,
+                        w=1, has_bias=bias)
+    dev = dict(codes=torch.from_numpy(codes).cuda(), scales=torch.from_numpy(scales).cuda(), dy=dy.cuda(),
+               lengths=torch.from_numpy(lengths.astype(np.int32)).cuda() if ragged else None)
+    return desc, dev, xv, dyv
+
+
+def magnitudes(xv, dyv):
+    return np.einsum("ito,itk->iok", np.abs(dyv), np.abs(xv))
+
+
+def example_grad(desc, dev, stored, stride=0, stream=None):
+    n, pw, pb = desc.n, dp.dp_weight_count(desc), dp.dp_bias_count(desc)
+    need = dp.dp_checkpoint_workspace_bytes(desc)
+    ws = torch.full((need + 64,), 0xA5, dtype=torch.uint8, device="cuda:0")
+    sq = torch.full((n + 1,), -7.0, device="cuda:0")
+    gw = torch.full((n, stride or pw), -7.0, device="cuda:0") if stored else None
+    gb = torch.full((n, stride or pb), -7.0, device="cuda:0") if stored and pb else None
+    dp.dp_checkpoint_example_grad(desc, dev["codes"], dev["scales"], dev["dy"], gw, gb, sq, ws, lengths=dev["lengths"], g_stride=stride,
+                                  ws_bytes=need, stream=stream)
+    torch.cuda.synchronize()
+    assert (ws[need:] == 0xA5).all() and sq[n] == -7.0
+    if stride:
+        assert (gw[:, pw:] == -7.0).all() and (gb is None or (gb[:, pb:] == -7.0).all())
+    return (gw[:, :pw].reshape(n, desc.cout, desc.cin) if stored else None, gb[:, :pb] if stored and pb else None, sq[:n])
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("case", CASES, ids=str)
+def test_example_gradients_and_norms(case, dtype):
+    n, tokens, cin, cout, bias, ragged = case
+    desc, dev, xv, dyv = problem(case, dtype)
+    g = np.einsum("ito,itk->iok", dyv, xv)
+    b = dyv.sum(1)
+    sq = (g ** 2).sum((1, 2)) + (b ** 2).sum(1) * bias
+    planes = 1 if dtype == torch.bfloat16 else 3
+    off = (planes * tokens + 2) * U * magnitudes(xv, dyv)
+    off_b = (tokens + 2) * U * np.abs(dyv).sum(1)
+    for stride in (0, (cout * cin + 7) // 4 * 4):
+        gw, gb, got = example_grad(desc, dev, True, stride)
+        assert (np.abs(gw.double().cpu().numpy() - g) <= off).all()
+        if bias:
+            assert (np.abs(gb.double().cpu().numpy() - b) <= off_b).all()
+        # squares of values that are off by `off`, and additions of at most 256 in a row
+        far = (2 * np.abs(g) * off + off ** 2).sum((1, 2)) + bias * (2 * np.abs(b) * off_b + off_b ** 2).sum(1) + 256 * U * sq
+        assert (np.abs(got.double().cpu().numpy() - sq) <= far).all()
+    _, _, alone = example_grad(desc, dev, False)
+    # by Gram matrices, or as above: entries off by their K additions, then sums of them
+    gram = np.einsum("itk,iuk->itu", np.abs(xv), np.abs(xv)) + bias
+    terms = (gram * np.einsum("ito,iuo->itu", np.abs(dyv), np.abs(dyv))).sum((1, 2))
+    assert (np.abs(alone.double().cpu().numpy() - sq) <= np.maximum(far, (cin + cout + 256) * U * terms)).all()
+    zero = np.nonzero(np.abs(dyv).sum((1, 2)) == 0)[0]
+    assert (alone.cpu().numpy()[zero] == 0.0).all() and (got.cpu().numpy()[zero] == 0.0).all()
+    again = example_grad(desc, dev, False)[2]
+    assert torch.equal(alone, again)
+
+
+def clip(desc, dev, sq, clip_c, acc_w, acc_b, stream=None):
+    need = dp.dp_checkpoint_workspace_bytes(desc, dp.DP_WS_RECOMPUTE)
+    ws = torch.full((need + 64,), 0xA5, dtype=torch.uint8, device="cuda:0")
+    dp.dp_checkpoint_clip_accumulate(desc, dev["codes"], dev["scales"], dev["dy"], sq, clip_c, acc_w, acc_b, ws, lengths=dev["lengths"],
+                                     ws_bytes=need, stream=stream)
+    torch.cuda.synchronize()
+    assert (ws[need:] == 0xA5).all()
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("case", CASES + [(64, 48, 128, 100, True, True), (16, 128, 260, 136, True, False)], ids=str)
+def test_clipped_sum(case, dtype):
+    n, tokens, cin, cout, bias, ragged = case
+    broken = (1,) if n > 2 else ()
+    desc, dev, xv, dyv = problem(case, dtype, 1, broken)
+    rng = np.random.default_rng(7)
+    sq = (10.0 ** rng.uniform(-3, 3, n)).astype(np.float32)
+    sq[n // 2] = 0.0                                         # a factor of 1
+    if n > 3:
+        sq[n - 2] = 1e30                                     # a factor of 1e-15
+    for i in broken:
+        sq[i] = math.nan                                     # left out, whatever it holds
+        dyv[i] = 0.0
+    with np.errstate(divide="ignore", invalid="ignore"):
+        f = np.where(sq == 0, 1.0, np.minimum(1.0, 0.7 / np.sqrt(sq.astype(np.float64))))
+    f[np.isnan(f)] = 0.0
+    old_w, old_b = rng.standard_normal((cout, cin)).astype(np.float32), rng.standard_normal(cout).astype(np.float32)
+    want_w = old_w + np.einsum("i,ito,itk->ok", f, dyv, xv)
+    want_b = old_b + np.einsum("i,ito->o", f, dyv)
+    planes = 1 if dtype == torch.bfloat16 and tokens >= 16 else 3
+    # additions of all tokens; factors are off by 2^-22 and an example meets one rounding for every later one
+    off_w = (planes * n * tokens + 2 * n + 8) * U * np.einsum("i,iok->ok", f, magnitudes(xv, dyv)) + 2 * U * np.abs(old_w)
+    off_b = (n * tokens + 8) * U * np.einsum("i,ito->o", f, np.abs(dyv)) + 2 * U * np.abs(old_b)
+    res = []
+    for _ in range(2):
+        acc_w = torch.from_numpy(old_w.copy()).cuda()
+        acc_b = torch.from_numpy(old_b.copy()).cuda() if bias else None
+        clip(desc, dev, torch.from_numpy(sq).cuda(), 0.7, acc_w, acc_b)
+        assert (np.abs(acc_w.double().cpu().numpy() - want_w) <= off_w).all()
+        if bias:
+            assert (np.abs(acc_b.double().cpu().numpy() - want_b) <= off_b).all()
+        res.append(acc_w)
+    assert torch.equal(*res)
+
+
+def test_infinite_bound_and_no_example_left():
+    case = (3, 40, 64, 64, True, False)
+    desc, dev, xv, dyv = problem(case, torch.bfloat16, 3)
+    acc_w, acc_b = torch.zeros(64, 64, device="cuda:0"), torch.zeros(64, device="cuda:0")
+    clip(desc, dev, torch.full((3,), 5.0, device="cuda:0"), math.inf, acc_w, acc_b)
+    off = (3 * 40 + 16) * U * magnitudes(xv, dyv).sum(0)
+    assert (np.abs(acc_w.double().cpu().numpy() - np.einsum("ito,itk->ok", dyv, xv)) <= off).all()
+    before = acc_w.clone()
+    clip(desc, dev, torch.full((3,), math.nan, device="cuda:0"), 1.0, acc_w, acc_b)
+    assert torch.equal(before, acc_w)
+
+
+def test_gradient_is_that_of_the_loss_by_differences():
+    """Loss sum_t,o w[t,o] (x W^T)[t,o] over the checkpoint's values, whose dY is w: differences of it in 64 bits."""
+    case = (2, 6, 10, 8, False, False)
+    desc, dev, xv, dyv = problem(case, torch.float32, 4)
+    gw, _, _ = example_grad(desc, dev, True)
+    rng = np.random.default_rng(0)
+    w = rng.standard_normal((8, 10))
+
+    def loss(i, w):
+        return (dyv[i] * (xv[i] @ w.T)).sum()
+    for i in range(2):
+        for o, k in ((0, 0), (7, 9), (3, 4)):
+            h = np.zeros_like(w)
+            h[o, k] = 1.0
+            slope = (loss(i, w + h) - loss(i, w - h)) / 2
+            assert abs(slope - float(gw[i, o, k])) <= (3 * 6 + 2) * U * magnitudes(xv, dyv)[i, o, k] + 1e-12 * abs(loss(i, w))
+
+
+def test_other_streams_and_graphs():
+    """The calls run on the stream they are given, and can be recorded: every replay gives the eager result on new inputs."""
+    case = (6, 64, 96, 200, True, True)
+    desc, dev, _, _ = problem(case, torch.bfloat16)
+    want = example_grad(desc, dev, False)[2]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    assert torch.equal(want, example_grad(desc, dev, False, stream=side)[2])
+
+    x = torch.randn(6 * 64, 96, device="cuda:0").bfloat16()
+    codes, scales = torch.empty_like(dev["codes"]), torch.empty_like(dev["scales"])
+    sq, acc_w, acc_b = torch.empty(6, device="cuda:0"), torch.zeros(200, 96, device="cuda:0"), torch.zeros(200, device="cuda:0")
+    ws = torch.empty(max(dp.dp_checkpoint_workspace_bytes(desc, u) for u in (0, 1)) + 16, dtype=torch.uint8, device="cuda:0")
+
+    def step():
+        dp.dp_checkpoint_write(x, codes, scales)
+        dp.dp_checkpoint_example_grad(desc, codes, scales, dev["dy"], None, None, sq, ws, lengths=dev["lengths"])
+        acc_w.zero_()
+        acc_b.zero_()
+        dp.dp_checkpoint_clip_accumulate(desc, codes, scales, dev["dy"], sq, 0.5, acc_w, acc_b, ws, lengths=dev["lengths"])
+    step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for _ in range(4):
+        x.copy_(torch.randn(6 * 64, 96, device="cuda:0"))
+        step()
+        torch.cuda.synchronize()
+        eager = [t.clone() for t in (codes, scales, sq, acc_w, acc_b)]
+        for t in (codes, scales, sq, acc_w, acc_b):
+            t.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(eager, (codes, scales, sq, acc_w, acc_b)))
