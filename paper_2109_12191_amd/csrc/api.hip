@@ -1071,7 +1071,7 @@ static dp_status make_checkpoint_geo(const dp_layer_desc *desc, Geo &g)
     if (g.kind != DP_DENSE) return fail(DP_ERR_UNSUPPORTED, "a checkpoint is read for dense layers only");
     if (g.cin > (1 << 20) || g.cout > (1 << 20)) return fail(DP_ERR_UNSUPPORTED, "more than 2^20 features");
     const size_t lim = (size_t)1 << 31, wide = (size_t)ck_pitch(g.cin);
-    if ((size_t)g.n * ((size_t)(g.h + 31) / 32) >= lim || (size_t)g.h * wide >= lim ||
+    if ((size_t)g.n * g.h >= lim || (size_t)g.h * wide >= lim ||
         (size_t)g.n * ((wide + 127) / 128 + 1) * (((size_t)g.cout + 127) / 128) >= lim)
         return fail(DP_ERR_UNSUPPORTED, "layer too large for one call");
     return DP_OK;

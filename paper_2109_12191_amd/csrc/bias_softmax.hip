@@ -89,22 +89,6 @@ __device__ __forceinline__ int bias_end(const BiasArgs &a, const Rows &r, int q)
     return max(min(r.key_length, a.causal ? r.first + q + 1 : a.keys), 0);
 }
 
-template <bool BF16> struct Raw8;
-template <> struct Raw8<true> {
-    uint4 w;
-    __device__ __forceinline__ void load(const void *p, size_t at, int count) { w = load8(static_cast<const uint16_t *>(p) + at, count); }
-    __device__ __forceinline__ void get(float (&v)[8]) const { widen8(w, v); }
-};
-template <> struct Raw8<false> {
-    float w[8];
-    __device__ __forceinline__ void load(const void *p, size_t at, int count) { load8f(static_cast<const float *>(p) + at, count, w); }
-    __device__ __forceinline__ void get(float (&v)[8]) const
-    {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = w[i];
-    }
-};
-
 // Sums / maxima over the TPR threads of a row.  `red`: a word for each wave; every thread of the workgroup calls it.
 template <int TPR, bool MAX>
 __device__ __forceinline__ float row_reduce(float v, float *red)

@@ -28,10 +28,9 @@ struct CkDenseArgs {
     const float *group_sqnorm;
     float clip_c;
     int n, tokens, cin, cout, pitch;
-    int dy_bf16, has_bias, stored, add;
-    int tiles_k, tiles_o, columns;   // tiles along k, along o; tiles_k + 1 columns of tiles with a bias
-    int per_range;                   // weighted: chunks of a range
-    int chunks;                      // weighted: chunks in all (of examples, or of rows)
+    int has_bias, stored, add;
+    int tiles_k, tiles_o, slots;     // tiles along k, along o; examples, or ranges
+    int per_range, chunks, cpe;      // weighted: chunks of a range, in all (of examples, or of rows), of an example
 };
 
 __device__ __forceinline__ int ck_length(const CkDenseArgs &a, int i)
@@ -61,10 +60,11 @@ __device__ __forceinline__ void split8(const float (&v)[8], uint4 (&planes)[3])
 
 // ------------------------------------------------------------------------------------------
 // Contraction over tokens.  A workgroup of four waves owns a 128 (o) x 128 (k) tile, a wave 64 x 64 of it (2 x 2 blocks of 32 x 32).
-// A chunk is 32 tokens; both operands lie in LDS as they lie in memory, [token][feature], and the matrix operands, which want
-// consecutive tokens of a feature, are read with the transposing LDS loads (four tokens of 16 features each).  A row is 16 pieces
-// of 16 bytes; piece p of row r lies in slot p ^ 4 (r & 3): the four rows that a transposing load meets are in different banks.  Codes become bf16 on their
-// way into LDS, once per workgroup.  Two LDS buffers, one barrier per chunk, the next chunk's loads in flight during the products.
+// A chunk is 64 tokens (PLANES 3: 32); both operands lie in LDS as they lie in memory, [token][feature], and the matrix operands, which
+// want consecutive tokens of a feature, are read with the transposing LDS loads (four tokens of 16 features each).  A row is 16 pieces
+// of 16 bytes; piece p of row r lies in slot p ^ 4 (r & 3): the four rows that a transposing load meets are in different banks.  Codes
+// become bf16 on their way into LDS, once per workgroup.  Two LDS buffers, one barrier per chunk; the loads of the two chunks after the next
+// are in flight during the products.
 //
 // PLANES: 1: dY as bf16 numbers; 3: fp32 values of dY, split.
 // Per-example call (WEIGHTED false): a workgroup contracts one example's tile, squares it, and stores it if asked.
@@ -73,169 +73,174 @@ __device__ __forceinline__ void split8(const float (&v)[8], uint4 (&planes)[3])
 // the last m at the end.  One set of accumulators for any number of examples, and each example meets its factor in fp32.
 // WEIGHTED, PLANES 3: rows (example, token) of the whole call one after the other, dY times its factor in fp32, then split: for fp32 dY, and
 // for examples of a few tokens, of which 32 rows hold several.
-constexpr int CT = 128, CKC = 32, CK_ROW = 2 * CT, CK_PLANE = CKC * CK_ROW;      // bytes of a row, of an operand's chunk
+// Bias: the workgroups of the first column of tiles add up dY as they stage it.
+// ALIGNED: rows of dY are multiples of 16 bytes: whole pieces by buffer loads, which give zeros beyond the chunk's last row; else from any
+// element on, piece by piece.
+constexpr int CT = 128, CK_ROW = 2 * CT;                           // bytes of a row of an operand
+constexpr int ck_chunk(int planes) { return planes == 1 ? 64 : 32; }
+constexpr int ck_stage_bytes(int planes) { return (planes + 1) * ck_chunk(planes) * CK_ROW; }
+constexpr unsigned CK_NOWHERE = 0xFFFFFFF0u;                       // an offset beyond any buffer
 
-template <int PLANES, bool WEIGHTED>
-__global__ void __launch_bounds__(256, 2) ck_contract_kernel(const CkDenseArgs a)
+template <int PLANES, bool WEIGHTED, bool BF16, bool ALIGNED>
+__global__ void __launch_bounds__(256, PLANES == 1 ? 2 : 1) ck_contract_kernel(const CkDenseArgs a)
 {
     extern __shared__ __attribute__((aligned(16))) char ck_lds[];
     __shared__ float red[4];
+    typedef typename In<BF16>::type E;
     constexpr bool ROWS = WEIGHTED && PLANES == 3;
-    constexpr int STAGE = (PLANES + 1) * CK_PLANE;
-    const int tiles = a.tiles_o * a.columns;
-    const int slot = (int)(blockIdx.x / (unsigned)tiles), tile = (int)(blockIdx.x - (unsigned)slot * (unsigned)tiles);     // example or range
-    const int tile_o = tile / a.columns, tile_k = tile - tile_o * a.columns;
+    constexpr int CK = ck_chunk(PLANES), STAGE = ck_stage_bytes(PLANES), PLANE = CK * CK_ROW;
+    constexpr int XP = CK / 32, YP = CK / 16;                      // pieces of X (16 codes) and dY (eight values) of a thread and chunk
+    // workgroup -> XCD goes round robin: an XCD takes a run of consecutive tiles, which share an example's operands in its L2
+    const unsigned per_xcd = gridDim.x >> 3, block = (blockIdx.x & 7u) * per_xcd + (blockIdx.x >> 3);
+    const unsigned tiles = (unsigned)(a.tiles_o * a.tiles_k);
+    const int slot = (int)(block / tiles), tile = (int)(block - (unsigned)slot * tiles);     // example or range
+    if (slot >= a.slots) return;
+    const int tile_o = tile / a.tiles_k, tile_k = tile - tile_o * a.tiles_k;
     const int o0 = tile_o * CT, k0 = tile_k * CT;
     const int t = threadIdx.x, lane = t & 63, wave = t >> 6, wm = wave >> 1, wn = wave & 1;
-    const int cpe = (a.tokens + CKC - 1) / CKC;                    // chunks of an example
+    const bool bias_here = a.has_bias && tile_k == 0;
     int c_begin = 0, c_end, len = 0;
     if constexpr (WEIGHTED) {
         c_begin = slot * a.per_range;
         c_end = min(c_begin + a.per_range, a.chunks);
     } else {
         len = ck_length(a, slot);
-        c_end = (len + CKC - 1) / CKC;
+        c_end = (len + CK - 1) / CK;
     }
 
-    if (tile_k == a.tiles_k) {                                     // the bias column: sums of dY, two threads to a feature
-        const int o = o0 + (t & 127);
-        float sum = 0.0f;
-        if constexpr (WEIGHTED) {
-            const long long total = (long long)a.n * a.tokens, per = ROWS ? CKC : 0;
-            for (int c = c_begin; c < c_end; ++c) {
-                const int ex = ROWS ? 0 : c / cpe;
-                const long long first = ROWS ? c * per : (long long)ex * a.tokens + (c - ex * cpe) * CKC;
-                const long long stop = ROWS ? min(first + CKC, total) : min(first + CKC, (long long)(ex + 1) * a.tokens);
-                for (long long r = first + (t >> 7); r < stop; r += 2) {
-                    const int i = (int)(r / a.tokens);
-                    if (o >= a.cout || r - (long long)i * a.tokens >= ck_length(a, i)) continue;
-                    const float f = clip_factor(a.group_sqnorm[i], a.clip_c);
-                    if (f == 0.0f) continue;
-                    const size_t at = (size_t)r * a.cout + o;
-                    sum += f * (a.dy_bf16 ? bf16_bits_to_float(static_cast<const uint16_t *>(a.dy)[at]) : static_cast<const float *>(a.dy)[at]);
-                }
-            }
-        } else if (o < a.cout) {
-            for (int r = t >> 7; r < len; r += 2) {
-                const size_t at = ((size_t)slot * a.tokens + r) * a.cout + o;
-                sum += a.dy_bf16 ? bf16_bits_to_float(static_cast<const uint16_t *>(a.dy)[at]) : static_cast<const float *>(a.dy)[at];
-            }
-        }
-        float *half = reinterpret_cast<float *>(ck_lds);
-        half[t] = sum;
-        __syncthreads();
-        sum = t < 128 ? half[t] + half[t + 128] : 0.0f;
-        const bool mine = t < 128 && o < a.cout;
-        if constexpr (WEIGHTED) {
-            if (mine) {
-                float *out = a.out_b + (size_t)slot * a.stride_b + o;
-                *out = a.add ? *out + sum : sum;
-            }
-        } else {
-            if (mine && a.stored) a.out_b[(size_t)slot * a.stride_b + o] = sum;
-            const float tot = block_sum<4>(mine ? sum * sum : 0.0f, red);
-            if (t == 0) a.partials[(size_t)slot * tiles + tile] = tot;
-        }
-        return;
-    }
-
-    // this thread's pieces of a chunk: 16 codes of row t / 8; eight values of dY of rows t / 16 and t / 16 + 16
+    // this thread's pieces of a chunk: 16 codes of rows t / 8 + 32 u; eight values of dY of rows t / 16 + 16 u
     const int xr = t >> 3, xp = t & 7, x_col = k0 + xp * 16;
     const int yr = t >> 4, yp = t & 15, y_col = o0 + yp * 8, y_count = a.cout - y_col;
-    const bool x_there = x_col < a.pitch;
+    const unsigned x_off = x_col < a.pitch ? (unsigned)(xr * a.pitch + x_col) : CK_NOWHERE;
+    const int s_pitch = a.pitch / CK_BLOCK;
+    const unsigned s_off = x_col < a.pitch ? (unsigned)(xr * s_pitch + x_col / CK_BLOCK) : CK_NOWHERE;
+    const unsigned y_off = y_count > 0 ? (unsigned)(yr * a.cout + y_col) * (unsigned)sizeof(E) : CK_NOWHERE;
 
-    uint4 x_raw;
-    uint32_t x_exp = 0;                                            // biased exponent of the scale
-    uint4 y_raw[PLANES == 1 ? 2 : 1];
-    float y_val[PLANES == 1 ? 1 : 2][8];
-    int f_ex = 0, f_c = 0, f_len = len;                            // example mode: next chunk to fetch
-    bool f_first = false;                                          //   and whether an example begins with it
-    int f_pow = 0;                                                 //   its factor's exponent
-    float f_m = 1.0f;
-    if constexpr (WEIGHTED && !ROWS) { f_ex = c_begin / cpe; f_c = c_begin - f_ex * cpe; }
-    bool have;                                                     // the fetched chunk has rows
-
-    auto fetch_rows = [&](size_t row0, int rows, int pow) {        // rows row0 .. row0 + rows of both operands
-        x_raw = make_uint4(0, 0, 0, 0);
-        x_exp = 127;
-        if (xr < rows && x_there) {
-            const size_t row = row0 + xr;
-            x_raw = *reinterpret_cast<const uint4 *>(a.codes + row * a.pitch + x_col);
-            x_exp = (uint32_t)max((int)a.scales[row * (unsigned)(a.pitch / CK_BLOCK) + (x_col / CK_BLOCK)] + pow, 1);
-        }
-#pragma unroll
-        for (int u = 0; u < 2; ++u) {
-            const int r = yr + 16 * u, count = r < rows ? y_count : 0;
-            const size_t at = (row0 + r) * a.cout + y_col;
-            if constexpr (PLANES == 1) y_raw[u] = load8(static_cast<const uint16_t *>(a.dy) + at, count);
-            else load8f(static_cast<const float *>(a.dy) + at, count, y_val[u]);
-        }
+    struct Slot {                                                  // a chunk on its way
+        uint4 x[XP];
+        uint32_t scale[XP];
+        Raw8<BF16> y[YP];
+        int rows;                                                  // of the chunk (0: it adds nothing)
+        bool begins;                                               // an example begins with it, of
+        int power;                                                 //   factor f = m 2^power
+        float m, f;
+        float x_sq[ROWS ? XP : 1], y_sq[ROWS ? YP : 1];            // rows of any examples: squared norms, lengths and tokens of this thread's rows
+        int x_left[ROWS ? XP : 1], y_left[ROWS ? YP : 1], x_len[ROWS ? XP : 1], y_len[ROWS ? YP : 1];
     };
-    auto fetch = [&](int c) {
-        if constexpr (ROWS) {
-            // rows of any examples: each has its own length and factor
-            const long long total = (long long)a.n * a.tokens, row0 = (long long)c * CKC;
-            auto factor = [&](long long row) {
-                if (row >= total) return 0.0f;
-                const int i = (int)(row / a.tokens);
-                if (row - (long long)i * a.tokens >= ck_length(a, i)) return 0.0f;
-                return clip_factor(a.group_sqnorm[i], a.clip_c);
-            };
-            have = true;
-            x_raw = make_uint4(0, 0, 0, 0);
-            x_exp = 127;
-            const long long xrow = row0 + xr;
-            if (x_there && factor(xrow) != 0.0f) {
-                x_raw = *reinterpret_cast<const uint4 *>(a.codes + xrow * a.pitch + x_col);
-                x_exp = a.scales[xrow * (a.pitch / CK_BLOCK) + (x_col / CK_BLOCK)];
-            }
+    int f_ex = 0, f_c = 0, f_len = len, f_power = 0;               // weighted, by example: what the next chunk belongs to
+    float f_m = 1.0f, f_f = 1.0f;
+    if constexpr (WEIGHTED && !ROWS) { f_ex = c_begin / a.cpe; f_c = c_begin - f_ex * a.cpe; }
+
+    auto load_rows = [&](Slot &s, size_t row0, int rows) {
+        const __amdgpu_buffer_rsrc_t xb = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(a.codes) + row0 * (unsigned)a.pitch, 0, rows * a.pitch, 0x00020000);
+        const __amdgpu_buffer_rsrc_t sb = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(a.scales) + row0 * (unsigned)s_pitch, 0, rows * s_pitch, 0x00020000);
+        typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 #pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                const long long row = row0 + yr + 16 * u;
-                const float f = factor(row);
-                const int count = f != 0.0f ? y_count : 0;
-                const size_t at = (size_t)row * a.cout + y_col;
-                if (a.dy_bf16) widen8(load8(static_cast<const uint16_t *>(a.dy) + at, count), y_val[u]);
-                else load8f(static_cast<const float *>(a.dy) + at, count, y_val[u]);
+        for (int u = 0; u < XP; ++u) {
+            const u32x4 v = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(xb, x_off + (x_off == CK_NOWHERE ? 0u : (unsigned)(32 * u * a.pitch)), 0, 0));
+            s.x[u] = make_uint4(v.x, v.y, v.z, v.w);
+            s.scale[u] = __builtin_amdgcn_raw_buffer_load_b8(sb, s_off + (s_off == CK_NOWHERE ? 0u : (unsigned)(32 * u * s_pitch)), 0, 0);
+        }
+        const E *dy = static_cast<const E *>(a.dy) + row0 * (unsigned)a.cout;
+        if constexpr (ALIGNED) {
+            const __amdgpu_buffer_rsrc_t yb = __builtin_amdgcn_make_buffer_rsrc(const_cast<E *>(dy), 0, rows * a.cout * (int)sizeof(E), 0x00020000);
 #pragma unroll
-                for (int j = 0; j < 8; ++j) y_val[u][j] *= f;
+            for (int u = 0; u < YP; ++u) {
+                const unsigned at = y_off + (y_off == CK_NOWHERE ? 0u : (unsigned)(16 * u * a.cout) * (unsigned)sizeof(E));
+                const u32x4 v = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(yb, at, 0, 0));
+                if constexpr (BF16) {
+                    s.y[u].w = make_uint4(v.x, v.y, v.z, v.w);
+                } else {
+                    const u32x4 n = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(yb, at == CK_NOWHERE ? at : at + 16u, 0, 0));
+                    s.y[u].w[0] = __uint_as_float(v.x); s.y[u].w[1] = __uint_as_float(v.y); s.y[u].w[2] = __uint_as_float(v.z); s.y[u].w[3] = __uint_as_float(v.w);
+                    s.y[u].w[4] = __uint_as_float(n.x); s.y[u].w[5] = __uint_as_float(n.y); s.y[u].w[6] = __uint_as_float(n.z); s.y[u].w[7] = __uint_as_float(n.w);
+                }
             }
-        } else if constexpr (WEIGHTED) {
-            f_first = f_c == 0 || c == c_begin;
-            if (f_first) {
-                f_len = ck_length(a, f_ex);
-                const float f = clip_factor(a.group_sqnorm[f_ex], a.clip_c);
-                if (f == 0.0f) f_len = 0;                          // adds nothing, and no 0 * inf
-                f_pow = f > 0.0f ? (int)(__float_as_uint(f) >> 23) - 127 : 0;
-                f_m = f > 0.0f ? f * pow2_of(127 - f_pow) : 1.0f;
-            }
-            const int rows = min(f_len - f_c * CKC, CKC);
-            have = rows > 0;
-            if (have) fetch_rows((size_t)f_ex * a.tokens + f_c * CKC, rows, f_pow);
-            if (++f_c == cpe) { f_c = 0; ++f_ex; }
         } else {
-            have = true;
-            fetch_rows((size_t)slot * a.tokens + c * CKC, min(len - c * CKC, CKC), 0);
+#pragma unroll
+            for (int u = 0; u < YP; ++u) s.y[u].load(dy, (size_t)(yr + 16 * u) * a.cout + y_col, yr + 16 * u < rows ? y_count : 0);
         }
     };
-    auto stage = [&](int buf) {
-        char *s = ck_lds + buf * STAGE;
-        const float scale = pow2_of((int)x_exp);
-        const uint2 w0 = ck_bf16(x_raw.x, scale), w1 = ck_bf16(x_raw.y, scale), w2 = ck_bf16(x_raw.z, scale), w3 = ck_bf16(x_raw.w, scale);
-        char *x = s + PLANES * CK_PLANE + xr * CK_ROW;
-        *reinterpret_cast<uint4 *>(x + (((2 * xp) ^ ((xr & 3) << 2)) << 4)) = make_uint4(w0.x, w0.y, w1.x, w1.y);
-        *reinterpret_cast<uint4 *>(x + (((2 * xp + 1) ^ ((xr & 3) << 2)) << 4)) = make_uint4(w2.x, w2.y, w3.x, w3.y);
+    auto fetch = [&](Slot &s, int c) {
+        s.rows = 0;
+        s.begins = false;
+        if (c >= c_end) return;
+        if constexpr (ROWS) {
+            const unsigned total = (unsigned)a.n * (unsigned)a.tokens, row0 = (unsigned)c * CK;
+            s.rows = (int)min(total - row0, (unsigned)CK);
+            auto about = [&](unsigned row, float &sq, int &left, int &l) {
+                const unsigned at = min(row, total - 1), i = at / (unsigned)a.tokens;
+                sq = a.group_sqnorm[i];
+                l = a.lengths ? a.lengths[i] : a.tokens;
+                left = row < total ? (int)(at - i * (unsigned)a.tokens) : a.tokens;
+            };
 #pragma unroll
-        for (int u = 0; u < 2; ++u) {
+            for (int u = 0; u < XP; ++u) about(row0 + xr + 32 * u, s.x_sq[u], s.x_left[u], s.x_len[u]);
+#pragma unroll
+            for (int u = 0; u < YP; ++u) about(row0 + yr + 16 * u, s.y_sq[u], s.y_left[u], s.y_len[u]);
+            load_rows(s, row0, s.rows);
+        } else if constexpr (WEIGHTED) {
+            s.begins = f_c == 0 || c == c_begin;
+            if (s.begins) {
+                f_len = ck_length(a, f_ex);
+                f_f = clip_factor(a.group_sqnorm[f_ex], a.clip_c);
+                if (f_f == 0.0f) f_len = 0;                        // adds nothing, and no 0 * inf
+                f_power = f_f > 0.0f ? (int)(__float_as_uint(f_f) >> 23) - 127 : 0;
+                f_m = f_f > 0.0f ? f_f * pow2_of(127 - f_power) : 1.0f;
+            }
+            s.rows = max(min(f_len - f_c * CK, CK), 0);
+            s.power = f_power; s.m = f_m; s.f = f_f;
+            if (s.rows > 0) load_rows(s, (size_t)f_ex * (unsigned)a.tokens + (unsigned)(f_c * CK), s.rows);
+            if (++f_c == a.cpe) { f_c = 0; ++f_ex; }
+        } else {
+            s.rows = min(len - c * CK, CK);
+            load_rows(s, (size_t)slot * (unsigned)a.tokens + (unsigned)(c * CK), s.rows);
+        }
+    };
+    float bias_sum[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) bias_sum[j] = 0.0f;
+    auto stage = [&](const Slot &s, int buf) {
+        char *lds = ck_lds + buf * STAGE;
+#pragma unroll
+        for (int u = 0; u < XP; ++u) {
+            const int r = xr + 32 * u;
+            uint4 x = s.x[u];
+            if constexpr (ROWS)
+                if (s.x_left[u] >= s.x_len[u] || clip_factor(s.x_sq[u], a.clip_c) == 0.0f) x = make_uint4(0, 0, 0, 0);
+            const float scale = pow2_of(WEIGHTED && !ROWS ? max((int)s.scale[u] + s.power, 1) : (int)s.scale[u]);
+            const uint2 w0 = ck_bf16(x.x, scale), w1 = ck_bf16(x.y, scale), w2 = ck_bf16(x.z, scale), w3 = ck_bf16(x.w, scale);
+            char *to = lds + PLANES * PLANE + r * CK_ROW;
+            *reinterpret_cast<uint4 *>(to + (((2 * xp) ^ ((r & 3) << 2)) << 4)) = make_uint4(w0.x, w0.y, w1.x, w1.y);
+            *reinterpret_cast<uint4 *>(to + (((2 * xp + 1) ^ ((r & 3) << 2)) << 4)) = make_uint4(w2.x, w2.y, w3.x, w3.y);
+        }
+#pragma unroll
+        for (int u = 0; u < YP; ++u) {
             const int r = yr + 16 * u;
-            char *y = s + r * CK_ROW + ((yp ^ ((r & 3) << 2)) << 4);
+            char *to = lds + r * CK_ROW + ((yp ^ ((r & 3) << 2)) << 4);
+            float v[8];
             if constexpr (PLANES == 1) {
-                *reinterpret_cast<uint4 *>(y) = y_raw[u];
-            } else {
-                uint4 p[3];
-                split8(y_val[u], p);
+                *reinterpret_cast<uint4 *>(to) = s.y[u].w;
+                if (bias_here) {
+                    s.y[u].get(v);
 #pragma unroll
-                for (int q = 0; q < 3; ++q) *reinterpret_cast<uint4 *>(y + q * CK_PLANE) = p[q];
+                    for (int j = 0; j < 8; ++j) bias_sum[j] = WEIGHTED ? fmaf(s.f, v[j], bias_sum[j]) : bias_sum[j] + v[j];
+                }
+            } else {
+                s.y[u].get(v);
+                if constexpr (ROWS) {
+                    const float f = s.y_left[u] < s.y_len[u] ? clip_factor(s.y_sq[u], a.clip_c) : 0.0f;
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) v[j] = f == 0.0f ? 0.0f : v[j] * f;
+                }
+                uint4 p[3];
+                split8(v, p);
+#pragma unroll
+                for (int q = 0; q < 3; ++q) *reinterpret_cast<uint4 *>(to + q * PLANE) = p[q];
+                if (bias_here) {
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) bias_sum[j] += v[j];
+                }
             }
         }
     };
@@ -261,51 +266,58 @@ __global__ void __launch_bounds__(256, 2) ck_contract_kernel(const CkDenseArgs a
         for (int j = 0; j < 2; ++j)
 #pragma unroll
             for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.0f;
+    float unit = 1.0f;                                             // the sum's unit: m of the last example that was added
 
-    float unit = 1.0f;                                             // the sum's unit (m of the last example that was added)
-    if (c_begin < c_end) { fetch(c_begin); if (have) stage(0); }
-    bool now = have && c_begin < c_end, begins = f_first;
-    float m = f_m;
-    int buf = 0;
-    __syncthreads();
-    for (int c = c_begin; c < c_end; ++c) {
-        const bool more = c + 1 < c_end;
-        if (more) fetch(c + 1);
-        if (now) {
-            if (WEIGHTED && !ROWS && begins) {
-                const float ratio = unit / m;
-                unit = m;
-                if (ratio != 1.0f) {
+    struct Now { int rows; bool begins; float m; };                // of the chunk in LDS
+    auto compute = [&](const Now &now, int buf) {
+        if (now.rows <= 0) return;
+        if (WEIGHTED && !ROWS && now.begins) {
+            const float ratio = unit / now.m;
+            unit = now.m;
+            if (ratio != 1.0f) {
 #pragma unroll
-                    for (int i = 0; i < 2; ++i)
+                for (int i = 0; i < 2; ++i)
 #pragma unroll
-                        for (int j = 0; j < 2; ++j)
+                    for (int j = 0; j < 2; ++j)
 #pragma unroll
-                            for (int r = 0; r < 16; ++r) acc[i][j][r] *= ratio;
-                }
-            }
-            const char *s = ck_lds + buf * STAGE;
-#pragma unroll
-            for (int ks = 0; ks < CKC / 16; ++ks) {
-                bf16x8 vb[2];
-#pragma unroll
-                for (int j = 0; j < 2; ++j) vb[j] = operand(s + PLANES * CK_PLANE, wn * 64 + j * 32, ks);
-#pragma unroll
-                for (int q = 0; q < PLANES; ++q)
-#pragma unroll
-                    for (int i = 0; i < 2; ++i) {
-                        const bf16x8 va = operand(s + q * CK_PLANE, wm * 64 + i * 32, ks);
-#pragma unroll
-                        for (int j = 0; j < 2; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(va, vb[j], acc[i][j], 0, 0, 0);
-                    }
+                        for (int r = 0; r < 16; ++r) acc[i][j][r] *= ratio;
             }
         }
-        now = more && have;
-        begins = f_first;
-        m = f_m;
-        buf ^= 1;
-        if (now) stage(buf);
+        const char *s = ck_lds + buf * STAGE;
+#pragma unroll
+        for (int ks = 0; ks < CK / 16; ++ks) {
+            if (ks * 16 >= now.rows) break;
+            bf16x8 vb[2];
+#pragma unroll
+            for (int j = 0; j < 2; ++j) vb[j] = operand(s + PLANES * PLANE, wn * 64 + j * 32, ks);
+#pragma unroll
+            for (int q = 0; q < PLANES; ++q)
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    const bf16x8 va = operand(s + q * PLANE, wm * 64 + i * 32, ks);
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(va, vb[j], acc[i][j], 0, 0, 0);
+                }
+        }
+    };
+    // chunk c is in LDS buffer c & 1 (counted from the first), the two after it in registers; `next` holds c + 1 and takes c + 3
+    Slot s0, s1;
+    fetch(s0, c_begin);
+    fetch(s1, c_begin + 1);
+    Now now = {s0.rows, s0.begins, s0.m};
+    if (now.rows > 0) stage(s0, 0);
+    fetch(s0, c_begin + 2);
+    __syncthreads();
+    auto turn = [&](Slot &next, int buf, int c) {
+        compute(now, buf);
+        now = {next.rows, next.begins, next.m};
+        if (now.rows > 0) stage(next, buf ^ 1);
+        fetch(next, c + 3);
         __syncthreads();
+    };
+    for (int c = c_begin; c < c_end; c += 2) {
+        turn(s1, 0, c);
+        if (c + 1 < c_end) turn(s0, 1, c + 1);
     }
 
     float ss = 0.0f;
@@ -330,6 +342,24 @@ __global__ void __launch_bounds__(256, 2) ck_contract_kernel(const CkDenseArgs a
                 }
             }
         }
+    if (bias_here) {
+        float *sums = reinterpret_cast<float *>(ck_lds);           // (the last barrier is behind the last products)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) sums[yr * CT + yp * 8 + j] = bias_sum[j];
+        __syncthreads();
+        if (t < CT && o0 + t < a.cout) {
+            float v = 0.0f;
+#pragma unroll
+            for (int r = 0; r < 16; ++r) v += sums[r * CT + t];
+            if constexpr (WEIGHTED) {
+                float *out = a.out_b + (size_t)slot * a.stride_b + o0 + t;
+                *out = a.add ? *out + v : v;
+            } else {
+                ss += v * v;
+                if (a.stored) a.out_b[(size_t)slot * a.stride_b + o0 + t] = v;
+            }
+        }
+    }
     if constexpr (!WEIGHTED) {
         const float tot = block_sum<4>(ss, red);
         if (t == 0) a.partials[(size_t)slot * tiles + tile] = tot;
@@ -491,7 +521,7 @@ struct CkPlan {
     int gram_tiles;                  // tiles of 32 B tokens of an example
     int gram_b;
     size_t per_example;              // partial squared norms
-    int ranges, per_range, chunks;   // weighted
+    int ranges, per_range, chunks, cpe;   // weighted
     bool rows;
 };
 
@@ -501,30 +531,39 @@ int ck_tiles(int v) { return (v + CT - 1) / CT; }
 CkPlan ck_plan(const Geo &g, int mode)
 {
     CkPlan p = {};
-    const int tiles_o = ck_tiles(g.cout), columns = ck_tiles(g.cin) + g.has_bias;
+    const int tiles_o = ck_tiles(g.cout), tiles_k = ck_tiles(g.cin);
     if (mode == MODE_WEIGHTED) {
         // 32 rows hold several examples of a few tokens each, at three products for one
         p.rows = !g.bf16 || g.h < 16;
-        const long long chunks = p.rows ? ((long long)g.n * g.h + CKC - 1) / CKC : (long long)g.n * ((g.h + CKC - 1) / CKC);
+        const int chunk = ck_chunk(p.rows ? 3 : 1);
+        p.cpe = (g.h + chunk - 1) / chunk;
+        const long long chunks = p.rows ? ((long long)g.n * g.h + chunk - 1) / chunk : (long long)g.n * p.cpe;
         p.chunks = (int)chunks;
-        // ranges of the call's chunks until there are two workgroups for each compute unit; a range has eight chunks at least
-        const long long want = (512 + tiles_o * columns - 1) / (tiles_o * columns);
-        const long long ranges = std::max(1ll, std::min(want, chunks / 8));
+        // ranges of the call's chunks until there are two workgroups for each compute unit; a range has four chunks at least
+        const long long want = (512 + tiles_o * tiles_k - 1) / (tiles_o * tiles_k);
+        const long long ranges = std::max(1ll, std::min(want, chunks / 4));
         p.per_range = (int)((chunks + ranges - 1) / ranges);
         p.ranges = (int)((chunks + p.per_range - 1) / p.per_range);
         return p;
     }
-    p.per_example = (size_t)tiles_o * columns;
+    p.per_example = (size_t)tiles_o * tiles_k;
     if (mode == MODE_NORM && g.bf16) {
         p.gram_b = g.h <= 32 ? 1 : 2;
         p.gram_tiles = (g.h + 32 * p.gram_b - 1) / (32 * p.gram_b);
         const double pairs = 0.5 * p.gram_tiles * (p.gram_tiles + 1), side = 32.0 * p.gram_b;
         const double gram = pairs * side * side * ((double)g.cin + g.cout);
-        const double direct = (double)((g.h + CKC - 1) / CKC * CKC) * tiles_o * CT * (double)ck_tiles(g.cin) * CT;
-        p.gram = gram < direct;
+        const double direct = (double)((g.h + 15) / 16 * 16) * tiles_o * CT * (double)tiles_k * CT;
+        p.gram = 4 * gram < direct;
         if (p.gram) p.per_example = (size_t)p.gram_tiles * (p.gram_tiles + 1) / 2;
     }
     return p;
+}
+
+template <int PLANES, bool WEIGHTED, bool BF16>
+dp_status run_contract(bool aligned, dim3 grid, const CkDenseArgs &a, hipStream_t s)
+{
+    return aligned ? launch_lds<ck_contract_kernel<PLANES, WEIGHTED, BF16, true>>(grid, 256, 2 * ck_stage_bytes(PLANES), s, a)
+                   : launch_lds<ck_contract_kernel<PLANES, WEIGHTED, BF16, false>>(grid, 256, 2 * ck_stage_bytes(PLANES), s, a);
 }
 
 size_t align16(size_t b) { return (b + 15) & ~(size_t)15; }
@@ -549,12 +588,15 @@ dp_status launch_checkpoint_dense(const Geo &g, int mode, const uint8_t *codes, 
     CkDenseArgs a = {};
     a.codes = codes; a.scales = scales; a.dy = dy; a.lengths = lengths;
     a.n = g.n; a.tokens = g.h; a.cin = g.cin; a.cout = g.cout; a.pitch = ck_pitch(g.cin);
-    a.dy_bf16 = g.bf16; a.has_bias = g.has_bias;
-    a.tiles_o = ck_tiles(g.cout); a.tiles_k = ck_tiles(g.cin); a.columns = a.tiles_k + g.has_bias;
-    const size_t tiles = (size_t)a.tiles_o * a.columns;
+    a.has_bias = g.has_bias;
+    a.tiles_o = ck_tiles(g.cout); a.tiles_k = ck_tiles(g.cin);
+    const bool aligned = g.bf16 ? g.cout % 8 == 0 : g.cout % 4 == 0;
+    // workgroups of all XCDs alike (the kernel's map), those beyond the last one end at once
+    auto grid = [&](int slots) { return dim3((unsigned)(((size_t)a.tiles_o * a.tiles_k * slots + 7) / 8 * 8)); };
+    dp_status st;
     if (mode == MODE_WEIGHTED) {
         a.group_sqnorm = group_sqnorm; a.clip_c = clip_c;
-        a.chunks = p.chunks; a.per_range = p.per_range;
+        a.chunks = p.chunks; a.per_range = p.per_range; a.cpe = p.cpe; a.slots = p.ranges;
         a.add = p.ranges == 1;
         a.out_w = out_w; a.out_b = out_b;
         if (p.ranges > 1) {
@@ -563,10 +605,10 @@ dp_status launch_checkpoint_dense(const Geo &g, int mode, const uint8_t *codes, 
             a.out_b = a.out_w + p.ranges * a.stride_w;
             a.stride_b = align4(g.pb);
         }
-        const dim3 grid((unsigned)(tiles * p.ranges));
         profile_begin(s);
-        dp_status st = p.rows ? launch_lds<ck_contract_kernel<3, true>>(grid, 256, 2 * 4 * CK_PLANE, s, a)
-                              : launch_lds<ck_contract_kernel<1, true>>(grid, 256, 2 * 2 * CK_PLANE, s, a);
+        if (!p.rows) st = run_contract<1, true, true>(aligned, grid(p.ranges), a, s);
+        else if (g.bf16) st = run_contract<3, true, true>(aligned, grid(p.ranges), a, s);
+        else st = run_contract<3, true, false>(aligned, grid(p.ranges), a, s);
         profile_end(s);
         if (st != DP_OK || p.ranges == 1) return st;
         hipLaunchKernelGGL(ck_ranges_kernel, dim3((unsigned)((g.pw + 1023) / 1024)), dim3(256), 0, s, a.out_w, a.stride_w, p.ranges, g.pw, out_w);
@@ -579,16 +621,16 @@ dp_status launch_checkpoint_dense(const Geo &g, int mode, const uint8_t *codes, 
     a.out_w = out_w; a.out_b = out_b;
     a.stride_w = out_stride ? out_stride : g.pw;
     a.stride_b = out_stride ? out_stride : g.pb;
-    dp_status st;
+    a.slots = g.n;
     profile_begin(s);
     if (p.gram) {
-        const dim3 grid((unsigned)(g.n * p.per_example));
-        st = p.gram_b == 1 ? launch_lds<ck_gram_kernel<1, 8>>(grid, 512, 8 * 16 * 64 * 4, s, a, (int)p.per_example)
-                           : launch_lds<ck_gram_kernel<2, 4>>(grid, 256, 4 * 64 * 64 * 4, s, a, (int)p.per_example);
+        const dim3 blocks((unsigned)(g.n * p.per_example));
+        st = p.gram_b == 1 ? launch_lds<ck_gram_kernel<1, 8>>(blocks, 512, 8 * 16 * 64 * 4, s, a, (int)p.per_example)
+                           : launch_lds<ck_gram_kernel<2, 4>>(blocks, 256, 4 * 64 * 64 * 4, s, a, (int)p.per_example);
+    } else if (g.bf16) {
+        st = run_contract<1, false, true>(aligned, grid(g.n), a, s);
     } else {
-        const dim3 grid((unsigned)(tiles * g.n));
-        st = g.bf16 ? launch_lds<ck_contract_kernel<1, false>>(grid, 256, 2 * 2 * CK_PLANE, s, a)
-                    : launch_lds<ck_contract_kernel<3, false>>(grid, 256, 2 * 4 * CK_PLANE, s, a);
+        st = run_contract<3, false, false>(aligned, grid(g.n), a, s);
     }
     profile_end(s);
     if (st != DP_OK || !sqnorm) return st;

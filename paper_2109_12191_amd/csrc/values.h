@@ -60,6 +60,23 @@ __device__ __forceinline__ uint32_t pack_bf16(float a, float b)
     return __builtin_bit_cast(uint32_t, __builtin_convertvector(p, bf16x2_t));       // nearest, ties to even
 }
 
+// Eight values as they were loaded.
+template <bool BF16> struct Raw8;
+template <> struct Raw8<true> {
+    uint4 w;
+    __device__ __forceinline__ void load(const void *p, size_t at, int count) { w = load8(static_cast<const uint16_t *>(p) + at, count); }
+    __device__ __forceinline__ void get(float (&v)[8]) const { widen8(w, v); }
+};
+template <> struct Raw8<false> {
+    float w[8];
+    __device__ __forceinline__ void load(const void *p, size_t at, int count) { load8f(static_cast<const float *>(p) + at, count, w); }
+    __device__ __forceinline__ void get(float (&v)[8]) const
+    {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = w[i];
+    }
+};
+
 // Eight values to memory, the first `count` of them.
 __device__ __forceinline__ void store8(uint16_t *p, int count, const float (&v)[8])
 {
