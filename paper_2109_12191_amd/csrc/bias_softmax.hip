@@ -10,7 +10,10 @@
 // example and head.  Forward, it makes the biases of the distances in between once, in LDS.  Backward, a wave adds its rows'
 // dz by distance into sums of its own in LDS (the lanes' distances differ, so no two lanes meet in one place and the order is fixed), dz beyond
 // `far` into registers, and the workgroup adds up the runs of its buckets at the end; bias_table_kernel adds up workgroups.
-// Distance d lies in plane d mod 8 of eight: lanes eight keys apart read neighbouring words.
+// A lane holds runs of eight keys, so the distances of a run go down by one from word to word: slot d + low + 16 lies in plane (slot mod 8)
+// of eight, at slot / 8, lanes eight keys apart meet neighbouring words of a plane, and where a run's eight values lie is one number for the
+// lane and eight that all lanes share.  The slots before -low and after far, which a run that straddles the border reaches, hold what
+// belongs to the border's bucket.
 //
 // A row is held in registers between its two passes (its sums and its results), by one wave up to 2048 keys and by four up to
 // 16384; longer ones are read twice.
@@ -32,7 +35,7 @@ struct BiasArgs {
     float scale;
     size_t row_stride;
     int near, border_count, far, low;    // low: distances from -low down are one bucket (0 where there is one side)
-    int plane;                           // words of a plane of distances
+    int plane, last;                     // words of a plane of distances; slots at `last - 1` and beyond in each are beyond `far`
     int rows, blocks;                    // rows of a workgroup, workgroups of a head
     int borders[BIAS_BORDERS];
 };
@@ -51,13 +54,39 @@ __device__ __forceinline__ int bias_bucket_of(const BiasArgs &a, int d)
     return side + b;
 }
 
-__device__ __forceinline__ int bias_word(const BiasArgs &a, int index) { return (index & 7) * a.plane + (index >> 3); }
-
-__device__ __forceinline__ float wave_max(float v)
-{
+// Where the values of a run that starts at distance d lie: value i at word `lane` + `shared[i]`.
+struct RunWords {
+    int lane, shared[8];
+    __device__ __forceinline__ static int slot(const BiasArgs &a, int d) { return d + a.low + 16; }
+    // the part that all lanes share, from any lane's distance (they differ by multiples of eight)
+    __device__ __forceinline__ void set_shared(const BiasArgs &a, int d)
+    {
+        const int m = slot(a, d) & 7;
 #pragma unroll
-    for (int off = 32; off > 0; off >>= 1) v = fmaxf(v, __shfl_xor(v, off, 64));
-    return v;
+        for (int i = 0; i < 8; ++i) shared[i] = ((m - i) & 7) * a.plane + ((m - i) >> 31);      // (one row earlier where i > m)
+    }
+};
+__device__ __forceinline__ int bias_word(const BiasArgs &a, int slot) { return (slot & 7) * a.plane + (slot >> 3); }
+
+// Sum and largest of a wave's values, in every lane, by data-parallel-primitive moves.
+__device__ __forceinline__ float wave_all_sum(float v)
+{
+    return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, wave_sum_last_lane(v)), 63));
+}
+__device__ __forceinline__ float wave_all_max(float v)
+{
+    auto step = [](float x, auto ctrl, auto rows) {              // lanes without a source keep their own value
+        const int bits = __builtin_bit_cast(int, x);
+        return fmaxf(x, __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(bits, bits, decltype(ctrl)::value, decltype(rows)::value, 0xf, false)));
+    };
+    typedef std::integral_constant<int, 0xf> all_rows;
+    v = step(v, std::integral_constant<int, 0x111>{}, all_rows{});
+    v = step(v, std::integral_constant<int, 0x112>{}, all_rows{});
+    v = step(v, std::integral_constant<int, 0x114>{}, all_rows{});
+    v = step(v, std::integral_constant<int, 0x118>{}, all_rows{});
+    v = step(v, std::integral_constant<int, 0x142>{}, std::integral_constant<int, 0xa>{});
+    v = step(v, std::integral_constant<int, 0x143>{}, std::integral_constant<int, 0xc>{});
+    return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), 63));
 }
 
 // What a workgroup works on.
@@ -93,7 +122,7 @@ __device__ __forceinline__ int bias_end(const BiasArgs &a, const Rows &r, int q)
 template <int TPR, bool MAX>
 __device__ __forceinline__ float row_reduce(float v, float *red)
 {
-    v = MAX ? wave_max(v) : wave_sum(v);
+    v = MAX ? wave_all_max(v) : wave_all_sum(v);
     if constexpr (TPR > 64) {
         __syncthreads();
         if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
@@ -105,57 +134,135 @@ __device__ __forceinline__ float row_reduce(float v, float *red)
     return v;
 }
 
-// NV > 0: a thread holds NV runs of eight keys, run j at 8 (thread + TPR j).  NV == 0: rows of any length, read twice.
-template <bool BF16, int TPR, int NV>
-__global__ void __launch_bounds__(256) bias_softmax_kernel(const BiasArgs a)
-{
+// The rows of a tensor as runs of eight keys.  WORDS: fp32 rows, and bf16 rows that begin at whole dwords and have an even number of keys: a row is
+// a buffer that ends where the keys that count do (or the row), and the 16-byte accesses of a run leave out, dword by dword, what lies
+// beyond: no branch, and masked keys are not read but for the other half of a last dword.  Else value by value where a run is cut.
+// What a cut run holds after its keys is unspecified.
+typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
+template <bool BF16, bool WORDS>
+struct RowOf {
     typedef typename In<BF16>::type E;
-    extern __shared__ float bias_lds[];
-    __shared__ float red[4];
-    const Rows r = bias_rows(a);
-    for (int i = threadIdx.x; i <= a.low + a.far; i += 256)
-        bias_lds[bias_word(a, i)] = a.table[(size_t)bias_bucket_of(a, i - a.low) * a.heads + r.head];
-    __syncthreads();
-    const float bias_far = bias_lds[bias_word(a, a.low + a.far)], bias_low = bias_lds[bias_word(a, 0)];
-    const int t = threadIdx.x % TPR, wave_first = t & ~63;
-
-    // the scores of a run of eight keys that starts at key k (the run of the wave's first lane at kw), as logits
-    auto logits = [&](const Raw8<BF16> &raw, int k, int kw, int position, int end, float (&z)[8]) {
-        raw.get(z);
-        const int most = position - kw, least = most - 511;        // distances of the wave's runs
-        if (least >= a.far || most <= -a.low) {
-            const float b = least >= a.far ? bias_far : bias_low;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) z[i] = fmaf(z[i], a.scale, b);
+    __amdgpu_buffer_rsrc_t buffer;
+    E *first;
+    int keys;
+    __device__ __forceinline__ RowOf(void *p, size_t row, int count) : first(static_cast<E *>(p) + row), keys(count)
+    {
+        if constexpr (WORDS) buffer = __builtin_amdgcn_make_buffer_rsrc(first, 0, (int)(((unsigned)count * (unsigned)sizeof(E) + 3u) & ~3u), 0x00020000);
+    }
+    __device__ __forceinline__ void load(Raw8<BF16> &raw, int k) const
+    {
+        if constexpr (!WORDS) {
+            raw.load(first, (size_t)k, keys - k);
         } else {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const int at = min(max(position - k - i, -a.low), a.far) + a.low;
-                z[i] = fmaf(z[i], a.scale, bias_lds[bias_word(a, at)]);
+            const u32x4_t v = __builtin_bit_cast(u32x4_t, __builtin_amdgcn_raw_buffer_load_b128(buffer, k * (int)sizeof(E), 0, 0));
+            if constexpr (BF16) {
+                raw.w = make_uint4(v.x, v.y, v.z, v.w);
+            } else {
+                const u32x4_t w = __builtin_bit_cast(u32x4_t, __builtin_amdgcn_raw_buffer_load_b128(buffer, k * (int)sizeof(E) + 16, 0, 0));
+                raw.w[0] = __uint_as_float(v.x); raw.w[1] = __uint_as_float(v.y); raw.w[2] = __uint_as_float(v.z); raw.w[3] = __uint_as_float(v.w);
+                raw.w[4] = __uint_as_float(w.x); raw.w[5] = __uint_as_float(w.y); raw.w[6] = __uint_as_float(w.z); raw.w[7] = __uint_as_float(w.w);
             }
         }
-        if (end - k < 8) {
+    }
+    __device__ __forceinline__ void store(int k, const float (&v)[8]) const
+    {
+        if constexpr (!WORDS) {
+            if (k < keys) store8(first + k, keys - k, v);
+        } else if constexpr (BF16) {
+            const u32x4_t w = {pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7])};
+            __builtin_amdgcn_raw_buffer_store_b128(w, buffer, k * (int)sizeof(E), 0, 0);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const u32x4_t w = {__float_as_uint(v[4 * i]), __float_as_uint(v[4 * i + 1]), __float_as_uint(v[4 * i + 2]), __float_as_uint(v[4 * i + 3])};
+                __builtin_amdgcn_raw_buffer_store_b128(w, buffer, k * (int)sizeof(E) + 16 * i, 0, 0);
+            }
+        }
+    }
+};
+
+// The sums of a workgroup's four waves, by distance in LDS and beyond the borders in registers, by bucket into its place of the workspace: a
+// wave takes every fourth bucket, its lanes the distances of the bucket's run.
+__device__ __forceinline__ void bias_bucket_sums(const BiasArgs &a, const float *lds, float sum_far, float sum_low, float (&ends)[4][2])
+{
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const float far_wave = wave_all_sum(sum_far), low_wave = wave_all_sum(sum_low);
+    if (lane == 0) { ends[wave][0] = far_wave; ends[wave][1] = low_wave; }
+    __syncthreads();
+    float *part = a.partials + (size_t)blockIdx.x * a.buckets;
+    const int side_buckets = a.bidirectional ? a.buckets / 2 : a.buckets;
+    auto start = [&](int m) { return m <= a.near ? m : a.borders[m - a.near - 1]; };       // smallest magnitude of a side's bucket m
+    for (int b = wave; b < a.buckets; b += 4) {
+        const bool after = b >= side_buckets;                      // keys after the query
+        const int m = after ? b - side_buckets : b;
+        const bool outer = m == side_buckets - 1, inner = !a.bidirectional && b == 0;
+        // magnitudes lo .. hi; the outer bucket's and, with one side, bucket 0's run on into the slots beyond the border (runs reach 13 beyond)
+        const int hi = outer ? a.far + 13 : start(m + 1) - 1, lo = inner ? -13 : after ? max(start(m), 1) : start(m);
+        float s = 0.0f;
+        for (int d = lo + lane; d <= hi; d += 64) {
+            const int word = bias_word(a, RunWords::slot(a, after ? -d : d));
+#pragma unroll
+            for (int w = 0; w < 4; ++w) s += lds[w * 8 * a.plane + word];
+        }
+        s = wave_all_sum(s);
+        if (outer || inner) {
+            const int which = after || inner ? 1 : 0;
+            s += ends[0][which] + ends[1][which] + ends[2][which] + ends[3][which];
+        }
+        if (lane == 0) part[b] = s;
+    }
+}
+
+// NV > 0: a thread holds NV runs of eight keys, run j at 8 (thread + TPR j), and the next row's are on their way while it works on one.
+// NV == 0: rows of any length, read twice.
+template <bool BF16, bool WORDS, int TPR, int NV>
+__global__ void __launch_bounds__(256) bias_softmax_kernel(const BiasArgs a)
+{
+    extern __shared__ float bias_lds[];
+    __shared__ float red[4];
+    typedef RowOf<BF16, WORDS> Row;
+    const Rows r = bias_rows(a);
+    for (int i = threadIdx.x; i < 8 * a.plane; i += 256)
+        bias_lds[bias_word(a, i)] = a.table[(size_t)bias_bucket_of(a, min(max(i - 16 - a.low, -a.low), a.far)) * a.heads + r.head];
+    __syncthreads();
+    const int t = threadIdx.x % TPR;
+    const int wave_first = __builtin_amdgcn_readfirstlane(t & ~63), row_first = __builtin_amdgcn_readfirstlane(threadIdx.x / TPR);
+    constexpr int STEP = 256 / TPR;                                // rows that are worked on together
+
+    // the scores of a run of eight keys from key k on, as logits; `whole`: the same for the wave, every run of it counts to its end
+    RunWords at;
+    auto logits = [&](const Raw8<BF16> &raw, int k, bool whole, int position, int end, float (&z)[8]) {
+        raw.get(z);
+        at.lane = min(max(RunWords::slot(a, position - k) >> 3, 1), a.last);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) z[i] = fmaf(z[i], a.scale, bias_lds[at.lane + at.shared[i]]);
+        if (!whole) {
+            asm volatile("");                                      // (a branch: most runs are whole)
 #pragma unroll
             for (int i = 0; i < 8; ++i) z[i] = k + i < end ? z[i] : -INFINITY;
         }
     };
 
-    for (int q = r.q0 + (int)(threadIdx.x / TPR); q < r.q1; q += 256 / TPR) {
-        const int end = bias_end(a, r, q), position = r.first + q;
-        const size_t row = (r.base + q) * a.row_stride;
-        E *out = static_cast<E *>(a.out) + row;
-        if constexpr (NV > 0) {
-            Raw8<BF16> raw[NV];
-            float z[NV][8];
+    if constexpr (NV > 0) {
+        Raw8<BF16> raw[NV];
+        auto load_row = [&](int q) {
+            const Row row(const_cast<void *>(a.in), (r.base + q) * a.row_stride, bias_end(a, r, q));
 #pragma unroll
-            for (int j = 0; j < NV; ++j) raw[j].load(a.in, row + 8 * (t + TPR * j), end - 8 * (t + TPR * j));
+            for (int j = 0; j < NV; ++j) row.load(raw[j], 8 * (t + TPR * j));
+        };
+        if (r.q0 + row_first < r.q1) load_row(r.q0 + row_first);
+        for (int q = r.q0 + row_first; q < r.q1; q += STEP) {
+            const int end = bias_end(a, r, q), position = r.first + q;
+            at.set_shared(a, position);
+            float z[NV][8];
             float top = -INFINITY;
 #pragma unroll
-            for (int j = 0; j < NV; ++j) {
-                logits(raw[j], 8 * (t + TPR * j), 8 * (wave_first + TPR * j), position, end, z[j]);
+            for (int j = 0; j < NV; ++j) logits(raw[j], 8 * (t + TPR * j), 8 * (wave_first + TPR * j + 64) <= end, position, end, z[j]);
+            if (q + STEP < r.q1) load_row(q + STEP);
+#pragma unroll
+            for (int j = 0; j < NV; ++j)
 #pragma unroll
                 for (int i = 0; i < 8; ++i) top = fmaxf(top, z[j][i]);
-            }
             top = row_reduce<TPR, true>(top, red);
             top = top == -INFINITY ? 0.0f : top;
             float sum = 0.0f;
@@ -164,21 +271,26 @@ __global__ void __launch_bounds__(256) bias_softmax_kernel(const BiasArgs a)
 #pragma unroll
                 for (int i = 0; i < 8; ++i) { z[j][i] = exp_of(z[j][i] - top); sum += z[j][i]; }
             sum = row_reduce<TPR, false>(sum, red);
-            const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+            const float inv = sum == 0.0f ? 0.0f : __builtin_amdgcn_rcpf(sum);     // good to a step
+            const Row out(a.out, (r.base + q) * a.row_stride, a.keys);
 #pragma unroll
             for (int j = 0; j < NV; ++j) {
-                const int k = 8 * (t + TPR * j);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) z[j][i] *= inv;
-                if (k < a.keys) store8(out + k, a.keys - k, z[j]);
+                out.store(8 * (t + TPR * j), z[j]);
             }
-        } else {
+        }
+    } else {
+        for (int q = r.q0; q < r.q1; ++q) {
+            const int end = bias_end(a, r, q), position = r.first + q;
+            const RowOf<BF16, false> row(const_cast<void *>(a.in), (r.base + q) * a.row_stride, end), out(a.out, (r.base + q) * a.row_stride, a.keys);
+            at.set_shared(a, position);
             float top = -INFINITY, sum = 0.0f;
             for (int k = 8 * t; k < end; k += 8 * TPR) {
                 Raw8<BF16> raw;
                 float z[8];
-                raw.load(a.in, row + k, end - k);
-                logits(raw, k, k - 8 * (t - wave_first), position, end, z);
+                row.load(raw, k);
+                logits(raw, k, false, position, end, z);
                 float here = z[0];
 #pragma unroll
                 for (int i = 1; i < 8; ++i) here = fmaxf(here, z[i]);
@@ -190,242 +302,455 @@ __global__ void __launch_bounds__(256) bias_softmax_kernel(const BiasArgs a)
             }
             const float best = row_reduce<TPR, true>(top, red), base = best == -INFINITY ? 0.0f : best;
             sum = row_reduce<TPR, false>(sum * exp_of(top - base), red);
-            const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+            const float inv = sum == 0.0f ? 0.0f : __builtin_amdgcn_rcpf(sum);
             for (int k = 8 * t; k < a.keys; k += 8 * TPR) {
                 Raw8<BF16> raw;
                 float z[8];
-                raw.load(a.in, row + k, end - k);
-                logits(raw, k, k - 8 * (t - wave_first), position, end, z);
+                row.load(raw, k);
+                logits(raw, k, false, position, end, z);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) z[i] = exp_of(z[i] - base) * inv;
-                store8(out + k, a.keys - k, z);
+                out.store(k, z);
             }
         }
     }
 }
 
-template <bool BF16, int TPR, int NV>
+template <bool BF16, bool WORDS, int TPR, int NV>
 __global__ void __launch_bounds__(256) bias_backward_kernel(const BiasArgs a)
 {
-    typedef typename In<BF16>::type E;
     extern __shared__ float bias_lds[];                            // a wave's sums by distance, four times
     __shared__ float red[4], ends[4][2];
+    typedef RowOf<BF16, WORDS> Row;
+    const Rows r = bias_rows(a);
+    const int wave = threadIdx.x >> 6;
+    for (int i = threadIdx.x; i < 4 * 8 * a.plane; i += 256) bias_lds[i] = 0.0f;
+    __syncthreads();
+    float *const mine = bias_lds + wave * 8 * a.plane;
+    const int t = threadIdx.x % TPR;
+    const int wave_first = __builtin_amdgcn_readfirstlane(t & ~63), row_first = __builtin_amdgcn_readfirstlane(threadIdx.x / TPR);
+    constexpr int STEP = 256 / TPR;
+    float sum_far = 0.0f, sum_low = 0.0f;
+
+    // zeros at the places of a run that do not count; `whole`: the same for the wave, there is none
+    auto cut = [&](float (&v)[8], int k, bool whole, int end) {
+        if (!whole) {
+            asm volatile("");                                      // (a branch: most runs are whole)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = k + i < end ? v[i] : 0.0f;
+        }
+    };
+    // dz of a run from key k on into the sums
+    RunWords at;
+    auto add = [&](const float (&dz)[8], int k, int position) {
+        const int d = position - k;                                // .. d - 7
+        if (d - 7 >= a.far || d <= -a.low) {
+            float s = dz[0];
+#pragma unroll
+            for (int i = 1; i < 8; ++i) s += dz[i];
+            sum_far += d > 0 ? s : 0.0f;
+            sum_low += d > 0 ? 0.0f : s;
+        } else {
+            at.lane = RunWords::slot(a, d) >> 3;
+            float sum[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) sum[i] = mine[at.lane + at.shared[i]];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) mine[at.lane + at.shared[i]] = sum[i] + dz[i];
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");  // the next row's lanes meet other lanes' words
+        }
+    };
+
+    if constexpr (NV > 0) {
+        Raw8<BF16> rp[NV], rd[NV];
+        auto load_row = [&](int q) {
+            const int end = bias_end(a, r, q);
+            const size_t row = (r.base + q) * a.row_stride;
+            const Row p(const_cast<void *>(a.in), row, end), d(const_cast<void *>(a.in2), row, end);
+#pragma unroll
+            for (int j = 0; j < NV; ++j) { p.load(rp[j], 8 * (t + TPR * j)); d.load(rd[j], 8 * (t + TPR * j)); }
+        };
+        if (r.q0 + row_first < r.q1) load_row(r.q0 + row_first);
+        for (int q = r.q0 + row_first; q < r.q1; q += STEP) {
+            const int end = bias_end(a, r, q), position = r.first + q;
+            at.set_shared(a, position);
+            float p[NV][8], d[NV][8];
+            float dot = 0.0f;
+#pragma unroll
+            for (int j = 0; j < NV; ++j) {
+                const int k = 8 * (t + TPR * j);
+                const bool whole = 8 * (wave_first + TPR * j + 64) <= end;
+                rp[j].get(p[j]); rd[j].get(d[j]);
+                cut(p[j], k, whole, end);
+                cut(d[j], k, whole, end);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) dot = fmaf(p[j][i], d[j][i], dot);
+            }
+            if (q + STEP < r.q1) load_row(q + STEP);
+            dot = row_reduce<TPR, false>(dot, red);
+            const bool broken = !(fabsf(dot) < INFINITY);          // its places that do not count are zeros all the same
+            const Row out(a.out, (r.base + q) * a.row_stride, a.keys);
+#pragma unroll
+            for (int j = 0; j < NV; ++j) {
+                const int k = 8 * (t + TPR * j);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) p[j][i] *= d[j][i] - dot;
+                cut(p[j], k, !broken, end);
+                add(p[j], k, position);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) p[j][i] *= a.scale;
+                out.store(k, p[j]);
+            }
+        }
+    } else {
+        for (int q = r.q0; q < r.q1; ++q) {
+            const int end = bias_end(a, r, q), position = r.first + q;
+            const size_t row = (r.base + q) * a.row_stride;
+            const RowOf<BF16, false> rows_p(const_cast<void *>(a.in), row, end), rows_d(const_cast<void *>(a.in2), row, end), out(a.out, row, a.keys);
+            at.set_shared(a, position);
+            float dot = 0.0f;
+            for (int k = 8 * t; k < end; k += 8 * TPR) {
+                Raw8<BF16> rp, rd;
+                float p[8], d[8];
+                rows_p.load(rp, k); rows_d.load(rd, k);
+                rp.get(p); rd.get(d);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) dot = fmaf(p[i], d[i], dot);
+            }
+            dot = row_reduce<TPR, false>(dot, red);
+            for (int k = 8 * t; k < a.keys; k += 8 * TPR) {
+                Raw8<BF16> rp, rd;
+                float p[8], d[8];
+                rows_p.load(rp, k); rows_d.load(rd, k);
+                rp.get(p); rd.get(d);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) p[i] *= d[i] - dot;
+                cut(p, k, false, end);
+                if (k < end) add(p, k, position);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) p[i] *= a.scale;
+                out.store(k, p);
+            }
+        }
+    }
+
+    bias_bucket_sums(a, bias_lds, sum_far, sum_low, ends);
+}
+
+// ---- rows of at most 256 keys: TPR lanes of a wave to a row, 64 / TPR rows of a wave together, and eight rows of each of these in turn.  The
+// rows of a wave lie eight apart, so that the words of their runs have the shared part in common (RunWords).
+
+// Sum or largest of the TPR lanes of a row, in each of them.
+template <int TPR, bool MAX>
+__device__ __forceinline__ float lanes_reduce(float v)
+{
+    auto step = [](float x, auto ctrl) {
+        const float y = __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), decltype(ctrl)::value, 0xf, 0xf, true));
+        return MAX ? fmaxf(x, y) : x + y;
+    };
+    v = step(v, std::integral_constant<int, 0xB1>{});              // lane ^ 1
+    v = step(v, std::integral_constant<int, 0x4E>{});              // lane ^ 2
+    v = step(v, std::integral_constant<int, 0x141>{});             // the other four of eight
+    if constexpr (TPR >= 16) v = step(v, std::integral_constant<int, 0x140>{});    // the other eight of sixteen
+    if constexpr (TPR >= 32) {
+        const float y = __shfl_xor(v, 16, 64);
+        v = MAX ? fmaxf(v, y) : v + y;
+    }
+    return v;
+}
+
+// A workgroup's rows of a tensor, each lane with a run of a row of its own.  WORDS: runs are 16-byte pieces that lie in their row altogether or
+// not at all (bf16: keys in eights; fp32: in fours; rows at whole dwords), by buffer accesses, left out by an offset beyond the buffer.
+template <bool BF16, bool WORDS>
+struct NarrowRows {
+    typedef typename In<BF16>::type E;
+    __amdgpu_buffer_rsrc_t buffer;
+    E *first;
+    size_t stride;
+    int keys;
+    __device__ __forceinline__ NarrowRows(void *p, const BiasArgs &a, const Rows &r) : first(static_cast<E *>(p) + (r.base + r.q0) * a.row_stride), stride(a.row_stride), keys(a.keys)
+    {
+        if constexpr (WORDS) buffer = __builtin_amdgcn_make_buffer_rsrc(first, 0, (int)(((r.q1 - r.q0 - 1) * (unsigned)stride + (unsigned)keys) * (unsigned)sizeof(E)), 0x00020000);
+    }
+    // row q of the workgroup's, keys k .. k + 7, of which those before `end` count; cut runs hold anything after them
+    __device__ __forceinline__ void load(Raw8<BF16> &raw, int q, int k, int end) const
+    {
+        if constexpr (!WORDS) {
+            raw.load(first, (size_t)q * stride + k, end - k);
+        } else {
+            const unsigned at = ((unsigned)q * (unsigned)stride + (unsigned)k) * (unsigned)sizeof(E);
+            const u32x4_t v = __builtin_bit_cast(u32x4_t, __builtin_amdgcn_raw_buffer_load_b128(buffer, k < end ? at : NOWHERE, 0, 0));
+            if constexpr (BF16) {
+                raw.w = make_uint4(v.x, v.y, v.z, v.w);
+            } else {
+                const u32x4_t w = __builtin_bit_cast(u32x4_t, __builtin_amdgcn_raw_buffer_load_b128(buffer, k + 4 < end ? at + 16 : NOWHERE, 0, 0));
+                raw.w[0] = __uint_as_float(v.x); raw.w[1] = __uint_as_float(v.y); raw.w[2] = __uint_as_float(v.z); raw.w[3] = __uint_as_float(v.w);
+                raw.w[4] = __uint_as_float(w.x); raw.w[5] = __uint_as_float(w.y); raw.w[6] = __uint_as_float(w.z); raw.w[7] = __uint_as_float(w.w);
+            }
+        }
+    }
+    __device__ __forceinline__ void store(bool there, int q, int k, const float (&v)[8]) const
+    {
+        if constexpr (!WORDS) {
+            if (there && k < keys) store8(first + (size_t)q * stride + k, keys - k, v);
+        } else {
+            const unsigned at = ((unsigned)q * (unsigned)stride + (unsigned)k) * (unsigned)sizeof(E);
+            if constexpr (BF16) {
+                const u32x4_t w = {pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7])};
+                __builtin_amdgcn_raw_buffer_store_b128(w, buffer, there && k < keys ? at : NOWHERE, 0, 0);
+            } else {
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    const u32x4_t w = {__float_as_uint(v[4 * i]), __float_as_uint(v[4 * i + 1]), __float_as_uint(v[4 * i + 2]), __float_as_uint(v[4 * i + 3])};
+                    __builtin_amdgcn_raw_buffer_store_b128(w, buffer, there && k + 4 * i < keys ? at + 16 * i : NOWHERE, 0, 0);
+                }
+            }
+        }
+    }
+    static constexpr unsigned NOWHERE = 0xFFFFFFE0u;
+};
+
+template <bool BF16, bool WORDS, int TPR>
+__global__ void __launch_bounds__(256) bias_softmax_narrow_kernel(const BiasArgs a)
+{
+    extern __shared__ float bias_lds[];
+    const Rows r = bias_rows(a);
+    for (int i = threadIdx.x; i < 8 * a.plane; i += 256)
+        bias_lds[bias_word(a, i)] = a.table[(size_t)bias_bucket_of(a, min(max(i - 16 - a.low, -a.low), a.far)) * a.heads + r.head];
+    __syncthreads();
+    const int k = 8 * (threadIdx.x % TPR), row0 = 8 * (threadIdx.x / TPR);         // of the workgroup's rows: row0 .. row0 + 7
+    const NarrowRows<BF16, WORDS> in(const_cast<void *>(a.in), a, r), out(a.out, a, r);
+    auto end_of = [&](int row) { return r.q0 + row < r.q1 ? bias_end(a, r, r.q0 + row) : 0; };
+    Raw8<BF16> raw;
+    in.load(raw, row0, k, end_of(row0));
+    RunWords at;
+    for (int s = 0; s < 8; ++s) {
+        const int row = row0 + s, end = end_of(row), position = r.first + r.q0 + row;
+        at.set_shared(a, r.first + r.q0 + s);
+        at.lane = min(max(RunWords::slot(a, position - k) >> 3, 1), a.last);
+        float z[8];
+        raw.get(z);
+        if (s < 7) in.load(raw, row + 1, k, end_of(row + 1));      // on its way during this row
+        float top = -INFINITY;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            z[i] = fmaf(z[i], a.scale, bias_lds[at.lane + at.shared[i]]);
+            z[i] = k + i < end ? z[i] : -INFINITY;
+            top = fmaxf(top, z[i]);
+        }
+        top = lanes_reduce<TPR, true>(top);
+        top = top == -INFINITY ? 0.0f : top;
+        float sum = 0.0f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) { z[i] = exp_of(z[i] - top); sum += z[i]; }
+        sum = lanes_reduce<TPR, false>(sum);
+        const float inv = sum == 0.0f ? 0.0f : __builtin_amdgcn_rcpf(sum);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) z[i] *= inv;
+        out.store(r.q0 + row < r.q1, row, k, z);
+    }
+}
+
+// Backward: a lane's runs of its eight rows meet fifteen distances, row s's key i that of s - i; their sums stay in registers and go into the wave's
+// words once, rows eight apart (whose runs have distances in common) one after the other.
+template <bool BF16, bool WORDS, int TPR>
+__global__ void __launch_bounds__(256) bias_backward_narrow_kernel(const BiasArgs a)
+{
+    extern __shared__ float bias_lds[];
+    __shared__ float ends[4][2];
     const Rows r = bias_rows(a);
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     for (int i = threadIdx.x; i < 4 * 8 * a.plane; i += 256) bias_lds[i] = 0.0f;
     __syncthreads();
     float *const mine = bias_lds + wave * 8 * a.plane;
-    const int t = threadIdx.x % TPR, wave_first = t & ~63;
+    const int k = 8 * (threadIdx.x % TPR), row0 = 8 * (threadIdx.x / TPR);
+    const NarrowRows<BF16, WORDS> probs(const_cast<void *>(a.in), a, r), dprobs(const_cast<void *>(a.in2), a, r), out(a.out, a, r);
+    auto end_of = [&](int row) { return r.q0 + row < r.q1 ? bias_end(a, r, r.q0 + row) : 0; };
+    Raw8<BF16> rp, rd;
+    probs.load(rp, row0, k, end_of(row0));
+    dprobs.load(rd, row0, k, end_of(row0));
+    float line[15];
+#pragma unroll
+    for (int c = 0; c < 15; ++c) line[c] = 0.0f;
+#pragma unroll
+    for (int s = 0; s < 8; ++s) {
+        const int row = row0 + s, end = end_of(row);
+        float p[8], d[8];
+        rp.get(p); rd.get(d);
+        if (s < 7) { probs.load(rp, row + 1, k, end_of(row + 1)); dprobs.load(rd, row + 1, k, end_of(row + 1)); }
+        float dot = 0.0f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            p[i] = k + i < end ? p[i] : 0.0f;
+            d[i] = k + i < end ? d[i] : 0.0f;
+            dot = fmaf(p[i], d[i], dot);
+        }
+        dot = lanes_reduce<TPR, false>(dot);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            p[i] = k + i < end ? p[i] * (d[i] - dot) : 0.0f;
+            line[7 + s - i] += p[i];
+            p[i] *= a.scale;
+        }
+        out.store(r.q0 + row < r.q1, row, k, p);
+    }
+    const int d0 = r.first + r.q0 + row0 - k;                      // line c has distance d0 + c - 7
     float sum_far = 0.0f, sum_low = 0.0f;
-
-    // zeros after the first `count` values (not 0 * dot: a broken row's sum may be NaN)
-    auto cut = [&](float (&v)[8], int count) {
+    const bool beyond = d0 - 7 >= a.far || d0 + 7 <= -a.low;
+    if (beyond) {
+        float s = line[0];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = i < count ? v[i] : 0.0f;
-    };
-    // dz of a run of eight keys into the sums; what does not count is zero there
-    auto add = [&](const float (&dz)[8], int k, int kw, int position) {
-        const int most = position - kw, least = most - 511;
-        if (least >= a.far || most <= -a.low) {
-            float s = 0.0f;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) s += dz[i];
-            if (least >= a.far) sum_far += s;
-            else sum_low += s;
-        } else {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const int d = position - k - i;
-                sum_far += d >= a.far ? dz[i] : 0.0f;
-                sum_low += d <= -a.low ? dz[i] : 0.0f;
-                if (d < a.far && d > -a.low) __hip_atomic_fetch_add(mine + bias_word(a, d + a.low), dz[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WAVEFRONT);
-            }
-        }
-    };
-
-    for (int q = r.q0 + (int)(threadIdx.x / TPR); q < r.q1; q += 256 / TPR) {
-        const int end = bias_end(a, r, q), position = r.first + q;
-        const size_t row = (r.base + q) * a.row_stride;
-        E *out = static_cast<E *>(a.out) + row;
-        if constexpr (NV > 0) {
-            Raw8<BF16> rp[NV], rd[NV];
-#pragma unroll
-            for (int j = 0; j < NV; ++j) {
-                const int k = 8 * (t + TPR * j);
-                rp[j].load(a.in, row + k, end - k);
-                rd[j].load(a.in2, row + k, end - k);
-            }
-            float dot = 0.0f;
-#pragma unroll
-            for (int j = 0; j < NV; ++j) {
-                float p[8], d[8];
-                rp[j].get(p); rd[j].get(d);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) dot = fmaf(p[i], d[i], dot);
-            }
-            dot = row_reduce<TPR, false>(dot, red);
-#pragma unroll
-            for (int j = 0; j < NV; ++j) {
-                const int k = 8 * (t + TPR * j);
-                float p[8], d[8];
-                rp[j].get(p); rd[j].get(d);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) p[i] *= d[i] - dot;
-                if (end - k < 8) cut(p, end - k);
-                if (8 * (wave_first + TPR * j) < end) add(p, k, 8 * (wave_first + TPR * j), position);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) p[i] *= a.scale;
-                if (k < a.keys) store8(out + k, a.keys - k, p);
-            }
-        } else {
-            float dot = 0.0f;
-            for (int k = 8 * t; k < end; k += 8 * TPR) {
-                Raw8<BF16> rp, rd;
-                float p[8], d[8];
-                rp.load(a.in, row + k, end - k); rd.load(a.in2, row + k, end - k);
-                rp.get(p); rd.get(d);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) dot = fmaf(p[i], d[i], dot);
-            }
-            dot = row_reduce<TPR, false>(dot, red);
-            for (int k = 8 * t; k < a.keys; k += 8 * TPR) {
-                Raw8<BF16> rp, rd;
-                float p[8], d[8];
-                rp.load(a.in, row + k, end - k); rd.load(a.in2, row + k, end - k);
-                rp.get(p); rd.get(d);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) p[i] *= d[i] - dot;
-                if (end - k < 8) cut(p, end - k);
-                if (k < end) add(p, k, k - 8 * (t - wave_first), position);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) p[i] *= a.scale;
-                store8(out + k, a.keys - k, p);
-            }
-        }
+        for (int c = 1; c < 15; ++c) s += line[c];
+        (d0 > 0 ? sum_far : sum_low) = s;
     }
-
-    // the workgroup's sums by bucket: a wave takes every fourth bucket, its lanes the distances of the run
-    const float far_wave = wave_sum(sum_far), low_wave = wave_sum(sum_low);
-    if (lane == 0) { ends[wave][0] = far_wave; ends[wave][1] = low_wave; }
-    __syncthreads();
-    float *part = a.partials + (size_t)blockIdx.x * a.buckets;
-    const int side_buckets = a.bidirectional ? a.buckets / 2 : a.buckets;
-    for (int b = wave; b < a.buckets; b += 4) {
-        const bool after = b >= side_buckets;
-        const int m = after ? b - side_buckets : b;
-        int lo = m <= a.near ? m : a.borders[m - a.near - 1];      // magnitudes lo .. hi - 1
-        const int next = m + 1, hi = m == side_buckets - 1 ? a.far : (next <= a.near ? next : a.borders[next - a.near - 1]);
-        if (after || !a.bidirectional) lo = max(lo, 1);            // no distance of 0 on the side of later keys; 0 is in sum_low where there is one side
-        float s = 0.0f;
-        for (int d = lo + lane; d < hi; d += 64) {
-            const int word = bias_word(a, (after ? -d : d) + a.low);
+    const int top = RunWords::slot(a, d0 + 7), m = RunWords::slot(a, r.first + r.q0 + 7) & 7;
+#pragma unroll 1
+    for (int g = 0; g < 64 / TPR; ++g) {
+        if (lane / TPR == g && !beyond) {
 #pragma unroll
-            for (int w = 0; w < 4; ++w) s += bias_lds[w * 8 * a.plane + word];
-        }
-        s = wave_sum(s);
-        if (lane == 0) {
-            if (m == side_buckets - 1) {
-                const int which = after ? 1 : 0;
-                s += ends[0][which] + ends[1][which] + ends[2][which] + ends[3][which];
+            for (int c = 0; c < 15; ++c) {                         // slots top - c, which line 14 - c goes to
+                float *word = mine + (top >> 3) + ((m - c) & 7) * a.plane + ((m - c) >> 3);
+                *word += line[14 - c];
             }
-            if (!a.bidirectional && b == 0) s += ends[0][1] + ends[1][1] + ends[2][1] + ends[3][1];
-            part[b] = s;
         }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");     // the next rows' lanes meet other lanes' words
     }
+    bias_bucket_sums(a, bias_lds, sum_far, sum_low, ends);
 }
-
-// Tables of an example from its workgroups' sums, in order, and their squared norm: one workgroup an example.
-__global__ void __launch_bounds__(256) bias_table_kernel(const float *partials, int heads, int blocks, int buckets, float *g_table, size_t g_stride,
-                                                         float *sqnorm)
+// Tables of an example from its workgroups' sums, and their squared norm: one workgroup an example.  Several threads share an
+// entry's sums where there are fewer entries than threads; their shares are added in order.
+__global__ void __launch_bounds__(1024) bias_table_kernel(const float *partials, int heads, int blocks, int buckets, float *g_table, size_t g_stride,
+                                                          float *sqnorm)
 {
-    __shared__ float red[4];
-    const float *p = partials + (size_t)blockIdx.x * heads * blocks * buckets;
+    __shared__ float red[16], share[1024];
+    const int entries = heads * buckets, parts = max(1, 1024 / entries);
+    const float *p = partials + (size_t)blockIdx.x * entries * blocks;
     float *g = g_table + (size_t)blockIdx.x * g_stride;
     float ss = 0.0f;
-    for (int e = threadIdx.x; e < heads * buckets; e += 256) {
-        const int h = e / buckets, b = e - h * buckets;
-        const float *line = p + (size_t)h * blocks * buckets + b;
+    for (int e0 = 0; e0 < entries; e0 += 1024) {
+        const int width = min(entries - e0, 1024);
+        const int part = (int)threadIdx.x / width, e = e0 + (int)threadIdx.x - part * width, h = e / buckets, b = e - h * buckets;
         float s = 0.0f;
-        for (int k = 0; k < blocks; ++k) s += line[(size_t)k * buckets];
-        g[(size_t)b * heads + h] = s;
-        ss += s * s;
+        if (part < parts) {
+            const float *line = p + (size_t)h * blocks * buckets + b;
+#pragma unroll 4
+            for (int k = part; k < blocks; k += parts) s += line[(size_t)k * buckets];
+        }
+        share[threadIdx.x] = s;
+        __syncthreads();
+        if (part == 0) {
+            for (int k = 1; k < parts; ++k) s += share[threadIdx.x + k * width];
+            g[(size_t)b * heads + h] = s;
+            ss += s * s;
+        }
+        __syncthreads();
     }
-    ss = block_sum<4>(ss, red);
+    ss = block_sum<16>(ss, red);
     if (threadIdx.x == 0 && sqnorm) sqnorm[blockIdx.x] = ss;
 }
 
-// Rows of a workgroup: several, so that what it does once (the biases, or the sums by bucket) is shared by them, as long as there
-// are 2048 workgroups.
-BiasArgs bias_args(const BiasGeo &g, int at_once)
+// Lanes of a wave that share a row in the kernels for short ones, or 0 where a row has a wave of its own or several.  A call with fewer than
+// eight queries would leave most of those lanes idle.
+int narrow_lanes(const BiasGeo &g)
+{
+    if (g.keys > 256 || g.queries < 8 || g.row_stride > ((size_t)1 << 20)) return 0;
+    return g.keys <= 64 ? 8 : g.keys <= 128 ? 16 : 32;
+}
+
+BiasArgs bias_args(const BiasGeo &g)
 {
     BiasArgs a = {};
     a.n = g.n; a.heads = g.heads; a.queries = g.queries; a.keys = g.keys; a.buckets = g.buckets; a.bidirectional = g.bidirectional;
     a.causal = g.causal; a.query_offset = g.query_offset; a.scale = g.scale; a.row_stride = g.row_stride;
     a.near = g.near; a.border_count = g.border_count; a.far = g.far; a.low = g.bidirectional ? g.far : 0;
     std::copy(g.borders, g.borders + BIAS_BORDERS, a.borders);
-    a.plane = (a.low + a.far) / 8 + 1;
-    const long long rows = (long long)g.n * g.heads * g.queries;
-    const long long each = std::max(1ll, std::min(rows / (2048ll * at_once), 64ll / at_once));
-    a.rows = (int)std::min((long long)at_once * each, (long long)(g.queries + at_once - 1) / at_once * at_once);
+    a.last = (a.low + a.far + 16 + 7) / 8 + 1;
+    a.plane = a.last + 1;
+    if (const int lanes = narrow_lanes(g)) {
+        a.rows = 8 * 256 / lanes;
+    } else {
+        // several rows, so that what a workgroup does once (the biases, or the sums by bucket) is shared by them, as long as there are 2048 workgroups
+        const int at_once = g.keys <= 2048 ? 4 : 1;
+        const long long rows = (long long)g.n * g.heads * g.queries;
+        const long long each = std::max(1ll, std::min(rows / (2048ll * at_once), 64ll / at_once));
+        a.rows = (int)std::min((long long)at_once * each, (long long)(g.queries + at_once - 1) / at_once * at_once);
+    }
     a.blocks = (g.queries + a.rows - 1) / a.rows;
     return a;
 }
 
-int rows_at_once(const BiasGeo &g) { return g.keys <= 2048 ? 4 : 1; }
+// Whether a tensor's rows can be read by whole dwords (and those of the kernels for short ones by whole pieces).
+bool bias_words(const BiasGeo &g, const void *p)
+{
+    if (narrow_lanes(g) && g.keys % (g.bf16 ? 8 : 4)) return false;
+    return !g.bf16 || ((reinterpret_cast<uintptr_t>(p) & 3) == 0 && g.keys % 2 == 0 && g.row_stride % 2 == 0);
+}
 
-template <bool BF16>
+template <bool BF16, bool WORDS>
 dp_status run_forward(const BiasGeo &g, const BiasArgs &a, hipStream_t s)
 {
     const dim3 grid((unsigned)((size_t)g.n * g.heads * a.blocks));
     const unsigned lds = 8u * a.plane * 4u;
-    if (g.keys <= 512) return launch_lds<bias_softmax_kernel<BF16, 64, 1>>(grid, 256, lds, s, a);
-    if (g.keys <= 1024) return launch_lds<bias_softmax_kernel<BF16, 64, 2>>(grid, 256, lds, s, a);
-    if (g.keys <= 2048) return launch_lds<bias_softmax_kernel<BF16, 64, 4>>(grid, 256, lds, s, a);
-    if (g.keys <= 4096) return launch_lds<bias_softmax_kernel<BF16, 256, 2>>(grid, 256, lds, s, a);
-    if (g.keys <= 8192) return launch_lds<bias_softmax_kernel<BF16, 256, 4>>(grid, 256, lds, s, a);
-    if (g.keys <= 16384) return launch_lds<bias_softmax_kernel<BF16, 256, 8>>(grid, 256, lds, s, a);
-    return launch_lds<bias_softmax_kernel<BF16, 256, 0>>(grid, 256, lds, s, a);
+    const int lanes = narrow_lanes(g);
+    if (lanes == 8) return launch_lds<bias_softmax_narrow_kernel<BF16, WORDS, 8>>(grid, 256, lds, s, a);
+    if (lanes == 16) return launch_lds<bias_softmax_narrow_kernel<BF16, WORDS, 16>>(grid, 256, lds, s, a);
+    if (lanes == 32) return launch_lds<bias_softmax_narrow_kernel<BF16, WORDS, 32>>(grid, 256, lds, s, a);
+    if (g.keys <= 512) return launch_lds<bias_softmax_kernel<BF16, WORDS, 64, 1>>(grid, 256, lds, s, a);
+    if (g.keys <= 1024) return launch_lds<bias_softmax_kernel<BF16, WORDS, 64, 2>>(grid, 256, lds, s, a);
+    if (g.keys <= 2048) return launch_lds<bias_softmax_kernel<BF16, WORDS, 64, 4>>(grid, 256, lds, s, a);
+    if (g.keys <= 4096) return launch_lds<bias_softmax_kernel<BF16, WORDS, 256, 2>>(grid, 256, lds, s, a);
+    if (g.keys <= 8192) return launch_lds<bias_softmax_kernel<BF16, WORDS, 256, 4>>(grid, 256, lds, s, a);
+    if (g.keys <= 16384) return launch_lds<bias_softmax_kernel<BF16, WORDS, 256, 8>>(grid, 256, lds, s, a);
+    return launch_lds<bias_softmax_kernel<BF16, WORDS, 256, 0>>(grid, 256, lds, s, a);
 }
 
-template <bool BF16>
+template <bool BF16, bool WORDS>
 dp_status run_backward(const BiasGeo &g, const BiasArgs &a, hipStream_t s)
 {
     const dim3 grid((unsigned)((size_t)g.n * g.heads * a.blocks));
     const unsigned lds = 4u * 8u * a.plane * 4u;
-    if (g.keys <= 512) return launch_lds<bias_backward_kernel<BF16, 64, 1>>(grid, 256, lds, s, a);
-    if (g.keys <= 1024) return launch_lds<bias_backward_kernel<BF16, 64, 2>>(grid, 256, lds, s, a);
-    if (g.keys <= 2048) return launch_lds<bias_backward_kernel<BF16, 64, 4>>(grid, 256, lds, s, a);
-    if (g.keys <= 4096) return launch_lds<bias_backward_kernel<BF16, 256, 2>>(grid, 256, lds, s, a);
-    if (g.keys <= 8192) return launch_lds<bias_backward_kernel<BF16, 256, 4>>(grid, 256, lds, s, a);
-    return launch_lds<bias_backward_kernel<BF16, 256, 0>>(grid, 256, lds, s, a);
+    const int lanes = narrow_lanes(g);
+    if (lanes == 8) return launch_lds<bias_backward_narrow_kernel<BF16, WORDS, 8>>(grid, 256, lds, s, a);
+    if (lanes == 16) return launch_lds<bias_backward_narrow_kernel<BF16, WORDS, 16>>(grid, 256, lds, s, a);
+    if (lanes == 32) return launch_lds<bias_backward_narrow_kernel<BF16, WORDS, 32>>(grid, 256, lds, s, a);
+    if (g.keys <= 512) return launch_lds<bias_backward_kernel<BF16, WORDS, 64, 1>>(grid, 256, lds, s, a);
+    if (g.keys <= 1024) return launch_lds<bias_backward_kernel<BF16, WORDS, 64, 2>>(grid, 256, lds, s, a);
+    if (g.keys <= 2048) return launch_lds<bias_backward_kernel<BF16, WORDS, 64, 4>>(grid, 256, lds, s, a);
+    if (g.keys <= 4096) return launch_lds<bias_backward_kernel<BF16, WORDS, 256, 2>>(grid, 256, lds, s, a);
+    if (g.keys <= 8192) return launch_lds<bias_backward_kernel<BF16, WORDS, 256, 4>>(grid, 256, lds, s, a);
+    return launch_lds<bias_backward_kernel<BF16, WORDS, 256, 0>>(grid, 256, lds, s, a);
 }
 
 }  // namespace
 
 size_t bias_ws_bytes(const BiasGeo &g)
 {
-    const BiasArgs a = bias_args(g, rows_at_once(g));
+    const BiasArgs a = bias_args(g);
     return ((size_t)g.n * g.heads * a.blocks * g.buckets * 4 + 15) & ~(size_t)15;
 }
 
 dp_status launch_bias_softmax(const BiasGeo &g, const void *scores, const float *table, const int32_t *query_lengths,
                               const int32_t *key_lengths, void *probs, hipStream_t s)
 {
-    BiasArgs a = bias_args(g, rows_at_once(g));
+    BiasArgs a = bias_args(g);
     a.in = scores; a.out = probs; a.table = table; a.query_lengths = query_lengths; a.key_lengths = key_lengths;
-    return g.bf16 ? run_forward<true>(g, a, s) : run_forward<false>(g, a, s);
+    const bool words = bias_words(g, scores) && bias_words(g, probs);
+    if (g.bf16) return words ? run_forward<true, true>(g, a, s) : run_forward<true, false>(g, a, s);
+    return words ? run_forward<false, true>(g, a, s) : run_forward<false, false>(g, a, s);
 }
 
 dp_status launch_bias_softmax_backward(const BiasGeo &g, const void *probs, const void *dprobs, const int32_t *query_lengths,
                                        const int32_t *key_lengths, void *dscores, float *g_table, size_t g_stride, float *sqnorm, void *ws,
                                        hipStream_t s)
 {
-    BiasArgs a = bias_args(g, rows_at_once(g));
+    BiasArgs a = bias_args(g);
     a.in = probs; a.in2 = dprobs; a.out = dscores; a.query_lengths = query_lengths; a.key_lengths = key_lengths;
     a.partials = static_cast<float *>(ws);
-    const dp_status st = g.bf16 ? run_backward<true>(g, a, s) : run_backward<false>(g, a, s);
+    const bool words = bias_words(g, probs) && bias_words(g, dprobs) && bias_words(g, dscores);
+    const dp_status st = g.bf16 ? (words ? run_backward<true, true>(g, a, s) : run_backward<true, false>(g, a, s))
+                                : (words ? run_backward<false, true>(g, a, s) : run_backward<false, false>(g, a, s));
     if (st != DP_OK) return st;
-    hipLaunchKernelGGL(bias_table_kernel, dim3((unsigned)g.n), dim3(256), 0, s, a.partials, g.heads, a.blocks, g.buckets, g_table, g_stride, sqnorm);
+    hipLaunchKernelGGL(bias_table_kernel, dim3((unsigned)g.n), dim3(1024), 0, s, a.partials, g.heads, a.blocks, g.buckets, g_table, g_stride, sqnorm);
     return check_launch("bias_table");
 }
 

@@ -86,6 +86,13 @@ CASES = [
     (2, 1, 20, 30, False, dict(buckets=4, max_distance=9)),
     (2, 2, 150, 130, True, dict(stride=133)),
     (2, 2, 150, 130, True, dict(stride=136, causal=1)),
+    (2, 3, 300, 64, False, {}),                                                # several rows to a wave
+    (2, 2, 70, 8, True, dict(causal=1)),
+    (4, 2, 140, 128, True, dict(causal=1, bidirectional=0)),
+    (3, 2, 270, 256, True, dict(offset=-1, buckets=8, max_distance=20)),
+    (2, 2, 65, 36, False, dict(causal=1, offset=5)),
+    (2, 1, 260, 201, False, dict(buckets=4, max_distance=4000)),
+    (2, 2, 40, 120, True, dict(stride=124)),
 ]
 
 
