@@ -30,7 +30,8 @@ struct CkDenseArgs {
     int n, tokens, cin, cout, pitch;
     int has_bias, stored, add;
     int tiles_k, tiles_o, slots;     // tiles along k, along o; examples, or ranges
-    int per_range, chunks, cpe;      // weighted: chunks of a range, in all (of examples, or of rows), of an example
+    int columns;                     // of tiles: tiles_k, and one more for a bias
+    int chunks;                      // weighted, rows of any examples: chunks in all
 };
 
 __device__ __forceinline__ int ck_length(const CkDenseArgs &a, int i)
@@ -59,57 +60,59 @@ __device__ __forceinline__ void split8(const float (&v)[8], uint4 (&planes)[3])
 }
 
 // ------------------------------------------------------------------------------------------
-// Contraction over tokens.  A workgroup of four waves owns a 128 (o) x 128 (k) tile, a wave 64 x 64 of it (2 x 2 blocks of 32 x 32).
-// A chunk is 64 tokens (PLANES 3: 32); both operands lie in LDS as they lie in memory, [token][feature], and the matrix operands, which
+// Contraction over tokens.  A workgroup of four waves owns a tile of 128 (o) x 64 NJ (k), NJ 2 or 4, a wave 64 x 32 NJ of it (2 x NJ blocks of
+// 32 x 32).  A chunk is 64 tokens (NJ 4 or PLANES 3: 32); both operands lie in LDS as they lie in memory, [token][feature], and the matrix operands, which
 // want consecutive tokens of a feature, are read with the transposing LDS loads (four tokens of 16 features each).  A row is 16 pieces
 // of 16 bytes; piece p of row r lies in slot p ^ 4 (r & 3): the four rows that a transposing load meets are in different banks.  Codes
 // become bf16 on their way into LDS, once per workgroup.  Two LDS buffers, one barrier per chunk; the loads of the two chunks after the next
-// are in flight during the products.
+// are in flight during the products.  The wider tile takes in two thirds of the bytes for a product (a code is one byte, dY's value two).
 //
 // PLANES: 1: dY as bf16 numbers; 3: fp32 values of dY, split.
 // Per-example call (WEIGHTED false): a workgroup contracts one example's tile, squares it, and stores it if asked.
-// WEIGHTED, PLANES 1: a workgroup walks over the chunks of many examples.  With f_i = m_i 2^e_i, 1 <= m_i < 2, the power is put into
+// WEIGHTED, PLANES 1: a workgroup walks over a range of the chunks of all examples that are not left out, as many as any other range's; chunks
+// after an example's last token are not among them.  With f_i = m_i 2^e_i, 1 <= m_i < 2, the power is put into
 // the scales of X, exactly, and the running sum is kept in units of m_i: it is multiplied by m_(i-1) / m_i where an example begins, and by
 // the last m at the end.  One set of accumulators for any number of examples, and each example meets its factor in fp32.
 // WEIGHTED, PLANES 3: rows (example, token) of the whole call one after the other, dY times its factor in fp32, then split: for fp32 dY, and
 // for examples of a few tokens, of which 32 rows hold several.
-// Bias: the workgroups of the first column of tiles add up dY as they stage it.
-// ALIGNED: rows of dY are multiples of 16 bytes: whole pieces by buffer loads, which give zeros beyond the chunk's last row; else from any
-// element on, piece by piece.
-constexpr int CT = 128, CK_ROW = 2 * CT;                           // bytes of a row of an operand
-constexpr int ck_chunk(int planes) { return planes == 1 ? 64 : 32; }
-constexpr int ck_stage_bytes(int planes) { return (planes + 1) * ck_chunk(planes) * CK_ROW; }
-constexpr unsigned CK_NOWHERE = 0xFFFFFFF0u;                       // an offset beyond any buffer
+// Bias: a column of workgroups of its own adds up dY.
+// WORDS: rows of dY begin at whole dwords: pieces by buffer loads, which give zeros beyond the chunk's last row (what a row's last piece takes
+// from the next row is multiplied into features beyond the last, which nobody reads); else (bf16, an odd number of features) piece by piece.
+constexpr int CT = 128;                                            // o of a tile
+constexpr int ck_chunk(int planes, int nj) { return planes == 1 && nj == 2 ? 64 : 32; }
+constexpr int ck_stage_bytes(int planes, int nj) { return ck_chunk(planes, nj) * (planes * 2 * CT + nj * 128); }
+constexpr int CK_TABLE = 1024;                                     // examples of a weighted call
+constexpr unsigned CK_NOWHERE = 0xFFFFFFE0u;                       // an offset beyond any buffer
 
-template <int PLANES, bool WEIGHTED, bool BF16, bool ALIGNED>
+template <int PLANES, int NJ, bool WEIGHTED, bool BF16, bool WORDS>
 __global__ void __launch_bounds__(256, PLANES == 1 ? 2 : 1) ck_contract_kernel(const CkDenseArgs a)
 {
     extern __shared__ __attribute__((aligned(16))) char ck_lds[];
     __shared__ float red[4];
     typedef typename In<BF16>::type E;
     constexpr bool ROWS = WEIGHTED && PLANES == 3;
-    constexpr int CK = ck_chunk(PLANES), STAGE = ck_stage_bytes(PLANES), PLANE = CK * CK_ROW;
-    constexpr int XP = CK / 32, YP = CK / 16;                      // pieces of X (16 codes) and dY (eight values) of a thread and chunk
+    constexpr int CK = ck_chunk(PLANES, NJ), STAGE = ck_stage_bytes(PLANES, NJ);
+    constexpr int CTK = 64 * NJ, X_ROW = 2 * CTK, Y_ROW = 2 * CT, PLANE = CK * Y_ROW;      // k of a tile; bytes of a row of an operand, of a plane of dY
+    constexpr int XW = CTK / 16, XS = 256 / XW, XP = CK / XS, YP = CK / 16;        // pieces of X (16 codes) in a row, rows between a thread's, pieces of a thread and chunk
     // workgroup -> XCD goes round robin: an XCD takes a run of consecutive tiles, which share an example's operands in its L2
     const unsigned per_xcd = gridDim.x >> 3, block = (blockIdx.x & 7u) * per_xcd + (blockIdx.x >> 3);
-    const unsigned tiles = (unsigned)(a.tiles_o * a.tiles_k);
+    const unsigned tiles = (unsigned)(a.tiles_o * a.columns);
     const int slot = (int)(block / tiles), tile = (int)(block - (unsigned)slot * tiles);     // example or range
     if (slot >= a.slots) return;
-    const int tile_o = tile / a.tiles_k, tile_k = tile - tile_o * a.tiles_k;
-    const int o0 = tile_o * CT, k0 = tile_k * CT;
+    const int tile_o = tile / a.columns, tile_k = tile - tile_o * a.columns;
+    const int o0 = tile_o * CT, k0 = tile_k * CTK;
     const int t = threadIdx.x, lane = t & 63, wave = t >> 6, wm = wave >> 1, wn = wave & 1;
-    const bool bias_here = a.has_bias && tile_k == 0;
-    int c_begin = 0, c_end, len = 0;
-    if constexpr (WEIGHTED) {
-        c_begin = slot * a.per_range;
-        c_end = min(c_begin + a.per_range, a.chunks);
-    } else {
+    int c_begin = 0, c_end = 0, len = 0;
+    if constexpr (ROWS) {
+        c_begin = (int)((long long)a.chunks * slot / a.slots);
+        c_end = (int)((long long)a.chunks * (slot + 1) / a.slots);
+    } else if constexpr (!WEIGHTED) {
         len = ck_length(a, slot);
         c_end = (len + CK - 1) / CK;
     }
 
-    // this thread's pieces of a chunk: 16 codes of rows t / 8 + 32 u; eight values of dY of rows t / 16 + 16 u
-    const int xr = t >> 3, xp = t & 7, x_col = k0 + xp * 16;
+    // this thread's pieces of a chunk: 16 codes of rows t / XW + XS u; eight values of dY of rows t / 16 + 16 u
+    const int xr = t / XW, xp = t % XW, x_col = k0 + xp * 16;
     const int yr = t >> 4, yp = t & 15, y_col = o0 + yp * 8, y_count = a.cout - y_col;
     const unsigned x_off = x_col < a.pitch ? (unsigned)(xr * a.pitch + x_col) : CK_NOWHERE;
     const int s_pitch = a.pitch / CK_BLOCK;
@@ -129,20 +132,69 @@ __global__ void __launch_bounds__(256, PLANES == 1 ? 2 : 1) ck_contract_kernel(c
     };
     int f_ex = 0, f_c = 0, f_len = len, f_power = 0;               // weighted, by example: what the next chunk belongs to
     float f_m = 1.0f, f_f = 1.0f;
-    if constexpr (WEIGHTED && !ROWS) { f_ex = c_begin / a.cpe; f_c = c_begin - f_ex * a.cpe; }
+    // lengths (0 where an example is left out), factors, and chunks of the examples before each
+    constexpr int TABLE = WEIGHTED && !ROWS ? CK_TABLE : 1;
+    __shared__ int ex_len[TABLE], ex_before[TABLE + 1], found, wave_chunks[4];
+    __shared__ float ex_f[TABLE];
+    if constexpr (WEIGHTED && !ROWS) {
+        int mine = 0, before[4], count[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const int i = 4 * t + u;
+            int l = 0;
+            if (i < a.n) {
+                const float f = clip_factor(a.group_sqnorm[i], a.clip_c);
+                l = f == 0.0f ? 0 : ck_length(a, i);               // of factor 0: adds nothing, and no 0 * inf
+                ex_len[i] = l;
+                ex_f[i] = f;
+            }
+            before[u] = mine;
+            mine += count[u] = (l + CK - 1) / CK;
+        }
+        int upto = mine;                                           // of this wave's threads up to this one
+#pragma unroll
+        for (int off = 1; off < 64; off <<= 1) {
+            const int v = __shfl_up(upto, off, 64);
+            upto += lane >= off ? v : 0;
+        }
+        if (lane == 63) wave_chunks[wave] = upto;
+        if (t == 0) found = 0;
+        __syncthreads();
+        int base = upto - mine, total = 0;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            base += w < wave ? wave_chunks[w] : 0;
+            total += wave_chunks[w];
+        }
+        total = __builtin_amdgcn_readfirstlane(total);
+        c_begin = (int)((long long)total * slot / a.slots);
+        c_end = (int)((long long)total * (slot + 1) / a.slots);
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const int i = 4 * t + u, first = base + before[u];
+            if (i < a.n) ex_before[i] = first;
+            if (c_begin >= first && c_begin < first + count[u]) found = i;
+        }
+        __syncthreads();
+        f_ex = __builtin_amdgcn_readfirstlane(found);
+        f_c = c_begin - __builtin_amdgcn_readfirstlane(ex_before[f_ex]);
+    }
 
-    auto load_rows = [&](Slot &s, size_t row0, int rows) {
+    auto load_rows = [&](Slot &s, unsigned row0_any, int rows_any) {
+        // the same in every lane, which the compiler does not always see (and a buffer in vector registers is read lane by lane)
+        const size_t row0 = (unsigned)__builtin_amdgcn_readfirstlane((int)row0_any);
+        const int rows = __builtin_amdgcn_readfirstlane(rows_any);
         const __amdgpu_buffer_rsrc_t xb = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(a.codes) + row0 * (unsigned)a.pitch, 0, rows * a.pitch, 0x00020000);
         const __amdgpu_buffer_rsrc_t sb = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(a.scales) + row0 * (unsigned)s_pitch, 0, rows * s_pitch, 0x00020000);
         typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 #pragma unroll
         for (int u = 0; u < XP; ++u) {
-            const u32x4 v = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(xb, x_off + (x_off == CK_NOWHERE ? 0u : (unsigned)(32 * u * a.pitch)), 0, 0));
+            const u32x4 v = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(xb, x_off + (x_off == CK_NOWHERE ? 0u : (unsigned)(XS * u * a.pitch)), 0, 0));
             s.x[u] = make_uint4(v.x, v.y, v.z, v.w);
-            s.scale[u] = __builtin_amdgcn_raw_buffer_load_b8(sb, s_off + (s_off == CK_NOWHERE ? 0u : (unsigned)(32 * u * s_pitch)), 0, 0);
+            s.scale[u] = __builtin_amdgcn_raw_buffer_load_b8(sb, s_off + (s_off == CK_NOWHERE ? 0u : (unsigned)(XS * u * s_pitch)), 0, 0);
         }
         const E *dy = static_cast<const E *>(a.dy) + row0 * (unsigned)a.cout;
-        if constexpr (ALIGNED) {
+        if constexpr (WORDS) {
             const __amdgpu_buffer_rsrc_t yb = __builtin_amdgcn_make_buffer_rsrc(const_cast<E *>(dy), 0, rows * a.cout * (int)sizeof(E), 0x00020000);
 #pragma unroll
             for (int u = 0; u < YP; ++u) {
@@ -164,6 +216,7 @@ __global__ void __launch_bounds__(256, PLANES == 1 ? 2 : 1) ck_contract_kernel(c
     auto fetch = [&](Slot &s, int c) {
         s.rows = 0;
         s.begins = false;
+        s.power = 0;
         if (c >= c_end) return;
         if constexpr (ROWS) {
             const unsigned total = (unsigned)a.n * (unsigned)a.tokens, row0 = (unsigned)c * CK;
@@ -175,130 +228,169 @@ __global__ void __launch_bounds__(256, PLANES == 1 ? 2 : 1) ck_contract_kernel(c
                 left = row < total ? (int)(at - i * (unsigned)a.tokens) : a.tokens;
             };
 #pragma unroll
-            for (int u = 0; u < XP; ++u) about(row0 + xr + 32 * u, s.x_sq[u], s.x_left[u], s.x_len[u]);
+            for (int u = 0; u < XP; ++u) about(row0 + xr + XS * u, s.x_sq[u], s.x_left[u], s.x_len[u]);
 #pragma unroll
             for (int u = 0; u < YP; ++u) about(row0 + yr + 16 * u, s.y_sq[u], s.y_left[u], s.y_len[u]);
             load_rows(s, row0, s.rows);
         } else if constexpr (WEIGHTED) {
             s.begins = f_c == 0 || c == c_begin;
             if (s.begins) {
-                f_len = ck_length(a, f_ex);
-                f_f = clip_factor(a.group_sqnorm[f_ex], a.clip_c);
-                if (f_f == 0.0f) f_len = 0;                        // adds nothing, and no 0 * inf
-                f_power = f_f > 0.0f ? (int)(__float_as_uint(f_f) >> 23) - 127 : 0;
-                f_m = f_f > 0.0f ? f_f * pow2_of(127 - f_power) : 1.0f;
+                while (__builtin_amdgcn_readfirstlane(ex_len[f_ex]) == 0) ++f_ex;         // (there are chunks: an example with some follows)
+                f_len = __builtin_amdgcn_readfirstlane(ex_len[f_ex]);
+                f_f = __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, ex_f[f_ex])));
+                f_power = (int)(__float_as_uint(f_f) >> 23) - 127;
+                f_m = f_f * pow2_of(127 - f_power);
             }
-            s.rows = max(min(f_len - f_c * CK, CK), 0);
+            s.rows = min(f_len - f_c * CK, CK);
             s.power = f_power; s.m = f_m; s.f = f_f;
-            if (s.rows > 0) load_rows(s, (size_t)f_ex * (unsigned)a.tokens + (unsigned)(f_c * CK), s.rows);
-            if (++f_c == a.cpe) { f_c = 0; ++f_ex; }
+            load_rows(s, (unsigned)f_ex * (unsigned)a.tokens + (unsigned)(f_c * CK), s.rows);
+            if (++f_c * CK >= f_len) { f_c = 0; ++f_ex; }
         } else {
             s.rows = min(len - c * CK, CK);
-            load_rows(s, (size_t)slot * (unsigned)a.tokens + (unsigned)(c * CK), s.rows);
+            load_rows(s, (unsigned)slot * (unsigned)a.tokens + (unsigned)(c * CK), s.rows);
         }
     };
-    float bias_sum[8];
-#pragma unroll
-    for (int j = 0; j < 8; ++j) bias_sum[j] = 0.0f;
-    auto stage = [&](const Slot &s, int buf) {
-        char *lds = ck_lds + buf * STAGE;
-#pragma unroll
-        for (int u = 0; u < XP; ++u) {
-            const int r = xr + 32 * u;
-            uint4 x = s.x[u];
-            if constexpr (ROWS)
-                if (s.x_left[u] >= s.x_len[u] || clip_factor(s.x_sq[u], a.clip_c) == 0.0f) x = make_uint4(0, 0, 0, 0);
-            const float scale = pow2_of(WEIGHTED && !ROWS ? max((int)s.scale[u] + s.power, 1) : (int)s.scale[u]);
-            const uint2 w0 = ck_bf16(x.x, scale), w1 = ck_bf16(x.y, scale), w2 = ck_bf16(x.z, scale), w3 = ck_bf16(x.w, scale);
-            char *to = lds + PLANES * PLANE + r * CK_ROW;
-            *reinterpret_cast<uint4 *>(to + (((2 * xp) ^ ((r & 3) << 2)) << 4)) = make_uint4(w0.x, w0.y, w1.x, w1.y);
-            *reinterpret_cast<uint4 *>(to + (((2 * xp + 1) ^ ((r & 3) << 2)) << 4)) = make_uint4(w2.x, w2.y, w3.x, w3.y);
-        }
-#pragma unroll
-        for (int u = 0; u < YP; ++u) {
-            const int r = yr + 16 * u;
-            char *to = lds + r * CK_ROW + ((yp ^ ((r & 3) << 2)) << 4);
+    auto row_factor = [&](const Slot &s, int u) { return s.y_left[u] < s.y_len[u] ? clip_factor(s.y_sq[u], a.clip_c) : 0.0f; };
+    auto stage_x = [&](const Slot &s, int u, int buf) {            // piece u of X into LDS
+        const int r = xr + XS * u;
+        uint4 x = s.x[u];
+        if constexpr (ROWS)
+            if (s.x_left[u] >= s.x_len[u] || clip_factor(s.x_sq[u], a.clip_c) == 0.0f) x = make_uint4(0, 0, 0, 0);
+        const float scale = pow2_of(WEIGHTED && !ROWS ? max((int)s.scale[u] + s.power, 1) : (int)s.scale[u]);
+        const uint2 w0 = ck_bf16(x.x, scale), w1 = ck_bf16(x.y, scale), w2 = ck_bf16(x.z, scale), w3 = ck_bf16(x.w, scale);
+        char *to = ck_lds + buf * STAGE + PLANES * PLANE + r * X_ROW;
+        *reinterpret_cast<uint4 *>(to + (((2 * xp) ^ ((r & 3) << 2)) << 4)) = make_uint4(w0.x, w0.y, w1.x, w1.y);
+        *reinterpret_cast<uint4 *>(to + (((2 * xp + 1) ^ ((r & 3) << 2)) << 4)) = make_uint4(w2.x, w2.y, w3.x, w3.y);
+    };
+    auto stage_y = [&](const Slot &s, int u, int buf) {            // piece u of dY
+        const int r = yr + 16 * u;
+        char *to = ck_lds + buf * STAGE + r * Y_ROW + ((yp ^ ((r & 3) << 2)) << 4);
+        if constexpr (PLANES == 1) {
+            *reinterpret_cast<uint4 *>(to) = s.y[u].w;
+        } else {
             float v[8];
-            if constexpr (PLANES == 1) {
-                *reinterpret_cast<uint4 *>(to) = s.y[u].w;
-                if (bias_here) {
-                    s.y[u].get(v);
+            s.y[u].get(v);
+            if constexpr (ROWS) {
+                const float f = row_factor(s, u);
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) bias_sum[j] = WEIGHTED ? fmaf(s.f, v[j], bias_sum[j]) : bias_sum[j] + v[j];
-                }
-            } else {
+                for (int j = 0; j < 8; ++j) v[j] = f == 0.0f ? 0.0f : v[j] * f;
+            }
+            uint4 p[3];
+            split8(v, p);
+#pragma unroll
+            for (int q = 0; q < 3; ++q) *reinterpret_cast<uint4 *>(to + q * PLANE) = p[q];
+        }
+    };
+    auto stage = [&](const Slot &s, int buf) {
+#pragma unroll
+        for (int u = 0; u < XP; ++u) stage_x(s, u, buf);
+#pragma unroll
+        for (int u = 0; u < YP; ++u) stage_y(s, u, buf);
+    };
+
+    if (tile_k == a.tiles_k) {                                     // the column of the bias: sums of dY (X's pieces lie beyond its rows)
+        float sum[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) sum[j] = 0.0f;
+        auto add = [&](const Slot &s) {
+            if (s.rows <= 0) return;
+#pragma unroll
+            for (int u = 0; u < YP; ++u) {
+                float v[8], f = 1.0f;
                 s.y[u].get(v);
-                if constexpr (ROWS) {
-                    const float f = s.y_left[u] < s.y_len[u] ? clip_factor(s.y_sq[u], a.clip_c) : 0.0f;
+                if constexpr (ROWS) f = row_factor(s, u);
+                else if constexpr (WEIGHTED) f = s.f;
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) v[j] = f == 0.0f ? 0.0f : v[j] * f;
-                }
-                uint4 p[3];
-                split8(v, p);
+                for (int j = 0; j < 8; ++j) sum[j] = f == 0.0f ? sum[j] : fmaf(f, v[j], sum[j]);
+            }
+        };
+        Slot b0, b1;
+        fetch(b0, c_begin);
+        for (int c = c_begin; c < c_end; c += 2) {
+            fetch(b1, c + 1);
+            add(b0);
+            fetch(b0, c + 2);
+            add(b1);
+        }
+        float *sums = reinterpret_cast<float *>(ck_lds);
 #pragma unroll
-                for (int q = 0; q < 3; ++q) *reinterpret_cast<uint4 *>(to + q * PLANE) = p[q];
-                if (bias_here) {
+        for (int j = 0; j < 8; ++j) sums[yr * CT + yp * 8 + j] = sum[j];
+        __syncthreads();
+        float ss = 0.0f;
+        if (t < CT && o0 + t < a.cout) {
+            float v = 0.0f;
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) bias_sum[j] += v[j];
-                }
+            for (int r = 0; r < 16; ++r) v += sums[r * CT + t];
+            if constexpr (WEIGHTED) {
+                float *out = a.out_b + (size_t)slot * a.stride_b + o0 + t;
+                *out = a.add ? *out + v : v;
+            } else {
+                ss = v * v;
+                if (a.stored) a.out_b[(size_t)slot * a.stride_b + o0 + t] = v;
             }
         }
-    };
+        if constexpr (!WEIGHTED) {
+            const float tot = block_sum<4>(ss, red);
+            if (t == 0) a.partials[(size_t)slot * tiles + tile] = tot;
+        }
+        return;
+    }
 
     // A lane's part of a transposing load: row (lane / 4) % 4 of four, features 4 (lane % 4) .. of 16; the second group of 16 lanes takes the
     // next 16 features, the upper half of the wave the tokens eight further on.
     const int tr = (lane >> 2) & 3, tf = ((lane >> 4) & 1) * 16 + (lane & 3) * 4, th = lane >> 5;
-    auto operand = [&](const char *base, int f0, int ks) {         // features f0 .. f0 + 31, tokens 16 ks .. 16 ks + 15
+    auto operand = [&](const char *base, int row, int f0, int ks) {        // features f0 .. f0 + 31, tokens 16 ks .. 16 ks + 15, rows of `row` bytes
         const int f = f0 + tf;
-        const char *p = base + (ks * 16 + th * 8 + tr) * CK_ROW + (((f >> 3) ^ (tr << 2)) << 4) + ((f >> 2) & 1) * 8;
+        const char *p = base + (ks * 16 + th * 8 + tr) * row + (((f >> 3) ^ (tr << 2)) << 4) + ((f >> 2) & 1) * 8;
         typedef short s16x4 __attribute__((ext_vector_type(4)));
         typedef __attribute__((address_space(3))) s16x4 *lds_ptr;
         typedef short s16x8 __attribute__((ext_vector_type(8)));
         const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(p));
-        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(p + 4 * CK_ROW));
+        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(p + 4 * row));
         return __builtin_bit_cast(bf16x8, s16x8{lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w});
     };
 
-    f32x16 acc[2][2];
+    f32x16 acc[2][NJ];
 #pragma unroll
     for (int i = 0; i < 2; ++i)
 #pragma unroll
-        for (int j = 0; j < 2; ++j)
+        for (int j = 0; j < NJ; ++j)
 #pragma unroll
             for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.0f;
     float unit = 1.0f;                                             // the sum's unit: m of the last example that was added
 
     struct Now { int rows; bool begins; float m; };                // of the chunk in LDS
-    auto compute = [&](const Now &now, int buf) {
-        if (now.rows <= 0) return;
-        if (WEIGHTED && !ROWS && now.begins) {
-            const float ratio = unit / now.m;
-            unit = now.m;
+    auto rescale = [&](const Now &now) {
+        if constexpr (WEIGHTED && !ROWS) {
+            const float ratio = now.begins && now.rows > 0 ? unit / now.m : 1.0f;
+            unit = now.begins && now.rows > 0 ? now.m : unit;
             if (ratio != 1.0f) {
 #pragma unroll
                 for (int i = 0; i < 2; ++i)
 #pragma unroll
-                    for (int j = 0; j < 2; ++j)
+                    for (int j = 0; j < NJ; ++j)
 #pragma unroll
                         for (int r = 0; r < 16; ++r) acc[i][j][r] *= ratio;
             }
         }
-        const char *s = ck_lds + buf * STAGE;
+    };
+    struct Operands { bf16x8 a[PLANES][2], b[NJ]; };               // of a K step (16 tokens)
+    auto read = [&](Operands &o, int ks, int buf) {
+        const char *base = ck_lds + buf * STAGE;
 #pragma unroll
-        for (int ks = 0; ks < CK / 16; ++ks) {
-            if (ks * 16 >= now.rows) break;
-            bf16x8 vb[2];
+        for (int j = 0; j < NJ; ++j) o.b[j] = operand(base + PLANES * PLANE, X_ROW, wn * 32 * NJ + j * 32, ks);
 #pragma unroll
-            for (int j = 0; j < 2; ++j) vb[j] = operand(s + PLANES * PLANE, wn * 64 + j * 32, ks);
+        for (int q = 0; q < PLANES; ++q)
 #pragma unroll
-            for (int q = 0; q < PLANES; ++q)
+            for (int i = 0; i < 2; ++i) o.a[q][i] = operand(base + q * PLANE, Y_ROW, wm * 64 + i * 32, ks);
+    };
+    auto products = [&](const Operands &o) {
 #pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    const bf16x8 va = operand(s + q * PLANE, wm * 64 + i * 32, ks);
+        for (int q = 0; q < PLANES; ++q)
 #pragma unroll
-                    for (int j = 0; j < 2; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(va, vb[j], acc[i][j], 0, 0, 0);
-                }
-        }
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+                for (int j = 0; j < NJ; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(o.a[q][i], o.b[j], acc[i][j], 0, 0, 0);
     };
     // chunk c is in LDS buffer c & 1 (counted from the first), the two after it in registers; `next` holds c + 1 and takes c + 3
     Slot s0, s1;
@@ -308,10 +400,58 @@ __global__ void __launch_bounds__(256, PLANES == 1 ? 2 : 1) ck_contract_kernel(c
     if (now.rows > 0) stage(s0, 0);
     fetch(s0, c_begin + 2);
     __syncthreads();
+    // A chunk's products in two halves (the second one left out where no row reaches it), the next chunk staged in between: one set of
+    // accumulators on every path.  Where the next chunk adds nothing, what is staged is not used.
     auto turn = [&](Slot &next, int buf, int c) {
-        compute(now, buf);
+        rescale(now);
+        auto stage_xs = [&]() {
+#pragma unroll
+            for (int u = 0; u < XP; ++u) stage_x(next, u, buf ^ 1);
+        };
+        auto stage_ys = [&]() {
+#pragma unroll
+            for (int u = 0; u < YP; ++u) stage_y(next, u, buf ^ 1);
+        };
+        if constexpr (CK == 64) {
+            if (now.rows > 0) {
+                Operands p, q, r;
+                read(p, 0, buf);
+                read(q, 1, buf);
+                products(p);
+                stage_xs();
+                read(r, 2, buf);
+                products(q);
+                if (now.rows > 32) {
+                    read(p, 3, buf);
+                    products(r);
+                    stage_ys();
+                    products(p);
+                } else {
+                    stage_ys();
+                }
+            } else {
+                stage_xs();
+                stage_ys();
+            }
+        } else {
+            if (now.rows > 0) {
+                Operands p, q;
+                read(p, 0, buf);
+                stage_xs();
+                products(p);
+                if (now.rows > 16) {
+                    read(q, 1, buf);
+                    stage_ys();
+                    products(q);
+                } else {
+                    stage_ys();
+                }
+            } else {
+                stage_xs();
+                stage_ys();
+            }
+        }
         now = {next.rows, next.begins, next.m};
-        if (now.rows > 0) stage(next, buf ^ 1);
         fetch(next, c + 3);
         __syncthreads();
     };
@@ -320,45 +460,53 @@ __global__ void __launch_bounds__(256, PLANES == 1 ? 2 : 1) ck_contract_kernel(c
         if (c + 1 < c_end) turn(s0, 1, c + 1);
     }
 
+    // Rows beyond the last hold products of what followed in memory: gone.  (Columns beyond the last are sums of zeros.)
+    const int out_row = wm * 64 + (lane >> 5) * 4, out_col = k0 + wn * 32 * NJ + (lane & 31);       // of the tile; row (r >> 2) * 8 + (r & 3) of a block
+    if (o0 + CT > a.cout) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                const bool there = o0 + out_row + i * 32 + (r >> 2) * 8 + (r & 3) < a.cout;
+#pragma unroll
+                for (int j = 0; j < NJ; ++j) acc[i][j][r] = there ? acc[i][j][r] : 0.0f;
+            }
+    }
     float ss = 0.0f;
 #pragma unroll
     for (int i = 0; i < 2; ++i)
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
-            const int col = k0 + wn * 64 + j * 32 + (lane & 31), row0 = o0 + wm * 64 + i * 32 + (lane >> 5) * 4;
+        for (int j = 0; j < NJ; ++j)
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
-                const int row = row0 + (r >> 2) * 8 + (r & 3);
-                const bool there = row < a.cout && col < a.cin;
-                const float v = WEIGHTED && !ROWS ? acc[i][j][r] * unit : acc[i][j][r];
-                if constexpr (WEIGHTED) {
-                    if (there) {
-                        float *out = a.out_w + (size_t)slot * a.stride_w + (size_t)row * a.cin + col;
-                        *out = a.add ? *out + v : v;
-                    }
-                } else {
-                    if (there) ss += v * v;
-                    if (there && a.stored) a.out_w[(size_t)slot * a.stride_w + (size_t)row * a.cin + col] = v;
+                if constexpr (WEIGHTED && !ROWS) acc[i][j][r] *= unit;
+                if constexpr (!WEIGHTED) ss = fmaf(acc[i][j][r], acc[i][j][r], ss);
+            }
+    if (WEIGHTED || a.stored) {
+        // the tile's rows as a buffer that ends with the last of them; columns beyond the last have no place in it
+        float *first = a.out_w + (size_t)slot * a.stride_w + (size_t)o0 * a.cin;
+        const __amdgpu_buffer_rsrc_t out = __builtin_amdgcn_make_buffer_rsrc(first, 0, min(CT, a.cout - o0) * a.cin * 4, 0x00020000);
+        const bool add = WEIGHTED && a.add;
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int j = 0; j < NJ; ++j) {
+                const int col = out_col + j * 32;
+                const unsigned at = col < a.cin ? (unsigned)((out_row + i * 32) * a.cin + col) * 4u : CK_NOWHERE;
+                const unsigned step = col < a.cin ? (unsigned)a.cin * 4u : 0u;
+                float old[16];
+                if (add) {
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) old[r] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(out, at + step * ((r >> 2) * 8 + (r & 3)), 0, 0));
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) acc[i][j][r] += old[r];
+                }
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    const float v = acc[i][j][r];
+                    __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(v), out, at + step * ((r >> 2) * 8 + (r & 3)), 0, 0);
                 }
             }
-        }
-    if (bias_here) {
-        float *sums = reinterpret_cast<float *>(ck_lds);           // (the last barrier is behind the last products)
-#pragma unroll
-        for (int j = 0; j < 8; ++j) sums[yr * CT + yp * 8 + j] = bias_sum[j];
-        __syncthreads();
-        if (t < CT && o0 + t < a.cout) {
-            float v = 0.0f;
-#pragma unroll
-            for (int r = 0; r < 16; ++r) v += sums[r * CT + t];
-            if constexpr (WEIGHTED) {
-                float *out = a.out_b + (size_t)slot * a.stride_b + o0 + t;
-                *out = a.add ? *out + v : v;
-            } else {
-                ss += v * v;
-                if (a.stored) a.out_b[(size_t)slot * a.stride_b + o0 + t] = v;
-            }
-        }
     }
     if constexpr (!WEIGHTED) {
         const float tot = block_sum<4>(ss, red);
@@ -366,27 +514,34 @@ __global__ void __launch_bounds__(256, PLANES == 1 ? 2 : 1) ck_contract_kernel(c
     }
 }
 
-// acc[e] += sum of the ranges' sums, in order (four values a thread where the count allows it)
-__global__ void __launch_bounds__(256) ck_ranges_kernel(const float *part, size_t stride, int ranges, size_t count, float *acc)
+// acc[e] += sum of the ranges' sums, in order: `count_w` values of the weights, then those of the bias, which a range's sums hold one after the
+// other (from `stride_w` on).
+__global__ void __launch_bounds__(256) ck_ranges_kernel(const float *part, size_t stride, size_t stride_w, int ranges, size_t count_w, size_t count_b,
+                                                        float *acc_w, float *acc_b)
 {
-    const size_t e = ((size_t)blockIdx.x * 256 + threadIdx.x) * 4;
-    if (e >= count) return;
+    size_t e = ((size_t)blockIdx.x * 256 + threadIdx.x) * 4;
+    if (e >= stride_w + count_b) return;
+    const float *p = part + e;
+    float4 s = *reinterpret_cast<const float4 *>(p);
+#pragma unroll 4
+    for (int r = 1; r < ranges; ++r) {
+        const float4 v = *reinterpret_cast<const float4 *>(p + r * stride);
+        s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
+    }
+    const bool bias = e >= stride_w;
+    float *acc = bias ? acc_b : acc_w;
+    const size_t count = bias ? count_b : count_w;
+    if (bias) e -= stride_w;
     if (e + 4 <= count) {
-        float4 s = *reinterpret_cast<const float4 *>(part + e);
-        for (int r = 1; r < ranges; ++r) {
-            const float4 v = *reinterpret_cast<const float4 *>(part + r * stride + e);
-            s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
-        }
         float4 *out = reinterpret_cast<float4 *>(acc + e);
         const float4 o = *out;
         *out = make_float4(o.x + s.x, o.y + s.y, o.z + s.z, o.w + s.w);
         return;
     }
-    for (size_t i = e; i < count; ++i) {
-        float s = part[i];
-        for (int r = 1; r < ranges; ++r) s += part[r * stride + i];
-        acc[i] += s;
-    }
+    const float v[4] = {s.x, s.y, s.z, s.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        if (e + i < count) acc[e + i] += v[i];
 }
 
 // ------------------------------------------------------------------------------------------
@@ -521,49 +676,53 @@ struct CkPlan {
     int gram_tiles;                  // tiles of 32 B tokens of an example
     int gram_b;
     size_t per_example;              // partial squared norms
-    int ranges, per_range, chunks, cpe;   // weighted
+    int nj;                          // the contraction's tiles are 64 nj wide
+    int ranges, chunks;              // weighted
     bool rows;
 };
 
-int ck_tiles(int v) { return (v + CT - 1) / CT; }
+int ck_tiles(int v, int width) { return (v + width - 1) / width; }
 
 // Gram matrices where they take fewer operations than the contraction, tiles counted whole.
 CkPlan ck_plan(const Geo &g, int mode)
 {
     CkPlan p = {};
-    const int tiles_o = ck_tiles(g.cout), tiles_k = ck_tiles(g.cin);
+    const int tiles_o = ck_tiles(g.cout, CT);
+    p.nj = 2;
     if (mode == MODE_WEIGHTED) {
         // 32 rows hold several examples of a few tokens each, at three products for one
         p.rows = !g.bf16 || g.h < 16;
-        const int chunk = ck_chunk(p.rows ? 3 : 1);
-        p.cpe = (g.h + chunk - 1) / chunk;
-        const long long chunks = p.rows ? ((long long)g.n * g.h + chunk - 1) / chunk : (long long)g.n * p.cpe;
+        if (!p.rows && (long long)tiles_o * ck_tiles(g.cin, 256) >= 384) p.nj = 4;
+        const int chunk = ck_chunk(p.rows ? 3 : 1, p.nj);
+        const long long chunks = p.rows ? ((long long)g.n * g.h + chunk - 1) / chunk : (long long)std::min(g.n, CK_TABLE) * ((g.h + chunk - 1) / chunk);
         p.chunks = (int)chunks;
         // ranges of the call's chunks until there are two workgroups for each compute unit; a range has four chunks at least
-        const long long want = (512 + tiles_o * tiles_k - 1) / (tiles_o * tiles_k);
-        const long long ranges = std::max(1ll, std::min(want, chunks / 4));
-        p.per_range = (int)((chunks + ranges - 1) / ranges);
-        p.ranges = (int)((chunks + p.per_range - 1) / p.per_range);
+        const long long tiles = (long long)tiles_o * ck_tiles(g.cin, 64 * p.nj);
+        p.ranges = (int)std::max(1ll, std::min((512 + tiles - 1) / tiles, chunks / 4));
         return p;
     }
-    p.per_example = (size_t)tiles_o * tiles_k;
+    if (g.bf16 && (long long)g.n * tiles_o * ck_tiles(g.cin, 256) >= 384) p.nj = 4;
+    const int tiles_k = ck_tiles(g.cin, 64 * p.nj);
+    p.per_example = (size_t)tiles_o * (tiles_k + g.has_bias);
     if (mode == MODE_NORM && g.bf16) {
         p.gram_b = g.h <= 32 ? 1 : 2;
         p.gram_tiles = (g.h + 32 * p.gram_b - 1) / (32 * p.gram_b);
         const double pairs = 0.5 * p.gram_tiles * (p.gram_tiles + 1), side = 32.0 * p.gram_b;
         const double gram = pairs * side * side * ((double)g.cin + g.cout);
-        const double direct = (double)((g.h + 15) / 16 * 16) * tiles_o * CT * (double)tiles_k * CT;
+        const double direct = (double)((g.h + 15) / 16 * 16) * tiles_o * CT * (double)tiles_k * 64 * p.nj;
         p.gram = 4 * gram < direct;
         if (p.gram) p.per_example = (size_t)p.gram_tiles * (p.gram_tiles + 1) / 2;
     }
     return p;
 }
 
-template <int PLANES, bool WEIGHTED, bool BF16>
-dp_status run_contract(bool aligned, dim3 grid, const CkDenseArgs &a, hipStream_t s)
+template <int PLANES, int NJ, bool WEIGHTED, bool BF16>
+dp_status run_contract(bool words, dim3 grid, const CkDenseArgs &a, hipStream_t s)
 {
-    return aligned ? launch_lds<ck_contract_kernel<PLANES, WEIGHTED, BF16, true>>(grid, 256, 2 * ck_stage_bytes(PLANES), s, a)
-                   : launch_lds<ck_contract_kernel<PLANES, WEIGHTED, BF16, false>>(grid, 256, 2 * ck_stage_bytes(PLANES), s, a);
+    constexpr unsigned lds = 2 * ck_stage_bytes(PLANES, NJ);
+    if constexpr (BF16)
+        if (!words) return launch_lds<ck_contract_kernel<PLANES, NJ, WEIGHTED, BF16, false>>(grid, 256, lds, s, a);
+    return launch_lds<ck_contract_kernel<PLANES, NJ, WEIGHTED, BF16, true>>(grid, 256, lds, s, a);
 }
 
 size_t align16(size_t b) { return (b + 15) & ~(size_t)15; }
@@ -580,6 +739,31 @@ size_t checkpoint_ws_bytes(const Geo &g, int mode)
     return align16(4 * (size_t)g.n * std::max(p.per_example, q.per_example));
 }
 
+static dp_status launch_weighted(const Geo &g, CkDenseArgs a, float *out_w, float *out_b, void *ws, hipStream_t s)
+{
+    const CkPlan p = ck_plan(g, MODE_WEIGHTED);
+    a.tiles_k = ck_tiles(g.cin, 64 * p.nj); a.columns = a.tiles_k + g.has_bias;
+    a.chunks = p.chunks; a.slots = p.ranges;
+    a.add = p.ranges == 1;
+    a.out_w = out_w; a.out_b = out_b;
+    if (p.ranges > 1) {
+        a.out_w = static_cast<float *>(ws);
+        a.out_b = a.out_w + align4(g.pw);
+        a.stride_w = a.stride_b = align4(g.pw) + align4(g.pb);
+    }
+    const bool words = !g.bf16 || g.cout % 2 == 0;
+    const dim3 grid((unsigned)(((size_t)a.tiles_o * a.columns * p.ranges + 7) / 8 * 8));
+    dp_status st;
+    profile_begin(s);
+    if (!p.rows) st = p.nj == 4 ? run_contract<1, 4, true, true>(words, grid, a, s) : run_contract<1, 2, true, true>(words, grid, a, s);
+    else st = g.bf16 ? run_contract<3, 2, true, true>(words, grid, a, s) : run_contract<3, 2, true, false>(words, grid, a, s);
+    profile_end(s);
+    if (st != DP_OK || p.ranges == 1) return st;
+    const size_t groups = (align4(g.pw) + align4(g.pb)) / 4;
+    hipLaunchKernelGGL(ck_ranges_kernel, dim3((unsigned)((groups + 255) / 256)), dim3(256), 0, s, a.out_w, a.stride_w, align4(g.pw), p.ranges, g.pw, g.pb, out_w, out_b);
+    return check_launch("checkpoint_ranges");
+}
+
 dp_status launch_checkpoint_dense(const Geo &g, int mode, const uint8_t *codes, const uint8_t *scales, const void *dy, const int32_t *lengths,
                                   float *out_w, float *out_b, size_t out_stride, float *sqnorm, const float *group_sqnorm, float clip_c,
                                   void *ws, hipStream_t s)
@@ -589,33 +773,30 @@ dp_status launch_checkpoint_dense(const Geo &g, int mode, const uint8_t *codes, 
     a.codes = codes; a.scales = scales; a.dy = dy; a.lengths = lengths;
     a.n = g.n; a.tokens = g.h; a.cin = g.cin; a.cout = g.cout; a.pitch = ck_pitch(g.cin);
     a.has_bias = g.has_bias;
-    a.tiles_o = ck_tiles(g.cout); a.tiles_k = ck_tiles(g.cin);
-    const bool aligned = g.bf16 ? g.cout % 8 == 0 : g.cout % 4 == 0;
-    // workgroups of all XCDs alike (the kernel's map), those beyond the last one end at once
-    auto grid = [&](int slots) { return dim3((unsigned)(((size_t)a.tiles_o * a.tiles_k * slots + 7) / 8 * 8)); };
-    dp_status st;
+    a.tiles_o = ck_tiles(g.cout, CT);
     if (mode == MODE_WEIGHTED) {
         a.group_sqnorm = group_sqnorm; a.clip_c = clip_c;
-        a.chunks = p.chunks; a.per_range = p.per_range; a.cpe = p.cpe; a.slots = p.ranges;
-        a.add = p.ranges == 1;
-        a.out_w = out_w; a.out_b = out_b;
-        if (p.ranges > 1) {
-            a.out_w = static_cast<float *>(ws);
-            a.stride_w = align4(g.pw);
-            a.out_b = a.out_w + p.ranges * a.stride_w;
-            a.stride_b = align4(g.pb);
+        if (p.rows) return launch_weighted(g, a, out_w, out_b, ws, s);
+        // as many examples to a launch as the kernel's table has room for
+        for (int i = 0; i < g.n; i += CK_TABLE) {
+            Geo part = g;
+            part.n = a.n = std::min(g.n - i, CK_TABLE);
+            const dp_status st = launch_weighted(part, a, out_w, out_b, ws, s);
+            if (st != DP_OK) return st;
+            const size_t rows = (size_t)a.n * g.h;
+            a.codes += rows * a.pitch;
+            a.scales += rows * (a.pitch / CK_BLOCK);
+            a.dy = static_cast<const uint16_t *>(a.dy) + rows * g.cout;
+            if (a.lengths) a.lengths += a.n;
+            a.group_sqnorm += a.n;
         }
-        profile_begin(s);
-        if (!p.rows) st = run_contract<1, true, true>(aligned, grid(p.ranges), a, s);
-        else if (g.bf16) st = run_contract<3, true, true>(aligned, grid(p.ranges), a, s);
-        else st = run_contract<3, true, false>(aligned, grid(p.ranges), a, s);
-        profile_end(s);
-        if (st != DP_OK || p.ranges == 1) return st;
-        hipLaunchKernelGGL(ck_ranges_kernel, dim3((unsigned)((g.pw + 1023) / 1024)), dim3(256), 0, s, a.out_w, a.stride_w, p.ranges, g.pw, out_w);
-        if (g.pb)
-            hipLaunchKernelGGL(ck_ranges_kernel, dim3((unsigned)((g.pb + 1023) / 1024)), dim3(256), 0, s, a.out_b, a.stride_b, p.ranges, g.pb, out_b);
-        return check_launch("checkpoint_ranges");
+        return DP_OK;
     }
+    a.tiles_k = ck_tiles(g.cin, 64 * p.nj); a.columns = a.tiles_k + g.has_bias;
+    const bool words = !g.bf16 || g.cout % 2 == 0;
+    // workgroups of all XCDs alike (the kernel's map), those beyond the last one end at once
+    const dim3 grid((unsigned)(((size_t)a.tiles_o * a.columns * g.n + 7) / 8 * 8));
+    dp_status st;
     a.partials = static_cast<float *>(ws);
     a.stored = out_w != nullptr;
     a.out_w = out_w; a.out_b = out_b;
@@ -628,9 +809,9 @@ dp_status launch_checkpoint_dense(const Geo &g, int mode, const uint8_t *codes, 
         st = p.gram_b == 1 ? launch_lds<ck_gram_kernel<1, 8>>(blocks, 512, 8 * 16 * 64 * 4, s, a, (int)p.per_example)
                            : launch_lds<ck_gram_kernel<2, 4>>(blocks, 256, 4 * 64 * 64 * 4, s, a, (int)p.per_example);
     } else if (g.bf16) {
-        st = run_contract<1, false, true>(aligned, grid(g.n), a, s);
+        st = p.nj == 4 ? run_contract<1, 4, false, true>(words, grid, a, s) : run_contract<1, 2, false, true>(words, grid, a, s);
     } else {
-        st = run_contract<3, false, false>(aligned, grid(g.n), a, s);
+        st = run_contract<3, 2, false, false>(words, grid, a, s);
     }
     profile_end(s);
     if (st != DP_OK || !sqnorm) return st;

@@ -20,7 +20,7 @@ dp_status check_launch(const char *what);
 void profile_begin(hipStream_t s);
 void profile_end(hipStream_t s);
 
-// Launch of a kernel with `lds` bytes of dynamic LDS; the runtime is told once for a kernel and device that it may pass 64 KB (telling it
+// Launch of a kernel with `lds` bytes of dynamic LDS; the runtime is told once for a kernel and device that it may pass 64 KB (with its static LDS at most 160; telling it
 // twice is harmless).
 template <auto Kernel, typename... Args>
 dp_status launch_lds(dim3 grid, unsigned threads, unsigned lds, hipStream_t s, const Args &...args)
@@ -31,7 +31,7 @@ dp_status launch_lds(dim3 grid, unsigned threads, unsigned lds, hipStream_t s, c
         if (hipGetDevice(&dev) != hipSuccess) return fail(DP_ERR_DEVICE, "hipGetDevice failed");
         const uint64_t bit = 1ull << (dev & 63);
         if (!(told.load() & bit)) {
-            if (hipFuncSetAttribute(reinterpret_cast<const void *>(Kernel), hipFuncAttributeMaxDynamicSharedMemorySize, 152 * 1024) != hipSuccess)
+            if (hipFuncSetAttribute(reinterpret_cast<const void *>(Kernel), hipFuncAttributeMaxDynamicSharedMemorySize, 140 * 1024) != hipSuccess)
                 return fail(DP_ERR_DEVICE, "cannot reserve %u bytes of LDS", lds);
             told.fetch_or(bit);
         }

@@ -166,6 +166,7 @@ CASES = [
     (1, 300, 64, 72, True, False),
     (2, 257, 300, 256, True, True),
     (40, 20, 256, 300, True, True),
+    (150, 40, 520, 260, True, True),
 ]
 
 
@@ -258,7 +259,7 @@ def clip(desc, dev, sq, clip_c, acc_w, acc_b, stream=None):
 
 
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
-@pytest.mark.parametrize("case", CASES + [(64, 48, 128, 100, True, True), (16, 128, 260, 136, True, False)], ids=str)
+@pytest.mark.parametrize("case", CASES + [(64, 48, 128, 100, True, True), (16, 128, 260, 136, True, False), (1030, 17, 32, 40, True, True), (2, 40, 2600, 5000, True, True)], ids=str)
 def test_clipped_sum(case, dtype):
     n, tokens, cin, cout, bias, ragged = case
     broken = (1,) if n > 2 else ()
