@@ -547,134 +547,210 @@ __global__ void __launch_bounds__(256) ck_ranges_kernel(const float *part, size_
 // ------------------------------------------------------------------------------------------
 // Norms of short examples from the two Gram matrices of their tokens, T^2 (F + O) operations for 2 T F O:
 //     |dW_i|^2 + |db_i|^2 = sum_{t, u} (dY_t . dY_u) (X_t . X_u + bias).
-// A workgroup takes one pair of tiles of 32 B tokens of one example (those above the diagonal once, counted twice); its waves share the
-// features, and their sums meet in LDS in the order of the waves.  Tokens and features both operands agree on need no order: a lane
-// loads 16 consecutive features of a token, codes or bf16, and gives eight to each of two matrix instructions; nothing goes through
-// LDS on the way in.
-template <int B, int NW>
-__global__ void __launch_bounds__(64 * NW) ck_gram_kernel(const CkDenseArgs a, int pairs)
+// A workgroup of four waves takes one pair of tiles of 64 tokens of one example (those above the diagonal once, counted twice), chunk by chunk of 128
+// features: whole lines of memory into LDS, as bf16, the next chunk on its way; features both operands agree on need no order, so that
+// operands are 16-byte reads of a token's row, and each wave takes a quarter of a chunk's features for the whole 64 x 64.  Bound by what a
+// compute unit takes in, hence the tiles; where there are few pairs, several workgroups share a pair's features (splits) and
+// ck_gram_join_kernel adds up their sums before it multiplies.
+// WORDS: rows of dY begin at whole dwords.
+constexpr int GT = 64, GC = 128, G_ROW = 2 * GC + 16, G_SIDE = GT * G_ROW, G_STAGE = 2 * G_SIDE;      // tokens, features; bytes (16 of a row keep rows in different banks)
+constexpr int G_VALUES = GT * GT;
+
+template <bool WORDS>
+__global__ void __launch_bounds__(256, 2) ck_gram_kernel(const CkDenseArgs a, int pairs, int splits, float *tiles)
 {
     extern __shared__ __attribute__((aligned(16))) char ck_lds[];
-    __shared__ float red[NW];
-    const int ex = (int)(blockIdx.x / (unsigned)pairs);
-    int pair = (int)(blockIdx.x - (unsigned)ex * (unsigned)pairs), tile_a = 0;
+    __shared__ float red[4];
+    const unsigned whole = blockIdx.x / (unsigned)splits;          // example and pair
+    const int split = (int)(blockIdx.x - whole * (unsigned)splits), ex = (int)(whole / (unsigned)pairs);
+    int pair = (int)(whole - (unsigned)ex * (unsigned)pairs), tile_a = 0;
     while (pair > tile_a) { ++tile_a; pair -= tile_a; }            // pairs (0,0) (1,0) (1,1) (2,0) ...
     const int tile_b = pair;
     const bool diagonal = tile_a == tile_b;
-    const int t = threadIdx.x, lane = t & 63, wave = t >> 6, half = lane >> 5;
-    const int len = ck_length(a, ex);
-    if (tile_a * 32 * B >= len) {                                  // (tile_b is not the larger one)
-        if (t == 0) a.partials[blockIdx.x] = 0.0f;
+    const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
+    const int len = __builtin_amdgcn_readfirstlane(ck_length(a, ex));
+    if (tile_a * GT >= len) {                                      // (tile_b is not the larger one)
+        if (t == 0 && splits == 1) a.partials[whole] = 0.0f;
         return;
     }
+    const size_t row0 = (size_t)ex * (unsigned)a.tokens;
+    const int s_pitch = a.pitch / CK_BLOCK;
+    const uint16_t *dy = static_cast<const uint16_t *>(a.dy) + row0 * (unsigned)a.cout;
+    // the example's tokens as buffers that end with its last one: those that are not there are zeros
+    const __amdgpu_buffer_rsrc_t xb = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(a.codes) + row0 * (unsigned)a.pitch, 0, len * a.pitch, 0x00020000);
+    const __amdgpu_buffer_rsrc_t sb = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(a.scales) + row0 * (unsigned)s_pitch, 0, len * s_pitch, 0x00020000);
+    const __amdgpu_buffer_rsrc_t yb = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t *>(dy), 0, len * a.cout * 2, 0x00020000);
+    // this workgroup's chunks, first those of X, then those of dY
+    const int all_x = (a.pitch + GC - 1) / GC, all_y = (a.cout + GC - 1) / GC;
+    const int x0 = all_x * split / splits, nx = all_x * (split + 1) / splits - x0, y0 = all_y * split / splits, ny = all_y * (split + 1) / splits - y0;
+    const int xr = t >> 3, xp = t & 7, yr = t >> 4, yp = t & 15;   // pieces: 16 codes of rows xr + 32 u, eight values of dY of rows yr + 16 u
 
-    f32x16 gx[B][B], gy[B][B];
+    typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+    uint4 held[2][4];                                              // a chunk on its way
+    uint32_t scale[2][2];
+    auto fetch = [&](int i) {
 #pragma unroll
-    for (int i = 0; i < B; ++i)
+        for (int side = 0; side < 2; ++side) {
+            if (side == 1 && diagonal) break;
+            const int first = (side ? tile_b : tile_a) * GT;
+            if (i < nx) {
+                const int c = x0 + i;
 #pragma unroll
-        for (int j = 0; j < B; ++j)
+                for (int u = 0; u < 2; ++u) {
+                    const int row = first + xr + 32 * u;
+                    const u32x4 v = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(xb, row * a.pitch + xp * 16, c * GC, 0));
+                    held[side][u] = make_uint4(v.x, v.y, v.z, v.w);
+                    scale[side][u] = __builtin_amdgcn_raw_buffer_load_b8(sb, row * s_pitch + (xp >> 1), c * (GC / CK_BLOCK), 0);
+                }
+            } else if (i < nx + ny) {
+                const int c = y0 + i - nx;
+#pragma unroll
+                for (int u = 0; u < 4; ++u) {
+                    const int row = first + yr + 16 * u;
+                    if constexpr (WORDS) {
+                        const u32x4 v = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(yb, (row * a.cout + yp * 8) * 2, c * GC * 2, 0));
+                        held[side][u] = make_uint4(v.x, v.y, v.z, v.w);
+                    } else {
+                        held[side][u] = load8(dy + (size_t)row * (unsigned)a.cout + c * GC + yp * 8, row < len ? a.cout - c * GC - yp * 8 : 0);
+                    }
+                }
+            }
+        }
+    };
+    auto stage = [&](int i, int buf) {
+#pragma unroll
+        for (int side = 0; side < 2; ++side) {
+            if (side == 1 && diagonal) break;
+            char *to = ck_lds + buf * G_STAGE + side * G_SIDE;
+            if (i < nx) {
+                const bool there = (x0 + i) * GC + xp * 16 < a.pitch;      // (beyond: the next token's codes)
+#pragma unroll
+                for (int u = 0; u < 2; ++u) {
+                    const float f = pow2_of((int)scale[side][u]);
+                    const uint4 c = there ? held[side][u] : make_uint4(0, 0, 0, 0);
+                    const uint2 w0 = ck_bf16(c.x, f), w1 = ck_bf16(c.y, f), w2 = ck_bf16(c.z, f), w3 = ck_bf16(c.w, f);
+                    uint4 *at = reinterpret_cast<uint4 *>(to + (xr + 32 * u) * G_ROW + xp * 32);
+                    at[0] = make_uint4(w0.x, w0.y, w1.x, w1.y);
+                    at[1] = make_uint4(w2.x, w2.y, w3.x, w3.y);
+                }
+            } else {
+                const int left = a.cout - (y0 + i - nx) * GC - yp * 8;
+#pragma unroll
+                for (int u = 0; u < 4; ++u) {
+                    uint32_t w[4] = {held[side][u].x, held[side][u].y, held[side][u].z, held[side][u].w};
+                    if (WORDS && (y0 + i - nx + 1) * GC > a.cout) mask_piece<true>(w, 0, left);       // beyond: the next token's values
+                    *reinterpret_cast<uint4 *>(to + (yr + 16 * u) * G_ROW + yp * 16) = make_uint4(w[0], w[1], w[2], w[3]);
+                }
+            }
+        }
+    };
+    f32x16 gx[2][2], gy[2][2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
 #pragma unroll
             for (int r = 0; r < 16; ++r) gx[i][j][r] = gy[i][j][r] = 0.0f;
-
-    size_t row[2][B];
-    bool there[2][B];
+    auto products = [&](f32x16 (&g)[2][2], int buf) {
+        const char *base_a = ck_lds + buf * G_STAGE + (lane & 31) * G_ROW + (lane >> 5) * 16 + wave * 64, *base_b = base_a + (diagonal ? 0 : G_SIDE);
 #pragma unroll
-    for (int i = 0; i < B; ++i) {
-        const int ta = (tile_a * B + i) * 32 + (lane & 31), tb = (tile_b * B + i) * 32 + (lane & 31);
-        there[0][i] = ta < len; row[0][i] = (size_t)ex * a.tokens + ta;
-        there[1][i] = tb < len; row[1][i] = (size_t)ex * a.tokens + tb;
-    }
-    auto products = [&](const uint4 (&va)[B][2], const uint4 (&vb)[B][2], f32x16 (&g)[B][B]) {
+        for (int ks = 0; ks < 2; ++ks) {
+            bf16x8 va[2], vb[2];
 #pragma unroll
-        for (int q = 0; q < 2; ++q)
-#pragma unroll
-            for (int i = 0; i < B; ++i)
-#pragma unroll
-                for (int j = 0; j < B; ++j)
-                    g[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, va[i][q]), __builtin_bit_cast(bf16x8, vb[j][q]), g[i][j], 0, 0, 0);
-    };
-
-    const int x_blocks = a.pitch / CK_BLOCK;
-    auto load_x = [&](int side, int blk, uint4 (&v)[B][2]) {
-#pragma unroll
-        for (int i = 0; i < B; ++i) {
-            uint4 c = make_uint4(0, 0, 0, 0);
-            float scale = 1.0f;
-            if (there[side][i]) {
-                c = *reinterpret_cast<const uint4 *>(a.codes + row[side][i] * a.pitch + blk * 32 + half * 16);
-                scale = pow2_of(a.scales[row[side][i] * (unsigned)x_blocks + blk]);
+            for (int i = 0; i < 2; ++i) {
+                va[i] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4 *>(base_a + i * 32 * G_ROW + ks * 32));
+                vb[i] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4 *>(base_b + i * 32 * G_ROW + ks * 32));
             }
-            const uint2 w0 = ck_bf16(c.x, scale), w1 = ck_bf16(c.y, scale), w2 = ck_bf16(c.z, scale), w3 = ck_bf16(c.w, scale);
-            v[i][0] = make_uint4(w0.x, w0.y, w1.x, w1.y);
-            v[i][1] = make_uint4(w2.x, w2.y, w3.x, w3.y);
-        }
-    };
-    for (int blk = wave; blk < x_blocks; blk += NW) {
-        uint4 va[B][2], vb[B][2];
-        load_x(0, blk, va);
-        if (diagonal) products(va, va, gx);
-        else { load_x(1, blk, vb); products(va, vb, gx); }
-    }
-
-    const int y_blocks = (a.cout + 31) / 32;
-    auto load_y = [&](int side, int blk, uint4 (&v)[B][2]) {
-        const int col = blk * 32 + half * 16;
 #pragma unroll
-        for (int i = 0; i < B; ++i) {
-            const int count = there[side][i] ? a.cout - col : 0;
-            const uint16_t *p = static_cast<const uint16_t *>(a.dy) + row[side][i] * a.cout + col;
-            v[i][0] = load8(p, count);
-            v[i][1] = load8(p + 8, count - 8);
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+                for (int j = 0; j < 2; ++j) g[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(va[i], vb[j], g[i][j], 0, 0, 0);
         }
     };
-    for (int blk = wave; blk < y_blocks; blk += NW) {
-        uint4 va[B][2], vb[B][2];
-        load_y(0, blk, va);
-        if (diagonal) products(va, va, gy);
-        else { load_y(1, blk, vb); products(va, vb, gy); }
+    const int all = nx + ny;
+    fetch(0);
+    if (all > 0) stage(0, 0);
+    fetch(1);
+    __syncthreads();
+    for (int i = 0; i < nx; ++i) {
+        products(gx, i & 1);
+        if (i + 1 < all) stage(i + 1, (i + 1) & 1);
+        fetch(i + 2);
+        __syncthreads();
+    }
+    for (int i = nx; i < all; ++i) {
+        products(gy, i & 1);
+        if (i + 1 < all) stage(i + 1, (i + 1) & 1);
+        fetch(i + 2);
+        __syncthreads();
     }
 
-    // the waves' sums: wave w's value q of lane l at [w][q][l]; a thread adds up values of its own lane position
+    // the waves' sums meet in LDS, in the order of the waves: a wave adds up sixteen of a lane's 64 values
     float *buf = reinterpret_cast<float *>(ck_lds);
-    constexpr int Q = 16 * B * B, MINE = Q / NW;                   // values of a lane; of which this wave adds up MINE
-    static_assert(Q % NW == 0, "values are dealt to waves evenly");
-    auto put = [&](const f32x16 (&g)[B][B]) {
+    auto meet = [&](const f32x16 (&g)[2][2], float (&s)[16]) {
 #pragma unroll
-        for (int i = 0; i < B; ++i)
+        for (int i = 0; i < 2; ++i)
 #pragma unroll
-            for (int j = 0; j < B; ++j)
+            for (int j = 0; j < 2; ++j)
 #pragma unroll
-                for (int r = 0; r < 16; ++r) buf[(wave * Q + (i * B + j) * 16 + r) * 64 + lane] = g[i][j][r];
-    };
-    auto get = [&](float (&s)[MINE]) {
+                for (int r = 0; r < 16; ++r) buf[(wave * 64 + (i * 2 + j) * 16 + r) * 64 + lane] = g[i][j][r];
+        __syncthreads();
 #pragma unroll
-        for (int q = 0; q < MINE; ++q) {
+        for (int q = 0; q < 16; ++q) {
             s[q] = 0.0f;
 #pragma unroll
-            for (int w = 0; w < NW; ++w) s[q] += buf[(w * Q + wave * MINE + q) * 64 + lane];
+            for (int w = 0; w < 4; ++w) s[q] += buf[(w * 64 + wave * 16 + q) * 64 + lane];
         }
+        __syncthreads();
     };
-    float sx[MINE], sy[MINE];
-    put(gx);
-    __syncthreads();
-    get(sx);
-    __syncthreads();
-    put(gy);
-    __syncthreads();
-    get(sy);
+    float sx[16], sy[16];
+    meet(gx, sx);
+    meet(gy, sy);
+    if (splits > 1) {                                              // the other features' sums come first
+        float *to = tiles + (size_t)blockIdx.x * 2 * G_VALUES + wave * 16 * 64 + lane;
+#pragma unroll
+        for (int q = 0; q < 16; ++q) { to[q * 64] = sx[q]; to[G_VALUES + q * 64] = sy[q]; }
+        return;
+    }
     float ss = 0.0f;
 #pragma unroll
-    for (int q = 0; q < MINE; ++q) ss += (a.has_bias ? sx[q] + 1.0f : sx[q]) * sy[q];        // tokens that are not there: 0 dY . dY
-    const float tot = block_sum<NW>(ss, red);
-    if (t == 0) a.partials[blockIdx.x] = diagonal ? tot : 2.0f * tot;
+    for (int q = 0; q < 16; ++q) ss += (a.has_bias ? sx[q] + 1.0f : sx[q]) * sy[q];          // tokens that are not there: 0 dY . dY
+    const float tot = block_sum<4>(ss, red);
+    if (t == 0) a.partials[whole] = diagonal ? tot : 2.0f * tot;
+}
+
+// The products of a pair of tiles whose features several workgroups shared: their sums in order, then value by value.
+__global__ void __launch_bounds__(512) ck_gram_join_kernel(const CkDenseArgs a, int pairs, int splits, const float *tiles)
+{
+    __shared__ float red[8];
+    const int ex = (int)(blockIdx.x / (unsigned)pairs);
+    int pair = (int)(blockIdx.x - (unsigned)ex * (unsigned)pairs), tile_a = 0;
+    while (pair > tile_a) { ++tile_a; pair -= tile_a; }
+    float ss = 0.0f;
+    if (tile_a * GT < ck_length(a, ex)) {
+        constexpr int values = G_VALUES;
+        const float *p = tiles + (size_t)blockIdx.x * splits * 2 * values;
+#pragma unroll 1
+        for (int e = (int)threadIdx.x * 2; e < values; e += 1024) {
+            float2 x = make_float2(0.0f, 0.0f), y = x;
+#pragma unroll 4
+            for (int k = 0; k < splits; ++k) {
+                const float2 u = *reinterpret_cast<const float2 *>(p + (size_t)k * 2 * values + e), v = *reinterpret_cast<const float2 *>(p + (size_t)(2 * k + 1) * values + e);
+                x.x += u.x; x.y += u.y; y.x += v.x; y.y += v.y;
+            }
+            if (a.has_bias) { x.x += 1.0f; x.y += 1.0f; }
+            ss += x.x * y.x + x.y * y.y;
+        }
+    }
+    const float tot = block_sum<8>(ss, red);
+    if (threadIdx.x == 0) a.partials[blockIdx.x] = tile_a == pair ? tot : 2.0f * tot;
 }
 
 // ---- plans --------------------------------------------------------------------------------
 
 struct CkPlan {
     bool gram;
-    int gram_tiles;                  // tiles of 32 B tokens of an example
-    int gram_b;
+    int gram_splits;                 // workgroups that share a pair's features
     size_t per_example;              // partial squared norms
     int nj;                          // the contraction's tiles are 64 nj wide
     int ranges, chunks;              // weighted
@@ -683,7 +759,19 @@ struct CkPlan {
 
 int ck_tiles(int v, int width) { return (v + width - 1) / width; }
 
-// Gram matrices where they take fewer operations than the contraction, tiles counted whole.
+// Which of the two forms of norms: what they take, in microseconds, fitted to (n, T, F, O: Gram form / contraction) 32, 64, 768, 768: 12.4 / 11.4;
+// 8, 128, 2048, 2048: 21.7 / 19.5; 8, 512, 2048, 2048: 52 / 43; 16, 64, 4096, 4096: 20 / 68; 16, 128, 4096, 4096: 28 / 98; 16, 256, 4096, 4096: 50 / 155.
+// 512 workgroups of either kind fill the chip; a small launch afterwards is 4.
+double gram_us(const Geo &g, double pairs, int splits, double chunks)
+{
+    const double groups = g.n * pairs * splits;
+    return 5.0 + std::max(1.0, groups / 512.0) * chunks / splits * (pairs > 1.0 ? 1.4 : 0.6) + (splits > 1 ? 4.0 + groups / 128.0 : 0.0) + (pairs > 1.0 ? 4.0 : 0.0);
+}
+double contract_us(const Geo &g, double tiles, int chunk)
+{
+    return 4.0 + std::max(1.0, g.n * tiles / 512.0) * (1.8 + 0.95 * ((g.h + chunk - 1) / chunk)) + (tiles > 1.0 ? 4.0 : 0.0);
+}
+
 CkPlan ck_plan(const Geo &g, int mode)
 {
     CkPlan p = {};
@@ -705,13 +793,10 @@ CkPlan ck_plan(const Geo &g, int mode)
     const int tiles_k = ck_tiles(g.cin, 64 * p.nj);
     p.per_example = (size_t)tiles_o * (tiles_k + g.has_bias);
     if (mode == MODE_NORM && g.bf16) {
-        p.gram_b = g.h <= 32 ? 1 : 2;
-        p.gram_tiles = (g.h + 32 * p.gram_b - 1) / (32 * p.gram_b);
-        const double pairs = 0.5 * p.gram_tiles * (p.gram_tiles + 1), side = 32.0 * p.gram_b;
-        const double gram = pairs * side * side * ((double)g.cin + g.cout);
-        const double direct = (double)((g.h + 15) / 16 * 16) * tiles_o * CT * (double)tiles_k * 64 * p.nj;
-        p.gram = 4 * gram < direct;
-        if (p.gram) p.per_example = (size_t)p.gram_tiles * (p.gram_tiles + 1) / 2;
+        const long long tiles = (g.h + GT - 1) / GT, pairs = tiles * (tiles + 1) / 2, chunks = (ck_pitch(g.cin) + GC - 1) / GC + (g.cout + GC - 1) / GC;
+        p.gram_splits = (int)std::max(1ll, std::min({512 / (g.n * pairs), chunks / 8, 16ll}));
+        p.gram = gram_us(g, (double)pairs, p.gram_splits, (double)chunks) < contract_us(g, (double)p.per_example, ck_chunk(1, p.nj));
+        if (p.gram) p.per_example = (size_t)pairs;
     }
     return p;
 }
@@ -730,13 +815,19 @@ size_t align4(size_t v) { return (v + 3) & ~(size_t)3; }
 
 }  // namespace
 
+// What the workgroups that share a pair's features leave, behind the partial squared norms.
+static size_t gram_tile_bytes(const Geo &g, const CkPlan &p)
+{
+    return p.gram && p.gram_splits > 1 ? (size_t)g.n * p.per_example * p.gram_splits * 2 * G_VALUES * 4 : 0;
+}
+
 size_t checkpoint_ws_bytes(const Geo &g, int mode)
 {
     const CkPlan p = ck_plan(g, mode);
     if (mode == MODE_WEIGHTED) return p.ranges > 1 ? 4 * (size_t)p.ranges * (align4(g.pw) + align4(g.pb)) : 0;
     // both per-example forms: a caller sizes its workspace once
     const CkPlan q = ck_plan(g, mode == MODE_NORM ? MODE_MATERIALISE : MODE_NORM);
-    return align16(4 * (size_t)g.n * std::max(p.per_example, q.per_example));
+    return align16(4 * (size_t)g.n * std::max(p.per_example, q.per_example)) + std::max(gram_tile_bytes(g, p), gram_tile_bytes(g, q));
 }
 
 static dp_status launch_weighted(const Geo &g, CkDenseArgs a, float *out_w, float *out_b, void *ws, hipStream_t s)
@@ -797,7 +888,8 @@ dp_status launch_checkpoint_dense(const Geo &g, int mode, const uint8_t *codes, 
     // workgroups of all XCDs alike (the kernel's map), those beyond the last one end at once
     const dim3 grid((unsigned)(((size_t)a.tiles_o * a.columns * g.n + 7) / 8 * 8));
     dp_status st;
-    a.partials = static_cast<float *>(ws);
+    const bool alone = p.per_example == 1 && sqnorm;               // an example's only partial sum is its squared norm
+    a.partials = alone ? sqnorm : static_cast<float *>(ws);
     a.stored = out_w != nullptr;
     a.out_w = out_w; a.out_b = out_b;
     a.stride_w = out_stride ? out_stride : g.pw;
@@ -805,16 +897,19 @@ dp_status launch_checkpoint_dense(const Geo &g, int mode, const uint8_t *codes, 
     a.slots = g.n;
     profile_begin(s);
     if (p.gram) {
-        const dim3 blocks((unsigned)(g.n * p.per_example));
-        st = p.gram_b == 1 ? launch_lds<ck_gram_kernel<1, 8>>(blocks, 512, 8 * 16 * 64 * 4, s, a, (int)p.per_example)
-                           : launch_lds<ck_gram_kernel<2, 4>>(blocks, 256, 4 * 64 * 64 * 4, s, a, (int)p.per_example);
+        const int pairs = (int)p.per_example;
+        const dim3 joins((unsigned)(g.n * p.per_example)), blocks(joins.x * (unsigned)p.gram_splits);
+        float *tiles = reinterpret_cast<float *>(static_cast<char *>(ws) + align16(4 * (size_t)g.n * p.per_example));
+        st = words ? launch_lds<ck_gram_kernel<true>>(blocks, 256, 2 * G_STAGE, s, a, pairs, p.gram_splits, tiles)
+                   : launch_lds<ck_gram_kernel<false>>(blocks, 256, 2 * G_STAGE, s, a, pairs, p.gram_splits, tiles);
+        if (st == DP_OK && p.gram_splits > 1) st = launch_lds<ck_gram_join_kernel>(joins, 512, 0, s, a, pairs, p.gram_splits, tiles);
     } else if (g.bf16) {
         st = p.nj == 4 ? run_contract<1, 4, false, true>(words, grid, a, s) : run_contract<1, 2, false, true>(words, grid, a, s);
     } else {
         st = run_contract<3, 2, false, false>(words, grid, a, s);
     }
     profile_end(s);
-    if (st != DP_OK || !sqnorm) return st;
+    if (st != DP_OK || !sqnorm || alone) return st;
     return launch_sum_partials(a.partials, g.n, (int)p.per_example, sqnorm, s);
 }
 
