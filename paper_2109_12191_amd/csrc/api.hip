@@ -1168,10 +1168,12 @@ static dp_status make_bias_geo(const dp_bias_desc *d, BiasGeo &g)
     if (g.row_stride >= ((size_t)1 << 40) || (size_t)g.n * g.heads * g.queries >= ((size_t)1 << 31))
         return fail(DP_ERR_UNSUPPORTED, "2^31 rows or more");
     g.near = near;
-    const long double step = logl((long double)d->max_distance / near) / span;
+    const long double step = expl(logl((long double)d->max_distance / near) / span);
+    long double at = near;
     for (int k = 1; k < span; ++k) {
-        const long double at = near * expl(step * k), whole = rintl(at);
-        g.borders[g.border_count++] = (int)(fabsl(at - whole) < 1e-15L * at ? whole : ceill(at));
+        at *= step;                                      // 128 roundings at most, 2^-64 each
+        const int below = (int)at;
+        g.borders[g.border_count++] = at - below < 1e-15L * at ? below : below + 1;
     }
     g.far = g.border_count ? g.borders[g.border_count - 1] : near;
     return DP_OK;

@@ -459,8 +459,8 @@ __device__ __forceinline__ float lanes_reduce(float v)
     return v;
 }
 
-// A workgroup's rows of a tensor, each lane with a run of a row of its own.  WORDS: runs are 16-byte pieces that lie in their row altogether or
-// not at all (bf16: keys in eights; fp32: in fours; rows at whole dwords), by buffer accesses, left out by an offset beyond the buffer.
+// A workgroup's rows of a tensor, each lane with a run of a row of its own.  WORDS (as RowOf): buffer accesses, left out by an offset beyond the
+// buffer.  A run that a row ends in is loaded whole, with the next row's first values, and stored dword by dword.
 template <bool BF16, bool WORDS>
 struct NarrowRows {
     typedef typename In<BF16>::type E;
@@ -495,15 +495,18 @@ struct NarrowRows {
             if (there && k < keys) store8(first + (size_t)q * stride + k, keys - k, v);
         } else {
             const unsigned at = ((unsigned)q * (unsigned)stride + (unsigned)k) * (unsigned)sizeof(E);
-            if constexpr (BF16) {
-                const u32x4_t w = {pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7])};
-                __builtin_amdgcn_raw_buffer_store_b128(w, buffer, there && k < keys ? at : NOWHERE, 0, 0);
-            } else {
+            constexpr int PER = BF16 ? 2 : 1, WORDS_OF_RUN = 8 / PER;      // values of a dword, dwords of a run
+            uint32_t w[WORDS_OF_RUN];
 #pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    const u32x4_t w = {__float_as_uint(v[4 * i]), __float_as_uint(v[4 * i + 1]), __float_as_uint(v[4 * i + 2]), __float_as_uint(v[4 * i + 3])};
-                    __builtin_amdgcn_raw_buffer_store_b128(w, buffer, there && k + 4 * i < keys ? at + 16 * i : NOWHERE, 0, 0);
-                }
+            for (int i = 0; i < WORDS_OF_RUN; ++i) w[i] = BF16 ? pack_bf16(v[PER * i], v[PER * i + PER - 1]) : __float_as_uint(v[i]);
+            const bool whole = k + 8 <= keys;
+#pragma unroll
+            for (int i = 0; i < WORDS_OF_RUN; i += 4)
+                __builtin_amdgcn_raw_buffer_store_b128(u32x4_t{w[i], w[i + 1], w[i + 2], w[i + 3]}, buffer, there && whole ? at + 4 * i : NOWHERE, 0, 0);
+            if (keys & 7) {
+#pragma unroll
+                for (int i = 0; i < WORDS_OF_RUN; ++i)
+                    __builtin_amdgcn_raw_buffer_store_b32(w[i], buffer, there && !whole && k + PER * i < keys ? at + 4 * i : NOWHERE, 0, 0);
             }
         }
     }
@@ -649,11 +652,12 @@ __global__ void __launch_bounds__(1024) bias_table_kernel(const float *partials,
     if (threadIdx.x == 0 && sqnorm) sqnorm[blockIdx.x] = ss;
 }
 
-// Lanes of a wave that share a row in the kernels for short ones, or 0 where a row has a wave of its own or several.  A call with fewer than
-// eight queries would leave most of those lanes idle.
+// Lanes of a wave that share a row in the kernels for short ones, or 0 where a row has a wave of its own or several: a call with fewer than eight
+// queries would leave most of those lanes idle, and a few thousand rows are all under way at once that way (backward of 64 x 64, 4096
+// rows: 9.0 us, 12.8 with several rows to a wave and eight in turn; 16384 rows: 15.2 and 13.4; 131072 of 128 keys: 47 and 26).
 int narrow_lanes(const BiasGeo &g)
 {
-    if (g.keys > 256 || g.queries < 8 || g.row_stride > ((size_t)1 << 20)) return 0;
+    if (g.keys > 256 || g.queries < 8 || (long long)g.n * g.heads * g.queries < 16384 || g.row_stride > ((size_t)1 << 20)) return 0;
     return g.keys <= 64 ? 8 : g.keys <= 128 ? 16 : 32;
 }
 
@@ -679,11 +683,10 @@ BiasArgs bias_args(const BiasGeo &g)
     return a;
 }
 
-// Whether a tensor's rows can be read by whole dwords (and those of the kernels for short ones by whole pieces).
+// Whether a bf16 tensor's rows can be read by whole dwords (fp32 ones always can).
 bool bias_words(const BiasGeo &g, const void *p)
 {
-    if (narrow_lanes(g) && g.keys % (g.bf16 ? 8 : 4)) return false;
-    return !g.bf16 || ((reinterpret_cast<uintptr_t>(p) & 3) == 0 && g.keys % 2 == 0 && g.row_stride % 2 == 0);
+    return (reinterpret_cast<uintptr_t>(p) & 3) == 0 && g.keys % 2 == 0 && g.row_stride % 2 == 0;
 }
 
 template <bool BF16, bool WORDS>
@@ -734,9 +737,8 @@ dp_status launch_bias_softmax(const BiasGeo &g, const void *scores, const float 
 {
     BiasArgs a = bias_args(g);
     a.in = scores; a.out = probs; a.table = table; a.query_lengths = query_lengths; a.key_lengths = key_lengths;
-    const bool words = bias_words(g, scores) && bias_words(g, probs);
-    if (g.bf16) return words ? run_forward<true, true>(g, a, s) : run_forward<true, false>(g, a, s);
-    return words ? run_forward<false, true>(g, a, s) : run_forward<false, false>(g, a, s);
+    if (!g.bf16) return run_forward<false, true>(g, a, s);
+    return bias_words(g, scores) && bias_words(g, probs) ? run_forward<true, true>(g, a, s) : run_forward<true, false>(g, a, s);
 }
 
 dp_status launch_bias_softmax_backward(const BiasGeo &g, const void *probs, const void *dprobs, const int32_t *query_lengths,
@@ -747,8 +749,7 @@ dp_status launch_bias_softmax_backward(const BiasGeo &g, const void *probs, cons
     a.in = probs; a.in2 = dprobs; a.out = dscores; a.query_lengths = query_lengths; a.key_lengths = key_lengths;
     a.partials = static_cast<float *>(ws);
     const bool words = bias_words(g, probs) && bias_words(g, dprobs) && bias_words(g, dscores);
-    const dp_status st = g.bf16 ? (words ? run_backward<true, true>(g, a, s) : run_backward<true, false>(g, a, s))
-                                : (words ? run_backward<false, true>(g, a, s) : run_backward<false, false>(g, a, s));
+    const dp_status st = !g.bf16 ? run_backward<false, true>(g, a, s) : words ? run_backward<true, true>(g, a, s) : run_backward<true, false>(g, a, s);
     if (st != DP_OK) return st;
     hipLaunchKernelGGL(bias_table_kernel, dim3((unsigned)g.n), dim3(1024), 0, s, a.partials, g.heads, a.blocks, g.buckets, g_table, g_stride, sqnorm);
     return check_launch("bias_table");

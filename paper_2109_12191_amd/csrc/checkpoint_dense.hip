@@ -13,6 +13,7 @@
 #include "checkpoint.h"
 
 #include <algorithm>
+#include <cmath>
 
 namespace dp {
 
@@ -69,8 +70,8 @@ __device__ __forceinline__ void split8(const float (&v)[8], uint4 (&planes)[3])
 //
 // PLANES: 1: dY as bf16 numbers; 3: fp32 values of dY, split.
 // Per-example call (WEIGHTED false): a workgroup contracts one example's tile, squares it, and stores it if asked.
-// WEIGHTED, PLANES 1: a workgroup walks over a range of the chunks of all examples that are not left out, as many as any other range's; chunks
-// after an example's last token are not among them.  With f_i = m_i 2^e_i, 1 <= m_i < 2, the power is put into
+// WEIGHTED, PLANES 1: a workgroup walks over a range of the chunks of all examples, as many as any other range's; chunks after an example's
+// last token are not among them.  With f_i = m_i 2^e_i, 1 <= m_i < 2, the power is put into
 // the scales of X, exactly, and the running sum is kept in units of m_i: it is multiplied by m_(i-1) / m_i where an example begins, and by
 // the last m at the end.  One set of accumulators for any number of examples, and each example meets its factor in fp32.
 // WEIGHTED, PLANES 3: rows (example, token) of the whole call one after the other, dY times its factor in fp32, then split: for fp32 dY, and
@@ -125,60 +126,64 @@ __global__ void __launch_bounds__(256, PLANES == 1 ? 2 : 1) ck_contract_kernel(c
         Raw8<BF16> y[YP];
         int rows;                                                  // of the chunk (0: it adds nothing)
         bool begins;                                               // an example begins with it, of
+        uint32_t sq;                                               //   this squared norm (as loaded), hence
         int power;                                                 //   factor f = m 2^power
         float m, f;
         float x_sq[ROWS ? XP : 1], y_sq[ROWS ? YP : 1];            // rows of any examples: squared norms, lengths and tokens of this thread's rows
         int x_left[ROWS ? XP : 1], y_left[ROWS ? YP : 1], x_len[ROWS ? XP : 1], y_len[ROWS ? YP : 1];
     };
-    int f_ex = 0, f_c = 0, f_len = len, f_power = 0;               // weighted, by example: what the next chunk belongs to
-    float f_m = 1.0f, f_f = 1.0f;
-    // lengths (0 where an example is left out), factors, and chunks of the examples before each
+    int f_ex = 0, f_c = 0, f_len = len;                            // weighted, by example: what the next chunk belongs to
+    // Ragged examples: lengths, and chunks of the examples before each, fetched together (one after the other they are a trip to memory each).
+    // Factors come with the chunks: an example that is left out is walked over without products.
     constexpr int TABLE = WEIGHTED && !ROWS ? CK_TABLE : 1;
-    __shared__ int ex_len[TABLE], ex_before[TABLE + 1], found, wave_chunks[4];
-    __shared__ float ex_f[TABLE];
+    __shared__ int ex_len[TABLE], ex_before[TABLE], found, wave_chunks[4];
     if constexpr (WEIGHTED && !ROWS) {
-        int mine = 0, before[4], count[4];
+        if (!a.lengths) {
+            const int cpe = (a.tokens + CK - 1) / CK;
+            c_begin = (int)((long long)a.n * cpe * slot / a.slots);
+            c_end = (int)((long long)a.n * cpe * (slot + 1) / a.slots);
+            f_ex = c_begin / cpe;
+            f_c = c_begin - f_ex * cpe;
+            f_len = a.tokens;
+        } else {
+            int mine = 0, before[4], count[4];
 #pragma unroll
-        for (int u = 0; u < 4; ++u) {
-            const int i = 4 * t + u;
-            int l = 0;
-            if (i < a.n) {
-                const float f = clip_factor(a.group_sqnorm[i], a.clip_c);
-                l = f == 0.0f ? 0 : ck_length(a, i);               // of factor 0: adds nothing, and no 0 * inf
-                ex_len[i] = l;
-                ex_f[i] = f;
+            for (int u = 0; u < 4; ++u) {
+                const int i = 4 * t + u, l = i < a.n ? ck_length(a, i) : 0;
+                if (i < a.n) ex_len[i] = l;
+                before[u] = mine;
+                mine += count[u] = (l + CK - 1) / CK;
             }
-            before[u] = mine;
-            mine += count[u] = (l + CK - 1) / CK;
-        }
-        int upto = mine;                                           // of this wave's threads up to this one
+            int upto = mine;                                       // of this wave's threads up to this one
 #pragma unroll
-        for (int off = 1; off < 64; off <<= 1) {
-            const int v = __shfl_up(upto, off, 64);
-            upto += lane >= off ? v : 0;
-        }
-        if (lane == 63) wave_chunks[wave] = upto;
-        if (t == 0) found = 0;
-        __syncthreads();
-        int base = upto - mine, total = 0;
+            for (int off = 1; off < 64; off <<= 1) {
+                const int v = __shfl_up(upto, off, 64);
+                upto += lane >= off ? v : 0;
+            }
+            if (lane == 63) wave_chunks[wave] = upto;
+            if (t == 0) found = 0;
+            __syncthreads();
+            int base = upto - mine, total = 0;
 #pragma unroll
-        for (int w = 0; w < 4; ++w) {
-            base += w < wave ? wave_chunks[w] : 0;
-            total += wave_chunks[w];
-        }
-        total = __builtin_amdgcn_readfirstlane(total);
-        c_begin = (int)((long long)total * slot / a.slots);
-        c_end = (int)((long long)total * (slot + 1) / a.slots);
+            for (int w = 0; w < 4; ++w) {
+                base += w < wave ? wave_chunks[w] : 0;
+                total += wave_chunks[w];
+            }
+            total = __builtin_amdgcn_readfirstlane(total);
+            c_begin = (int)((long long)total * slot / a.slots);
+            c_end = (int)((long long)total * (slot + 1) / a.slots);
 #pragma unroll
-        for (int u = 0; u < 4; ++u) {
-            const int i = 4 * t + u, first = base + before[u];
-            if (i < a.n) ex_before[i] = first;
-            if (c_begin >= first && c_begin < first + count[u]) found = i;
+            for (int u = 0; u < 4; ++u) {
+                const int i = 4 * t + u, first = base + before[u];
+                if (i < a.n) ex_before[i] = first;
+                if (c_begin >= first && c_begin < first + count[u]) found = i;
+            }
+            __syncthreads();
+            f_ex = __builtin_amdgcn_readfirstlane(found);
+            f_c = c_begin - __builtin_amdgcn_readfirstlane(ex_before[f_ex]);
         }
-        __syncthreads();
-        f_ex = __builtin_amdgcn_readfirstlane(found);
-        f_c = c_begin - __builtin_amdgcn_readfirstlane(ex_before[f_ex]);
     }
+    const __amdgpu_buffer_rsrc_t sq_buffer = __builtin_amdgcn_make_buffer_rsrc(const_cast<float *>(a.group_sqnorm), 0, a.n * 4, 0x00020000);
 
     auto load_rows = [&](Slot &s, unsigned row0_any, int rows_any) {
         // the same in every lane, which the compiler does not always see (and a buffer in vector registers is read lane by lane)
@@ -216,7 +221,7 @@ __global__ void __launch_bounds__(256, PLANES == 1 ? 2 : 1) ck_contract_kernel(c
     auto fetch = [&](Slot &s, int c) {
         s.rows = 0;
         s.begins = false;
-        s.power = 0;
+        s.sq = 0;
         if (c >= c_end) return;
         if constexpr (ROWS) {
             const unsigned total = (unsigned)a.n * (unsigned)a.tokens, row0 = (unsigned)c * CK;
@@ -234,20 +239,26 @@ __global__ void __launch_bounds__(256, PLANES == 1 ? 2 : 1) ck_contract_kernel(c
             load_rows(s, row0, s.rows);
         } else if constexpr (WEIGHTED) {
             s.begins = f_c == 0 || c == c_begin;
-            if (s.begins) {
+            if (s.begins && a.lengths) {
                 while (__builtin_amdgcn_readfirstlane(ex_len[f_ex]) == 0) ++f_ex;         // (there are chunks: an example with some follows)
                 f_len = __builtin_amdgcn_readfirstlane(ex_len[f_ex]);
-                f_f = __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, ex_f[f_ex])));
-                f_power = (int)(__float_as_uint(f_f) >> 23) - 127;
-                f_m = f_f * pow2_of(127 - f_power);
             }
+            s.sq = __builtin_amdgcn_raw_buffer_load_b32(sq_buffer, 4 * f_ex, 0, 0);
             s.rows = min(f_len - f_c * CK, CK);
-            s.power = f_power; s.m = f_m; s.f = f_f;
             load_rows(s, (unsigned)f_ex * (unsigned)a.tokens + (unsigned)(f_c * CK), s.rows);
             if (++f_c * CK >= f_len) { f_c = 0; ++f_ex; }
         } else {
             s.rows = min(len - c * CK, CK);
             load_rows(s, (unsigned)slot * (unsigned)a.tokens + (unsigned)(c * CK), s.rows);
+        }
+    };
+    // weighted, by example: the factor of a chunk that has arrived; one of factor 0 adds nothing (and no 0 * inf)
+    auto ready = [&](Slot &s) {
+        if constexpr (WEIGHTED && !ROWS) {
+            s.f = __uint_as_float((uint32_t)__builtin_amdgcn_readfirstlane((int)__float_as_uint(clip_factor(__uint_as_float(s.sq), a.clip_c))));
+            s.power = (int)(__float_as_uint(s.f) >> 23) - 127;
+            s.m = s.f * pow2_of(127 - s.power);
+            if (s.f == 0.0f) { s.rows = 0; s.power = 0; }
         }
     };
     auto row_factor = [&](const Slot &s, int u) { return s.y_left[u] < s.y_len[u] ? clip_factor(s.y_sq[u], a.clip_c) : 0.0f; };
@@ -292,7 +303,8 @@ __global__ void __launch_bounds__(256, PLANES == 1 ? 2 : 1) ck_contract_kernel(c
         float sum[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) sum[j] = 0.0f;
-        auto add = [&](const Slot &s) {
+        auto add = [&](Slot &s) {
+            ready(s);
             if (s.rows <= 0) return;
 #pragma unroll
             for (int u = 0; u < YP; ++u) {
@@ -396,6 +408,7 @@ __global__ void __launch_bounds__(256, PLANES == 1 ? 2 : 1) ck_contract_kernel(c
     Slot s0, s1;
     fetch(s0, c_begin);
     fetch(s1, c_begin + 1);
+    ready(s0);
     Now now = {s0.rows, s0.begins, s0.m};
     if (now.rows > 0) stage(s0, 0);
     fetch(s0, c_begin + 2);
@@ -404,6 +417,7 @@ __global__ void __launch_bounds__(256, PLANES == 1 ? 2 : 1) ck_contract_kernel(c
     // accumulators on every path.  Where the next chunk adds nothing, what is staged is not used.
     auto turn = [&](Slot &next, int buf, int c) {
         rescale(now);
+        ready(next);
         auto stage_xs = [&]() {
 #pragma unroll
             for (int u = 0; u < XP; ++u) stage_x(next, u, buf ^ 1);
@@ -437,15 +451,11 @@ __global__ void __launch_bounds__(256, PLANES == 1 ? 2 : 1) ck_contract_kernel(c
             if (now.rows > 0) {
                 Operands p, q;
                 read(p, 0, buf);
-                stage_xs();
+                read(q, 1, buf);
                 products(p);
-                if (now.rows > 16) {
-                    read(q, 1, buf);
-                    stage_ys();
-                    products(q);
-                } else {
-                    stage_ys();
-                }
+                stage_xs();
+                if (now.rows > 16) products(q);
+                stage_ys();
             } else {
                 stage_xs();
                 stage_ys();
@@ -784,9 +794,17 @@ CkPlan ck_plan(const Geo &g, int mode)
         const int chunk = ck_chunk(p.rows ? 3 : 1, p.nj);
         const long long chunks = p.rows ? ((long long)g.n * g.h + chunk - 1) / chunk : (long long)std::min(g.n, CK_TABLE) * ((g.h + chunk - 1) / chunk);
         p.chunks = (int)chunks;
-        // ranges of the call's chunks until there are two workgroups for each compute unit; a range has four chunks at least
-        const long long tiles = (long long)tiles_o * ck_tiles(g.cin, 64 * p.nj);
-        p.ranges = (int)std::max(1ll, std::min((512 + tiles - 1) / tiles, chunks / 4));
+        // Ranges of the call's chunks: fewer chunks in a row against more sums to write and join.  What R of them take, in microseconds, fitted
+        // to 16 x 128 tokens 768 -> 768 (R 1: 36, 3: 22.5, 6: 19.4, 16: 27), 16 x 512 2048 -> 2048 (1: 124, 2: 101, 4: 111, 8: 145) and
+        // 64 x 64 512 -> 512 (1: 68, 4: 28, 16: 19): 9 at least, a chunk 0.85 where a workgroup has a compute unit to itself and 1.2 where two
+        // share it, a value of a range's sums written and read at 4.5 TB/s.
+        const double tiles = (double)tiles_o * ck_tiles(g.cin, 64 * p.nj), sums = 8.0 * g.pw / 4.5e6;
+        double best = 0.0;
+        for (int r = 1; r <= 64 && (r == 1 || r <= chunks / 2); ++r) {
+            const double groups = tiles * r, chunk_us = groups <= 256.0 ? 0.85 : std::min(1.2, 0.85 + 0.35 * (groups - 256.0) / 256.0) * std::max(1.0, groups / 512.0);
+            const double us = 9.0 + chunk_us * std::ceil((double)chunks / r) + (r > 1 ? sums * r : 0.0);
+            if (r == 1 || us < best) { best = us; p.ranges = r; }
+        }
         return p;
     }
     if (g.bf16 && (long long)g.n * tiles_o * ck_tiles(g.cin, 256) >= 384) p.nj = 4;

@@ -108,41 +108,4 @@ __device__ __forceinline__ void store8(float *p, int count, const float (&v)[8])
                                                              __float_as_uint(v[4 * i + 2]), __float_as_uint(v[4 * i + 3])};
 }
 
-// Sixteen consecutive values of a row: `count` of them exist (the others are neither read nor written).  bf16 rows may start at any
-// element: dwords where the first value lies in the low half of one, else a value, seven dwords and a value -- nothing outside the
-// sixteen is touched, so the last row of a tensor needs no care.
-template <bool BF16>
-__device__ __forceinline__ void load_values(const typename In<BF16>::type *p, int count, float (&v)[16])
-{
-    if (count < 16) {
-#pragma unroll
-        for (int i = 0; i < 16; ++i) v[i] = i < count ? In<BF16>::ld(p + i) : 0.0f;
-        return;
-    }
-    if constexpr (BF16) {
-        uint32_t w[8];
-        if ((reinterpret_cast<uintptr_t>(p) & 2) == 0) {
-            const u32x4_a4 a = *reinterpret_cast<const u32x4_a4 *>(p), b = *reinterpret_cast<const u32x4_a4 *>(p + 8);
-            w[0] = a.x; w[1] = a.y; w[2] = a.z; w[3] = a.w; w[4] = b.x; w[5] = b.y; w[6] = b.z; w[7] = b.w;
-        } else {
-            const uint32_t first = p[0], last = p[15];
-            const u32x4_a4 a = *reinterpret_cast<const u32x4_a4 *>(p + 1);
-            const u32x2_a4 b = *reinterpret_cast<const u32x2_a4 *>(p + 9);
-            const uint32_t c = *reinterpret_cast<const uint32_t *>(p + 13);
-            const uint32_t r[9] = {first << 16, a.x, a.y, a.z, a.w, b.x, b.y, c, last};
-#pragma unroll
-            for (int i = 0; i < 8; ++i) w[i] = funnel(r[i + 1], r[i], 16);
-        }
-#pragma unroll
-        for (int i = 0; i < 8; ++i) { v[2 * i] = __uint_as_float(w[i] << 16); v[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u); }
-    } else {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const u32x4_a4 a = *reinterpret_cast<const u32x4_a4 *>(p + 4 * i);
-            v[4 * i] = __uint_as_float(a.x); v[4 * i + 1] = __uint_as_float(a.y);
-            v[4 * i + 2] = __uint_as_float(a.z); v[4 * i + 3] = __uint_as_float(a.w);
-        }
-    }
-}
-
 }  // namespace dp

@@ -86,13 +86,16 @@ CASES = [
     (2, 1, 20, 30, False, dict(buckets=4, max_distance=9)),
     (2, 2, 150, 130, True, dict(stride=133)),
     (2, 2, 150, 130, True, dict(stride=136, causal=1)),
-    (2, 3, 300, 64, False, {}),                                                # several rows to a wave
-    (2, 2, 70, 8, True, dict(causal=1)),
-    (4, 2, 140, 128, True, dict(causal=1, bidirectional=0)),
-    (3, 2, 270, 256, True, dict(offset=-1, buckets=8, max_distance=20)),
-    (2, 2, 65, 36, False, dict(causal=1, offset=5)),
-    (2, 1, 260, 201, False, dict(buckets=4, max_distance=4000)),
-    (2, 2, 40, 120, True, dict(stride=124)),
+    # more than 16384 rows of at most 256 keys: several to a wave
+    (10, 9, 210, 64, True, dict(causal=1)),
+    (3, 19, 300, 128, False, {}),
+    (4, 22, 200, 250, True, dict(buckets=8, max_distance=20)),
+    (4, 22, 190, 201, True, dict(causal=1, bidirectional=0)),
+    (30, 14, 40, 9, True, {}),
+    (30, 14, 40, 6, True, dict(causal=1, offset=2)),
+    (2, 33, 260, 256, True, dict(offset=-1)),
+    (5, 24, 140, 120, True, dict(stride=124)),
+    (5, 24, 140, 119, True, dict(stride=123, buckets=4, max_distance=4000)),
 ]
 
 
