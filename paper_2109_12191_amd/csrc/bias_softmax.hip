@@ -183,7 +183,7 @@ struct RowOf {
 
 // The sums of a workgroup's four waves, by distance in LDS and beyond the borders in registers, by bucket into its place of the workspace: a
 // wave takes every fourth bucket, its lanes the distances of the bucket's run.
-__device__ __forceinline__ void bias_bucket_sums(const BiasArgs &a, const float *lds, float sum_far, float sum_low, float (&ends)[4][2])
+__device__ __forceinline__ void bias_bucket_sums(const BiasArgs &a, const Rows &r, const float *lds, float sum_far, float sum_low, float (&ends)[4][2])
 {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const float far_wave = wave_all_sum(sum_far), low_wave = wave_all_sum(sum_low);
@@ -198,13 +198,18 @@ __device__ __forceinline__ void bias_bucket_sums(const BiasArgs &a, const float 
         const bool outer = m == side_buckets - 1, inner = !a.bidirectional && b == 0;
         // magnitudes lo .. hi; the outer bucket's and, with one side, bucket 0's run on into the slots beyond the border (runs reach 13 beyond)
         const int hi = outer ? a.far + 13 : start(m + 1) - 1, lo = inner ? -13 : after ? max(start(m), 1) : start(m);
+        // of those, the ones that some place of these rows has (seven places more, where runs end)
+        const int first = after ? max(lo, -(r.first + r.q1 - 1)) : max(lo, r.first + r.q0 - a.keys - 6);
+        const int last = after ? min(hi, a.keys + 6 - r.first - r.q0) : min(hi, r.first + r.q1 - 1);
         float s = 0.0f;
-        for (int d = lo + lane; d <= hi; d += 64) {
-            const int word = bias_word(a, RunWords::slot(a, after ? -d : d));
+        if (first <= last) {
+            for (int d = first + lane; d <= last; d += 64) {
+                const int word = bias_word(a, RunWords::slot(a, after ? -d : d));
 #pragma unroll
-            for (int w = 0; w < 4; ++w) s += lds[w * 8 * a.plane + word];
+                for (int w = 0; w < 4; ++w) s += lds[w * 8 * a.plane + word];
+            }
+            s = wave_all_sum(s);
         }
-        s = wave_all_sum(s);
         if (outer || inner) {
             const int which = after || inner ? 1 : 0;
             s += ends[0][which] + ends[1][which] + ends[2][which] + ends[3][which];
@@ -434,7 +439,7 @@ __global__ void __launch_bounds__(256) bias_backward_kernel(const BiasArgs a)
         }
     }
 
-    bias_bucket_sums(a, bias_lds, sum_far, sum_low, ends);
+    bias_bucket_sums(a, r, bias_lds, sum_far, sum_low, ends);
 }
 
 // ---- rows of at most 256 keys: TPR lanes of a wave to a row, 64 / TPR rows of a wave together, and eight rows of each of these in turn.  The
@@ -618,7 +623,7 @@ __global__ void __launch_bounds__(256) bias_backward_narrow_kernel(const BiasArg
         }
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");     // the next rows' lanes meet other lanes' words
     }
-    bias_bucket_sums(a, bias_lds, sum_far, sum_low, ends);
+    bias_bucket_sums(a, r, bias_lds, sum_far, sum_low, ends);
 }
 // Tables of an example from its workgroups' sums, and their squared norm: one workgroup an example.  Several threads share an
 // entry's sums where there are fewer entries than threads; their shares are added in order.

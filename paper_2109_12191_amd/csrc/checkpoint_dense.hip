@@ -78,7 +78,8 @@ __device__ __forceinline__ void split8(const float (&v)[8], uint4 (&planes)[3])
 // for examples of a few tokens, of which 32 rows hold several.
 // Bias: a column of workgroups of its own adds up dY.
 // WORDS: rows of dY begin at whole dwords: pieces by buffer loads, which give zeros beyond the chunk's last row (what a row's last piece takes
-// from the next row is multiplied into features beyond the last, which nobody reads); else (bf16, an odd number of features) piece by piece.
+// from the next row is multiplied into features beyond the last, which nobody reads).  Else (bf16, an odd number of features) every other
+// row begins in the middle of a dword: five dwords around a piece, shifted into place on their way into LDS.
 constexpr int CT = 128;                                            // o of a tile
 constexpr int ck_chunk(int planes, int nj) { return planes == 1 && nj == 2 ? 64 : 32; }
 constexpr int ck_stage_bytes(int planes, int nj) { return ck_chunk(planes, nj) * (planes * 2 * CT + nj * 128); }
@@ -124,6 +125,8 @@ __global__ void __launch_bounds__(256, PLANES == 1 ? 2 : 1) ck_contract_kernel(c
         uint4 x[XP];
         uint32_t scale[XP];
         Raw8<BF16> y[YP];
+        uint32_t y_more[WORDS ? 1 : YP];                           // odd rows: the dword after
+        uint32_t odd;                                              //   and whether the chunk's first row begins in the middle of one
         int rows;                                                  // of the chunk (0: it adds nothing)
         bool begins;                                               // an example begins with it, of
         uint32_t sq;                                               //   this squared norm (as loaded), hence
@@ -214,8 +217,17 @@ __global__ void __launch_bounds__(256, PLANES == 1 ? 2 : 1) ck_contract_kernel(c
                 }
             }
         } else {
+            const uintptr_t first = reinterpret_cast<uintptr_t>(dy);
+            s.odd = (uint32_t)(first >> 1) & 1u;
+            const __amdgpu_buffer_rsrc_t yb = __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<void *>(first & ~(uintptr_t)3), 0, ((rows * a.cout + (int)s.odd) * 2 + 3) & ~3, 0x00020000);
 #pragma unroll
-            for (int u = 0; u < YP; ++u) s.y[u].load(dy, (size_t)(yr + 16 * u) * a.cout + y_col, yr + 16 * u < rows ? y_count : 0);
+            for (int u = 0; u < YP; ++u) {
+                // (the dword of the chunk's last value may hold the next row's first as well)
+                const unsigned at = y_off == CK_NOWHERE || yr + 16 * u >= rows ? CK_NOWHERE : (y_off + (unsigned)(16 * u * a.cout) * 2u + 2u * s.odd) & ~3u;
+                const u32x4 v = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(yb, at, 0, 0));
+                s.y[u].w = make_uint4(v.x, v.y, v.z, v.w);
+                s.y_more[u] = __builtin_amdgcn_raw_buffer_load_b32(yb, at == CK_NOWHERE ? at : at + 16u, 0, 0);
+            }
         }
     };
     auto fetch = [&](Slot &s, int c) {
@@ -261,6 +273,14 @@ __global__ void __launch_bounds__(256, PLANES == 1 ? 2 : 1) ck_contract_kernel(c
             if (s.f == 0.0f) { s.rows = 0; s.power = 0; }
         }
     };
+    auto piece_y = [&](const Slot &s, int u) {                     // piece u of dY as it is
+        Raw8<BF16> y = s.y[u];
+        if constexpr (!WORDS) {
+            const uint32_t bits = ((((uint32_t)yr & 1u) ^ s.odd) & 1u) * 16u;         // (an odd number of features: rows take turns)
+            y.w = make_uint4(funnel(y.w.y, y.w.x, bits), funnel(y.w.z, y.w.y, bits), funnel(y.w.w, y.w.z, bits), funnel(s.y_more[u], y.w.w, bits));
+        }
+        return y;
+    };
     auto row_factor = [&](const Slot &s, int u) { return s.y_left[u] < s.y_len[u] ? clip_factor(s.y_sq[u], a.clip_c) : 0.0f; };
     auto stage_x = [&](const Slot &s, int u, int buf) {            // piece u of X into LDS
         const int r = xr + XS * u;
@@ -277,10 +297,10 @@ __global__ void __launch_bounds__(256, PLANES == 1 ? 2 : 1) ck_contract_kernel(c
         const int r = yr + 16 * u;
         char *to = ck_lds + buf * STAGE + r * Y_ROW + ((yp ^ ((r & 3) << 2)) << 4);
         if constexpr (PLANES == 1) {
-            *reinterpret_cast<uint4 *>(to) = s.y[u].w;
+            *reinterpret_cast<uint4 *>(to) = piece_y(s, u).w;
         } else {
             float v[8];
-            s.y[u].get(v);
+            piece_y(s, u).get(v);
             if constexpr (ROWS) {
                 const float f = row_factor(s, u);
 #pragma unroll
@@ -309,7 +329,7 @@ __global__ void __launch_bounds__(256, PLANES == 1 ? 2 : 1) ck_contract_kernel(c
 #pragma unroll
             for (int u = 0; u < YP; ++u) {
                 float v[8], f = 1.0f;
-                s.y[u].get(v);
+                piece_y(s, u).get(v);
                 if constexpr (ROWS) f = row_factor(s, u);
                 else if constexpr (WEIGHTED) f = s.f;
 #pragma unroll
@@ -562,11 +582,11 @@ __global__ void __launch_bounds__(256) ck_ranges_kernel(const float *part, size_
 // operands are 16-byte reads of a token's row, and each wave takes a quarter of a chunk's features for the whole 64 x 64.  Bound by what a
 // compute unit takes in, hence the tiles; where there are few pairs, several workgroups share a pair's features (splits) and
 // ck_gram_join_kernel adds up their sums before it multiplies.
-// WORDS: rows of dY begin at whole dwords.
+// fp32 dY: chunks of 64 features as they are, fp32 matrix instructions.  WORDS: as above.
 constexpr int GT = 64, GC = 128, G_ROW = 2 * GC + 16, G_SIDE = GT * G_ROW, G_STAGE = 2 * G_SIDE;      // tokens, features; bytes (16 of a row keep rows in different banks)
 constexpr int G_VALUES = GT * GT;
 
-template <bool WORDS>
+template <bool BF16, bool WORDS>
 __global__ void __launch_bounds__(256, 2) ck_gram_kernel(const CkDenseArgs a, int pairs, int splits, float *tiles)
 {
     extern __shared__ __attribute__((aligned(16))) char ck_lds[];
@@ -585,19 +605,23 @@ __global__ void __launch_bounds__(256, 2) ck_gram_kernel(const CkDenseArgs a, in
     }
     const size_t row0 = (size_t)ex * (unsigned)a.tokens;
     const int s_pitch = a.pitch / CK_BLOCK;
-    const uint16_t *dy = static_cast<const uint16_t *>(a.dy) + row0 * (unsigned)a.cout;
+    typedef typename In<BF16>::type E;
+    constexpr int YC = BF16 ? GC : GC / 2, YV = YC / 16;           // features of a chunk of dY, of a piece (16 bytes)
+    const uintptr_t y_at = reinterpret_cast<uintptr_t>(static_cast<const E *>(a.dy) + row0 * (unsigned)a.cout);
+    const int odd = WORDS ? 0 : (int)(y_at >> 1) & 1;              // the first row begins in the middle of a dword
     // the example's tokens as buffers that end with its last one: those that are not there are zeros
     const __amdgpu_buffer_rsrc_t xb = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(a.codes) + row0 * (unsigned)a.pitch, 0, len * a.pitch, 0x00020000);
     const __amdgpu_buffer_rsrc_t sb = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(a.scales) + row0 * (unsigned)s_pitch, 0, len * s_pitch, 0x00020000);
-    const __amdgpu_buffer_rsrc_t yb = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t *>(dy), 0, len * a.cout * 2, 0x00020000);
+    const int y_bytes = ((len * a.cout + odd) * (int)sizeof(E) + 3) & ~3;
+    const __amdgpu_buffer_rsrc_t yb = __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<void *>(y_at & ~(uintptr_t)3), 0, y_bytes, 0x00020000);
     // this workgroup's chunks, first those of X, then those of dY
-    const int all_x = (a.pitch + GC - 1) / GC, all_y = (a.cout + GC - 1) / GC;
+    const int all_x = (a.pitch + GC - 1) / GC, all_y = (a.cout + YC - 1) / YC;
     const int x0 = all_x * split / splits, nx = all_x * (split + 1) / splits - x0, y0 = all_y * split / splits, ny = all_y * (split + 1) / splits - y0;
-    const int xr = t >> 3, xp = t & 7, yr = t >> 4, yp = t & 15;   // pieces: 16 codes of rows xr + 32 u, eight values of dY of rows yr + 16 u
+    const int xr = t >> 3, xp = t & 7, yr = t >> 4, yp = t & 15;   // pieces: 16 codes of rows xr + 32 u, YV values of dY of rows yr + 16 u
 
     typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
     uint4 held[2][4];                                              // a chunk on its way
-    uint32_t scale[2][2];
+    uint32_t scale[2][2], more[2][WORDS ? 1 : 4];
     auto fetch = [&](int i) {
 #pragma unroll
         for (int side = 0; side < 2; ++side) {
@@ -617,12 +641,11 @@ __global__ void __launch_bounds__(256, 2) ck_gram_kernel(const CkDenseArgs a, in
 #pragma unroll
                 for (int u = 0; u < 4; ++u) {
                     const int row = first + yr + 16 * u;
-                    if constexpr (WORDS) {
-                        const u32x4 v = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(yb, (row * a.cout + yp * 8) * 2, c * GC * 2, 0));
-                        held[side][u] = make_uint4(v.x, v.y, v.z, v.w);
-                    } else {
-                        held[side][u] = load8(dy + (size_t)row * (unsigned)a.cout + c * GC + yp * 8, row < len ? a.cout - c * GC - yp * 8 : 0);
-                    }
+                    unsigned at = (unsigned)(row * a.cout + yp * YV + odd) * (unsigned)sizeof(E) & ~3u;
+                    if constexpr (!WORDS) at = row < len ? at : (unsigned)y_bytes;        // (the last value's dword may hold another)
+                    const u32x4 v = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(yb, at, c * YC * (int)sizeof(E), 0));
+                    held[side][u] = make_uint4(v.x, v.y, v.z, v.w);
+                    if constexpr (!WORDS) more[side][u] = __builtin_amdgcn_raw_buffer_load_b32(yb, at + 16u, c * YC * (int)sizeof(E), 0);
                 }
             }
         }
@@ -644,11 +667,15 @@ __global__ void __launch_bounds__(256, 2) ck_gram_kernel(const CkDenseArgs a, in
                     at[1] = make_uint4(w2.x, w2.y, w3.x, w3.y);
                 }
             } else {
-                const int left = a.cout - (y0 + i - nx) * GC - yp * 8;
+                const int left = a.cout - (y0 + i - nx) * YC - yp * YV;
 #pragma unroll
                 for (int u = 0; u < 4; ++u) {
                     uint32_t w[4] = {held[side][u].x, held[side][u].y, held[side][u].z, held[side][u].w};
-                    if (WORDS && (y0 + i - nx + 1) * GC > a.cout) mask_piece<true>(w, 0, left);       // beyond: the next token's values
+                    if constexpr (!WORDS) {                        // (an odd number of features: rows take turns)
+                        const uint32_t bits = (uint32_t)((yr ^ odd) & 1) * 16u;
+                        w[0] = funnel(w[1], w[0], bits); w[1] = funnel(w[2], w[1], bits); w[2] = funnel(w[3], w[2], bits); w[3] = funnel(more[side][u], w[3], bits);
+                    }
+                    if ((y0 + i - nx + 1) * YC > a.cout) mask_piece<BF16>(w, 0, left);       // beyond: the next token's values
                     *reinterpret_cast<uint4 *>(to + (yr + 16 * u) * G_ROW + yp * 16) = make_uint4(w[0], w[1], w[2], w[3]);
                 }
             }
@@ -677,6 +704,29 @@ __global__ void __launch_bounds__(256, 2) ck_gram_kernel(const CkDenseArgs a, in
                 for (int j = 0; j < 2; ++j) g[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(va[i], vb[j], g[i][j], 0, 0, 0);
         }
     };
+    // fp32 dY: a wave takes 16 of a chunk's 64 features, the halves of the wave eight each: a matrix instruction multiplies one of either half
+    auto products_f32 = [&](int buf) {
+        const char *base_a = ck_lds + buf * G_STAGE + (lane & 31) * G_ROW + (lane >> 5) * 32 + wave * 64, *base_b = base_a + (diagonal ? 0 : G_SIDE);
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
+            float4 va[2], vb[2];
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                va[i] = *reinterpret_cast<const float4 *>(base_a + i * 32 * G_ROW + q * 16);
+                vb[i] = *reinterpret_cast<const float4 *>(base_b + i * 32 * G_ROW + q * 16);
+            }
+            auto step = [&](float a0, float a1, float b0, float b1) {
+                gy[0][0] = __builtin_amdgcn_mfma_f32_32x32x2f32(a0, b0, gy[0][0], 0, 0, 0);
+                gy[0][1] = __builtin_amdgcn_mfma_f32_32x32x2f32(a0, b1, gy[0][1], 0, 0, 0);
+                gy[1][0] = __builtin_amdgcn_mfma_f32_32x32x2f32(a1, b0, gy[1][0], 0, 0, 0);
+                gy[1][1] = __builtin_amdgcn_mfma_f32_32x32x2f32(a1, b1, gy[1][1], 0, 0, 0);
+            };
+            step(va[0].x, va[1].x, vb[0].x, vb[1].x);
+            step(va[0].y, va[1].y, vb[0].y, vb[1].y);
+            step(va[0].z, va[1].z, vb[0].z, vb[1].z);
+            step(va[0].w, va[1].w, vb[0].w, vb[1].w);
+        }
+    };
     const int all = nx + ny;
     fetch(0);
     if (all > 0) stage(0, 0);
@@ -689,7 +739,8 @@ __global__ void __launch_bounds__(256, 2) ck_gram_kernel(const CkDenseArgs a, in
         __syncthreads();
     }
     for (int i = nx; i < all; ++i) {
-        products(gy, i & 1);
+        if constexpr (BF16) products(gy, i & 1);
+        else products_f32(i & 1);
         if (i + 1 < all) stage(i + 1, (i + 1) & 1);
         fetch(i + 2);
         __syncthreads();
@@ -772,6 +823,7 @@ int ck_tiles(int v, int width) { return (v + width - 1) / width; }
 // Which of the two forms of norms: what they take, in microseconds, fitted to (n, T, F, O: Gram form / contraction) 32, 64, 768, 768: 12.4 / 11.4;
 // 8, 128, 2048, 2048: 21.7 / 19.5; 8, 512, 2048, 2048: 52 / 43; 16, 64, 4096, 4096: 20 / 68; 16, 128, 4096, 4096: 28 / 98; 16, 256, 4096, 4096: 50 / 155.
 // 512 workgroups of either kind fill the chip; a small launch afterwards is 4.
+// (fp32 dY, three products for one in the contraction: twice as long.)
 double gram_us(const Geo &g, double pairs, int splits, double chunks)
 {
     const double groups = g.n * pairs * splits;
@@ -779,7 +831,7 @@ double gram_us(const Geo &g, double pairs, int splits, double chunks)
 }
 double contract_us(const Geo &g, double tiles, int chunk)
 {
-    return 4.0 + std::max(1.0, g.n * tiles / 512.0) * (1.8 + 0.95 * ((g.h + chunk - 1) / chunk)) + (tiles > 1.0 ? 4.0 : 0.0);
+    return 4.0 + std::max(1.0, g.n * tiles / 512.0) * (1.8 + (g.bf16 ? 0.95 : 1.1) * ((g.h + chunk - 1) / chunk)) + (tiles > 1.0 ? 4.0 : 0.0);
 }
 
 CkPlan ck_plan(const Geo &g, int mode)
@@ -810,10 +862,11 @@ CkPlan ck_plan(const Geo &g, int mode)
     if (g.bf16 && (long long)g.n * tiles_o * ck_tiles(g.cin, 256) >= 384) p.nj = 4;
     const int tiles_k = ck_tiles(g.cin, 64 * p.nj);
     p.per_example = (size_t)tiles_o * (tiles_k + g.has_bias);
-    if (mode == MODE_NORM && g.bf16) {
-        const long long tiles = (g.h + GT - 1) / GT, pairs = tiles * (tiles + 1) / 2, chunks = (ck_pitch(g.cin) + GC - 1) / GC + (g.cout + GC - 1) / GC;
+    if (mode == MODE_NORM && (long long)g.h * std::max(ck_pitch(g.cin), g.cout * (g.bf16 ? 2 : 4)) < (1ll << 31)) {        // (offsets of an example's values: 32 bits)
+        const int yc = g.bf16 ? GC : GC / 2;
+        const long long tiles = (g.h + GT - 1) / GT, pairs = tiles * (tiles + 1) / 2, chunks = (ck_pitch(g.cin) + GC - 1) / GC + (g.cout + yc - 1) / yc;
         p.gram_splits = (int)std::max(1ll, std::min({512 / (g.n * pairs), chunks / 8, 16ll}));
-        p.gram = gram_us(g, (double)pairs, p.gram_splits, (double)chunks) < contract_us(g, (double)p.per_example, ck_chunk(1, p.nj));
+        p.gram = gram_us(g, (double)pairs, p.gram_splits, (double)chunks) < contract_us(g, (double)p.per_example, ck_chunk(g.bf16 ? 1 : 3, p.nj));
         if (p.gram) p.per_example = (size_t)pairs;
     }
     return p;
@@ -918,8 +971,9 @@ dp_status launch_checkpoint_dense(const Geo &g, int mode, const uint8_t *codes, 
         const int pairs = (int)p.per_example;
         const dim3 joins((unsigned)(g.n * p.per_example)), blocks(joins.x * (unsigned)p.gram_splits);
         float *tiles = reinterpret_cast<float *>(static_cast<char *>(ws) + align16(4 * (size_t)g.n * p.per_example));
-        st = words ? launch_lds<ck_gram_kernel<true>>(blocks, 256, 2 * G_STAGE, s, a, pairs, p.gram_splits, tiles)
-                   : launch_lds<ck_gram_kernel<false>>(blocks, 256, 2 * G_STAGE, s, a, pairs, p.gram_splits, tiles);
+        st = !g.bf16 ? launch_lds<ck_gram_kernel<false, true>>(blocks, 256, 2 * G_STAGE, s, a, pairs, p.gram_splits, tiles)
+             : words ? launch_lds<ck_gram_kernel<true, true>>(blocks, 256, 2 * G_STAGE, s, a, pairs, p.gram_splits, tiles)
+                     : launch_lds<ck_gram_kernel<true, false>>(blocks, 256, 2 * G_STAGE, s, a, pairs, p.gram_splits, tiles);
         if (st == DP_OK && p.gram_splits > 1) st = launch_lds<ck_gram_join_kernel>(joins, 512, 0, s, a, pairs, p.gram_splits, tiles);
     } else if (g.bf16) {
         st = p.nj == 4 ? run_contract<1, 4, false, true>(words, grid, a, s) : run_contract<1, 2, false, true>(words, grid, a, s);
