@@ -87,7 +87,7 @@ constexpr int CK_TABLE = 1024;                                     // examples o
 constexpr unsigned CK_NOWHERE = 0xFFFFFFE0u;                       // an offset beyond any buffer
 
 template <int PLANES, int NJ, bool WEIGHTED, bool BF16, bool WORDS>
-__global__ void __launch_bounds__(256, PLANES == 1 ? 2 : 1) ck_contract_kernel(const CkDenseArgs a)
+__global__ void __launch_bounds__(256, 2) ck_contract_kernel(const CkDenseArgs a)
 {
     extern __shared__ __attribute__((aligned(16))) char ck_lds[];
     __shared__ float red[4];
@@ -132,8 +132,6 @@ __global__ void __launch_bounds__(256, PLANES == 1 ? 2 : 1) ck_contract_kernel(c
         uint32_t sq;                                               //   this squared norm (as loaded), hence
         int power;                                                 //   factor f = m 2^power
         float m, f;
-        float x_sq[ROWS ? XP : 1], y_sq[ROWS ? YP : 1];            // rows of any examples: squared norms, lengths and tokens of this thread's rows
-        int x_left[ROWS ? XP : 1], y_left[ROWS ? YP : 1], x_len[ROWS ? XP : 1], y_len[ROWS ? YP : 1];
     };
     int f_ex = 0, f_c = 0, f_len = len;                            // weighted, by example: what the next chunk belongs to
     // Ragged examples: lengths, and chunks of the examples before each, fetched together (one after the other they are a trip to memory each).
@@ -186,7 +184,7 @@ __global__ void __launch_bounds__(256, PLANES == 1 ? 2 : 1) ck_contract_kernel(c
             f_c = c_begin - __builtin_amdgcn_readfirstlane(ex_before[f_ex]);
         }
     }
-    const __amdgpu_buffer_rsrc_t sq_buffer = __builtin_amdgcn_make_buffer_rsrc(const_cast<float *>(a.group_sqnorm), 0, a.n * 4, 0x00020000);
+    const __amdgpu_buffer_rsrc_t sq_buffer = __builtin_amdgcn_make_buffer_rsrc(const_cast<float *>(a.group_sqnorm), 0, (int)((unsigned)a.n * 4u), 0x00020000);
 
     auto load_rows = [&](Slot &s, unsigned row0_any, int rows_any) {
         // the same in every lane, which the compiler does not always see (and a buffer in vector registers is read lane by lane)
@@ -236,18 +234,8 @@ __global__ void __launch_bounds__(256, PLANES == 1 ? 2 : 1) ck_contract_kernel(c
         s.sq = 0;
         if (c >= c_end) return;
         if constexpr (ROWS) {
-            const unsigned total = (unsigned)a.n * (unsigned)a.tokens, row0 = (unsigned)c * CK;
-            s.rows = (int)min(total - row0, (unsigned)CK);
-            auto about = [&](unsigned row, float &sq, int &left, int &l) {
-                const unsigned at = min(row, total - 1), i = at / (unsigned)a.tokens;
-                sq = a.group_sqnorm[i];
-                l = a.lengths ? a.lengths[i] : a.tokens;
-                left = row < total ? (int)(at - i * (unsigned)a.tokens) : a.tokens;
-            };
-#pragma unroll
-            for (int u = 0; u < XP; ++u) about(row0 + xr + XS * u, s.x_sq[u], s.x_left[u], s.x_len[u]);
-#pragma unroll
-            for (int u = 0; u < YP; ++u) about(row0 + yr + 16 * u, s.y_sq[u], s.y_left[u], s.y_len[u]);
+            const unsigned row0 = (unsigned)c * CK;
+            s.rows = (int)min((unsigned)a.n * (unsigned)a.tokens - row0, (unsigned)CK);
             load_rows(s, row0, s.rows);
         } else if constexpr (WEIGHTED) {
             s.begins = f_c == 0 || c == c_begin;
@@ -281,12 +269,37 @@ __global__ void __launch_bounds__(256, PLANES == 1 ? 2 : 1) ck_contract_kernel(c
         }
         return y;
     };
-    auto row_factor = [&](const Slot &s, int u) { return s.y_left[u] < s.y_len[u] ? clip_factor(s.y_sq[u], a.clip_c) : 0.0f; };
+    // rows of any examples: the factors of a chunk's rows (0 beyond lengths and the last row) in LDS, two chunks ahead, from what was loaded
+    // four ahead; each row's example is a division, its factor a square root and another, once and not in every thread that holds a piece of it
+    struct About { float sq; int token, len; };
+    __shared__ float row_factors[2][ROWS ? 32 : 1];
+    const __amdgpu_buffer_rsrc_t len_buffer = __builtin_amdgcn_make_buffer_rsrc(const_cast<int32_t *>(a.lengths), 0, a.lengths ? (int)((unsigned)a.n * 4u) : 0, 0x00020000);
+    auto about = [&](About &b, int c) {
+        if constexpr (ROWS) {
+            const unsigned row = (unsigned)c * CK + (t & 31), i = row / (unsigned)a.tokens;        // beyond the last row: no squared norm there, token 0
+            b.sq = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(sq_buffer, 4 * i, 0, 0));
+            b.len = (int)__builtin_amdgcn_raw_buffer_load_b32(len_buffer, 4 * i, 0, 0);
+            b.token = i < (unsigned)a.n ? (int)(row - i * (unsigned)a.tokens) : a.tokens;
+        }
+    };
+    auto place = [&](const About &b, int buf) {
+        if constexpr (ROWS)
+            if (t < 32) row_factors[buf][t] = b.token < (a.lengths ? b.len : a.tokens) ? clip_factor(b.sq, a.clip_c) : 0.0f;
+    };
+    About r0, r1;
+    if constexpr (ROWS) {
+        about(r0, c_begin);
+        about(r1, c_begin + 1);
+        place(r0, 0);
+        place(r1, 1);
+        about(r0, c_begin + 2);
+        about(r1, c_begin + 3);
+    }
     auto stage_x = [&](const Slot &s, int u, int buf) {            // piece u of X into LDS
         const int r = xr + XS * u;
         uint4 x = s.x[u];
         if constexpr (ROWS)
-            if (s.x_left[u] >= s.x_len[u] || clip_factor(s.x_sq[u], a.clip_c) == 0.0f) x = make_uint4(0, 0, 0, 0);
+            if (row_factors[buf][r] == 0.0f) x = make_uint4(0, 0, 0, 0);
         const float scale = pow2_of(WEIGHTED && !ROWS ? max((int)s.scale[u] + s.power, 1) : (int)s.scale[u]);
         const uint2 w0 = ck_bf16(x.x, scale), w1 = ck_bf16(x.y, scale), w2 = ck_bf16(x.z, scale), w3 = ck_bf16(x.w, scale);
         char *to = ck_lds + buf * STAGE + PLANES * PLANE + r * X_ROW;
@@ -302,7 +315,7 @@ __global__ void __launch_bounds__(256, PLANES == 1 ? 2 : 1) ck_contract_kernel(c
             float v[8];
             piece_y(s, u).get(v);
             if constexpr (ROWS) {
-                const float f = row_factor(s, u);
+                const float f = row_factors[buf][r];
 #pragma unroll
                 for (int j = 0; j < 8; ++j) v[j] = f == 0.0f ? 0.0f : v[j] * f;
             }
@@ -323,14 +336,14 @@ __global__ void __launch_bounds__(256, PLANES == 1 ? 2 : 1) ck_contract_kernel(c
         float sum[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) sum[j] = 0.0f;
-        auto add = [&](Slot &s) {
+        auto add = [&](Slot &s, int buf) {
             ready(s);
             if (s.rows <= 0) return;
 #pragma unroll
             for (int u = 0; u < YP; ++u) {
                 float v[8], f = 1.0f;
                 piece_y(s, u).get(v);
-                if constexpr (ROWS) f = row_factor(s, u);
+                if constexpr (ROWS) f = row_factors[buf][yr + 16 * u];
                 else if constexpr (WEIGHTED) f = s.f;
 #pragma unroll
                 for (int j = 0; j < 8; ++j) sum[j] = f == 0.0f ? sum[j] : fmaf(f, v[j], sum[j]);
@@ -339,10 +352,18 @@ __global__ void __launch_bounds__(256, PLANES == 1 ? 2 : 1) ck_contract_kernel(c
         Slot b0, b1;
         fetch(b0, c_begin);
         for (int c = c_begin; c < c_end; c += 2) {
+            if constexpr (ROWS) __syncthreads();
             fetch(b1, c + 1);
-            add(b0);
+            add(b0, 0);
             fetch(b0, c + 2);
-            add(b1);
+            add(b1, 1);
+            if constexpr (ROWS) {
+                __syncthreads();
+                place(r0, 0);
+                place(r1, 1);
+                about(r0, c + 4);
+                about(r1, c + 5);
+            }
         }
         float *sums = reinterpret_cast<float *>(ck_lds);
 #pragma unroll
@@ -428,6 +449,7 @@ __global__ void __launch_bounds__(256, PLANES == 1 ? 2 : 1) ck_contract_kernel(c
     Slot s0, s1;
     fetch(s0, c_begin);
     fetch(s1, c_begin + 1);
+    if constexpr (ROWS) __syncthreads();
     ready(s0);
     Now now = {s0.rows, s0.begins, s0.m};
     if (now.rows > 0) stage(s0, 0);
@@ -435,7 +457,7 @@ __global__ void __launch_bounds__(256, PLANES == 1 ? 2 : 1) ck_contract_kernel(c
     __syncthreads();
     // A chunk's products in two halves (the second one left out where no row reaches it), the next chunk staged in between: one set of
     // accumulators on every path.  Where the next chunk adds nothing, what is staged is not used.
-    auto turn = [&](Slot &next, int buf, int c) {
+    auto turn = [&](Slot &next, About &rows, int buf, int c) {
         rescale(now);
         ready(next);
         auto stage_xs = [&]() {
@@ -482,12 +504,14 @@ __global__ void __launch_bounds__(256, PLANES == 1 ? 2 : 1) ck_contract_kernel(c
             }
         }
         now = {next.rows, next.begins, next.m};
+        place(rows, buf);                                          // of chunk c + 2 (those of c were used before the last barrier)
+        about(rows, c + 4);
         fetch(next, c + 3);
         __syncthreads();
     };
     for (int c = c_begin; c < c_end; c += 2) {
-        turn(s1, 0, c);
-        if (c + 1 < c_end) turn(s0, 1, c + 1);
+        turn(s1, r0, 0, c);
+        if (c + 1 < c_end) turn(s0, r1, 1, c + 1);
     }
 
     // Rows beyond the last hold products of what followed in memory: gone.  (Columns beyond the last are sums of zeros.)
@@ -553,7 +577,7 @@ __global__ void __launch_bounds__(256) ck_ranges_kernel(const float *part, size_
     if (e >= stride_w + count_b) return;
     const float *p = part + e;
     float4 s = *reinterpret_cast<const float4 *>(p);
-#pragma unroll 4
+#pragma unroll 8
     for (int r = 1; r < ranges; ++r) {
         const float4 v = *reinterpret_cast<const float4 *>(p + r * stride);
         s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
@@ -849,11 +873,11 @@ CkPlan ck_plan(const Geo &g, int mode)
         // Ranges of the call's chunks: fewer chunks in a row against more sums to write and join.  What R of them take, in microseconds, fitted
         // to 16 x 128 tokens 768 -> 768 (R 1: 36, 3: 22.5, 6: 19.4, 16: 27), 16 x 512 2048 -> 2048 (1: 124, 2: 101, 4: 111, 8: 145) and
         // 64 x 64 512 -> 512 (1: 68, 4: 28, 16: 19): 9 at least, a chunk 0.85 where a workgroup has a compute unit to itself and 1.2 where two
-        // share it, a value of a range's sums written and read at 4.5 TB/s.
-        const double tiles = (double)tiles_o * ck_tiles(g.cin, 64 * p.nj), sums = 8.0 * g.pw / 4.5e6;
+        // share it (three products for one: 1.15 and 1.6), a value of a range's sums written and read at 4.5 TB/s.
+        const double tiles = (double)tiles_o * ck_tiles(g.cin, 64 * p.nj), sums = 8.0 * g.pw / 4.5e6, one = p.rows ? 1.15 : 0.85, two = p.rows ? 1.6 : 1.2;
         double best = 0.0;
         for (int r = 1; r <= 64 && (r == 1 || r <= chunks / 2); ++r) {
-            const double groups = tiles * r, chunk_us = groups <= 256.0 ? 0.85 : std::min(1.2, 0.85 + 0.35 * (groups - 256.0) / 256.0) * std::max(1.0, groups / 512.0);
+            const double groups = tiles * r, chunk_us = groups <= 256.0 ? one : std::min(two, one + (two - one) * (groups - 256.0) / 256.0) * std::max(1.0, groups / 512.0);
             const double us = 9.0 + chunk_us * std::ceil((double)chunks / r) + (r > 1 ? sums * r : 0.0);
             if (r == 1 || us < best) { best = us; p.ranges = r; }
         }
