@@ -37,6 +37,7 @@ struct BiasArgs {
     int near, border_count, far, low;    // low: distances from -low down are one bucket (0 where there is one side)
     int plane, last;                     // words of a plane of distances; slots at `last - 1` and beyond in each are beyond `far`
     int rows, blocks;                    // rows of a workgroup, workgroups of a head
+    int share;                           // lanes that share a bucket's sum
     int borders[BIAS_BORDERS];
 };
 
@@ -181,8 +182,8 @@ struct RowOf {
     }
 };
 
-// The sums of a workgroup's four waves, by distance in LDS and beyond the borders in registers, by bucket into its place of the workspace: a
-// wave takes every fourth bucket, its lanes the distances of the bucket's run.
+// The sums of a workgroup's four waves, by distance in LDS and beyond the borders in registers, by bucket into its place of the workspace:
+// `share` lanes to a bucket, over the distances of its run.
 __device__ __forceinline__ void bias_bucket_sums(const BiasArgs &a, const Rows &r, const float *lds, float sum_far, float sum_low, float (&ends)[4][2])
 {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -192,7 +193,7 @@ __device__ __forceinline__ void bias_bucket_sums(const BiasArgs &a, const Rows &
     float *part = a.partials + (size_t)blockIdx.x * a.buckets;
     const int side_buckets = a.bidirectional ? a.buckets / 2 : a.buckets;
     auto start = [&](int m) { return m <= a.near ? m : a.borders[m - a.near - 1]; };       // smallest magnitude of a side's bucket m
-    for (int b = wave; b < a.buckets; b += 4) {
+    for (int b = (int)threadIdx.x / a.share; b < a.buckets; b += 256 / a.share) {
         const bool after = b >= side_buckets;                      // keys after the query
         const int m = after ? b - side_buckets : b;
         const bool outer = m == side_buckets - 1, inner = !a.bidirectional && b == 0;
@@ -202,19 +203,19 @@ __device__ __forceinline__ void bias_bucket_sums(const BiasArgs &a, const Rows &
         const int first = after ? max(lo, -(r.first + r.q1 - 1)) : max(lo, r.first + r.q0 - a.keys - 6);
         const int last = after ? min(hi, a.keys + 6 - r.first - r.q0) : min(hi, r.first + r.q1 - 1);
         float s = 0.0f;
-        if (first <= last) {
-            for (int d = first + lane; d <= last; d += 64) {
-                const int word = bias_word(a, RunWords::slot(a, after ? -d : d));
+        const int mine = (int)threadIdx.x & (a.share - 1);
+#pragma unroll 2
+        for (int d = first + mine; d <= last; d += a.share) {
+            const int word = bias_word(a, RunWords::slot(a, after ? -d : d));
 #pragma unroll
-                for (int w = 0; w < 4; ++w) s += lds[w * 8 * a.plane + word];
-            }
-            s = wave_all_sum(s);
+            for (int w = 0; w < 4; ++w) s += lds[w * 8 * a.plane + word];
         }
+        for (int off = a.share >> 1; off; off >>= 1) s += __shfl_xor(s, off, 64);
         if (outer || inner) {
             const int which = after || inner ? 1 : 0;
             s += ends[0][which] + ends[1][which] + ends[2][which] + ends[3][which];
         }
-        if (lane == 0) part[b] = s;
+        if (mine == 0) part[b] = s;
     }
 }
 
@@ -666,7 +667,7 @@ int narrow_lanes(const BiasGeo &g)
     return g.keys <= 64 ? 8 : g.keys <= 128 ? 16 : 32;
 }
 
-BiasArgs bias_args(const BiasGeo &g)
+BiasArgs bias_args(const BiasGeo &g, bool backward)
 {
     BiasArgs a = {};
     a.n = g.n; a.heads = g.heads; a.queries = g.queries; a.keys = g.keys; a.buckets = g.buckets; a.bidirectional = g.bidirectional;
@@ -678,13 +679,26 @@ BiasArgs bias_args(const BiasGeo &g)
     if (const int lanes = narrow_lanes(g)) {
         a.rows = 8 * 256 / lanes;
     } else {
-        // several rows, so that what a workgroup does once (the biases, or the sums by bucket) is shared by them, as long as there are 2048 workgroups
+        // several rows, so that what a workgroup does once (the biases, or the sums by bucket) is shared by them, as long as there are 2048
+        // workgroups; backward of rows of one run a lane, which leave more to what is done once, 1024 (512 keys, 98304 rows: 67.4 us and 61.6; 300
+        // keys, 9600 rows: 11.2 and 9.6; but 512 keys, 4096 rows: 6.8 and 8.2; fp32 rows of 1024 keys, 32768 of them: 67.2 and 71.7).
+        const long long workgroups = backward && g.keys <= 512 ? 1024 : 2048;
         const int at_once = g.keys <= 2048 ? 4 : 1;
         const long long rows = (long long)g.n * g.heads * g.queries;
-        const long long each = std::max(1ll, std::min(rows / (2048ll * at_once), 64ll / at_once));
+        const long long each = std::max(1ll, std::min(rows / (workgroups * at_once), 64ll / at_once));
         a.rows = (int)std::min((long long)at_once * each, (long long)(g.queries + at_once - 1) / at_once * at_once);
     }
     a.blocks = (g.queries + a.rows - 1) / a.rows;
+    // Lanes that share a bucket's sum: few where runs are short, so that all buckets are summed at once; a step over a run's distances against
+    // steps of the exchange between the lanes, both about a trip to LDS.
+    int longest = 14;                                              // the outer bucket's: beyond the border, as far as runs reach
+    for (int i = 0; i < a.border_count; ++i) longest = std::max(longest, a.borders[i] - (i ? a.borders[i - 1] : a.near));
+    longest = std::min(longest, a.keys + a.rows + 12);
+    int best = 0;
+    for (int share = 1, exchange = 0; share <= 64; share *= 2, ++exchange) {
+        const int steps = ((a.buckets * share + 255) / 256) * ((longest + share - 1) / share + exchange + 2);
+        if (!best || steps < best) { best = steps; a.share = share; }
+    }
     return a;
 }
 
@@ -733,14 +747,14 @@ dp_status run_backward(const BiasGeo &g, const BiasArgs &a, hipStream_t s)
 
 size_t bias_ws_bytes(const BiasGeo &g)
 {
-    const BiasArgs a = bias_args(g);
+    const BiasArgs a = bias_args(g, true);
     return ((size_t)g.n * g.heads * a.blocks * g.buckets * 4 + 15) & ~(size_t)15;
 }
 
 dp_status launch_bias_softmax(const BiasGeo &g, const void *scores, const float *table, const int32_t *query_lengths,
                               const int32_t *key_lengths, void *probs, hipStream_t s)
 {
-    BiasArgs a = bias_args(g);
+    BiasArgs a = bias_args(g, false);
     a.in = scores; a.out = probs; a.table = table; a.query_lengths = query_lengths; a.key_lengths = key_lengths;
     if (!g.bf16) return run_forward<false, true>(g, a, s);
     return bias_words(g, scores) && bias_words(g, probs) ? run_forward<true, true>(g, a, s) : run_forward<true, false>(g, a, s);
@@ -750,7 +764,7 @@ dp_status launch_bias_softmax_backward(const BiasGeo &g, const void *probs, cons
                                        const int32_t *key_lengths, void *dscores, float *g_table, size_t g_stride, float *sqnorm, void *ws,
                                        hipStream_t s)
 {
-    BiasArgs a = bias_args(g);
+    BiasArgs a = bias_args(g, true);
     a.in = probs; a.in2 = dprobs; a.out = dscores; a.query_lengths = query_lengths; a.key_lengths = key_lengths;
     a.partials = static_cast<float *>(ws);
     const bool words = bias_words(g, probs) && bias_words(g, dprobs) && bias_words(g, dscores);
