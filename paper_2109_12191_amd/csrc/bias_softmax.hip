@@ -15,8 +15,8 @@
 // lane and eight that all lanes share.  The slots before -low and after far, which a run that straddles the border reaches, hold what
 // belongs to the border's bucket.
 //
-// A row is held in registers between its two passes (its sums and its results), by one wave up to 2048 keys and by four up to
-// 16384; longer ones are read twice.
+// A row is held in registers between its two passes (its sums and its results), by one wave up to 2048 keys, by four up to
+// 16384 and by sixteen up to 32768 (backward: by four up to 8192); longer ones are read twice.
 #include "values.h"
 
 #include <algorithm>
@@ -222,18 +222,19 @@ __device__ __forceinline__ void bias_bucket_sums(const BiasArgs &a, const Rows &
 // NV > 0: a thread holds NV runs of eight keys, run j at 8 (thread + TPR j), and the next row's are on their way while it works on one.
 // NV == 0: rows of any length, read twice.
 template <bool BF16, bool WORDS, int TPR, int NV>
-__global__ void __launch_bounds__(256) bias_softmax_kernel(const BiasArgs a)
+__global__ void __launch_bounds__(TPR > 256 ? TPR : 256) bias_softmax_kernel(const BiasArgs a)
 {
     extern __shared__ float bias_lds[];
-    __shared__ float red[4];
+    constexpr int THREADS = TPR > 256 ? TPR : 256;
+    __shared__ float red[THREADS / 64];
     typedef RowOf<BF16, WORDS> Row;
     const Rows r = bias_rows(a);
-    for (int i = threadIdx.x; i < 8 * a.plane; i += 256)
+    for (int i = threadIdx.x; i < 8 * a.plane; i += THREADS)
         bias_lds[bias_word(a, i)] = a.table[(size_t)bias_bucket_of(a, min(max(i - 16 - a.low, -a.low), a.far)) * a.heads + r.head];
     __syncthreads();
     const int t = threadIdx.x % TPR;
     const int wave_first = __builtin_amdgcn_readfirstlane(t & ~63), row_first = __builtin_amdgcn_readfirstlane(threadIdx.x / TPR);
-    constexpr int STEP = 256 / TPR;                                // rows that are worked on together
+    constexpr int STEP = THREADS / TPR;                             // rows that are worked on together
 
     // the scores of a run of eight keys from key k on, as logits; `whole`: the same for the wave, every run of it counts to its end
     RunWords at;
@@ -723,7 +724,9 @@ dp_status run_forward(const BiasGeo &g, const BiasArgs &a, hipStream_t s)
     if (g.keys <= 4096) return launch_lds<bias_softmax_kernel<BF16, WORDS, 256, 2>>(grid, 256, lds, s, a);
     if (g.keys <= 8192) return launch_lds<bias_softmax_kernel<BF16, WORDS, 256, 4>>(grid, 256, lds, s, a);
     if (g.keys <= 16384) return launch_lds<bias_softmax_kernel<BF16, WORDS, 256, 8>>(grid, 256, lds, s, a);
-    return launch_lds<bias_softmax_kernel<BF16, WORDS, 256, 0>>(grid, 256, lds, s, a);
+    // sixteen waves a row (16 rows, four waves and two passes against these: 60000 keys 27.2 us and 15.0, 131072 54.0 and 27.4)
+    if (g.keys <= 32768) return launch_lds<bias_softmax_kernel<BF16, WORDS, 1024, 4>>(grid, 1024, lds, s, a);
+    return launch_lds<bias_softmax_kernel<BF16, WORDS, 1024, 0>>(grid, 1024, lds, s, a);
 }
 
 template <bool BF16, bool WORDS>

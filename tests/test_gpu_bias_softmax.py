@@ -82,6 +82,9 @@ CASES = [
     (1, 1, 40, 2049, False, dict(buckets=8, max_distance=4096)),
     (1, 1, 9, 9000, True, dict(offset=6000)),
     (1, 1, 3, 17001, False, dict(offset=9000)),
+    (2, 1, 2, 32768, True, dict(causal=1, offset=-1)),
+    (1, 2, 2, 32769, False, dict(offset=20000)),
+    (1, 1, 2, 70002, False, dict(causal=1, offset=-1, bidirectional=0)),
     (2, 1, 20, 30, False, dict(buckets=2, max_distance=2, bidirectional=0)),
     (2, 1, 20, 30, False, dict(buckets=4, max_distance=9)),
     (2, 2, 150, 130, True, dict(stride=133)),
