@@ -16,7 +16,9 @@
 // belongs to the border's bucket.
 //
 // A row is held in registers between its two passes (its sums and its results), by one wave up to 2048 keys, by four up to
-// 16384 and by sixteen up to 32768 (backward: by four up to 8192); longer ones are read twice.
+// 16384 and by sixteen up to 32768 (backward: by four up to 8192); longer ones are read twice.  Bound by memory: 16 x 12 x 512 x 512 bf16
+// forward 44 us, 4.6 TB/s, backward 61, 4.9 (and 4 to join the tables); 4 x 8 x 1500 x 1500 fp32 backward, causal and ragged, 104.  Four
+// waves to a row of 1100 keys: 97 us, one wave 68.
 #include "values.h"
 
 #include <algorithm>

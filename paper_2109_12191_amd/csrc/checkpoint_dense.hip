@@ -77,6 +77,10 @@ __device__ __forceinline__ void split8(const float (&v)[8], uint4 (&planes)[3])
 // WEIGHTED, PLANES 3: rows (example, token) of the whole call one after the other, dY times its factor in fp32, then split: for fp32 dY, and
 // for examples of a few tokens, of which 32 rows hold several.
 // Bias: a column of workgroups of its own adds up dY.
+// Measured: norms of 8 x 1024 tokens 1024 -> 2048 34.8 us, 988 TFLOP/s (a library product of 8192^3: 1282); clipped sum of 16 x 512 tokens
+// 2048 -> 2048 98 us, 700 TFLOP/s, and 11 us to join two ranges.  Bound by the LDS (a product's operands are 96 KB written and read a chunk and
+// workgroup, 0.3 us of its 0.75) and by the waits that two workgroups a compute unit leave uncovered; 16 x 128 tokens 768 -> 768, 5 chunks a
+// workgroup, by trips to memory one after the other.  Three stages of loads instead of two: no gain (registers); chunks of 32 with three workgroups: slower.
 // WORDS: rows of dY begin at whole dwords: pieces by buffer loads, which give zeros beyond the chunk's last row (what a row's last piece takes
 // from the next row is multiplied into features beyond the last, which nobody reads).  Else (bf16, an odd number of features) every other
 // row begins in the middle of a dword: five dwords around a piece, shifted into place on their way into LDS.
@@ -607,6 +611,7 @@ __global__ void __launch_bounds__(256) ck_ranges_kernel(const float *part, size_
 // compute unit takes in, hence the tiles; where there are few pairs, several workgroups share a pair's features (splits) and
 // ck_gram_join_kernel adds up their sums before it multiplies.
 // fp32 dY: chunks of 64 features as they are, fp32 matrix instructions.  WORDS: as above.
+// 32 x 64 tokens 768 -> 768: 12 to 13 us, twelve chunks one after the other; 55 x 2 tokens 1792 -> 576 fp32: 21.6 us a call (by contraction 32).
 constexpr int GT = 64, GC = 128, G_ROW = 2 * GC + 16, G_SIDE = GT * G_ROW, G_STAGE = 2 * G_SIDE;      // tokens, features; bytes (16 of a row keep rows in different banks)
 constexpr int G_VALUES = GT * GT;
 
@@ -847,7 +852,7 @@ int ck_tiles(int v, int width) { return (v + width - 1) / width; }
 // Which of the two forms of norms: what they take, in microseconds, fitted to (n, T, F, O: Gram form / contraction) 32, 64, 768, 768: 12.4 / 11.4;
 // 8, 128, 2048, 2048: 21.7 / 19.5; 8, 512, 2048, 2048: 52 / 43; 16, 64, 4096, 4096: 20 / 68; 16, 128, 4096, 4096: 28 / 98; 16, 256, 4096, 4096: 50 / 155.
 // 512 workgroups of either kind fill the chip; a small launch afterwards is 4.
-// (fp32 dY, three products for one in the contraction: twice as long.)
+// (fp32 dY, three products for one: chunks of 32 in 1.1.)
 double gram_us(const Geo &g, double pairs, int splits, double chunks)
 {
     const double groups = g.n * pairs * splits;
