@@ -65,6 +65,15 @@ class PrivateAttention:
         self.qkv_weight = torch.cat([w.to(torch.bfloat16) for w in self.weights[:3]])        # [3 width, width]
         self.o_weight = self.weights[3].to(torch.bfloat16)
 
+    def _want(self, name, t, shape, dtype=torch.bfloat16):
+        """The calls below take addresses: what is behind them has to be what the descriptors say."""
+        if tuple(t.shape) != shape or t.dtype is not dtype or t.device.type != self.theta.device.type or not t.is_contiguous():
+            raise ValueError(f"{name} must be contiguous {dtype} {list(shape)} on {self.theta.device}, not {t.dtype} {list(t.shape)} on {t.device}")
+
+    def _want_lengths(self, lengths):
+        if lengths is not None:
+            self._want("lengths", lengths, (self.n,), torch.int32)
+
     def _heads(self, x):
         return x.view(self.n, -1, self.heads, self.head).transpose(1, 2).contiguous()         # [n, heads, tokens, head]
 
@@ -73,6 +82,8 @@ class PrivateAttention:
 
     def forward(self, x, lengths=None):
         """x [n, tokens, width] bf16 -> what the block makes of it, alike."""
+        self._want("x", x, (self.n, self.tokens, self.width))
+        self._want_lengths(lengths)
         self.lengths = lengths
         B.dp_checkpoint_write(x, *self.inputs)
         self.q, self.k, self.v = (self._heads(part) for part in (x @ self.qkv_weight.t()).chunk(3, dim=-1))
@@ -86,6 +97,10 @@ class PrivateAttention:
     def attend_last(self, q, k, v, lengths=None):
         """One token an example against a cache: q [n, width], k and v [n, heads, tokens, head], `lengths` keys of which are there, the query's
         own the last -> [n, width]."""
+        self._want("q", q, (self.n, self.width))
+        for name, t in (("k", k), ("v", v)):
+            self._want(name, t, (self.n, self.heads, self.tokens, self.head))
+        self._want_lengths(lengths)
         scores = self._heads(q.view(self.n, 1, self.width)) @ k.transpose(2, 3).contiguous()
         probs = torch.empty_like(scores)
         B.dp_bias_softmax(self.last, scores, self.weights[4], probs, None, lengths)
@@ -95,6 +110,7 @@ class PrivateAttention:
         """Gradient of forward's result, per example (of a sum over examples, not of a mean) -> gradient of its input; the clipped gradients of
         the weights go into the accumulator."""
         dy = dy.contiguous()
+        self._want("dy", dy, (self.n, self.tokens, self.width))
         dmixed = self._heads(dy @ self.o_weight)
         self.dprobs = dmixed @ self.v.transpose(2, 3).contiguous()
         dv = self.probs.transpose(2, 3).contiguous() @ dmixed

@@ -611,11 +611,14 @@ __global__ void __launch_bounds__(256) ck_ranges_kernel(const float *part, size_
 // compute unit takes in, hence the tiles; where there are few pairs, several workgroups share a pair's features (splits) and
 // ck_gram_join_kernel adds up their sums before it multiplies.
 // fp32 dY: chunks of 64 features as they are, fp32 matrix instructions.  WORDS: as above.
-// 32 x 64 tokens 768 -> 768: 12 to 13 us, twelve chunks one after the other; 55 x 2 tokens 1792 -> 576 fp32: 21.6 us a call (by contraction 32).
+// ONE: every example has one pair (64 tokens at most): half the operands, the products above the diagonal once, those of tokens from the 32nd on
+// only where there are some, and three chunks on their way instead of one (32 x 64 tokens 768 -> 768:
+// 12.7 us and 11.3, twelve chunks of which each waits for the one before it; 400 of them 17.6 and 16.0).  55 x 2 tokens 1792 -> 576 fp32: 20 us a
+// call (by contraction 32).
 constexpr int GT = 64, GC = 128, G_ROW = 2 * GC + 16, G_SIDE = GT * G_ROW, G_STAGE = 2 * G_SIDE;      // tokens, features; bytes (16 of a row keep rows in different banks)
 constexpr int G_VALUES = GT * GT;
 
-template <bool BF16, bool WORDS>
+template <bool BF16, bool WORDS, bool ONE>
 __global__ void __launch_bounds__(256, 2) ck_gram_kernel(const CkDenseArgs a, int pairs, int splits, float *tiles)
 {
     extern __shared__ __attribute__((aligned(16))) char ck_lds[];
@@ -623,9 +626,10 @@ __global__ void __launch_bounds__(256, 2) ck_gram_kernel(const CkDenseArgs a, in
     const unsigned whole = blockIdx.x / (unsigned)splits;          // example and pair
     const int split = (int)(blockIdx.x - whole * (unsigned)splits), ex = (int)(whole / (unsigned)pairs);
     int pair = (int)(whole - (unsigned)ex * (unsigned)pairs), tile_a = 0;
-    while (pair > tile_a) { ++tile_a; pair -= tile_a; }            // pairs (0,0) (1,0) (1,1) (2,0) ...
+    if constexpr (!ONE)
+        while (pair > tile_a) { ++tile_a; pair -= tile_a; }        // pairs (0,0) (1,0) (1,1) (2,0) ...
     const int tile_b = pair;
-    const bool diagonal = tile_a == tile_b;
+    const bool diagonal = ONE || tile_a == tile_b;
     const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
     const int len = __builtin_amdgcn_readfirstlane(ck_length(a, ex));
     if (tile_a * GT >= len) {                                      // (tile_b is not the larger one)
@@ -649,11 +653,14 @@ __global__ void __launch_bounds__(256, 2) ck_gram_kernel(const CkDenseArgs a, in
     const int xr = t >> 3, xp = t & 7, yr = t >> 4, yp = t & 15;   // pieces: 16 codes of rows xr + 32 u, YV values of dY of rows yr + 16 u
 
     typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-    uint4 held[2][4];                                              // a chunk on its way
-    uint32_t scale[2][2], more[2][WORDS ? 1 : 4];
-    auto fetch = [&](int i) {
+    constexpr int SIDES = ONE ? 1 : 2, AHEAD = ONE ? 3 : 1;
+    const int nx_up = (nx + AHEAD - 1) / AHEAD * AHEAD, all = nx_up + ny;          // chunk i: nx of X, none up to nx_up, then those of dY
+    struct Held { uint4 v[SIDES][4]; };                            // a chunk on its way, X's scales, the dwords after dY's pieces
+    struct Scale { uint32_t v[SIDES][2]; };                        // (one by one, not together, so that all of them are registers)
+    struct More { uint32_t v[SIDES][WORDS ? 1 : 4]; };
+    auto fetch = [&](Held &held, Scale &scale, More &more, int i) {
 #pragma unroll
-        for (int side = 0; side < 2; ++side) {
+        for (int side = 0; side < SIDES; ++side) {
             if (side == 1 && diagonal) break;
             const int first = (side ? tile_b : tile_a) * GT;
             if (i < nx) {
@@ -662,49 +669,49 @@ __global__ void __launch_bounds__(256, 2) ck_gram_kernel(const CkDenseArgs a, in
                 for (int u = 0; u < 2; ++u) {
                     const int row = first + xr + 32 * u;
                     const u32x4 v = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(xb, row * a.pitch + xp * 16, c * GC, 0));
-                    held[side][u] = make_uint4(v.x, v.y, v.z, v.w);
-                    scale[side][u] = __builtin_amdgcn_raw_buffer_load_b8(sb, row * s_pitch + (xp >> 1), c * (GC / CK_BLOCK), 0);
+                    held.v[side][u] = make_uint4(v.x, v.y, v.z, v.w);
+                    scale.v[side][u] = __builtin_amdgcn_raw_buffer_load_b8(sb, row * s_pitch + (xp >> 1), c * (GC / CK_BLOCK), 0);
                 }
-            } else if (i < nx + ny) {
-                const int c = y0 + i - nx;
+            } else if (i >= nx_up && i < all) {
+                const int c = y0 + i - nx_up;
 #pragma unroll
                 for (int u = 0; u < 4; ++u) {
                     const int row = first + yr + 16 * u;
                     unsigned at = (unsigned)(row * a.cout + yp * YV + odd) * (unsigned)sizeof(E) & ~3u;
                     if constexpr (!WORDS) at = row < len ? at : (unsigned)y_bytes;        // (the last value's dword may hold another)
                     const u32x4 v = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(yb, at, c * YC * (int)sizeof(E), 0));
-                    held[side][u] = make_uint4(v.x, v.y, v.z, v.w);
-                    if constexpr (!WORDS) more[side][u] = __builtin_amdgcn_raw_buffer_load_b32(yb, at + 16u, c * YC * (int)sizeof(E), 0);
+                    held.v[side][u] = make_uint4(v.x, v.y, v.z, v.w);
+                    if constexpr (!WORDS) more.v[side][u] = __builtin_amdgcn_raw_buffer_load_b32(yb, at + 16u, c * YC * (int)sizeof(E), 0);
                 }
             }
         }
     };
-    auto stage = [&](int i, int buf) {
+    auto stage = [&](const Held &held, const Scale &scale, const More &more, int i) {
 #pragma unroll
-        for (int side = 0; side < 2; ++side) {
+        for (int side = 0; side < SIDES; ++side) {
             if (side == 1 && diagonal) break;
-            char *to = ck_lds + buf * G_STAGE + side * G_SIDE;
+            char *to = ck_lds + (i & 1) * G_STAGE + side * G_SIDE;
             if (i < nx) {
                 const bool there = (x0 + i) * GC + xp * 16 < a.pitch;      // (beyond: the next token's codes)
 #pragma unroll
                 for (int u = 0; u < 2; ++u) {
-                    const float f = pow2_of((int)scale[side][u]);
-                    const uint4 c = there ? held[side][u] : make_uint4(0, 0, 0, 0);
+                    const float f = pow2_of((int)scale.v[side][u]);
+                    const uint4 c = there ? held.v[side][u] : make_uint4(0, 0, 0, 0);
                     const uint2 w0 = ck_bf16(c.x, f), w1 = ck_bf16(c.y, f), w2 = ck_bf16(c.z, f), w3 = ck_bf16(c.w, f);
                     uint4 *at = reinterpret_cast<uint4 *>(to + (xr + 32 * u) * G_ROW + xp * 32);
                     at[0] = make_uint4(w0.x, w0.y, w1.x, w1.y);
                     at[1] = make_uint4(w2.x, w2.y, w3.x, w3.y);
                 }
-            } else {
-                const int left = a.cout - (y0 + i - nx) * YC - yp * YV;
+            } else if (i >= nx_up && i < all) {
+                const int left = a.cout - (y0 + i - nx_up) * YC - yp * YV;
 #pragma unroll
                 for (int u = 0; u < 4; ++u) {
-                    uint32_t w[4] = {held[side][u].x, held[side][u].y, held[side][u].z, held[side][u].w};
+                    uint32_t w[4] = {held.v[side][u].x, held.v[side][u].y, held.v[side][u].z, held.v[side][u].w};
                     if constexpr (!WORDS) {                        // (an odd number of features: rows take turns)
                         const uint32_t bits = (uint32_t)((yr ^ odd) & 1) * 16u;
-                        w[0] = funnel(w[1], w[0], bits); w[1] = funnel(w[2], w[1], bits); w[2] = funnel(w[3], w[2], bits); w[3] = funnel(more[side][u], w[3], bits);
+                        w[0] = funnel(w[1], w[0], bits); w[1] = funnel(w[2], w[1], bits); w[2] = funnel(w[3], w[2], bits); w[3] = funnel(more.v[side][u], w[3], bits);
                     }
-                    if ((y0 + i - nx + 1) * YC > a.cout) mask_piece<BF16>(w, 0, left);       // beyond: the next token's values
+                    if ((y0 + i - nx_up + 1) * YC > a.cout) mask_piece<BF16>(w, 0, left);       // beyond: the next token's values
                     *reinterpret_cast<uint4 *>(to + (yr + 16 * u) * G_ROW + yp * 16) = make_uint4(w[0], w[1], w[2], w[3]);
                 }
             }
@@ -721,16 +728,15 @@ __global__ void __launch_bounds__(256, 2) ck_gram_kernel(const CkDenseArgs a, in
         const char *base_a = ck_lds + buf * G_STAGE + (lane & 31) * G_ROW + (lane >> 5) * 16 + wave * 64, *base_b = base_a + (diagonal ? 0 : G_SIDE);
 #pragma unroll
         for (int ks = 0; ks < 2; ++ks) {
-            bf16x8 va[2], vb[2];
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                va[i] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4 *>(base_a + i * 32 * G_ROW + ks * 32));
-                vb[i] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4 *>(base_b + i * 32 * G_ROW + ks * 32));
+            auto read = [&](const char *base, int i) { return __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4 *>(base + i * 32 * G_ROW + ks * 32)); };
+            const bf16x8 va = read(base_a, 0), vb = read(base_b, 0);
+            g[0][0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(va, vb, g[0][0], 0, 0, 0);
+            if (!ONE || len > 32) {
+                const bf16x8 wb = read(base_b, 1), wa = ONE ? wb : read(base_a, 1);
+                g[0][1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(va, wb, g[0][1], 0, 0, 0);
+                if (!ONE) g[1][0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wa, vb, g[1][0], 0, 0, 0);
+                g[1][1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wa, wb, g[1][1], 0, 0, 0);
             }
-#pragma unroll
-            for (int i = 0; i < 2; ++i)
-#pragma unroll
-                for (int j = 0; j < 2; ++j) g[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(va[i], vb[j], g[i][j], 0, 0, 0);
         }
     };
     // fp32 dY: a wave takes 16 of a chunk's 64 features, the halves of the wave eight each: a matrix instruction multiplies one of either half
@@ -738,41 +744,54 @@ __global__ void __launch_bounds__(256, 2) ck_gram_kernel(const CkDenseArgs a, in
         const char *base_a = ck_lds + buf * G_STAGE + (lane & 31) * G_ROW + (lane >> 5) * 32 + wave * 64, *base_b = base_a + (diagonal ? 0 : G_SIDE);
 #pragma unroll
         for (int q = 0; q < 2; ++q) {
-            float4 va[2], vb[2];
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                va[i] = *reinterpret_cast<const float4 *>(base_a + i * 32 * G_ROW + q * 16);
-                vb[i] = *reinterpret_cast<const float4 *>(base_b + i * 32 * G_ROW + q * 16);
-            }
-            auto step = [&](float a0, float a1, float b0, float b1) {
-                gy[0][0] = __builtin_amdgcn_mfma_f32_32x32x2f32(a0, b0, gy[0][0], 0, 0, 0);
-                gy[0][1] = __builtin_amdgcn_mfma_f32_32x32x2f32(a0, b1, gy[0][1], 0, 0, 0);
-                gy[1][0] = __builtin_amdgcn_mfma_f32_32x32x2f32(a1, b0, gy[1][0], 0, 0, 0);
-                gy[1][1] = __builtin_amdgcn_mfma_f32_32x32x2f32(a1, b1, gy[1][1], 0, 0, 0);
+            auto read = [&](const char *base, int i) { return *reinterpret_cast<const float4 *>(base + i * 32 * G_ROW + q * 16); };
+            auto step = [&](f32x16 &g, const float4 &a, const float4 &b) {
+                g = __builtin_amdgcn_mfma_f32_32x32x2f32(a.x, b.x, g, 0, 0, 0);
+                g = __builtin_amdgcn_mfma_f32_32x32x2f32(a.y, b.y, g, 0, 0, 0);
+                g = __builtin_amdgcn_mfma_f32_32x32x2f32(a.z, b.z, g, 0, 0, 0);
+                g = __builtin_amdgcn_mfma_f32_32x32x2f32(a.w, b.w, g, 0, 0, 0);
             };
-            step(va[0].x, va[1].x, vb[0].x, vb[1].x);
-            step(va[0].y, va[1].y, vb[0].y, vb[1].y);
-            step(va[0].z, va[1].z, vb[0].z, vb[1].z);
-            step(va[0].w, va[1].w, vb[0].w, vb[1].w);
+            const float4 va = read(base_a, 0), vb = read(base_b, 0);
+            step(gy[0][0], va, vb);
+            if (!ONE || len > 32) {
+                const float4 wb = read(base_b, 1), wa = ONE ? wb : read(base_a, 1);
+                step(gy[0][1], va, wb);
+                if (!ONE) step(gy[1][0], wa, vb);
+                step(gy[1][1], wa, wb);
+            }
         }
     };
-    const int all = nx + ny;
-    fetch(0);
-    if (all > 0) stage(0, 0);
-    fetch(1);
-    __syncthreads();
-    for (int i = 0; i < nx; ++i) {
-        products(gx, i & 1);
-        if (i + 1 < all) stage(i + 1, (i + 1) & 1);
-        fetch(i + 2);
+    // chunk i is in LDS buffer i & 1, the AHEAD after it on their way
+    auto after = [&](Held &held, Scale &scale, More &more, int i) {                             // chunk i + 1, and the next to be fetched there
+        stage(held, scale, more, i + 1);
+        fetch(held, scale, more, i + 1 + AHEAD);
         __syncthreads();
-    }
-    for (int i = nx; i < all; ++i) {
+    };
+    auto turn_x = [&](Held &held, Scale &scale, More &more, int i) {
+        if (!ONE || i < nx) products(gx, i & 1);
+        after(held, scale, more, i);
+    };
+    auto turn_y = [&](Held &held, Scale &scale, More &more, int i) {
         if constexpr (BF16) products(gy, i & 1);
         else products_f32(i & 1);
-        if (i + 1 < all) stage(i + 1, (i + 1) & 1);
-        fetch(i + 2);
-        __syncthreads();
+        after(held, scale, more, i);
+    };
+    Held h0, h1, h2;
+    Scale c0, c1, c2;
+    More m0, m1, m2;
+    fetch(h0, c0, m0, 0);
+    if constexpr (ONE) { fetch(h1, c1, m1, 1); fetch(h2, c2, m2, 2); }
+    after(h0, c0, m0, -1);
+    if constexpr (ONE) {
+        for (int i = 0; i < nx_up; i += 3) { turn_x(h1, c1, m1, i); turn_x(h2, c2, m2, i + 1); turn_x(h0, c0, m0, i + 2); }
+        for (int i = nx_up; i < all; i += 3) {
+            turn_y(h1, c1, m1, i);
+            if (i + 1 < all) turn_y(h2, c2, m2, i + 1);
+            if (i + 2 < all) turn_y(h0, c0, m0, i + 2);
+        }
+    } else {
+        for (int i = 0; i < nx; ++i) turn_x(h0, c0, m0, i);
+        for (int i = nx; i < all; ++i) turn_y(h0, c0, m0, i);
     }
 
     // the waves' sums meet in LDS, in the order of the waves: a wave adds up sixteen of a lane's 64 values
@@ -805,6 +824,7 @@ __global__ void __launch_bounds__(256, 2) ck_gram_kernel(const CkDenseArgs a, in
     float ss = 0.0f;
 #pragma unroll
     for (int q = 0; q < 16; ++q) ss += (a.has_bias ? sx[q] + 1.0f : sx[q]) * sy[q];          // tokens that are not there: 0 dY . dY
+    if (ONE && wave == 1) ss *= 2.0f;                              // a wave has one of the four blocks: block (0, 1), and (1, 0) is zeros
     const float tot = block_sum<4>(ss, red);
     if (t == 0) a.partials[whole] = diagonal ? tot : 2.0f * tot;
 }
@@ -829,7 +849,8 @@ __global__ void __launch_bounds__(512) ck_gram_join_kernel(const CkDenseArgs a, 
                 x.x += u.x; x.y += u.y; y.x += v.x; y.y += v.y;
             }
             if (a.has_bias) { x.x += 1.0f; x.y += 1.0f; }
-            ss += x.x * y.x + x.y * y.y;
+            const float twice = pairs == 1 && e / (G_VALUES / 4) == 1 ? 2.0f : 1.0f;          // block (0, 1), and (1, 0) is zeros
+            ss += twice * (x.x * y.x + x.y * y.y);
         }
     }
     const float tot = block_sum<8>(ss, red);
@@ -930,6 +951,14 @@ size_t checkpoint_ws_bytes(const Geo &g, int mode)
     return align16(4 * (size_t)g.n * std::max(p.per_example, q.per_example)) + std::max(gram_tile_bytes(g, p), gram_tile_bytes(g, q));
 }
 
+template <bool ONE>
+static dp_status run_gram(bool bf16, bool words, dim3 grid, const CkDenseArgs &a, int pairs, int splits, float *tiles, hipStream_t s)
+{
+    if (!bf16) return launch_lds<ck_gram_kernel<false, true, ONE>>(grid, 256, 2 * G_STAGE, s, a, pairs, splits, tiles);
+    if (!words) return launch_lds<ck_gram_kernel<true, false, ONE>>(grid, 256, 2 * G_STAGE, s, a, pairs, splits, tiles);
+    return launch_lds<ck_gram_kernel<true, true, ONE>>(grid, 256, 2 * G_STAGE, s, a, pairs, splits, tiles);
+}
+
 static dp_status launch_weighted(const Geo &g, CkDenseArgs a, float *out_w, float *out_b, void *ws, hipStream_t s)
 {
     const CkPlan p = ck_plan(g, MODE_WEIGHTED);
@@ -1000,9 +1029,8 @@ dp_status launch_checkpoint_dense(const Geo &g, int mode, const uint8_t *codes, 
         const int pairs = (int)p.per_example;
         const dim3 joins((unsigned)(g.n * p.per_example)), blocks(joins.x * (unsigned)p.gram_splits);
         float *tiles = reinterpret_cast<float *>(static_cast<char *>(ws) + align16(4 * (size_t)g.n * p.per_example));
-        st = !g.bf16 ? launch_lds<ck_gram_kernel<false, true>>(blocks, 256, 2 * G_STAGE, s, a, pairs, p.gram_splits, tiles)
-             : words ? launch_lds<ck_gram_kernel<true, true>>(blocks, 256, 2 * G_STAGE, s, a, pairs, p.gram_splits, tiles)
-                     : launch_lds<ck_gram_kernel<true, false>>(blocks, 256, 2 * G_STAGE, s, a, pairs, p.gram_splits, tiles);
+        st = pairs == 1 ? run_gram<true>(g.bf16, words, blocks, a, pairs, p.gram_splits, tiles, s)
+                        : run_gram<false>(g.bf16, words, blocks, a, pairs, p.gram_splits, tiles, s);
         if (st == DP_OK && p.gram_splits > 1) st = launch_lds<ck_gram_join_kernel>(joins, 512, 0, s, a, pairs, p.gram_splits, tiles);
     } else if (g.bf16) {
         st = p.nj == 4 ? run_contract<1, 4, false, true>(words, grid, a, s) : run_contract<1, 2, false, true>(words, grid, a, s);

@@ -220,7 +220,7 @@ def example_grad(desc, dev, stored, stride=0, stream=None):
 
 
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
-@pytest.mark.parametrize("case", CASES, ids=str)
+@pytest.mark.parametrize("case", CASES + [(16, 50, 1300, 1301, True, True), (16, 30, 1300, 1300, False, True), (8, 100, 2600, 2600, True, True)], ids=str)
 def test_example_gradients_and_norms(case, dtype):
     n, tokens, cin, cout, bias, ragged = case
     desc, dev, xv, dyv = problem(case, dtype)

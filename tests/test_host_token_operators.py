@@ -173,3 +173,26 @@ def test_buckets_against_whole_numbers(lib, buckets, max_distance, bidirectional
         want = nb + (mag(-d) if -d <= max_distance else nb - 1) if bidirectional else 0
         assert dp.dp_bias_bucket(desc, d) == want
     assert dp.dp_bias_bucket(desc, (1 << 31) - 1) == nb - 1
+
+
+def test_attention_block_refuses_other_shapes():
+    with pytest.raises(ValueError):
+        dp.PrivateAttention(2, 4, 32, 5, clip_c=1.0, sigma=1.0, total_batch=2, device="cpu")
+    block = dp.PrivateAttention(2, 4, 32, 4, clip_c=1.0, sigma=1.0, total_batch=2, device="cpu")
+    x = torch.zeros((2, 4, 32), dtype=torch.bfloat16)
+    cache = torch.zeros((2, 4, 4, 8), dtype=torch.bfloat16)
+    lengths = torch.zeros(2, dtype=torch.int32)
+    for bad in (x.float(), x[:1], x[:, :3].contiguous(), x.transpose(0, 1), torch.zeros((2, 4, 33), dtype=torch.bfloat16)):
+        with pytest.raises(ValueError):
+            block.forward(bad)
+        if bad.is_contiguous():
+            with pytest.raises(ValueError):
+                block.backward(bad)
+    for bad in (lengths.long(), lengths[:1], torch.zeros((2, 2), dtype=torch.int32)):
+        with pytest.raises(ValueError):
+            block.forward(x, bad)
+        with pytest.raises(ValueError):
+            block.attend_last(x[:, 0].contiguous(), cache, cache, bad)
+    for q, k, v in ((x[:, 0].contiguous(), cache[:, :, :3].contiguous(), cache), (x[:, 0].contiguous(), cache, cache.float()), (x[:1, 0].contiguous(), cache, cache)):
+        with pytest.raises(ValueError):
+            block.attend_last(q, k, v)
