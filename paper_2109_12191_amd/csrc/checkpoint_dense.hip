@@ -78,9 +78,10 @@ __device__ __forceinline__ void split8(const float (&v)[8], uint4 (&planes)[3])
 // for examples of a few tokens, of which 32 rows hold several.
 // Bias: a column of workgroups of its own adds up dY.
 // Measured: norms of 8 x 1024 tokens 1024 -> 2048 34.8 us, 988 TFLOP/s (a library product of 8192^3: 1282); clipped sum of 16 x 512 tokens
-// 2048 -> 2048 98 us, 700 TFLOP/s, and 11 us to join two ranges.  Bound by the LDS (a product's operands are 96 KB written and read a chunk and
-// workgroup, 0.3 us of its 0.75) and by the waits that two workgroups a compute unit leave uncovered; 16 x 128 tokens 768 -> 768, 5 chunks a
-// workgroup, by trips to memory one after the other.  Three stages of loads instead of two: no gain (registers); chunks of 32 with three workgroups: slower.
+// 2048 -> 2048 93.5 us, 735 TFLOP/s, and 11 us to join two ranges (factors worked out by every chunk instead of once: 94.4; 2 x 512 tokens
+// 4096 -> 1024 24.6 instead of 23.2).  Bound by the LDS (a chunk's operands are 96 KB written and read for a workgroup, 0.3 us of its 0.75) and by
+// the waits that two workgroups a compute unit leave uncovered; 16 x 128 tokens 768 -> 768, 8 chunks a workgroup at most, by trips to memory one after
+// the other.  Three stages of loads instead of two: no gain (registers); chunks of 32 with three workgroups: slower.
 // WORDS: rows of dY begin at whole dwords: pieces by buffer loads, which give zeros beyond the chunk's last row (what a row's last piece takes
 // from the next row is multiplied into features beyond the last, which nobody reads).  Else (bf16, an odd number of features) every other
 // row begins in the middle of a dword: five dwords around a piece, shifted into place on their way into LDS.
@@ -133,15 +134,30 @@ __global__ void __launch_bounds__(256, 2) ck_contract_kernel(const CkDenseArgs a
         uint32_t odd;                                              //   and whether the chunk's first row begins in the middle of one
         int rows;                                                  // of the chunk (0: it adds nothing)
         bool begins;                                               // an example begins with it, of
-        uint32_t sq;                                               //   this squared norm (as loaded), hence
+        int ex;                                                    //   this number, hence
         int power;                                                 //   factor f = m 2^power
         float m, f;
     };
     int f_ex = 0, f_c = 0, f_len = len;                            // weighted, by example: what the next chunk belongs to
     // Ragged examples: lengths, and chunks of the examples before each, fetched together (one after the other they are a trip to memory each).
-    // Factors come with the chunks: an example that is left out is walked over without products.
+    // Factors as well, once for all chunks: an example that is left out is walked over without products.
     constexpr int TABLE = WEIGHTED && !ROWS ? CK_TABLE : 1;
     __shared__ int ex_len[TABLE], ex_before[TABLE], found, wave_chunks[4];
+    __shared__ float ex_factor[TABLE];
+    const __amdgpu_buffer_rsrc_t sq_buffer = __builtin_amdgcn_make_buffer_rsrc(const_cast<float *>(a.group_sqnorm), 0, (int)((unsigned)a.n * 4u), 0x00020000);
+    float sq[4];
+    if constexpr (WEIGHTED && !ROWS) {
+#pragma unroll
+        for (int u = 0; u < 4; ++u) sq[u] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(sq_buffer, 16 * t + 4 * u, 0, 0));
+    }
+    auto place_factors = [&]() {                                   // (after the first chunks are on their way)
+        if constexpr (WEIGHTED && !ROWS) {
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+                if (4 * t + u < a.n) ex_factor[4 * t + u] = clip_factor(sq[u], a.clip_c);
+            __syncthreads();
+        }
+    };
     if constexpr (WEIGHTED && !ROWS) {
         if (!a.lengths) {
             const int cpe = (a.tokens + CK - 1) / CK;
@@ -188,7 +204,6 @@ __global__ void __launch_bounds__(256, 2) ck_contract_kernel(const CkDenseArgs a
             f_c = c_begin - __builtin_amdgcn_readfirstlane(ex_before[f_ex]);
         }
     }
-    const __amdgpu_buffer_rsrc_t sq_buffer = __builtin_amdgcn_make_buffer_rsrc(const_cast<float *>(a.group_sqnorm), 0, (int)((unsigned)a.n * 4u), 0x00020000);
 
     auto load_rows = [&](Slot &s, unsigned row0_any, int rows_any) {
         // the same in every lane, which the compiler does not always see (and a buffer in vector registers is read lane by lane)
@@ -235,7 +250,7 @@ __global__ void __launch_bounds__(256, 2) ck_contract_kernel(const CkDenseArgs a
     auto fetch = [&](Slot &s, int c) {
         s.rows = 0;
         s.begins = false;
-        s.sq = 0;
+        s.ex = 0;
         if (c >= c_end) return;
         if constexpr (ROWS) {
             const unsigned row0 = (unsigned)c * CK;
@@ -247,7 +262,7 @@ __global__ void __launch_bounds__(256, 2) ck_contract_kernel(const CkDenseArgs a
                 while (__builtin_amdgcn_readfirstlane(ex_len[f_ex]) == 0) ++f_ex;         // (there are chunks: an example with some follows)
                 f_len = __builtin_amdgcn_readfirstlane(ex_len[f_ex]);
             }
-            s.sq = __builtin_amdgcn_raw_buffer_load_b32(sq_buffer, 4 * f_ex, 0, 0);
+            s.ex = f_ex;
             s.rows = min(f_len - f_c * CK, CK);
             load_rows(s, (unsigned)f_ex * (unsigned)a.tokens + (unsigned)(f_c * CK), s.rows);
             if (++f_c * CK >= f_len) { f_c = 0; ++f_ex; }
@@ -259,7 +274,7 @@ __global__ void __launch_bounds__(256, 2) ck_contract_kernel(const CkDenseArgs a
     // weighted, by example: the factor of a chunk that has arrived; one of factor 0 adds nothing (and no 0 * inf)
     auto ready = [&](Slot &s) {
         if constexpr (WEIGHTED && !ROWS) {
-            s.f = __uint_as_float((uint32_t)__builtin_amdgcn_readfirstlane((int)__float_as_uint(clip_factor(__uint_as_float(s.sq), a.clip_c))));
+            s.f = __uint_as_float((uint32_t)__builtin_amdgcn_readfirstlane((int)__float_as_uint(ex_factor[s.ex])));
             s.power = (int)(__float_as_uint(s.f) >> 23) - 127;
             s.m = s.f * pow2_of(127 - s.power);
             if (s.f == 0.0f) { s.rows = 0; s.power = 0; }
@@ -355,6 +370,7 @@ __global__ void __launch_bounds__(256, 2) ck_contract_kernel(const CkDenseArgs a
         };
         Slot b0, b1;
         fetch(b0, c_begin);
+        place_factors();
         for (int c = c_begin; c < c_end; c += 2) {
             if constexpr (ROWS) __syncthreads();
             fetch(b1, c + 1);
@@ -453,6 +469,7 @@ __global__ void __launch_bounds__(256, 2) ck_contract_kernel(const CkDenseArgs a
     Slot s0, s1;
     fetch(s0, c_begin);
     fetch(s1, c_begin + 1);
+    place_factors();
     if constexpr (ROWS) __syncthreads();
     ready(s0);
     Now now = {s0.rows, s0.begins, s0.m};
@@ -916,7 +933,8 @@ CkPlan ck_plan(const Geo &g, int mode)
         const int yc = g.bf16 ? GC : GC / 2;
         const long long tiles = (g.h + GT - 1) / GT, pairs = tiles * (tiles + 1) / 2, chunks = (ck_pitch(g.cin) + GC - 1) / GC + (g.cout + yc - 1) / yc;
         p.gram_splits = (int)std::max(1ll, std::min({512 / (g.n * pairs), chunks / 8, 16ll}));
-        p.gram = gram_us(g, (double)pairs, p.gram_splits, (double)chunks) < contract_us(g, (double)p.per_example, ck_chunk(g.bf16 ? 1 : 3, p.nj));
+        p.gram = g.n * pairs < (1ll << 30) &&
+                 gram_us(g, (double)pairs, p.gram_splits, (double)chunks) < contract_us(g, (double)p.per_example, ck_chunk(g.bf16 ? 1 : 3, p.nj));
         if (p.gram) p.per_example = (size_t)pairs;
     }
     return p;
