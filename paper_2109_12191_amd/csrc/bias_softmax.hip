@@ -662,8 +662,9 @@ __global__ void __launch_bounds__(1024) bias_table_kernel(const float *partials,
 }
 
 // Lanes of a wave that share a row in the kernels for short ones, or 0 where a row has a wave of its own or several: a call with fewer than eight
-// queries would leave most of those lanes idle, and a few thousand rows are all under way at once that way (backward of 64 x 64, 4096
-// rows: 9.0 us, 12.8 with several rows to a wave and eight in turn; 16384 rows: 15.2 and 13.4; 131072 of 128 keys: 47 and 26).
+// queries would leave most of those lanes idle, and a few thousand rows are all under way at once that way (us, a wave to a row and
+// several with eight in turn: backward, 64 keys, 8192 rows 7.6 and 10.8, 16384 11.4 and 11.6, 32768 15.7 and 11.3; 128 keys, 65536 rows 25.6 and
+// 14.5; forward, 64 keys, 8192 rows 6.5 and 7.2, 16384 8.8 and 7.5, 65536 20.9 and 9.2).
 int narrow_lanes(const BiasGeo &g)
 {
     if (g.keys > 256 || g.queries < 8 || (long long)g.n * g.heads * g.queries < 16384 || g.row_stride > ((size_t)1 << 20)) return 0;
