@@ -438,7 +438,7 @@ dp_status dp_checkpoint_read(const uint8_t *codes, const uint8_t *scales, size_t
  * lengths    [device] [n] int32 tokens of each example (taken as 0 .. tokens), or NULL: all of them.  What lies in later tokens of
  *            either operand is not used, whatever it is.  An example of no token has zero gradients and norm 0.
  * Products of bf16 dY are those of bf16 matrix instructions with fp32 sums and nothing is rounded in between; fp32 dY is split into three
- * bf16 numbers that add up to it (magnitudes below 2^127).  Norms alone of bf16 layers with few tokens go by way of Gram matrices,
+ * bf16 numbers that add up to it (magnitudes below 2^127).  Norms alone of layers with few tokens go by way of Gram matrices (fp32 dY: fp32 products),
  *   |dW_i|^2 = sum_{t,u} (X_t . X_u)(dY_t . dY_u),
  * which lose digits where the sum over the tokens cancels (a norm below 2^-20 of what its terms add up to is not resolved, and can come out
  * negative: such an example is left out, dp_clip_factors); stored gradients give sums of squares always.
@@ -448,7 +448,7 @@ dp_status dp_checkpoint_example_grad(const dp_layer_desc *desc /*[host]*/, const
                                      const int32_t *lengths, float *g_w, float *g_b, size_t g_stride, float *sqnorm, void *ws,
                                      size_t ws_bytes, dp_stream stream);
 /* H4, recomputing form, from a checkpoint: acc_w += sum_i f_i dW_i, acc_b += sum_i f_i db_i (dp_clip_accumulate_recompute).  The factors meet
- * fp32 values; an example of factor 0 is not read.  ws: dp_checkpoint_workspace_bytes(desc, DP_WS_RECOMPUTE), which may be 0.     */
+ * fp32 values; what an example of factor 0 holds is not used.  ws: dp_checkpoint_workspace_bytes(desc, DP_WS_RECOMPUTE), which may be 0.     */
 dp_status dp_checkpoint_clip_accumulate(const dp_layer_desc *desc /*[host]*/, const uint8_t *codes, const uint8_t *scales, const void *dy,
                                         const int32_t *lengths, const float *sqnorm, float clip_c, float *acc_w, float *acc_b, void *ws,
                                         size_t ws_bytes, dp_stream stream);
