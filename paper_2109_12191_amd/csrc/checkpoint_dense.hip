@@ -960,10 +960,24 @@ static size_t gram_tile_bytes(const Geo &g, const CkPlan &p)
     return p.gram && p.gram_splits > 1 ? (size_t)g.n * p.per_example * p.gram_splits * 2 * G_VALUES * 4 : 0;
 }
 
+// A weighted call goes in launches of CK_TABLE examples and one of those that are left, which plan their own ranges; ranges do not grow
+// steadily with the chunks (645 examples of 64 tokens, 768 -> 768, take 15, 1024 of them 14): room for the most.
+static size_t weighted_ws_bytes(const Geo &g)
+{
+    const CkPlan p = ck_plan(g, MODE_WEIGHTED);
+    int most = p.ranges;
+    if (!p.rows && g.n > CK_TABLE && g.n % CK_TABLE) {
+        Geo rest = g;
+        rest.n = g.n % CK_TABLE;
+        most = std::max(most, ck_plan(rest, MODE_WEIGHTED).ranges);
+    }
+    return most > 1 ? 4 * (size_t)most * (align4(g.pw) + align4(g.pb)) : 0;
+}
+
 size_t checkpoint_ws_bytes(const Geo &g, int mode)
 {
+    if (mode == MODE_WEIGHTED) return weighted_ws_bytes(g);
     const CkPlan p = ck_plan(g, mode);
-    if (mode == MODE_WEIGHTED) return p.ranges > 1 ? 4 * (size_t)p.ranges * (align4(g.pw) + align4(g.pb)) : 0;
     // both per-example forms: a caller sizes its workspace once
     const CkPlan q = ck_plan(g, mode == MODE_NORM ? MODE_MATERIALISE : MODE_NORM);
     return align16(4 * (size_t)g.n * std::max(p.per_example, q.per_example)) + std::max(gram_tile_bytes(g, p), gram_tile_bytes(g, q));

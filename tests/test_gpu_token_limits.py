@@ -1,0 +1,48 @@
+"""The token operators at the ends of their ranges: calls that go in several launches, values and masks that leave the ordinary path."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2109_12191_amd as dp
+
+pytestmark = pytest.mark.gpu
+U = 2.0 ** -23
+
+
+def layer(n, tokens, cin, cout, dtype=torch.bfloat16, bias=0):
+    return dp.LayerDesc(kind=dp.DP_DENSE, in_dtype=dp.DP_BF16 if dtype == torch.bfloat16 else dp.DP_F32, n=n, cin=cin, cout=cout, h=tokens, w=1,
+                        has_bias=bias)
+
+
+def checkpoint(x):
+    """codes, scales, and the values they stand for in 64 bits."""
+    rows, features = x.shape
+    pitch = dp.dp_checkpoint_pitch(features)
+    codes = torch.empty((rows, pitch), dtype=torch.uint8, device="cuda:0")
+    scales = torch.empty((rows, pitch // 32), dtype=torch.uint8, device="cuda:0")
+    back = torch.empty((rows, features), dtype=torch.float32, device="cuda:0")
+    dp.dp_checkpoint_write(x, codes, scales)
+    dp.dp_checkpoint_read(codes, scales, back)
+    return codes, scales, back.double()
+
+
+@pytest.mark.parametrize("case", [(1669, 64, 768, 768), (1193, 100, 512, 512), (1256, 128, 384, 384)], ids=str)
+def test_clipped_sum_of_more_examples_than_a_launch_stays_in_its_workspace(case):
+    """The last launch takes more ranges than the ones before it; 8 MB behind the workspace are left alone."""
+    n, tokens, cin, cout = case
+    desc = layer(*case)
+    gen = torch.Generator("cuda:0").manual_seed(n)
+    codes, scales, x = checkpoint(torch.randn((n * tokens, cin), generator=gen, device="cuda:0").to(torch.bfloat16))
+    dy = (torch.randn((n * tokens, cout), generator=gen, device="cuda:0") * 0.01).to(torch.bfloat16)
+    sq = 10.0 ** (torch.rand((n,), generator=gen, device="cuda:0") * 4 - 2)
+    need = dp.dp_checkpoint_workspace_bytes(desc, dp.DP_WS_RECOMPUTE)
+    ws = torch.full((need + (8 << 20),), 0xA5, dtype=torch.uint8, device="cuda:0")
+    acc = torch.zeros((cout, cin), device="cuda:0")
+    dp.dp_checkpoint_clip_accumulate(desc, codes, scales, dy, sq, 0.7, acc, None, ws, ws_bytes=need)
+    assert bool((ws[need:] == 0xA5).all())
+    f = (0.7 / sq.double().sqrt()).clamp(max=1.0).repeat_interleave(tokens)[:, None]
+    g = dy.double() * f
+    off = (n * tokens + 2 * n + 8) * U * (g.abs().t() @ x.abs())          # every addition off by half a step, or cut
+    assert bool(((acc.double() - g.t() @ x).abs() <= off).all())

@@ -1,0 +1,29 @@
+"""CPU-only checks of what the token operators ask of their callers at the ends of their ranges."""
+import os
+
+import pytest
+
+import paper_2109_12191_amd as dp
+
+
+@pytest.fixture(scope="module", autouse=True)
+def lib():
+    if not os.path.exists(dp.lib_path()):
+        from paper_2109_12191_amd.build import build
+        build(verbose=False)
+    return dp.load_library()
+
+
+def _need(n, tokens, cin, cout, bias=0, dtype=dp.DP_BF16):
+    desc = dp.LayerDesc(kind=dp.DP_DENSE, in_dtype=dtype, n=n, cin=cin, cout=cout, h=tokens, w=1, has_bias=bias)
+    return dp.dp_checkpoint_workspace_bytes(desc, dp.DP_WS_RECOMPUTE)
+
+
+@pytest.mark.parametrize("tokens,cin,cout,bias", [(64, 768, 768, 0), (512, 512, 512, 0), (512, 384, 384, 1), (100, 512, 512, 0), (16, 768, 768, 1), (256, 512, 512, 0),
+                                                  (40, 100, 1000, 1), (17, 32, 40, 1), (700, 4096, 2048, 0)])
+def test_workspace_of_a_clipped_sum_holds_every_part_of_it(tokens, cin, cout, bias):
+    """Calls of more than 1024 examples go in launches of 1024 and one of the rest, each with the ranges that it takes by itself."""
+    whole = _need(1024, tokens, cin, cout, bias)
+    alone = {rest: _need(rest, tokens, cin, cout, bias) for rest in range(1, 1024)}
+    for n in list(range(1025, 2048)) + [2049, 3000, 5000, 65535]:
+        assert _need(n, tokens, cin, cout, bias) >= max(whole, alone.get(n % 1024, 0)), n
