@@ -8,7 +8,7 @@
 //
 // A bucket holds a run of distances, and from `far` on all distances of a side are in one bucket.  A workgroup takes rows of one
 // example and head.  Forward, it makes the biases of the distances in between once, in LDS.  Backward, a wave adds its rows'
-// dz by distance into sums of its own in LDS (the lanes' distances differ, so no two lanes meet in one place and the order is fixed), dz beyond
+// dz by distance into sums of its own in LDS (no two lanes meet in one place between two fences, so that the order is fixed), dz beyond
 // `far` into registers, and the workgroup adds up the runs of its buckets at the end; bias_table_kernel adds up workgroups.
 // A lane holds runs of eight keys, so the distances of a run go down by one from word to word: slot d + low + 16 lies in plane (slot mod 8)
 // of eight, at slot / 8, lanes eight keys apart meet neighbouring words of a plane, and where a run's eight values lie is one number for the
@@ -626,14 +626,19 @@ __global__ void __launch_bounds__(256) bias_backward_narrow_kernel(const BiasArg
     const int top = RunWords::slot(a, d0 + 7), m = RunWords::slot(a, r.first + r.q0 + 7) & 7;
 #pragma unroll 1
     for (int g = 0; g < 64 / TPR; ++g) {
-        if (lane / TPR == g && !beyond) {
+        // A row's neighbouring lanes are eight keys apart: slots 8 .. 14 of a lane are 0 .. 6 of the next one, and in either half no two lanes
+        // of a group have one in common.
 #pragma unroll
-            for (int c = 0; c < 15; ++c) {                         // slots top - c, which line 14 - c goes to
-                float *word = mine + (top >> 3) + ((m - c) & 7) * a.plane + ((m - c) >> 3);
-                *word += line[14 - c];
+        for (int half = 0; half < 2; ++half) {
+            if (lane / TPR == g && !beyond) {
+#pragma unroll
+                for (int c = 8 * half; c < 8 * half + 8 - half; ++c) {             // slots top - c, which line 14 - c goes to
+                    float *word = mine + (top >> 3) + ((m - c) & 7) * a.plane + ((m - c) >> 3);
+                    *word += line[14 - c];
+                }
             }
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");  // what follows meets words of other lanes
         }
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");     // the next rows' lanes meet other lanes' words
     }
     bias_bucket_sums(a, r, bias_lds, sum_far, sum_low, ends);
 }

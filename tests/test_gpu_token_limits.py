@@ -46,3 +46,27 @@ def test_clipped_sum_of_more_examples_than_a_launch_stays_in_its_workspace(case)
     g = dy.double() * f
     off = (n * tokens + 2 * n + 8) * U * (g.abs().t() @ x.abs())          # every addition off by half a step, or cut
     assert bool(((acc.double() - g.t() @ x).abs() <= off).all())
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("keys,more", [(8, {}), (64, {}), (64, dict(buckets=8, max_distance=20)), (128, dict(bidirectional=0)), (256, dict(max_distance=4096)),
+                                       (256, dict(buckets=64, max_distance=300, bidirectional=0))], ids=str)
+def test_table_gradient_of_short_rows_in_whole_numbers(keys, more, dtype):
+    """Equal probabilities and gradients that cancel in every row: dz are small whole numbers, and so is every sum of them, in any order.  A sum that is
+    lost where lanes meet the same word (a row's neighbouring lanes have seven distances in common) shows as a whole number that is missing."""
+    n, heads, queries = 9, 40, 60                    # more than 16384 rows: several to a wave
+    fields = dict(in_dtype=dp.DP_BF16 if dtype == torch.bfloat16 else dp.DP_F32, n=n, heads=heads, queries=queries, keys=keys, buckets=32, max_distance=128,
+                  bidirectional=1, causal=0, query_offset=keys // 3, scale=1.0)
+    desc = dp.BiasDesc(**{**fields, **more})
+    rng = np.random.default_rng(keys)
+    half = rng.integers(-3, 4, (n, heads, queries, keys // 2))
+    dz = rng.permuted(np.concatenate([half, -half], axis=3), axis=3)
+    probs = torch.full(dz.shape, 1.0 / keys, dtype=dtype, device="cuda:0")
+    dprobs = torch.from_numpy(dz * keys).to(dtype).cuda()
+    dscores, g = torch.empty_like(probs), torch.empty((n, desc.buckets, heads), device="cuda:0")
+    ws = torch.empty(dp.dp_bias_workspace_bytes(desc), dtype=torch.uint8, device="cuda:0")
+    dp.dp_bias_softmax_backward(desc, probs, dprobs, dscores, g, None, ws)
+    assert np.array_equal(dscores.double().cpu().numpy(), dz)
+    bucket = np.array([[dp.dp_bias_bucket(desc, keys // 3 + q - k) for k in range(keys)] for q in range(queries)])
+    want = np.stack([(dz * (bucket == b)).sum((2, 3)) for b in range(desc.buckets)], axis=1)
+    assert np.array_equal(g.double().cpu().numpy(), want)
