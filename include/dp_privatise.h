@@ -478,7 +478,8 @@ int dp_bias_bucket(const dp_bias_desc *desc /*[host]*/, int distance);
 
 /* probs[i,h,q,k] = exp(z_k) / sum_k' exp(z_k'),  z_k = scale * scores[i,h,q,k] + table[bucket(first_i + q - k), h], over the keys that count:
  * k < key_length_i, and not after the query if causal.  Zero for the others; a query at or beyond query_length_i, one with no key that
- * counts, and one whose z are all -inf have zeros throughout.  What lies in places that do not count is not used, whatever it is.
+ * counts, and one whose z are all -inf have zeros throughout; one with a NaN or +inf among them is NaN where it counts.  What lies in places
+ * that do not count is not used, whatever it is.
  * scores, probs [device] in_dtype, aligned to their element; probs may be scores.  table [device] fp32.
  * query_lengths, key_lengths [device] [n] int32 (taken as 0 .. queries, 0 .. keys), or NULL: all.                                 */
 dp_status dp_bias_softmax(const dp_bias_desc *desc /*[host]*/, const void *scores, const float *table, const int32_t *query_lengths,

@@ -252,6 +252,12 @@ __global__ void __launch_bounds__(TPR > 256 ? TPR : 256) bias_softmax_kernel(con
         }
     };
 
+    // zeros at the places of a run that do not count
+    auto cut = [&](float (&z)[8], int k, int end) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) z[i] = k + i < end ? z[i] : 0.0f;
+    };
+
     if constexpr (NV > 0) {
         Raw8<BF16> raw[NV];
         auto load_row = [&](int q) {
@@ -281,11 +287,13 @@ __global__ void __launch_bounds__(TPR > 256 ? TPR : 256) bias_softmax_kernel(con
                 for (int i = 0; i < 8; ++i) { z[j][i] = exp_of(z[j][i] - top); sum += z[j][i]; }
             sum = row_reduce<TPR, false>(sum, red);
             const float inv = sum == 0.0f ? 0.0f : __builtin_amdgcn_rcpf(sum);     // good to a step
+            const bool broken = !(sum < INFINITY);                  // a NaN or +inf among the keys that count; the others are zeros all the same
             const Row out(a.out, (r.base + q) * a.row_stride, a.keys);
 #pragma unroll
             for (int j = 0; j < NV; ++j) {
 #pragma unroll
                 for (int i = 0; i < 8; ++i) z[j][i] *= inv;
+                if (broken) cut(z[j], 8 * (t + TPR * j), end);
                 out.store(8 * (t + TPR * j), z[j]);
             }
         }
@@ -312,6 +320,7 @@ __global__ void __launch_bounds__(TPR > 256 ? TPR : 256) bias_softmax_kernel(con
             const float best = row_reduce<TPR, true>(top, red), base = best == -INFINITY ? 0.0f : best;
             sum = row_reduce<TPR, false>(sum * exp_of(top - base), red);
             const float inv = sum == 0.0f ? 0.0f : __builtin_amdgcn_rcpf(sum);
+            const bool broken = !(sum < INFINITY);
             for (int k = 8 * t; k < a.keys; k += 8 * TPR) {
                 Raw8<BF16> raw;
                 float z[8];
@@ -319,6 +328,7 @@ __global__ void __launch_bounds__(TPR > 256 ? TPR : 256) bias_softmax_kernel(con
                 logits(raw, k, false, position, end, z);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) z[i] = exp_of(z[i] - base) * inv;
+                if (broken) cut(z, k, end);
                 out.store(k, z);
             }
         }
@@ -567,6 +577,10 @@ __global__ void __launch_bounds__(256) bias_softmax_narrow_kernel(const BiasArgs
         const float inv = sum == 0.0f ? 0.0f : __builtin_amdgcn_rcpf(sum);
 #pragma unroll
         for (int i = 0; i < 8; ++i) z[i] *= inv;
+        if (!(sum < INFINITY)) {                                   // a NaN or +inf among the keys that count; the others are zeros all the same
+#pragma unroll
+            for (int i = 0; i < 8; ++i) z[i] = k + i < end ? z[i] : 0.0f;
+        }
         out.store(r.q0 + row < r.q1, row, k, z);
     }
 }

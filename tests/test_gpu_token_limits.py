@@ -70,3 +70,32 @@ def test_table_gradient_of_short_rows_in_whole_numbers(keys, more, dtype):
     bucket = np.array([[dp.dp_bias_bucket(desc, keys // 3 + q - k) for k in range(keys)] for q in range(queries)])
     want = np.stack([(dz * (bucket == b)).sum((2, 3)) for b in range(desc.buckets)], axis=1)
     assert np.array_equal(g.double().cpu().numpy(), want)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("shape", [(1, 1, 6, 70, 40), (1, 1, 6, 700, 513), (1, 1, 6, 1500, 900), (1, 1, 6, 3001, 2000), (1, 1, 6, 9000, 8191), (1, 1, 6, 20000, 16500),
+                                   (1, 1, 6, 40001, 33000), (30, 14, 40, 61, 40), (30, 14, 40, 120, 101), (30, 14, 40, 256, 9)], ids=str)
+def test_broken_scores_break_only_what_counts(shape, dtype):
+    """A NaN or an infinity among the keys that count: the row is NaN there and zero at the others, in every kernel; rows beside it are untouched."""
+    n, heads, queries, keys, length = shape
+    desc = dp.BiasDesc(in_dtype=dp.DP_BF16 if dtype == torch.bfloat16 else dp.DP_F32, n=n, heads=heads, queries=queries, keys=keys, buckets=32,
+                       max_distance=128, bidirectional=1, causal=0, query_offset=0, scale=1.0)
+    gen = torch.Generator("cuda:0").manual_seed(keys)
+    scores = torch.randn((n, heads, queries, keys), generator=gen, device="cuda:0").to(dtype)
+    table = torch.randn((32, heads), generator=gen, device="cuda:0")
+    key_lengths = torch.full((n,), length, dtype=torch.int32, device="cuda:0")
+    clean, probs = torch.empty_like(scores), torch.empty_like(scores)
+    dp.dp_bias_softmax(desc, scores, table, clean, key_lengths=key_lengths)
+    scores[:, :, 0, 3] = math.nan
+    scores[:, :, 2, length - 1] = math.inf
+    scores[:, :, 4, :length] = math.inf
+    scores[:, :, 5, 0] = -math.inf
+    scores[:, :, :, length:] = math.nan
+    dp.dp_bias_softmax(desc, scores, table, probs, key_lengths=key_lengths)
+    assert bool((probs[..., length:] == 0.0).all())
+    for q in (0, 2, 4):
+        assert bool(probs[:, :, q, :length].isnan().any(-1).all())
+    assert bool(probs[:, :, 0, :length].isnan().all())
+    for q in (1, 3):
+        assert torch.equal(probs[:, :, q], clean[:, :, q])
+    assert bool((probs[:, :, 5, 0] == 0.0).all()) and bool(probs[:, :, 5].isfinite().all())
