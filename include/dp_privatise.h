@@ -448,7 +448,7 @@ dp_status dp_checkpoint_example_grad(const dp_layer_desc *desc /*[host]*/, const
                                      const int32_t *lengths, float *g_w, float *g_b, size_t g_stride, float *sqnorm, void *ws,
                                      size_t ws_bytes, dp_stream stream);
 /* H4, recomputing form, from a checkpoint: acc_w += sum_i f_i dW_i, acc_b += sum_i f_i db_i (dp_clip_accumulate_recompute).  The factors meet
- * fp32 values; what an example of factor 0 holds is not used.  ws: dp_checkpoint_workspace_bytes(desc, DP_WS_RECOMPUTE), which may be 0.     */
+ * fp32 values; what an example of factor 0 holds is not used, and a factor below 2^-126 may count as 0.  ws: dp_checkpoint_workspace_bytes(desc, DP_WS_RECOMPUTE), which may be 0.     */
 dp_status dp_checkpoint_clip_accumulate(const dp_layer_desc *desc /*[host]*/, const uint8_t *codes, const uint8_t *scales, const void *dy,
                                         const int32_t *lengths, const float *sqnorm, float clip_c, float *acc_w, float *acc_b, void *ws,
                                         size_t ws_bytes, dp_stream stream);

@@ -71,9 +71,11 @@ __device__ __forceinline__ void split8(const float (&v)[8], uint4 (&planes)[3])
 // PLANES: 1: dY as bf16 numbers; 3: fp32 values of dY, split.
 // Per-example call (WEIGHTED false): a workgroup contracts one example's tile, squares it, and stores it if asked.
 // WEIGHTED, PLANES 1: a workgroup walks over a range of the chunks of all examples, as many as any other range's; chunks after an example's
-// last token are not among them.  With f_i = m_i 2^e_i, 1 <= m_i < 2, the power is put into
-// the scales of X, exactly, and the running sum is kept in units of m_i: it is multiplied by m_(i-1) / m_i where an example begins, and by
-// the last m at the end.  One set of accumulators for any number of examples, and each example meets its factor in fp32.
+// last token are not among them.  With f_i = m_i 2^e_i, -16 <= e_i <= 0, 1 <= m_i < 2 (below 2^-16: m_i < 1), the power is put into
+// the scales of X, exactly: values of a checkpoint times 2^-16 are normal bf16 numbers still (2^-9 2^-100 2^-16).  The running sum is kept in units of m_i: it is
+// multiplied by m_(i-1) / m_i where an example begins, and by the last m at the end.  It stays below n times an example's norm, as
+// f_i <= C / norm_i.  One set of accumulators for any number of examples, and each example meets its factor in fp32.  A factor that is no normal fp32
+// number counts as 0 (m_(i-1) / m_i would pass fp32's range).
 // WEIGHTED, PLANES 3: rows (example, token) of the whole call one after the other, dY times its factor in fp32, then split: for fp32 dY, and
 // for examples of a few tokens, of which 32 rows hold several.
 // Bias: a column of workgroups of its own adds up dY.
@@ -90,6 +92,9 @@ constexpr int ck_chunk(int planes, int nj) { return planes == 1 && nj == 2 ? 64 
 constexpr int ck_stage_bytes(int planes, int nj) { return ck_chunk(planes, nj) * (planes * 2 * CT + nj * 128); }
 constexpr int CK_TABLE = 1024;                                     // examples of a weighted call
 constexpr unsigned CK_NOWHERE = 0xFFFFFFE0u;                       // an offset beyond any buffer
+constexpr int CK_POWER = 16;                                       // of a factor, in the scales of X
+static_assert(CK_LOW - 9 - CK_POWER >= -126, "scaled values are normal bf16 numbers");
+constexpr float CK_LEAST_FACTOR = 0x1p-126f;
 
 template <int PLANES, int NJ, bool WEIGHTED, bool BF16, bool WORDS>
 __global__ void __launch_bounds__(256, 2) ck_contract_kernel(const CkDenseArgs a)
@@ -275,9 +280,9 @@ __global__ void __launch_bounds__(256, 2) ck_contract_kernel(const CkDenseArgs a
     auto ready = [&](Slot &s) {
         if constexpr (WEIGHTED && !ROWS) {
             s.f = __uint_as_float((uint32_t)__builtin_amdgcn_readfirstlane((int)__float_as_uint(ex_factor[s.ex])));
-            s.power = (int)(__float_as_uint(s.f) >> 23) - 127;
+            if (s.f < CK_LEAST_FACTOR) { s.f = 0.0f; s.rows = 0; }
+            s.power = max((int)(__float_as_uint(s.f) >> 23) - 127, -CK_POWER);
             s.m = s.f * pow2_of(127 - s.power);
-            if (s.f == 0.0f) { s.rows = 0; s.power = 0; }
         }
     };
     auto piece_y = [&](const Slot &s, int u) {                     // piece u of dY as it is
@@ -319,6 +324,7 @@ __global__ void __launch_bounds__(256, 2) ck_contract_kernel(const CkDenseArgs a
         uint4 x = s.x[u];
         if constexpr (ROWS)
             if (row_factors[buf][r] == 0.0f) x = make_uint4(0, 0, 0, 0);
+        // (beyond the checkpoint's rows scales are 0: no power of a factor there)
         const float scale = pow2_of(WEIGHTED && !ROWS ? max((int)s.scale[u] + s.power, 1) : (int)s.scale[u]);
         const uint2 w0 = ck_bf16(x.x, scale), w1 = ck_bf16(x.y, scale), w2 = ck_bf16(x.z, scale), w3 = ck_bf16(x.w, scale);
         char *to = ck_lds + buf * STAGE + PLANES * PLANE + r * X_ROW;

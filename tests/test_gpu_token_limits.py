@@ -99,3 +99,76 @@ def test_broken_scores_break_only_what_counts(shape, dtype):
     for q in (1, 3):
         assert torch.equal(probs[:, :, q], clean[:, :, q])
     assert bool((probs[:, :, 5, 0] == 0.0).all()) and bool(probs[:, :, 5].isfinite().all())
+
+
+@pytest.mark.parametrize("bias", [0, 1])
+def test_clipped_sum_of_tiny_activations_under_tiny_factors(bias):
+    """Scales at the format's lowest, gradients that make up for it, and factors from 1 down to 2^-60: no example adds more than its share.  Each
+    example is summed by itself, and all of them together."""
+    n, tokens, cin, cout = 12, 40, 96, 64
+    gen = torch.Generator("cuda:0").manual_seed(4)
+    small = torch.randn((n * tokens, cin), generator=gen, device="cuda:0") * 2.0 ** -97
+    small[:, 64:] *= 2.0 ** 40                       # other blocks of a row with ordinary scales
+    small[:, :32] *= 2.0 ** -10                      # and codes that are no normal e4m3 numbers
+    codes, scales, x = checkpoint(small.to(torch.bfloat16))
+    assert int(scales.min()) == 27
+    dy = (torch.randn((n * tokens, cout), generator=gen, device="cuda:0") * 2.0 ** 90).to(torch.bfloat16)
+    powers = torch.tensor([0, -1, -15, -16, -17, -26, -27, -28, -40, -50, -60, -3], dtype=torch.float64, device="cuda:0")
+    sq = (2.0 ** (-2 * powers) * (1.7 ** 2)).float()                       # f = min(1, 1 / sqrt(sq))
+    f = (1.0 / sq.double().sqrt()).clamp(max=1.0)
+
+    def run(first, count):
+        desc = layer(count, tokens, cin, cout, bias=bias)
+        rows = slice(first * tokens, (first + count) * tokens)
+        ws = torch.empty(max(dp.dp_checkpoint_workspace_bytes(desc, dp.DP_WS_RECOMPUTE), 16), dtype=torch.uint8, device="cuda:0")
+        acc, acc_b = torch.zeros((cout, cin), device="cuda:0"), torch.zeros(cout, device="cuda:0") if bias else None
+        dp.dp_checkpoint_clip_accumulate(desc, codes[rows], scales[rows].contiguous(), dy[rows], sq[first:first + count].clone(), 1.0, acc, acc_b, ws)
+        g = dy[rows].double() * f[first:first + count].repeat_interleave(tokens)[:, None]
+        off = (count * tokens + 2 * count + 8) * U * (g.abs().t() @ x[rows].abs()) + 2.0 ** -126
+        assert bool(((acc.double() - g.t() @ x[rows]).abs() <= off).all())
+        if bias:
+            assert bool(((acc_b.double() - g.sum(0)).abs() <= (count * tokens + 8) * U * g.abs().sum(0)).all())
+    for i in range(n):
+        run(i, 1)
+    run(0, n)
+
+
+def test_clipped_sum_leaves_out_factors_that_are_no_normal_numbers():
+    """Bounds so small that factors leave fp32's normal range beside factors that do not: sums stay finite, and right to fp32's smallest numbers."""
+    n, tokens, cin, cout = 4, 32, 64, 64
+    gen = torch.Generator("cuda:0").manual_seed(5)
+    codes, scales, x = checkpoint(torch.randn((n * tokens, cin), generator=gen, device="cuda:0").to(torch.bfloat16))
+    codes.view(n, tokens, cin)[:, :, :8] = 0         # sums that stay zero
+    x.view(n, tokens, cin)[:, :, :8] = 0.0
+    dy = torch.randn((n * tokens, cout), generator=gen, device="cuda:0").to(torch.bfloat16)
+    sq = torch.tensor([1e-6, 1e30, 1e-6, 1e38], device="cuda:0")
+    desc = layer(n, tokens, cin, cout)
+    for clip_c in (1e-22, 1e-25, 1e-28):
+        ws = torch.empty(max(dp.dp_checkpoint_workspace_bytes(desc, dp.DP_WS_RECOMPUTE), 16), dtype=torch.uint8, device="cuda:0")
+        acc = torch.zeros((cout, cin), device="cuda:0")
+        dp.dp_checkpoint_clip_accumulate(desc, codes, scales, dy, sq, clip_c, acc, None, ws)
+        g = dy.double() * (clip_c / sq.double().sqrt()).repeat_interleave(tokens)[:, None]
+        off = (n * tokens + 16) * U * (g.abs().t() @ x.abs()) + tokens * 2.0 ** -118
+        assert bool(((acc.double() - g.t() @ x).abs() <= off).all())
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_gradient_calls_on_another_stream(dtype):
+    """On a stream of their own, with everything that the calls read and overwrite in order before them."""
+    n, tokens, cin, cout = 6, 64, 96, 200
+    desc = layer(n, tokens, cin, cout, dtype, bias=1)
+    gen = torch.Generator("cuda:0").manual_seed(6)
+    codes, scales, _ = checkpoint(torch.randn((n * tokens, cin), generator=gen, device="cuda:0").to(torch.bfloat16))
+    dy = torch.randn((n * tokens, cout), generator=gen, device="cuda:0").to(dtype)
+    lengths = torch.tensor([0, 1, 64, 33, 32, 17], dtype=torch.int32, device="cuda:0")
+    room = max(dp.dp_checkpoint_workspace_bytes(desc, use) for use in (dp.DP_WS_PER_EXAMPLE_GRAD, dp.DP_WS_RECOMPUTE))
+    results = []
+    for stream in (torch.cuda.current_stream(), torch.cuda.Stream()):
+        sq, acc, acc_b = torch.full((n,), -7.0, device="cuda:0"), torch.zeros((cout, cin), device="cuda:0"), torch.zeros(cout, device="cuda:0")
+        ws = torch.empty(room, dtype=torch.uint8, device="cuda:0")
+        torch.cuda.synchronize()
+        dp.dp_checkpoint_example_grad(desc, codes, scales, dy, None, None, sq, ws, lengths=lengths, stream=stream)
+        dp.dp_checkpoint_clip_accumulate(desc, codes, scales, dy, sq, 0.5, acc, acc_b, ws, lengths=lengths, stream=stream)
+        torch.cuda.synchronize()
+        results.append((sq, acc, acc_b))
+    assert all(torch.equal(a, b) for a, b in zip(*results)) and bool((results[0][0] >= 0.0).all())
