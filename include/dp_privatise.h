@@ -438,10 +438,12 @@ dp_status dp_checkpoint_read(const uint8_t *codes, const uint8_t *scales, size_t
  * lengths    [device] [n] int32 tokens of each example (taken as 0 .. tokens), or NULL: all of them.  What lies in later tokens of
  *            either operand is not used, whatever it is.  An example of no token has zero gradients and norm 0.
  * Products of bf16 dY are those of bf16 matrix instructions with fp32 sums and nothing is rounded in between; fp32 dY is split into three
- * bf16 numbers that add up to it (magnitudes below 2^127).  Norms alone of layers with few tokens go by way of Gram matrices (fp32 dY: fp32 products),
+ * bf16 numbers that add up to it (magnitudes below 2^127).  Norms alone of layers with few tokens may go by way of Gram matrices (fp32 dY: fp32
+ * products),
  *   |dW_i|^2 = sum_{t,u} (X_t . X_u)(dY_t . dY_u),
- * which lose digits where the sum over the tokens cancels (a norm below 2^-20 of what its terms add up to is not resolved, and can come out
- * negative: such an example is left out, dp_clip_factors); stored gradients give sums of squares always.
+ * which lose digits where the sum over the tokens cancels.  Where it is small against what its terms could add up to (below 2^-11, or (cin + cout) 2^-23, of
+ * (sum_t |X_t| |dY_t|)^2) the example's norm is made again as a sum of squares of its gradient; a sum that stands is off by a quarter at worst if
+ * every rounding errs one way, by 2^-12 at most as measured.  Stored gradients give sums of squares always.
  * Other arguments, errors: as dp_per_example_grad.  ws: dp_checkpoint_workspace_bytes(desc, DP_WS_PER_EXAMPLE_GRAD).               */
 size_t dp_checkpoint_workspace_bytes(const dp_layer_desc *desc /*[host]*/, int use /*dp_ws_use*/);
 dp_status dp_checkpoint_example_grad(const dp_layer_desc *desc /*[host]*/, const uint8_t *codes, const uint8_t *scales, const void *dy,

@@ -9,8 +9,8 @@ Per micro-step of `n` examples of up to `tokens` tokens:
 and per optimiser step dp_add_noise_finalize_flat with the SGD update.  The projections themselves and the products of attention are the
 framework's user's own matrix products, here torch's.
 
-An example's gradient is that of its checkpoints' values, for the norm and for the clipped sum alike, so that no more than clip_c of an
-example gets into the sum, whatever the checkpoints round away.
+An example's gradient is that of its checkpoints' values, for the norm and for the clipped sum alike, so that what the checkpoints round away does
+not matter to the bound: no more than clip_c of an example gets into the sum, to within the norms' own rounding (dp_checkpoint_example_grad).
 
 examples/private_attention.py trains one on synthetic data.
 """

@@ -634,18 +634,44 @@ __global__ void __launch_bounds__(256) ck_ranges_kernel(const float *part, size_
 // compute unit takes in, hence the tiles; where there are few pairs, several workgroups share a pair's features (splits) and
 // ck_gram_join_kernel adds up their sums before it multiplies.
 // fp32 dY: chunks of 64 features as they are, fp32 matrix instructions.  WORDS: as above.
-// ONE: every example has one pair (64 tokens at most): half the operands, the products above the diagonal once, those of tokens from the 32nd on
-// only where there are some, and three chunks on their way instead of one (32 x 64 tokens 768 -> 768:
-// 12.7 us and 11.3, twelve chunks of which each waits for the one before it; 400 of them 17.6 and 16.0).  55 x 2 tokens 1792 -> 576 fp32: 20 us a
-// call (by contraction 32).
+//
+// The terms have signs, and where they cancel the sum has lost its digits: tokens nearly alike whose dY add up to nothing (a key projection: a query's
+// gradients of its scores add up to zero) can come out as 0, or less.  By Cauchy's inequality the terms add up to at most
+//     B_i^2,   B_i = sum_t |dY_t| sqrt(|X_t|^2 + bias),
+// which the diagonals hold, and every rounding is in proportion to it: with F / 4 or O / 4 additions in a row to an entry, the sum is off by
+// (F + O) / 4 2^-23 B^2 if all err one way; 2^-23.9 B^2 is the most that was seen (2 to 500 tokens, 64 to 8192 features, tokens of their own to tokens all
+// alike).  A sum stands if it is at least ck_resolution() of B^2: then it is within a quarter at worst, and within 2^-12 as measured.  Tokens of no common
+// direction give B^2 / T.  The other examples' norms are made again from their gradients' values, on the device (ck_again_kernel).
 constexpr int GT = 64, GC = 128, G_ROW = 2 * GC + 16, G_SIDE = GT * G_ROW, G_STAGE = 2 * G_SIDE;      // tokens, features; bytes (16 of a row keep rows in different banks)
 constexpr int G_VALUES = GT * GT;
 
+// Whether value wave * 16 + q of lane `lane` is on the diagonal (of q's, one at most): four blocks of 32 x 32 one after the other, row
+// (q >> 2) * 8 + (q & 3) + 4 (lane / 32) and column lane % 32 of a block.
+__device__ __forceinline__ bool gram_diagonal(int wave, int q, int lane)
+{
+    return (wave == 0 || wave == 3) && (q >> 2) * 8 + (q & 3) + (lane >> 5) * 4 == (lane & 31);
+}
+
+// Sums of two values over a workgroup of NW waves, on thread 0.
+template <int NW>
+__device__ __forceinline__ float2 gram_sums(float v, float w, float (&red)[NW][2])
+{
+    v = wave_sum_last_lane(v);
+    w = wave_sum_last_lane(w);
+    if ((threadIdx.x & 63) == 63) { red[threadIdx.x >> 6][0] = v; red[threadIdx.x >> 6][1] = w; }
+    __syncthreads();
+    float2 s = make_float2(0.0f, 0.0f);
+#pragma unroll
+    for (int i = 0; i < NW; ++i) { s.x += red[i][0]; s.y += red[i][1]; }
+    return s;
+}
+
+// bounds: [n, tiles of 64 tokens] shares of B_i; arrived: ck_again_kernel's counters, cleared for it
 template <bool BF16, bool WORDS, bool ONE>
-__global__ void __launch_bounds__(256, 2) ck_gram_kernel(const CkDenseArgs a, int pairs, int splits, float *tiles)
+__global__ void __launch_bounds__(256, 2) ck_gram_kernel(const CkDenseArgs a, int pairs, int splits, float *tiles, float *bounds, unsigned *arrived)
 {
     extern __shared__ __attribute__((aligned(16))) char ck_lds[];
-    __shared__ float red[4];
+    __shared__ float red[4][2];
     const unsigned whole = blockIdx.x / (unsigned)splits;          // example and pair
     const int split = (int)(blockIdx.x - whole * (unsigned)splits), ex = (int)(whole / (unsigned)pairs);
     int pair = (int)(whole - (unsigned)ex * (unsigned)pairs), tile_a = 0;
@@ -655,8 +681,13 @@ __global__ void __launch_bounds__(256, 2) ck_gram_kernel(const CkDenseArgs a, in
     const bool diagonal = ONE || tile_a == tile_b;
     const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
     const int len = __builtin_amdgcn_readfirstlane(ck_length(a, ex));
+    if (t == 0 && pair == 0 && tile_a == 0 && split == 0) arrived[ex] = 0;
+    float *const bound = bounds + (size_t)ex * (unsigned)((a.tokens + GT - 1) / GT) + tile_a;
     if (tile_a * GT >= len) {                                      // (tile_b is not the larger one)
-        if (t == 0 && splits == 1) a.partials[whole] = 0.0f;
+        if (t == 0 && splits == 1) {
+            a.partials[whole] = 0.0f;
+            if (diagonal) *bound = 0.0f;
+        }
         return;
     }
     const size_t row0 = (size_t)ex * (unsigned)a.tokens;
@@ -844,22 +875,29 @@ __global__ void __launch_bounds__(256, 2) ck_gram_kernel(const CkDenseArgs a, in
         for (int q = 0; q < 16; ++q) { to[q * 64] = sx[q]; to[G_VALUES + q * 64] = sy[q]; }
         return;
     }
-    float ss = 0.0f;
+    float ss = 0.0f, own = 0.0f;
 #pragma unroll
-    for (int q = 0; q < 16; ++q) ss += (a.has_bias ? sx[q] + 1.0f : sx[q]) * sy[q];          // tokens that are not there: 0 dY . dY
+    for (int q = 0; q < 16; ++q) {
+        const float p = (a.has_bias ? sx[q] + 1.0f : sx[q]) * sy[q];        // tokens that are not there: 0 dY . dY
+        ss += p;
+        own = gram_diagonal(wave, q, lane) ? p : own;
+    }
     if (ONE && wave == 1) ss *= 2.0f;                              // a wave has one of the four blocks: block (0, 1), and (1, 0) is zeros
-    const float tot = block_sum<4>(ss, red);
-    if (t == 0) a.partials[whole] = diagonal ? tot : 2.0f * tot;
+    const float2 sums = gram_sums<4>(ss, sqrtf(own), red);
+    if (t == 0) {
+        a.partials[whole] = diagonal ? sums.x : 2.0f * sums.x;
+        if (diagonal) *bound = sums.y;
+    }
 }
 
 // The products of a pair of tiles whose features several workgroups shared: their sums in order, then value by value.
-__global__ void __launch_bounds__(512) ck_gram_join_kernel(const CkDenseArgs a, int pairs, int splits, const float *tiles)
+__global__ void __launch_bounds__(512) ck_gram_join_kernel(const CkDenseArgs a, int pairs, int splits, const float *tiles, float *bounds)
 {
-    __shared__ float red[8];
+    __shared__ float red[8][2];
     const int ex = (int)(blockIdx.x / (unsigned)pairs);
     int pair = (int)(blockIdx.x - (unsigned)ex * (unsigned)pairs), tile_a = 0;
     while (pair > tile_a) { ++tile_a; pair -= tile_a; }
-    float ss = 0.0f;
+    float ss = 0.0f, own = 0.0f;
     if (tile_a * GT < ck_length(a, ex)) {
         constexpr int values = G_VALUES;
         const float *p = tiles + (size_t)blockIdx.x * splits * 2 * values;
@@ -874,10 +912,151 @@ __global__ void __launch_bounds__(512) ck_gram_join_kernel(const CkDenseArgs a, 
             if (a.has_bias) { x.x += 1.0f; x.y += 1.0f; }
             const float twice = pairs == 1 && e / (G_VALUES / 4) == 1 ? 2.0f : 1.0f;          // block (0, 1), and (1, 0) is zeros
             ss += twice * (x.x * y.x + x.y * y.y);
+            const int wave = e >> 10, q = (e >> 6) & 15, lane = e & 63;
+            if (gram_diagonal(wave, q, lane)) own += sqrtf(x.x * y.x);
+            if (gram_diagonal(wave, q, lane + 1)) own += sqrtf(x.y * y.y);
         }
     }
-    const float tot = block_sum<8>(ss, red);
-    if (threadIdx.x == 0) a.partials[blockIdx.x] = tile_a == pair ? tot : 2.0f * tot;
+    const float2 sums = gram_sums<8>(ss, own, red);
+    if (threadIdx.x == 0) {
+        a.partials[blockIdx.x] = tile_a == pair ? sums.x : 2.0f * sums.x;
+        if (tile_a == pair) bounds[(size_t)ex * (unsigned)((a.tokens + GT - 1) / GT) + tile_a] = sums.y;
+    }
+}
+
+// What the pairs of tiles of the examples left.
+struct GramSums {
+    const float *values, *bounds;    // [n, pairs], [n, tiles of 64 tokens]
+    int pairs, tiles;
+    float resolution;
+    // example i's squared norm, and whether it stands (not: a NaN)
+    __device__ __forceinline__ bool stands(int i, float &norm) const
+    {
+        const float *v = values + (size_t)i * pairs, *b = bounds + (size_t)i * tiles;
+        float sum = 0.0f, bound = 0.0f;
+#pragma unroll 4
+        for (int k = 0; k < pairs; ++k) sum += v[k];
+#pragma unroll 4
+        for (int k = 0; k < tiles; ++k) bound += b[k];
+        norm = sum;
+        return sum >= resolution * bound * bound;
+    }
+};
+
+// Squared norms of the examples whose sums do not stand, from their gradients' values, dW_i and db_i as one product with a further feature of X that
+// is 1.  `sharers` workgroups take an example's tiles of 64 x 64 in turn, a wave 32 x 32 of one, chunks of 32 tokens through LDS as [feature][token]; the
+// last one to arrive adds up what they leave, in order.  Every workgroup walks over all examples, as many of them at once as fill the chip; the
+// first one writes the norms that stand.  Small and with few registers, so that it costs little where there is nothing to do: 3.8 us of a launch
+// (the contraction in its place: 20, for its registers in a loop).   Where all fall: 16 examples of 64 tokens 4096 -> 4096
+// 528 us, the contraction 57; 512 of 8 tokens 768 -> 768 303 and 49.
+constexpr int AGAIN = 64, AGAIN_TOKENS = 32, AGAIN_ROW = AGAIN_TOKENS * 2 + 16;        // features of a tile, tokens of a chunk; bytes (16 more: banks, alignment)
+
+template <bool BF16>
+__global__ void __launch_bounds__(256) ck_again_kernel(const CkDenseArgs a, const GramSums g, int sharers, unsigned *arrived, float *sqnorm)
+{
+    typedef typename In<BF16>::type E;
+    constexpr int PLANES = BF16 ? 1 : 3;
+    __shared__ __attribute__((aligned(16))) char xs[AGAIN * AGAIN_ROW], ys[PLANES][AGAIN * AGAIN_ROW];
+    __shared__ uint32_t fallen[8];
+    __shared__ float red[4];
+    __shared__ unsigned before;
+    const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
+    const unsigned at_once = gridDim.x / (unsigned)sharers, mine = blockIdx.x / (unsigned)sharers;
+    const int sharer = (int)(blockIdx.x - mine * (unsigned)sharers);
+    const int features = a.cin + a.has_bias, s_pitch = a.pitch / CK_BLOCK;
+
+    auto squares = [&](int ex, int tile_o, int tile_k) {           // of a tile's values, this lane's share
+        const int o0 = tile_o * AGAIN, k0 = tile_k * AGAIN, len = ck_length(a, ex);
+        const size_t row0 = (size_t)ex * (unsigned)a.tokens;
+        f32x16 acc;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) acc[r] = 0.0f;
+        for (int c = 0; c < len; c += AGAIN_TOKENS) {
+            __syncthreads();
+#pragma unroll
+            for (int u = 0; u < AGAIN_TOKENS / 16; ++u) {          // token (t / 16) + 16 u, features 4 (t % 16) .. of either operand
+                const int token = (t >> 4) + 16 * u, f = 4 * (t & 15), k = k0 + f, o = o0 + f;
+                const bool there = c + token < len;
+                const size_t row = row0 + (unsigned)(c + token);
+                uint2 x = make_uint2(0, 0);
+                if (there && k < a.pitch)
+                    x = ck_bf16(*reinterpret_cast<const uint32_t *>(a.codes + row * (unsigned)a.pitch + k), pow2_of(a.scales[row * (unsigned)s_pitch + k / CK_BLOCK]));
+                uint16_t xv[4] = {(uint16_t)x.x, (uint16_t)(x.x >> 16), (uint16_t)x.y, (uint16_t)(x.y >> 16)};
+                char *to = xs + f * AGAIN_ROW + token * 2;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    if (k + i == a.cin && a.has_bias) xv[i] = there ? 0x3F80 : 0;
+                    *reinterpret_cast<uint16_t *>(to + i * AGAIN_ROW) = xv[i];
+                }
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    E v = 0;
+                    if (there && o + i < a.cout) v = static_cast<const E *>(a.dy)[row * (unsigned)a.cout + o + i];
+                    to = &ys[0][(f + i) * AGAIN_ROW + token * 2];
+                    if constexpr (BF16) {
+                        *reinterpret_cast<uint16_t *>(to) = v;
+                    } else {
+                        float rest = v;
+#pragma unroll
+                        for (int q = 0; q < 3; ++q) {              // (split8)
+                            const uint32_t w = pack_bf16(rest, 0.0f);
+                            rest -= __uint_as_float(w << 16);
+                            *reinterpret_cast<uint16_t *>(to + q * AGAIN * AGAIN_ROW) = (uint16_t)w;
+                        }
+                    }
+                }
+            }
+            __syncthreads();
+#pragma unroll
+            for (int ks = 0; ks < AGAIN_TOKENS / 16; ++ks) {
+                const int in_row = (lane & 31) * AGAIN_ROW + (lane >> 5) * 16 + ks * 32;
+                const bf16x8 b = __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4 *>(xs + (wave & 1) * 32 * AGAIN_ROW + in_row));
+#pragma unroll
+                for (int q = 0; q < PLANES; ++q) {
+                    const bf16x8 y = __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4 *>(&ys[q][(wave >> 1) * 32 * AGAIN_ROW + in_row]));
+                    acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(y, b, acc, 0, 0, 0);
+                }
+            }
+        }
+        float ss = 0.0f;                                           // (features beyond the last are zeros)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) ss = fmaf(acc[r], acc[r], ss);
+        return ss;
+    };
+
+    unsigned turn = 0;
+    for (int first = 0; first < a.n; first += 256) {
+        const int i = first + t;
+        float norm = 0.0f;
+        const bool stands = i >= a.n || g.stands(i, norm);
+        if (blockIdx.x == 0 && stands && i < a.n) sqnorm[i] = norm;
+        const unsigned long long those = __ballot(!stands);
+        __syncthreads();                                           // (the last ones have been read)
+        if (lane == 0) {
+            fallen[2 * wave] = (uint32_t)those;
+            fallen[2 * wave + 1] = (uint32_t)(those >> 32);
+        }
+        __syncthreads();
+        for (int w = 0; w < 8; ++w)
+            for (uint32_t left = (uint32_t)__builtin_amdgcn_readfirstlane((int)fallen[w]); left; left &= left - 1) {
+                if (turn++ % at_once != mine) continue;
+                const int ex = first + 32 * w + __builtin_ctz(left), tiles_k = (features + AGAIN - 1) / AGAIN, tiles = (a.cout + AGAIN - 1) / AGAIN * tiles_k;
+                float ss = 0.0f;
+                for (int tile = sharer; tile < tiles; tile += sharers) ss += squares(ex, tile / tiles_k, tile % tiles_k);
+                const float tot = block_sum<4>(ss, red);
+                float *const part = a.partials + (size_t)ex * sharers;
+                if (t == 0) {
+                    __hip_atomic_store(part + sharer, tot, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                    before = __hip_atomic_fetch_add(arrived + ex, 1u, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT);
+                }
+                __syncthreads();
+                if (before + 1 == (unsigned)sharers) {             // all of them are there
+                    const float v = t < sharers ? __hip_atomic_load(part + t, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) : 0.0f;
+                    const float sum = block_sum<4>(v, red);
+                    if (t == 0) sqnorm[ex] = sum;
+                }
+            }
+    }
 }
 
 // ---- plans --------------------------------------------------------------------------------
@@ -886,6 +1065,7 @@ struct CkPlan {
     bool gram;
     int gram_splits;                 // workgroups that share a pair's features
     size_t per_example;              // partial squared norms
+    int sharers;                     // workgroups of an example whose norm is made again
     int nj;                          // the contraction's tiles are 64 nj wide
     int ranges, chunks;              // weighted
     bool rows;
@@ -893,18 +1073,22 @@ struct CkPlan {
 
 int ck_tiles(int v, int width) { return (v + width - 1) / width; }
 
-// Which of the two forms of norms: what they take, in microseconds, fitted to (n, T, F, O: Gram form / contraction) 32, 64, 768, 768: 12.4 / 11.4;
-// 8, 128, 2048, 2048: 21.7 / 19.5; 8, 512, 2048, 2048: 52 / 43; 16, 64, 4096, 4096: 20 / 68; 16, 128, 4096, 4096: 28 / 98; 16, 256, 4096, 4096: 50 / 155.
-// 512 workgroups of either kind fill the chip; a small launch afterwards is 4.
-// (fp32 dY, three products for one: chunks of 32 in 1.1.)
+// What a sum of the Gram form has to be of its bound (ck_gram_kernel).
+float ck_resolution(const Geo &g) { return std::max(0x1p-11f, (float)(g.cin + g.cout) * 0x1p-23f); }
+
+// Which of the two forms of norms: what they take, in microseconds a call.  bf16 (n, T, F, O: Gram form / contraction): 32, 64, 768, 768 15.0 / 9.9, with a
+// bias 15.1 / 9.8; 400, 64, 768, 768 21.0 / 50.9; 8, 128, 2048, 2048 22.5 / 14.3; 16, 64, 2048, 2048 18.9 / 17.4; 64, 16, 2048, 2048 21.2 / 43.4;
+// 8, 512, 2048, 2048 50.3 / 36.2; 16, 64, 4096, 4096 22.3 / 56.6; 16, 128, 4096, 4096 28.9 / 79.3; 16, 256, 4096, 4096 48.6 / 137.  fp32: 32, 64, 768, 768 21.6 / 14.8;
+// 16, 64, 2048, 2048 24.6 / 36.2; 55, 2, 1792, 576 20.3 / 24.8; 16, 256, 4096, 4096 90.4 / 396.  512 workgroups of either kind fill the chip.
 double gram_us(const Geo &g, double pairs, int splits, double chunks)
 {
     const double groups = g.n * pairs * splits;
-    return 5.0 + std::max(1.0, groups / 512.0) * chunks / splits * (pairs > 1.0 ? 1.4 : 0.6) + (splits > 1 ? 4.0 + groups / 128.0 : 0.0) + (pairs > 1.0 ? 4.0 : 0.0);
+    const double chunk_us = pairs > 1.0 ? (g.bf16 ? 1.4 : 2.3) : groups <= 256.0 ? (g.bf16 ? 0.55 : g.h <= 32 ? 0.5 : 0.8) : (g.bf16 ? 1.0 : 1.65);
+    return (pairs > 1.0 ? 9.0 : 10.0) + std::max(1.0, groups / 512.0) * chunk_us * chunks / splits + (splits > 1 ? 4.5 + groups / 85.0 : 0.0);
 }
 double contract_us(const Geo &g, double tiles, int chunk)
 {
-    return 4.0 + std::max(1.0, g.n * tiles / 512.0) * (1.8 + (g.bf16 ? 0.95 : 1.1) * ((g.h + chunk - 1) / chunk)) + (tiles > 1.0 ? 4.0 : 0.0);
+    return 5.5 + std::max(1.0, g.n * tiles / 512.0) * ((g.bf16 ? 1.5 : 1.15) + (g.bf16 ? 0.85 : 1.37) * ((g.h + chunk - 1) / chunk));
 }
 
 CkPlan ck_plan(const Geo &g, int mode)
@@ -939,9 +1123,14 @@ CkPlan ck_plan(const Geo &g, int mode)
         const int yc = g.bf16 ? GC : GC / 2;
         const long long tiles = (g.h + GT - 1) / GT, pairs = tiles * (tiles + 1) / 2, chunks = (ck_pitch(g.cin) + GC - 1) / GC + (g.cout + yc - 1) / yc;
         p.gram_splits = (int)std::max(1ll, std::min({512 / (g.n * pairs), chunks / 8, 16ll}));
-        p.gram = g.n * pairs < (1ll << 30) &&
+        // (tokens of no common direction have a sum of 1 / T of its bound: they stand with room for four times less)
+        p.gram = g.n * pairs < (1ll << 30) && (double)g.h * ck_resolution(g) <= 0.25 &&
                  gram_us(g, (double)pairs, p.gram_splits, (double)chunks) < contract_us(g, (double)p.per_example, ck_chunk(g.bf16 ? 1 : 3, p.nj));
-        if (p.gram) p.per_example = (size_t)pairs;
+        if (p.gram) {
+            p.per_example = (size_t)pairs;
+            // (an example's workgroups meet on a counter, as long as a few tiles take: 16 tiles or more to each)
+            p.sharers = (int)std::min(256ll, ((long long)ck_tiles(g.cin + g.has_bias, AGAIN) * ck_tiles(g.cout, AGAIN) + 15) / 16);
+        }
     }
     return p;
 }
@@ -960,10 +1149,18 @@ size_t align4(size_t v) { return (v + 3) & ~(size_t)3; }
 
 }  // namespace
 
-// What the workgroups that share a pair's features leave, behind the partial squared norms.
-static size_t gram_tile_bytes(const Geo &g, const CkPlan &p)
+// Places in the workspace of norms by the Gram form, one after the other.
+struct GramRoom { size_t bounds, partials, arrived, tiles, bytes; };
+static GramRoom gram_room(const Geo &g, const CkPlan &p)
 {
-    return p.gram && p.gram_splits > 1 ? (size_t)g.n * p.per_example * p.gram_splits * 2 * G_VALUES * 4 : 0;
+    const size_t n = (size_t)g.n;
+    GramRoom r;
+    r.bounds = align16(4 * n * p.per_example);                     // behind the pairs' sums
+    r.partials = r.bounds + align16(4 * n * ((g.h + GT - 1) / GT));
+    r.arrived = r.partials + align16(4 * n * p.sharers);
+    r.tiles = r.arrived + align16(4 * n);
+    r.bytes = r.tiles + (p.gram_splits > 1 ? n * p.per_example * p.gram_splits * 2 * G_VALUES * 4 : 0);
+    return r;
 }
 
 // A weighted call goes in launches of CK_TABLE examples and one of those that are left, which plan their own ranges; ranges do not grow
@@ -983,18 +1180,41 @@ static size_t weighted_ws_bytes(const Geo &g)
 size_t checkpoint_ws_bytes(const Geo &g, int mode)
 {
     if (mode == MODE_WEIGHTED) return weighted_ws_bytes(g);
-    const CkPlan p = ck_plan(g, mode);
     // both per-example forms: a caller sizes its workspace once
-    const CkPlan q = ck_plan(g, mode == MODE_NORM ? MODE_MATERIALISE : MODE_NORM);
-    return align16(4 * (size_t)g.n * std::max(p.per_example, q.per_example)) + std::max(gram_tile_bytes(g, p), gram_tile_bytes(g, q));
+    const CkPlan p = ck_plan(g, MODE_NORM), q = ck_plan(g, MODE_MATERIALISE);
+    return std::max(align16(4 * (size_t)g.n * q.per_example), p.gram ? gram_room(g, p).bytes : 0);
 }
 
 template <bool ONE>
-static dp_status run_gram(bool bf16, bool words, dim3 grid, const CkDenseArgs &a, int pairs, int splits, float *tiles, hipStream_t s)
+static dp_status run_gram(bool bf16, bool words, dim3 grid, const CkDenseArgs &a, int pairs, int splits, float *tiles, float *bounds, unsigned *arrived,
+                          hipStream_t s)
 {
-    if (!bf16) return launch_lds<ck_gram_kernel<false, true, ONE>>(grid, 256, 2 * G_STAGE, s, a, pairs, splits, tiles);
-    if (!words) return launch_lds<ck_gram_kernel<true, false, ONE>>(grid, 256, 2 * G_STAGE, s, a, pairs, splits, tiles);
-    return launch_lds<ck_gram_kernel<true, true, ONE>>(grid, 256, 2 * G_STAGE, s, a, pairs, splits, tiles);
+    if (!bf16) return launch_lds<ck_gram_kernel<false, true, ONE>>(grid, 256, 2 * G_STAGE, s, a, pairs, splits, tiles, bounds, arrived);
+    if (!words) return launch_lds<ck_gram_kernel<true, false, ONE>>(grid, 256, 2 * G_STAGE, s, a, pairs, splits, tiles, bounds, arrived);
+    return launch_lds<ck_gram_kernel<true, true, ONE>>(grid, 256, 2 * G_STAGE, s, a, pairs, splits, tiles, bounds, arrived);
+}
+
+static dp_status launch_gram(const Geo &g, const CkPlan &p, CkDenseArgs a, bool words, float *sqnorm, void *ws, hipStream_t s)
+{
+    const GramRoom room = gram_room(g, p);
+    char *const base = static_cast<char *>(ws);
+    float *const values = reinterpret_cast<float *>(base), *const bounds = reinterpret_cast<float *>(base + room.bounds);
+    float *const tiles = reinterpret_cast<float *>(base + room.tiles);
+    unsigned *const arrived = reinterpret_cast<unsigned *>(base + room.arrived);
+    const int pairs = (int)p.per_example;
+    const dim3 joins((unsigned)(g.n * p.per_example)), blocks(joins.x * (unsigned)p.gram_splits);
+    a.partials = values;
+    profile_begin(s);
+    dp_status st = pairs == 1 ? run_gram<true>(g.bf16, words, blocks, a, pairs, p.gram_splits, tiles, bounds, arrived, s)
+                              : run_gram<false>(g.bf16, words, blocks, a, pairs, p.gram_splits, tiles, bounds, arrived, s);
+    if (st == DP_OK && p.gram_splits > 1) st = launch_lds<ck_gram_join_kernel>(joins, 512, 0, s, a, pairs, p.gram_splits, tiles, bounds);
+    profile_end(s);
+    if (st != DP_OK) return st;
+    const GramSums sums = {values, bounds, pairs, (g.h + GT - 1) / GT, ck_resolution(g)};
+    a.partials = reinterpret_cast<float *>(base + room.partials);
+    const dim3 again((unsigned)(p.sharers * std::min(std::max(512 / p.sharers, 1), g.n)));
+    return g.bf16 ? launch_lds<ck_again_kernel<true>>(again, 256, 0, s, a, sums, p.sharers, arrived, sqnorm)
+                  : launch_lds<ck_again_kernel<false>>(again, 256, 0, s, a, sums, p.sharers, arrived, sqnorm);
 }
 
 static dp_status launch_weighted(const Geo &g, CkDenseArgs a, float *out_w, float *out_b, void *ws, hipStream_t s)
@@ -1052,6 +1272,7 @@ dp_status launch_checkpoint_dense(const Geo &g, int mode, const uint8_t *codes, 
     }
     a.tiles_k = ck_tiles(g.cin, 64 * p.nj); a.columns = a.tiles_k + g.has_bias;
     const bool words = !g.bf16 || g.cout % 2 == 0;
+    if (p.gram) return launch_gram(g, p, a, words, sqnorm, ws, s);
     // workgroups of all XCDs alike (the kernel's map), those beyond the last one end at once
     const dim3 grid((unsigned)(((size_t)a.tiles_o * a.columns * g.n + 7) / 8 * 8));
     dp_status st;
@@ -1063,14 +1284,7 @@ dp_status launch_checkpoint_dense(const Geo &g, int mode, const uint8_t *codes, 
     a.stride_b = out_stride ? out_stride : g.pb;
     a.slots = g.n;
     profile_begin(s);
-    if (p.gram) {
-        const int pairs = (int)p.per_example;
-        const dim3 joins((unsigned)(g.n * p.per_example)), blocks(joins.x * (unsigned)p.gram_splits);
-        float *tiles = reinterpret_cast<float *>(static_cast<char *>(ws) + align16(4 * (size_t)g.n * p.per_example));
-        st = pairs == 1 ? run_gram<true>(g.bf16, words, blocks, a, pairs, p.gram_splits, tiles, s)
-                        : run_gram<false>(g.bf16, words, blocks, a, pairs, p.gram_splits, tiles, s);
-        if (st == DP_OK && p.gram_splits > 1) st = launch_lds<ck_gram_join_kernel>(joins, 512, 0, s, a, pairs, p.gram_splits, tiles);
-    } else if (g.bf16) {
+    if (g.bf16) {
         st = p.nj == 4 ? run_contract<1, 4, false, true>(words, grid, a, s) : run_contract<1, 2, false, true>(words, grid, a, s);
     } else {
         st = run_contract<3, 2, false, false>(words, grid, a, s);

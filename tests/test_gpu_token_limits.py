@@ -172,3 +172,136 @@ def test_gradient_calls_on_another_stream(dtype):
         torch.cuda.synchronize()
         results.append((sq, acc, acc_b))
     assert all(torch.equal(a, b) for a, b in zip(*results)) and bool((results[0][0] >= 0.0).all())
+
+
+def squared_norms(desc, codes, scales, dy, lengths=None):
+    need = dp.dp_checkpoint_workspace_bytes(desc)
+    ws = torch.full((need + 64,), 0xA5, dtype=torch.uint8, device="cuda:0")
+    sq = torch.full((desc.n + 1,), -7.0, device="cuda:0")
+    dp.dp_checkpoint_example_grad(desc, codes, scales, dy, None, None, sq, ws, lengths=lengths, ws_bytes=need)
+    assert bool((ws[need:] == 0xA5).all()) and float(sq[desc.n]) == -7.0
+    return sq[:desc.n].double()
+
+
+# few tokens of wide layers: norms by Gram matrices, some with features shared between workgroups, of one tile of tokens and of several; and small layers
+CANCELLING = [(20, 64, 2048, 2048, 0), (32, 64, 768, 768, 1), (12, 33, 1500, 1501, 1), (24, 16, 2048, 1030, 0), (300, 2, 1792, 576, 1), (6, 200, 2100, 2050, 0),
+              (3, 130, 4096, 4096, 1), (64, 32, 64, 64, 0), (700, 10, 520, 300, 1), (40, 33, 2048, 2049, 1), (10, 200, 4096, 4100, 1), (12, 64, 4096, 4096, 0)]
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("case", CANCELLING, ids=str)
+def test_norms_of_gradients_that_cancel(case, dtype):
+    """Tokens nearly alike, whose gradients add up to nothing, as a key projection's do: the weight gradient is far smaller than its terms.  Its norm is
+    what the contraction makes of it, or a sum over pairs of tokens that has not lost more than a quarter; never below zero and never zero."""
+    n, tokens, cin, cout, bias = case
+    desc = layer(n, tokens, cin, cout, dtype, bias)
+    gen = torch.Generator("cuda:0").manual_seed(n)
+    x = torch.randn((n, 1, cin), generator=gen, device="cuda:0") * 4.0
+    spread = 2.0 ** -(torch.arange(n, device="cuda:0") % 7 * 2.0)            # from tokens of their own to tokens all alike
+    x = x + spread[:, None, None] * torch.randn((n, tokens, cin), generator=gen, device="cuda:0")
+    codes, scales, x = checkpoint(x.reshape(n * tokens, cin).to(torch.bfloat16))
+    dy = torch.randn((n, tokens, cout), generator=gen, device="cuda:0").to(torch.bfloat16)
+    lengths = torch.full((n,), tokens, dtype=torch.int32, device="cuda:0")
+    lengths[n // 2] = 0
+    if tokens > 3:
+        lengths[n // 3] = tokens // 2 * 2 - 2
+    dy[:, 1::2] = -dy[:, 0:tokens // 2 * 2:2]                                # opposite pairs
+    if tokens % 2:
+        dy[:, -1] = 0.0
+    odd = torch.arange(n, device="cuda:0") % 7 == 5                          # and some that do not cancel
+    dy[odd] = torch.randn((int(odd.sum()), tokens, cout), generator=gen, device="cuda:0").to(torch.bfloat16)
+    there = torch.arange(tokens, device="cuda:0")[None] < lengths[:, None]
+    got = squared_norms(desc, codes, scales, torch.where(there[..., None], dy, math.nan).to(dtype), lengths)
+    g, x = dy.double() * there[..., None], x.view(n, tokens, cin)
+    planes = 1 if dtype == torch.bfloat16 else 3
+    for i in range(n):
+        w = g[i].t() @ x[i]
+        off = (planes * tokens + 2) * U * (g[i].abs().t() @ x[i].abs())
+        b, off_b = g[i].sum(0) * bias, (tokens + 2) * U * g[i].abs().sum(0) * bias
+        want = float((w ** 2).sum() + (b ** 2).sum())
+        far = float((2 * w.abs() * off + off ** 2).sum() + (2 * b.abs() * off_b + off_b ** 2).sum()) + 256 * U * want
+        terms = float(((g[i].abs() @ g[i].abs().t()) * (x[i].abs() @ x[i].abs().t() + bias)).sum())
+        gram = min((cin + cout + 256) * U * terms, want / 3)
+        assert abs(float(got[i]) - want) <= max(far, gram), (i, float(got[i]), want)
+        assert float(got[i]) >= 0.0 and (want <= far or float(got[i]) > 0.0), (i, float(got[i]), want)
+
+
+def test_norms_that_are_not_numbers_and_their_neighbours():
+    """A NaN or infinity in an example's operands: its squared norm is not a number that a factor above 0 comes from; the others are theirs."""
+    n, tokens, cin, cout = 20, 64, 2048, 2048
+    desc = layer(n, tokens, cin, cout)
+    gen = torch.Generator("cuda:0").manual_seed(8)
+    x = torch.randn((n * tokens, cin), generator=gen, device="cuda:0").to(torch.bfloat16)
+    dy = torch.randn((n, tokens, cout), generator=gen, device="cuda:0").to(torch.bfloat16)
+    clean = squared_norms(desc, *checkpoint(x)[:2], dy)
+    x.view(n, tokens, cin)[3, 5, 7] = math.nan
+    dy[5, 0, 0] = math.nan
+    dy[7, 63, 2047] = math.inf
+    dy[9] *= 1e30                                    # squares beyond fp32
+    codes, scales, _ = checkpoint(x)
+    got = squared_norms(desc, codes, scales, dy)
+    factors = torch.empty(n, device="cuda:0")
+    dp.dp_clip_factors(got.float(), 1.0, n, factors)
+    broken = torch.zeros(n, dtype=torch.bool, device="cuda:0")
+    broken[[3, 5, 7, 9]] = True
+    assert bool((factors[broken] == 0.0).all())
+    assert torch.equal(got[~broken], clean[~broken]) and bool((clean > 0.0).all())
+
+
+@pytest.mark.parametrize("width,tokens,n", [(64, 32, 64), (2048, 64, 16)])
+def test_share_of_an_example_whose_tokens_are_nearly_alike(width, tokens, n):
+    """The attention block on such inputs: the key projection's gradient cancels, the block's norm does not lose it, and no example's share of the
+    clipped sum passes the bound."""
+    block = dp.PrivateAttention(n, tokens, width, heads=4, clip_c=1e-4, sigma=0.0, total_batch=n, device="cuda:0")
+    gen = torch.Generator("cuda:0").manual_seed(9)
+    x = torch.randn((n, 1, width), generator=gen, device="cuda:0") * 3 + 2.0 ** -6 * torch.randn((n, tokens, width), generator=gen, device="cuda:0")
+    block.forward(x.to(torch.bfloat16).contiguous())
+    block.backward(torch.randn((n, tokens, width), generator=gen, device="cuda:0").to(torch.bfloat16))
+    values = []
+    for codes, scales in (block.inputs, block.mixed):
+        back = torch.empty((n * tokens, width), dtype=torch.float32, device="cuda:0")
+        dp.dp_checkpoint_read(codes, scales, back)
+        values.append(back.double().view(n, tokens, width))
+    for i in range(n):
+        squares = [float(((g[i].double().t() @ values[0 if k < 3 else 1][i]) ** 2).sum()) for k, g in enumerate(block.grads)]
+        total = sum(squares) + float((block.g_table[i].double() ** 2).sum())
+        f = min(1.0, block.clip_c / math.sqrt(float(block.total_sqnorm[i])))
+        assert f * math.sqrt(total) <= block.clip_c * (1.0 + 2.0 ** -9), (i, f * math.sqrt(total))
+        for k in range(4):
+            assert float(block.sqnorm[k, i]) >= squares[k] * (1.0 - 2.0 ** -8), (i, k)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_recorded_norms_of_gradients_that_cancel(dtype):
+    """Replays with other examples cancelling each time give the eager results."""
+    n, tokens, cin, cout = 20, 64, 2048, 2048
+    desc = layer(n, tokens, cin, cout, dtype)
+    gen = torch.Generator("cuda:0").manual_seed(10)
+    codes, scales, _ = checkpoint((torch.randn((n, 1, cin), generator=gen, device="cuda:0") + 2.0 ** -5 * torch.randn((n, tokens, cin), generator=gen, device="cuda:0"))
+                                  .reshape(n * tokens, cin).to(torch.bfloat16))
+    dy, sq = torch.empty((n, tokens, cout), dtype=dtype, device="cuda:0"), torch.empty(n, device="cuda:0")
+    ws = torch.empty(dp.dp_checkpoint_workspace_bytes(desc), dtype=torch.uint8, device="cuda:0")
+
+    def fresh(seed):
+        gen = torch.Generator("cuda:0").manual_seed(seed)
+        dy.copy_(torch.randn(dy.shape, generator=gen, device="cuda:0"))
+        some = torch.rand(n, generator=gen, device="cuda:0") < 0.5
+        dy[some, 1::2] = -dy[some, 0::2]
+
+    def call():
+        dp.dp_checkpoint_example_grad(desc, codes, scales, dy, None, None, sq, ws)
+    fresh(0)
+    call()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call()
+    for seed in range(1, 6):
+        fresh(seed)
+        call()
+        torch.cuda.synchronize()
+        eager = sq.clone()
+        sq.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(eager, sq) and bool((sq > 0.0).all())
