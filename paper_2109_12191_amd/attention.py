@@ -12,6 +12,9 @@ framework's user's own matrix products, here torch's.
 An example's gradient is that of its checkpoints' values, for the norm and for the clipped sum alike, so that what the checkpoints round away does
 not matter to the bound: no more than clip_c of an example gets into the sum, to within the norms' own rounding (dp_checkpoint_example_grad).
 
+forward's result carries a graph where its input requires a gradient: autograd's pass over it is `backward`, with the clipped sums of the weights that
+belong to it, and gives the input's gradient.  Elsewhere `backward` is called.  The block holds the values of one forward pass, for one such pass back.
+
 examples/private_attention.py trains one on synthetic data.
 """
 from __future__ import annotations
@@ -19,6 +22,23 @@ from __future__ import annotations
 import torch
 
 from . import binding as B
+
+
+class _Recorded(torch.autograd.Function):
+    """A forward pass that autograd knows of as a whole: its own products and softmax are not for it to see one by one."""
+
+    @staticmethod
+    def forward(ctx, x, block, lengths):
+        y = block._forward(x, lengths)
+        ctx.block, ctx.passes = block, block.passes
+        return y
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dy):
+        if ctx.block.passes != ctx.passes:
+            raise RuntimeError("the block no longer holds this forward pass: there was another one, or a pass back over it")
+        return ctx.block.backward(dy), None, None
 
 
 class PrivateAttention:
@@ -59,6 +79,7 @@ class PrivateAttention:
         self.g_table = torch.zeros((n, (buckets * heads + 3) // 4 * 4), **f32)
         self.sqnorm, self.total_sqnorm = torch.empty((5, n), **f32), torch.empty(n, **f32)
         self.one_group = torch.zeros(5, dtype=torch.int32, device=device)
+        self.passes = 0                                   # forward and back
         self._round()
 
     def _round(self):
@@ -84,6 +105,13 @@ class PrivateAttention:
         """x [n, tokens, width] bf16 -> what the block makes of it, alike."""
         self._want("x", x, (self.n, self.tokens, self.width))
         self._want_lengths(lengths)
+        if x.requires_grad and torch.is_grad_enabled():
+            return _Recorded.apply(x, self, lengths)
+        with torch.no_grad():
+            return self._forward(x, lengths)
+
+    def _forward(self, x, lengths):
+        self.passes += 1
         self.lengths = lengths
         B.dp_checkpoint_write(x, *self.inputs)
         self.q, self.k, self.v = (self._heads(part) for part in (x @ self.qkv_weight.t()).chunk(3, dim=-1))
@@ -94,9 +122,10 @@ class PrivateAttention:
         B.dp_checkpoint_write(mixed, *self.mixed)
         return mixed @ self.o_weight.t()
 
+    @torch.no_grad()
     def attend_last(self, q, k, v, lengths=None):
         """One token an example against a cache: q [n, width], k and v [n, heads, tokens, head], `lengths` keys of which are there, the query's
-        own the last -> [n, width]."""
+        own the last -> [n, width].  For serving: the result carries no graph."""
         self._want("q", q, (self.n, self.width))
         for name, t in (("k", k), ("v", v)):
             self._want(name, t, (self.n, self.heads, self.tokens, self.head))
@@ -106,11 +135,13 @@ class PrivateAttention:
         B.dp_bias_softmax(self.last, scores, self.weights[4], probs, None, lengths)
         return self._tokens(probs @ v).view(self.n, self.width) @ self.o_weight.t()
 
+    @torch.no_grad()
     def backward(self, dy):
         """Gradient of forward's result, per example (of a sum over examples, not of a mean) -> gradient of its input; the clipped gradients of
         the weights go into the accumulator."""
         dy = dy.contiguous()
         self._want("dy", dy, (self.n, self.tokens, self.width))
+        self.passes += 1
         dmixed = self._heads(dy @ self.o_weight)
         self.dprobs = dmixed @ self.v.transpose(2, 3).contiguous()
         dv = self.probs.transpose(2, 3).contiguous() @ dmixed
