@@ -87,9 +87,11 @@ class PrivateAttention:
         self.o_weight = self.weights[3].to(torch.bfloat16)
 
     def _want(self, name, t, shape, dtype=torch.bfloat16):
-        """The calls below take addresses: what is behind them has to be what the descriptors say."""
-        if tuple(t.shape) != shape or t.dtype is not dtype or t.device.type != self.theta.device.type or not t.is_contiguous():
+        """The calls below take addresses, on the current device: what is behind them has to be what the descriptors say, and there."""
+        if tuple(t.shape) != shape or t.dtype is not dtype or t.device != self.theta.device or not t.is_contiguous():
             raise ValueError(f"{name} must be contiguous {dtype} {list(shape)} on {self.theta.device}, not {t.dtype} {list(t.shape)} on {t.device}")
+        if t.device.type == "cuda" and t.device.index != torch.cuda.current_device():
+            raise ValueError(f"the block is on {self.theta.device}, the current device is {torch.cuda.current_device()}")
 
     def _want_lengths(self, lengths):
         if lengths is not None:

@@ -2,6 +2,7 @@
 import os
 
 import pytest
+import torch
 
 import paper_2109_12191_amd as dp
 
@@ -27,3 +28,31 @@ def test_workspace_of_a_clipped_sum_holds_every_part_of_it(tokens, cin, cout, bi
     alone = {rest: _need(rest, tokens, cin, cout, bias) for rest in range(1, 1024)}
     for n in list(range(1025, 2048)) + [2049, 3000, 5000, 65535]:
         assert _need(n, tokens, cin, cout, bias) >= max(whole, alone.get(n % 1024, 0)), n
+
+
+def test_attention_block_refuses_tensors_of_another_device(monkeypatch):
+    """The calls take addresses: a tensor of another GPU, or a block on another than the current one, is refused before any of them."""
+    block = dp.PrivateAttention(2, 4, 32, 4, clip_c=1.0, sigma=1.0, total_batch=2, device="cpu")
+
+    class Elsewhere:
+        """What the checks look at."""
+        def __init__(self, shape, device, dtype=torch.bfloat16):
+            self.shape, self.device, self.dtype = shape, torch.device(device), dtype
+
+        def is_contiguous(self):
+            return True
+
+        def contiguous(self):
+            return self
+    block.theta = Elsewhere((4,), "cuda:0", torch.float32)
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    for call in (block.forward, block.backward):
+        with pytest.raises(ValueError, match="cuda:1"):
+            call(Elsewhere((2, 4, 32), "cuda:1"))
+    with pytest.raises(ValueError, match="cuda:1"):
+        block.forward(Elsewhere((2, 4, 32), "cuda:0"), Elsewhere((2,), "cuda:1", torch.int32))
+    with pytest.raises(ValueError, match="cpu"):
+        block.forward(torch.zeros((2, 4, 32), dtype=torch.bfloat16))
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 1)
+    with pytest.raises(ValueError, match="current device is 1"):
+        block.forward(Elsewhere((2, 4, 32), "cuda:0"))
