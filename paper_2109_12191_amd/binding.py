@@ -432,6 +432,16 @@ def dp_philox_raw(raw, p: int, seed: int, step: int, tensor_id: int, stream=None
     _check(load_library().dp_philox_raw(_ptr(raw), p, seed, step, tensor_id, _stream(stream)))
 
 
+def _lengths(t, n: int, what: str) -> Optional[int]:
+    """Address of int32 lengths of n examples (or None).  torch's integers from lists are int64 and on the host: neither is what kernels read."""
+    dtype = getattr(t, "dtype", None)
+    if dtype is not None:
+        import torch
+        if dtype is not torch.int32 or t.numel() < n or not t.is_contiguous() or not (t.is_cuda or t.is_pinned()):
+            raise DpError(DP_ERR_INVALID_ARG, f"{what} must be {n} contiguous int32 on the device, not {dtype} {list(t.shape)} on {t.device}")
+    return _ptr(t)
+
+
 # ---- 8-bit activation checkpoints ---------------------------------------------------------------------------------
 
 def _rows_of(t):
@@ -490,7 +500,7 @@ def dp_checkpoint_workspace_bytes(desc: LayerDesc, use: int = DP_WS_PER_EXAMPLE_
 def dp_checkpoint_example_grad(desc: LayerDesc, codes, scales, dy, g_w, g_b, sqnorm, ws, lengths=None, g_stride: int = 0,
                                ws_bytes: Optional[int] = None, stream=None):
     """dp_per_example_grad of a dense layer with its input activations from a checkpoint; lengths: int32 tokens of each example."""
-    _check(load_library().dp_checkpoint_example_grad(C.byref(desc), _ptr(codes), _ptr(scales), _ptr(dy), _ptr(lengths), _ptr(g_w), _ptr(g_b),
+    _check(load_library().dp_checkpoint_example_grad(C.byref(desc), _ptr(codes), _ptr(scales), _ptr(dy), _lengths(lengths, desc.n, "lengths"), _ptr(g_w), _ptr(g_b),
                                                      g_stride, _ptr(sqnorm), _ptr(ws), _nbytes(ws) if ws_bytes is None else ws_bytes,
                                                      _stream(stream)))
 
@@ -498,7 +508,7 @@ def dp_checkpoint_example_grad(desc: LayerDesc, codes, scales, dy, g_w, g_b, sqn
 def dp_checkpoint_clip_accumulate(desc: LayerDesc, codes, scales, dy, sqnorm, clip_c: float, acc_w, acc_b, ws, lengths=None,
                                   ws_bytes: Optional[int] = None, stream=None):
     """dp_clip_accumulate_recompute of a dense layer with its input activations from a checkpoint."""
-    _check(load_library().dp_checkpoint_clip_accumulate(C.byref(desc), _ptr(codes), _ptr(scales), _ptr(dy), _ptr(lengths), _ptr(sqnorm), clip_c,
+    _check(load_library().dp_checkpoint_clip_accumulate(C.byref(desc), _ptr(codes), _ptr(scales), _ptr(dy), _lengths(lengths, desc.n, "lengths"), _ptr(sqnorm), clip_c,
                                                         _ptr(acc_w), _ptr(acc_b), _ptr(ws), _nbytes(ws) if ws_bytes is None else ws_bytes,
                                                         _stream(stream)))
 
@@ -514,7 +524,8 @@ def dp_bias_bucket(desc: BiasDesc, distance: int) -> int:
 
 
 def dp_bias_softmax(desc: BiasDesc, scores, table, probs, query_lengths=None, key_lengths=None, stream=None):
-    _check(load_library().dp_bias_softmax(C.byref(desc), _ptr(scores), _ptr(table), _ptr(query_lengths), _ptr(key_lengths), _ptr(probs),
+    _check(load_library().dp_bias_softmax(C.byref(desc), _ptr(scores), _ptr(table), _lengths(query_lengths, desc.n, "query_lengths"),
+                                          _lengths(key_lengths, desc.n, "key_lengths"), _ptr(probs),
                                           _stream(stream)))
 
 
@@ -525,6 +536,7 @@ def dp_bias_workspace_bytes(desc: BiasDesc) -> int:
 def dp_bias_softmax_backward(desc: BiasDesc, probs, dprobs, dscores, g_table, sqnorm, ws, query_lengths=None, key_lengths=None,
                              g_stride: int = 0, ws_bytes: Optional[int] = None, stream=None):
     """Gradient of the scores, and per example the gradient of the bias table and its squared norm."""
-    _check(load_library().dp_bias_softmax_backward(C.byref(desc), _ptr(probs), _ptr(dprobs), _ptr(query_lengths), _ptr(key_lengths), _ptr(dscores),
+    _check(load_library().dp_bias_softmax_backward(C.byref(desc), _ptr(probs), _ptr(dprobs), _lengths(query_lengths, desc.n, "query_lengths"),
+                                          _lengths(key_lengths, desc.n, "key_lengths"), _ptr(dscores),
                                                    _ptr(g_table), g_stride, _ptr(sqnorm), _ptr(ws),
                                                    _nbytes(ws) if ws_bytes is None else ws_bytes, _stream(stream)))

@@ -56,3 +56,23 @@ def test_attention_block_refuses_tensors_of_another_device(monkeypatch):
     monkeypatch.setattr(torch.cuda, "current_device", lambda: 1)
     with pytest.raises(ValueError, match="current device is 1"):
         block.forward(Elsewhere((2, 4, 32), "cuda:0"))
+
+
+def test_lengths_of_another_type_or_place_are_refused():
+    """torch makes int64 of a list of numbers, on the host."""
+    fake = 0x1000
+    dense = dp.LayerDesc(kind=dp.DP_DENSE, in_dtype=dp.DP_BF16, n=3, cin=48, cout=40, h=20, w=1, has_bias=0)
+    bias = dp.BiasDesc(in_dtype=dp.DP_BF16, n=3, heads=2, queries=5, keys=7, buckets=32, max_distance=128, bidirectional=1, causal=0, query_offset=0,
+                       scale=1.0, row_stride=0)
+    room = 1 << 30
+    calls = [("lengths", lambda t: dp.dp_checkpoint_example_grad(dense, fake, fake, fake, None, None, fake, fake, lengths=t, ws_bytes=room, stream=0)),
+             ("lengths", lambda t: dp.dp_checkpoint_clip_accumulate(dense, fake, fake, fake, fake, 1.0, fake, None, fake, lengths=t, ws_bytes=room, stream=0))]
+    for which in ("query_lengths", "key_lengths"):
+        calls.append((which, lambda t, w=which: dp.dp_bias_softmax(bias, fake, fake, fake, stream=0, **{w: t})))
+        calls.append((which, lambda t, w=which: dp.dp_bias_softmax_backward(bias, fake, fake, fake, fake, None, fake, ws_bytes=room, stream=0, **{w: t})))
+    for what, call in calls:
+        for bad in (torch.tensor([1, 2, 3]), torch.zeros(3), torch.zeros(2, dtype=torch.int32), torch.zeros(6, dtype=torch.int32)[::2],
+                    torch.zeros(3, dtype=torch.int32)):
+            with pytest.raises(dp.DpError, match=what) as error:
+                call(bad)
+            assert error.value.status == dp.binding.DP_ERR_INVALID_ARG
