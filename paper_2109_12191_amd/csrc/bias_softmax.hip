@@ -60,7 +60,7 @@ __device__ __forceinline__ int bias_bucket_of(const BiasArgs &a, int d)
 // Where the values of a run that starts at distance d lie: value i at word `lane` + `shared[i]`.
 struct RunWords {
     int lane, shared[8];
-    __device__ __forceinline__ static int slot(const BiasArgs &a, int d) { return d + a.low + 16; }
+    __device__ __forceinline__ static int slot(const BiasArgs &a, int d) { return (int)((unsigned)d + (unsigned)a.low + 16u); }
     // the part that all lanes share, from any lane's distance (they differ by multiples of eight)
     __device__ __forceinline__ void set_shared(const BiasArgs &a, int d)
     {
@@ -97,6 +97,9 @@ struct Rows {
     int ex, head, q0, q1;            // queries q0 .. q1 - 1
     int first, query_length, key_length;
     size_t base;                     // row number of query 0
+    // Position of query q.  Keys are below 2^30 and far below 2^12, so that a position beyond both together is as good as any further one, and a slot
+    // stays below 2^31.
+    __device__ __forceinline__ int position(int q) const { return first > 0 ? first + min(q, (1 << 30) + 8192 - first) : first + q; }
 };
 
 __device__ __forceinline__ Rows bias_rows(const BiasArgs &a)
@@ -267,7 +270,7 @@ __global__ void __launch_bounds__(TPR > 256 ? TPR : 256) bias_softmax_kernel(con
         };
         if (r.q0 + row_first < r.q1) load_row(r.q0 + row_first);
         for (int q = r.q0 + row_first; q < r.q1; q += STEP) {
-            const int end = bias_end(a, r, q), position = r.first + q;
+            const int end = bias_end(a, r, q), position = r.position(q);
             at.set_shared(a, position);
             float z[NV][8];
             float top = -INFINITY;
@@ -299,7 +302,7 @@ __global__ void __launch_bounds__(TPR > 256 ? TPR : 256) bias_softmax_kernel(con
         }
     } else {
         for (int q = r.q0; q < r.q1; ++q) {
-            const int end = bias_end(a, r, q), position = r.first + q;
+            const int end = bias_end(a, r, q), position = r.position(q);
             const RowOf<BF16, false> row(const_cast<void *>(a.in), (r.base + q) * a.row_stride, end), out(a.out, (r.base + q) * a.row_stride, a.keys);
             at.set_shared(a, position);
             float top = -INFINITY, sum = 0.0f;
@@ -555,8 +558,8 @@ __global__ void __launch_bounds__(256) bias_softmax_narrow_kernel(const BiasArgs
     in.load(raw, row0, k, end_of(row0));
     RunWords at;
     for (int s = 0; s < 8; ++s) {
-        const int row = row0 + s, end = end_of(row), position = r.first + r.q0 + row;
-        at.set_shared(a, r.first + r.q0 + s);
+        const int row = row0 + s, end = end_of(row), position = r.position(r.q0 + row);
+        at.set_shared(a, r.position(r.q0 + s));                    // (beyond the last position that is told apart, all words hold the same)
         at.lane = min(max(RunWords::slot(a, position - k) >> 3, 1), a.last);
         float z[8];
         raw.get(z);
@@ -630,14 +633,14 @@ __global__ void __launch_bounds__(256) bias_backward_narrow_kernel(const BiasArg
     }
     const int d0 = r.first + r.q0 + row0 - k;                      // line c has distance d0 + c - 7
     float sum_far = 0.0f, sum_low = 0.0f;
-    const bool beyond = d0 - 7 >= a.far || d0 + 7 <= -a.low;
+    const bool beyond = d0 - 7 >= a.far || d0 <= -a.low - 7;
     if (beyond) {
         float s = line[0];
 #pragma unroll
         for (int c = 1; c < 15; ++c) s += line[c];
         (d0 > 0 ? sum_far : sum_low) = s;
     }
-    const int top = RunWords::slot(a, d0 + 7), m = RunWords::slot(a, r.first + r.q0 + 7) & 7;
+    const int top = RunWords::slot(a, d0) + 7, m = (RunWords::slot(a, r.first + r.q0) + 7) & 7;
 #pragma unroll 1
     for (int g = 0; g < 64 / TPR; ++g) {
         // A row's neighbouring lanes are eight keys apart: slots 8 .. 14 of a lane are 0 .. 6 of the next one, and in either half no two lanes
