@@ -451,15 +451,14 @@ def _rows_of(t):
     if dtype is not torch.bfloat16 and dtype is not torch.float32:
         raise DpError(DP_ERR_UNSUPPORTED, f"activations are float32 or bfloat16, not {dtype}")
     shape, strides = t.shape, t.stride()
-    features = shape[-1] if shape else 0
-    spacing = strides[-2] if len(shape) > 1 else features
-    rows = 1
-    for size in shape[:-1]:
-        rows *= size
-    even = features > 0 and (features == 1 or strides[-1] == 1) and (rows <= 1 or spacing >= features)
-    for d in range(len(shape) - 2):
-        even = even and (shape[d] == 1 or strides[d] == shape[d + 1] * strides[d + 1])
-    if not even:
+    features, rows, spacing = shape[-1] if shape else 0, 1, 0
+    even = features > 0 and (features == 1 or strides[-1] == 1)
+    for d in range(len(shape) - 2, -1, -1):          # from the innermost on; the stride of a dimension of one means nothing
+        if shape[d] != 1:
+            even = even and (strides[d] == rows * spacing if spacing else strides[d] >= features)
+            spacing = spacing or strides[d]
+            rows *= shape[d]
+    if not even and (rows or features <= 0):
         raise DpError(DP_ERR_INVALID_ARG, f"not rows of consecutive values: shape {tuple(shape)}, strides {strides}")
     return (DP_BF16 if dtype is torch.bfloat16 else DP_F32), rows, features, max(spacing, features)
 

@@ -76,3 +76,20 @@ def test_lengths_of_another_type_or_place_are_refused():
             with pytest.raises(dp.DpError, match=what) as error:
                 call(bad)
             assert error.value.status == dp.binding.DP_ERR_INVALID_ARG
+
+
+def test_rows_of_views_with_dimensions_of_one():
+    """Rows that are evenly spaced, whatever stride a dimension of one element has."""
+    rows = dp.binding._rows_of
+    x = torch.zeros(4, 6, 48)
+    assert rows(x[:, 2:3]) == (dp.DP_F32, 4, 48, 6 * 48)                 # one token of each example
+    assert rows(x[:, 2:3, :40]) == (dp.DP_F32, 4, 40, 6 * 48)
+    assert rows(x[1:2]) == (dp.DP_F32, 6, 48, 48)
+    assert rows(torch.zeros(2, 1, 3, 48).as_strided((2, 1, 3, 48), (144, 7, 48, 1))) == (dp.DP_F32, 6, 48, 48)
+    assert rows(torch.zeros(5, 1, 1, 48)[::2]) == (dp.DP_F32, 3, 48, 96)
+    assert rows(torch.zeros(1, 1, 48)) == (dp.DP_F32, 1, 48, 48) and rows(torch.zeros(3, 1)) == (dp.DP_F32, 3, 1, 1)
+    assert rows(torch.zeros(1, 48).expand(1, 48)) == (dp.DP_F32, 1, 48, 48)
+    assert rows(torch.zeros(0, 48))[1:3] == (0, 48) and rows(torch.zeros(4, 0, 48))[1:3] == (0, 48)
+    for bad in (x[:, :2], x.transpose(0, 1), torch.zeros(1, 48).expand(3, 48), torch.zeros(48, 4).t(), torch.zeros(4, 0), x.expand(2, 4, 6, 48), torch.zeros(())):
+        with pytest.raises(dp.DpError):
+            rows(bad)
