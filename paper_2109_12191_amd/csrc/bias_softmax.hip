@@ -40,6 +40,7 @@ struct BiasArgs {
     int plane, last;                     // words of a plane of distances; slots at `last - 1` and beyond in each are beyond `far`
     int rows, blocks;                    // rows of a workgroup, workgroups of a head
     int share;                           // lanes that share a bucket's sum
+    unsigned first_block;                // workgroups of the launches before
     int borders[BIAS_BORDERS];
 };
 
@@ -94,6 +95,7 @@ __device__ __forceinline__ float wave_all_max(float v)
 
 // What a workgroup works on.
 struct Rows {
+    unsigned block;
     int ex, head, q0, q1;            // queries q0 .. q1 - 1
     int first, query_length, key_length;
     size_t base;                     // row number of query 0
@@ -105,10 +107,11 @@ struct Rows {
 __device__ __forceinline__ Rows bias_rows(const BiasArgs &a)
 {
     Rows r;
-    const unsigned lines = blockIdx.x / (unsigned)a.blocks;        // example and head
+    r.block = a.first_block + blockIdx.x;
+    const unsigned lines = r.block / (unsigned)a.blocks;           // example and head
     r.ex = (int)(lines / (unsigned)a.heads);
     r.head = (int)(lines - (unsigned)r.ex * (unsigned)a.heads);
-    r.q0 = (int)(blockIdx.x - lines * (unsigned)a.blocks) * a.rows;
+    r.q0 = (int)(r.block - lines * (unsigned)a.blocks) * a.rows;
     r.q1 = min(r.q0 + a.rows, a.queries);
     r.key_length = a.key_lengths ? min(max(a.key_lengths[r.ex], 0), a.keys) : a.keys;
     r.query_length = a.query_lengths ? min(max(a.query_lengths[r.ex], 0), a.queries) : a.queries;
@@ -195,7 +198,7 @@ __device__ __forceinline__ void bias_bucket_sums(const BiasArgs &a, const Rows &
     const float far_wave = wave_all_sum(sum_far), low_wave = wave_all_sum(sum_low);
     if (lane == 0) { ends[wave][0] = far_wave; ends[wave][1] = low_wave; }
     __syncthreads();
-    float *part = a.partials + (size_t)blockIdx.x * a.buckets;
+    float *part = a.partials + (size_t)r.block * a.buckets;
     const int side_buckets = a.bidirectional ? a.buckets / 2 : a.buckets;
     auto start = [&](int m) { return m <= a.near ? m : a.borders[m - a.near - 1]; };       // smallest magnitude of a side's bucket m
     for (int b = (int)threadIdx.x / a.share; b < a.buckets; b += 256 / a.share) {
@@ -745,38 +748,38 @@ bool bias_words(const BiasGeo &g, const void *p)
 template <bool BF16, bool WORDS>
 dp_status run_forward(const BiasGeo &g, const BiasArgs &a, hipStream_t s)
 {
-    const dim3 grid((unsigned)((size_t)g.n * g.heads * a.blocks));
+    const size_t grid = (size_t)g.n * g.heads * a.blocks;
     const unsigned lds = 8u * a.plane * 4u;
     const int lanes = narrow_lanes(g);
-    if (lanes == 8) return launch_lds<bias_softmax_narrow_kernel<BF16, WORDS, 8>>(grid, 256, lds, s, a);
-    if (lanes == 16) return launch_lds<bias_softmax_narrow_kernel<BF16, WORDS, 16>>(grid, 256, lds, s, a);
-    if (lanes == 32) return launch_lds<bias_softmax_narrow_kernel<BF16, WORDS, 32>>(grid, 256, lds, s, a);
-    if (g.keys <= 512) return launch_lds<bias_softmax_kernel<BF16, WORDS, 64, 1>>(grid, 256, lds, s, a);
-    if (g.keys <= 1024) return launch_lds<bias_softmax_kernel<BF16, WORDS, 64, 2>>(grid, 256, lds, s, a);
-    if (g.keys <= 2048) return launch_lds<bias_softmax_kernel<BF16, WORDS, 64, 4>>(grid, 256, lds, s, a);
-    if (g.keys <= 4096) return launch_lds<bias_softmax_kernel<BF16, WORDS, 256, 2>>(grid, 256, lds, s, a);
-    if (g.keys <= 8192) return launch_lds<bias_softmax_kernel<BF16, WORDS, 256, 4>>(grid, 256, lds, s, a);
-    if (g.keys <= 16384) return launch_lds<bias_softmax_kernel<BF16, WORDS, 256, 8>>(grid, 256, lds, s, a);
+    if (lanes == 8) return launch_blocks<bias_softmax_narrow_kernel<BF16, WORDS, 8>>(grid, 256, lds, s, a);
+    if (lanes == 16) return launch_blocks<bias_softmax_narrow_kernel<BF16, WORDS, 16>>(grid, 256, lds, s, a);
+    if (lanes == 32) return launch_blocks<bias_softmax_narrow_kernel<BF16, WORDS, 32>>(grid, 256, lds, s, a);
+    if (g.keys <= 512) return launch_blocks<bias_softmax_kernel<BF16, WORDS, 64, 1>>(grid, 256, lds, s, a);
+    if (g.keys <= 1024) return launch_blocks<bias_softmax_kernel<BF16, WORDS, 64, 2>>(grid, 256, lds, s, a);
+    if (g.keys <= 2048) return launch_blocks<bias_softmax_kernel<BF16, WORDS, 64, 4>>(grid, 256, lds, s, a);
+    if (g.keys <= 4096) return launch_blocks<bias_softmax_kernel<BF16, WORDS, 256, 2>>(grid, 256, lds, s, a);
+    if (g.keys <= 8192) return launch_blocks<bias_softmax_kernel<BF16, WORDS, 256, 4>>(grid, 256, lds, s, a);
+    if (g.keys <= 16384) return launch_blocks<bias_softmax_kernel<BF16, WORDS, 256, 8>>(grid, 256, lds, s, a);
     // sixteen waves a row (16 rows, four waves and two passes against these: 60000 keys 27.2 us and 15.0, 131072 54.0 and 27.4)
-    if (g.keys <= 32768) return launch_lds<bias_softmax_kernel<BF16, WORDS, 1024, 4>>(grid, 1024, lds, s, a);
-    return launch_lds<bias_softmax_kernel<BF16, WORDS, 1024, 0>>(grid, 1024, lds, s, a);
+    if (g.keys <= 32768) return launch_blocks<bias_softmax_kernel<BF16, WORDS, 1024, 4>>(grid, 1024, lds, s, a);
+    return launch_blocks<bias_softmax_kernel<BF16, WORDS, 1024, 0>>(grid, 1024, lds, s, a);
 }
 
 template <bool BF16, bool WORDS>
 dp_status run_backward(const BiasGeo &g, const BiasArgs &a, hipStream_t s)
 {
-    const dim3 grid((unsigned)((size_t)g.n * g.heads * a.blocks));
+    const size_t grid = (size_t)g.n * g.heads * a.blocks;
     const unsigned lds = 4u * 8u * a.plane * 4u;
     const int lanes = narrow_lanes(g);
-    if (lanes == 8) return launch_lds<bias_backward_narrow_kernel<BF16, WORDS, 8>>(grid, 256, lds, s, a);
-    if (lanes == 16) return launch_lds<bias_backward_narrow_kernel<BF16, WORDS, 16>>(grid, 256, lds, s, a);
-    if (lanes == 32) return launch_lds<bias_backward_narrow_kernel<BF16, WORDS, 32>>(grid, 256, lds, s, a);
-    if (g.keys <= 512) return launch_lds<bias_backward_kernel<BF16, WORDS, 64, 1>>(grid, 256, lds, s, a);
-    if (g.keys <= 1024) return launch_lds<bias_backward_kernel<BF16, WORDS, 64, 2>>(grid, 256, lds, s, a);
-    if (g.keys <= 2048) return launch_lds<bias_backward_kernel<BF16, WORDS, 64, 4>>(grid, 256, lds, s, a);
-    if (g.keys <= 4096) return launch_lds<bias_backward_kernel<BF16, WORDS, 256, 2>>(grid, 256, lds, s, a);
-    if (g.keys <= 8192) return launch_lds<bias_backward_kernel<BF16, WORDS, 256, 4>>(grid, 256, lds, s, a);
-    return launch_lds<bias_backward_kernel<BF16, WORDS, 256, 0>>(grid, 256, lds, s, a);
+    if (lanes == 8) return launch_blocks<bias_backward_narrow_kernel<BF16, WORDS, 8>>(grid, 256, lds, s, a);
+    if (lanes == 16) return launch_blocks<bias_backward_narrow_kernel<BF16, WORDS, 16>>(grid, 256, lds, s, a);
+    if (lanes == 32) return launch_blocks<bias_backward_narrow_kernel<BF16, WORDS, 32>>(grid, 256, lds, s, a);
+    if (g.keys <= 512) return launch_blocks<bias_backward_kernel<BF16, WORDS, 64, 1>>(grid, 256, lds, s, a);
+    if (g.keys <= 1024) return launch_blocks<bias_backward_kernel<BF16, WORDS, 64, 2>>(grid, 256, lds, s, a);
+    if (g.keys <= 2048) return launch_blocks<bias_backward_kernel<BF16, WORDS, 64, 4>>(grid, 256, lds, s, a);
+    if (g.keys <= 4096) return launch_blocks<bias_backward_kernel<BF16, WORDS, 256, 2>>(grid, 256, lds, s, a);
+    if (g.keys <= 8192) return launch_blocks<bias_backward_kernel<BF16, WORDS, 256, 4>>(grid, 256, lds, s, a);
+    return launch_blocks<bias_backward_kernel<BF16, WORDS, 256, 0>>(grid, 256, lds, s, a);
 }
 
 }  // namespace

@@ -24,6 +24,7 @@ struct CkArgs {
     const uint8_t *codes_in, *scales_in;
     size_t rows, stride, pieces;     // pieces of V features of all rows
     int features, per_row;           // pieces of a row (whole blocks of them)
+    size_t first_block;              // workgroups of the launches before
 };
 
 template <bool BF16> constexpr int ck_values() { return BF16 ? 8 : 4; }
@@ -32,7 +33,7 @@ constexpr int CK_TURNS = 2;                                        // pieces of 
 // Row and piece of this thread's turn u.  One 64-bit division per workgroup (scalar), a 32-bit one per piece.
 __device__ __forceinline__ bool ck_place(const CkArgs &a, int u, size_t &row, int &piece)
 {
-    const size_t first = (size_t)blockIdx.x * (256 * CK_TURNS), row0 = first / (unsigned)a.per_row;
+    const size_t first = (a.first_block + blockIdx.x) * (256 * CK_TURNS), row0 = first / (unsigned)a.per_row;
     const unsigned at = (unsigned)(first - row0 * (unsigned)a.per_row) + 256u * u + threadIdx.x, more = at / (unsigned)a.per_row;
     row = row0 + more;
     piece = (int)(at - more * (unsigned)a.per_row);
@@ -181,10 +182,8 @@ dp_status launch_checkpoint_write(const void *x, bool bf16, size_t rows, int fea
 {
     CkArgs a = ck_args(rows, features, stride, bf16);
     a.x = x; a.codes = codes; a.scales = scales;
-    const dim3 grid((unsigned)((a.pieces + 256 * CK_TURNS - 1) / (256 * CK_TURNS)));
-    if (bf16) hipLaunchKernelGGL(checkpoint_write_kernel<true>, grid, dim3(256), 0, s, a);
-    else hipLaunchKernelGGL(checkpoint_write_kernel<false>, grid, dim3(256), 0, s, a);
-    return check_launch("checkpoint_write");
+    const size_t grid = (a.pieces + 256 * CK_TURNS - 1) / (256 * CK_TURNS);
+    return bf16 ? launch_blocks<checkpoint_write_kernel<true>>(grid, 256, 0, s, a) : launch_blocks<checkpoint_write_kernel<false>>(grid, 256, 0, s, a);
 }
 
 dp_status launch_checkpoint_read(const uint8_t *codes, const uint8_t *scales, bool bf16, size_t rows, int features, void *x, size_t stride,
@@ -192,10 +191,8 @@ dp_status launch_checkpoint_read(const uint8_t *codes, const uint8_t *scales, bo
 {
     CkArgs a = ck_args(rows, features, stride, bf16);
     a.out = x; a.codes_in = codes; a.scales_in = scales;
-    const dim3 grid((unsigned)((a.pieces + 256 * CK_TURNS - 1) / (256 * CK_TURNS)));
-    if (bf16) hipLaunchKernelGGL(checkpoint_read_kernel<true>, grid, dim3(256), 0, s, a);
-    else hipLaunchKernelGGL(checkpoint_read_kernel<false>, grid, dim3(256), 0, s, a);
-    return check_launch("checkpoint_read");
+    const size_t grid = (a.pieces + 256 * CK_TURNS - 1) / (256 * CK_TURNS);
+    return bf16 ? launch_blocks<checkpoint_read_kernel<true>>(grid, 256, 0, s, a) : launch_blocks<checkpoint_read_kernel<false>>(grid, 256, 0, s, a);
 }
 
 }  // namespace dp

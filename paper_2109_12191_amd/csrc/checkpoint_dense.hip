@@ -91,6 +91,7 @@ constexpr int CT = 128;                                            // o of a til
 constexpr int ck_chunk(int planes, int nj) { return planes == 1 && nj == 2 ? 64 : 32; }
 constexpr int ck_stage_bytes(int planes, int nj) { return ck_chunk(planes, nj) * (planes * 2 * CT + nj * 128); }
 constexpr int CK_TABLE = 1024;                                     // examples of a weighted call
+constexpr size_t CK_GROUPS = (size_t)1 << 23;                      // workgroups of a launch (fewer than 2^32 threads)
 constexpr unsigned CK_NOWHERE = 0xFFFFFFE0u;                       // an offset beyond any buffer
 constexpr int CK_POWER = 16;                                       // of a factor, in the scales of X
 static_assert(CK_LOW - 9 - CK_POWER >= -126, "scaled values are normal bf16 numbers");
@@ -1124,7 +1125,7 @@ CkPlan ck_plan(const Geo &g, int mode)
         const long long tiles = (g.h + GT - 1) / GT, pairs = tiles * (tiles + 1) / 2, chunks = (ck_pitch(g.cin) + GC - 1) / GC + (g.cout + yc - 1) / yc;
         p.gram_splits = (int)std::max(1ll, std::min({512 / (g.n * pairs), chunks / 8, 16ll}));
         // (tokens of no common direction have a sum of 1 / T of its bound: they stand with room for four times less)
-        p.gram = g.n * pairs < (1ll << 30) && (double)g.h * ck_resolution(g) <= 0.25 &&
+        p.gram = g.n * pairs < (long long)CK_GROUPS && (double)g.h * ck_resolution(g) <= 0.25 &&
                  gram_us(g, (double)pairs, p.gram_splits, (double)chunks) < contract_us(g, (double)p.per_example, ck_chunk(g.bf16 ? 1 : 3, p.nj));
         if (p.gram) {
             p.per_example = (size_t)pairs;
@@ -1273,25 +1274,37 @@ dp_status launch_checkpoint_dense(const Geo &g, int mode, const uint8_t *codes, 
     a.tiles_k = ck_tiles(g.cin, 64 * p.nj); a.columns = a.tiles_k + g.has_bias;
     const bool words = !g.bf16 || g.cout % 2 == 0;
     if (p.gram) return launch_gram(g, p, a, words, sqnorm, ws, s);
-    // workgroups of all XCDs alike (the kernel's map), those beyond the last one end at once
-    const dim3 grid((unsigned)(((size_t)a.tiles_o * a.columns * g.n + 7) / 8 * 8));
-    dp_status st;
+    dp_status st = DP_OK;
     const bool alone = p.per_example == 1 && sqnorm;               // an example's only partial sum is its squared norm
     a.partials = alone ? sqnorm : static_cast<float *>(ws);
     a.stored = out_w != nullptr;
     a.out_w = out_w; a.out_b = out_b;
     a.stride_w = out_stride ? out_stride : g.pw;
     a.stride_b = out_stride ? out_stride : g.pb;
-    a.slots = g.n;
+    const float *const partials = a.partials;
+    const int at_once = (int)std::max<size_t>(1, CK_GROUPS / p.per_example);       // examples of a launch
     profile_begin(s);
-    if (g.bf16) {
-        st = p.nj == 4 ? run_contract<1, 4, false, true>(words, grid, a, s) : run_contract<1, 2, false, true>(words, grid, a, s);
-    } else {
-        st = run_contract<3, 2, false, false>(words, grid, a, s);
+    for (int i = 0; i < g.n && st == DP_OK; i += at_once) {
+        a.slots = std::min(g.n - i, at_once);
+        // workgroups of all XCDs alike (the kernel's map), those beyond the last one end at once
+        const dim3 grid((unsigned)((p.per_example * a.slots + 7) / 8 * 8));
+        if (g.bf16) {
+            st = p.nj == 4 ? run_contract<1, 4, false, true>(words, grid, a, s) : run_contract<1, 2, false, true>(words, grid, a, s);
+        } else {
+            st = run_contract<3, 2, false, false>(words, grid, a, s);
+        }
+        const size_t rows = (size_t)a.slots * g.h;
+        a.codes += rows * a.pitch;
+        a.scales += rows * (a.pitch / CK_BLOCK);
+        a.dy = static_cast<const char *>(a.dy) + rows * g.cout * (g.bf16 ? 2 : 4);
+        if (a.lengths) a.lengths += a.slots;
+        a.partials += p.per_example * a.slots;
+        if (a.out_w) a.out_w += a.stride_w * a.slots;
+        if (a.out_b) a.out_b += a.stride_b * a.slots;
     }
     profile_end(s);
     if (st != DP_OK || !sqnorm || alone) return st;
-    return launch_sum_partials(a.partials, g.n, (int)p.per_example, sqnorm, s);
+    return launch_sum_partials(partials, g.n, (int)p.per_example, sqnorm, s);
 }
 
 }  // namespace dp

@@ -40,6 +40,19 @@ dp_status launch_lds(dim3 grid, unsigned threads, unsigned lds, hipStream_t s, c
     return check_launch("kernel");
 }
 
+// The same for any number of workgroups: a launch has room for fewer than 2^32 threads.  Args::first_block goes before blockIdx.x.
+template <auto Kernel, typename Args>
+dp_status launch_blocks(size_t blocks, unsigned threads, unsigned lds, hipStream_t s, Args args)
+{
+    const size_t most = ((size_t)1 << 31) / threads;
+    for (size_t first = 0; first < blocks; first += most) {
+        args.first_block = (decltype(args.first_block))first;
+        const dp_status st = launch_lds<Kernel>(dim3((unsigned)(blocks - first < most ? blocks - first : most)), threads, lds, s, args);
+        if (st != DP_OK) return st;
+    }
+    return DP_OK;
+}
+
 // ---- geometry of a validated descriptor ------------------------------------------------
 struct Geo {
     int kind, bf16, n;
