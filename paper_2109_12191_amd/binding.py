@@ -434,12 +434,11 @@ def dp_philox_raw(raw, p: int, seed: int, step: int, tensor_id: int, stream=None
 
 def _lengths(t, n: int, what: str) -> Optional[int]:
     """Address of int32 lengths of n examples (or None).  torch's integers from lists are int64 and on the host: neither is what kernels read."""
-    dtype = getattr(t, "dtype", None)
-    if dtype is not None:
-        import torch
-        if dtype is not torch.int32 or t.numel() < n or not t.is_contiguous() or not (t.is_cuda or t.is_pinned()):
-            raise DpError(DP_ERR_INVALID_ARG, f"{what} must be {n} contiguous int32 on the device, not {dtype} {list(t.shape)} on {t.device}")
-    return _ptr(t)
+    if t is None or type(t) is int:
+        return t
+    if t.element_size() != 4 or t.is_floating_point() or t.numel() < n or not t.is_contiguous() or not (t.is_cuda or t.is_pinned()):
+        raise DpError(DP_ERR_INVALID_ARG, f"{what} must be {n} contiguous int32 on the device, not {t.dtype} {list(t.shape)} on {t.device}")
+    return t.data_ptr()
 
 
 # ---- 8-bit activation checkpoints ---------------------------------------------------------------------------------
