@@ -9,6 +9,7 @@
 // them exactly (8 + 8 + 8 significant bits), three products for one.
 //
 //   ck_gram_kernel     norms alone of short examples:  |dW_i|^2 = sum_{t, u} (X_t . X_u) (dY_t . dY_u)
+//   ck_again_kernel    those of them that cancellation has left without digits, as sums of squares
 //   ck_contract_kernel everything else
 #include "checkpoint.h"
 
@@ -82,7 +83,8 @@ __device__ __forceinline__ void split8(const float (&v)[8], uint4 (&planes)[3])
 // Measured: norms of 8 x 1024 tokens 1024 -> 2048 34.8 us, 988 TFLOP/s (a library product of 8192^3: 1282); clipped sum of 16 x 512 tokens
 // 2048 -> 2048 93.5 us, 735 TFLOP/s, and 11 us to join two ranges (factors worked out by every chunk instead of once: 94.4; 2 x 512 tokens
 // 4096 -> 1024 24.6 instead of 23.2).  Bound by the LDS (a chunk's operands are 96 KB written and read for a workgroup, 0.3 us of its 0.75) and by
-// the waits that two workgroups a compute unit leave uncovered; 16 x 128 tokens 768 -> 768, 8 chunks a workgroup at most, by trips to memory one after
+// the waits that two workgroups a compute unit leave uncovered (<1, 4, true, true, false>, wide sums of an odd number of features, keeps five registers
+// in memory; no other instance does); 16 x 128 tokens 768 -> 768, 8 chunks a workgroup at most, by trips to memory one after
 // the other.  Three stages of loads instead of two: no gain (registers); chunks of 32 with three workgroups: slower.
 // WORDS: rows of dY begin at whole dwords: pieces by buffer loads, which give zeros beyond the chunk's last row (what a row's last piece takes
 // from the next row is multiplied into features beyond the last, which nobody reads).  Else (bf16, an odd number of features) every other
@@ -643,6 +645,9 @@ __global__ void __launch_bounds__(256) ck_ranges_kernel(const float *part, size_
 // (F + O) / 4 2^-23 B^2 if all err one way; 2^-23.9 B^2 is the most that was seen (2 to 500 tokens, 64 to 8192 features, tokens of their own to tokens all
 // alike).  A sum stands if it is at least ck_resolution() of B^2: then it is within a quarter at worst, and within 2^-12 as measured.  Tokens of no common
 // direction give B^2 / T.  The other examples' norms are made again from their gradients' values, on the device (ck_again_kernel).
+// ONE: every example has one pair (64 tokens at most): half the operands, the products above the diagonal once, those of tokens from the 32nd on
+// only where there are some, and three chunks on their way instead of one (32 x 64 tokens 768 -> 768 12.7 us and 11.3 before the bounds were summed
+// here, 12.5 with them).  16 x 64 tokens 4096 -> 4096: 12.4, 8.5 to join; 400 x 64 768 -> 768: 17.2.
 constexpr int GT = 64, GC = 128, G_ROW = 2 * GC + 16, G_SIDE = GT * G_ROW, G_STAGE = 2 * G_SIDE;      // tokens, features; bytes (16 of a row keep rows in different banks)
 constexpr int G_VALUES = GT * GT;
 
@@ -948,7 +953,7 @@ struct GramSums {
 // is 1.  `sharers` workgroups take an example's tiles of 64 x 64 in turn, a wave 32 x 32 of one, chunks of 32 tokens through LDS as [feature][token]; the
 // last one to arrive adds up what they leave, in order.  Every workgroup walks over all examples, as many of them at once as fill the chip; the
 // first one writes the norms that stand.  Small and with few registers, so that it costs little where there is nothing to do: 3.8 us of a launch
-// (the contraction in its place: 20, for its registers in a loop).   Where all fall: 16 examples of 64 tokens 4096 -> 4096
+// (the contraction in its place: 20, for its registers in a loop).  Where all fall: 16 examples of 64 tokens 4096 -> 4096
 // 528 us, the contraction 57; 512 of 8 tokens 768 -> 768 303 and 49.
 constexpr int AGAIN = 64, AGAIN_TOKENS = 32, AGAIN_ROW = AGAIN_TOKENS * 2 + 16;        // features of a tile, tokens of a chunk; bytes (16 more: banks, alignment)
 
