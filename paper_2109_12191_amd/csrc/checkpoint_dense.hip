@@ -935,35 +935,34 @@ struct GramSums {
     const float *values, *bounds;    // [n, pairs], [n, tiles of 64 tokens]
     int pairs, tiles;
     float resolution;
-    // example i's squared norm, and whether it stands (not: a NaN)
-    __device__ __forceinline__ bool stands(int i, float &norm) const
+    // example i's sum and the root of its bound
+    __device__ __forceinline__ void load(int i, float &sum, float &bound) const
     {
         const float *v = values + (size_t)i * pairs, *b = bounds + (size_t)i * tiles;
-        float sum = 0.0f, bound = 0.0f;
+        sum = bound = 0.0f;
 #pragma unroll 4
         for (int k = 0; k < pairs; ++k) sum += v[k];
 #pragma unroll 4
         for (int k = 0; k < tiles; ++k) bound += b[k];
-        norm = sum;
-        return sum >= resolution * bound * bound;
     }
+    __device__ __forceinline__ bool stands(float sum, float bound) const { return sum >= resolution * bound * bound; }        // (not: a NaN)
 };
 
 // Squared norms of the examples whose sums do not stand, from their gradients' values, dW_i and db_i as one product with a further feature of X that
 // is 1.  `sharers` workgroups take an example's tiles of 64 x 64 in turn, a wave 32 x 32 of one, chunks of 32 tokens through LDS as [feature][token]; the
-// last one to arrive adds up what they leave, in order.  Every workgroup walks over all examples, as many of them at once as fill the chip; the
-// first one writes the norms that stand.  Small and with few registers, so that it costs little where there is nothing to do: 3.8 us of a launch
-// (the contraction in its place: 20, for its registers in a loop).  Where all fall: 16 examples of 64 tokens 4096 -> 4096
-// 528 us, the contraction 57; 512 of 8 tokens 768 -> 768 303 and 49.
+// last one to arrive adds up what they leave, in order.  Every workgroup walks over all examples, AGAIN_TURNS to a thread at a time; as many examples at
+// once as fill the chip.  The first workgroup writes the norms that stand.  Small and with few registers, so that it costs little where there is nothing to
+// do: a launch of 3.4 us (the contraction in its place: 20, for its registers in a loop).  Where all fall: 16 examples of 64 tokens 4096 -> 4096
+// 529 us, the contraction 57; 512 of 8 tokens 768 -> 768 303 and 49.
 constexpr int AGAIN = 64, AGAIN_TOKENS = 32, AGAIN_ROW = AGAIN_TOKENS * 2 + 16;        // features of a tile, tokens of a chunk; bytes (16 more: banks, alignment)
 
-template <bool BF16>
+template <bool BF16, int AGAIN_TURNS>
 __global__ void __launch_bounds__(256) ck_again_kernel(const CkDenseArgs a, const GramSums g, int sharers, unsigned *arrived, float *sqnorm)
 {
     typedef typename In<BF16>::type E;
     constexpr int PLANES = BF16 ? 1 : 3;
     __shared__ __attribute__((aligned(16))) char xs[AGAIN * AGAIN_ROW], ys[PLANES][AGAIN * AGAIN_ROW];
-    __shared__ uint32_t fallen[8];
+    __shared__ uint32_t fallen[8 * AGAIN_TURNS];
     __shared__ float red[4];
     __shared__ unsigned before;
     const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
@@ -1031,19 +1030,37 @@ __global__ void __launch_bounds__(256) ck_again_kernel(const CkDenseArgs a, cons
     };
 
     unsigned turn = 0;
-    for (int first = 0; first < a.n; first += 256) {
-        const int i = first + t;
-        float norm = 0.0f;
-        const bool stands = i >= a.n || g.stands(i, norm);
-        if (blockIdx.x == 0 && stands && i < a.n) sqnorm[i] = norm;
-        const unsigned long long those = __ballot(!stands);
-        __syncthreads();                                           // (the last ones have been read)
-        if (lane == 0) {
-            fallen[2 * wave] = (uint32_t)those;
-            fallen[2 * wave + 1] = (uint32_t)(those >> 32);
+    for (int first = 0; first < a.n; first += 256 * AGAIN_TURNS) {
+        float sum[AGAIN_TURNS], bound[AGAIN_TURNS];
+        unsigned long long those[AGAIN_TURNS];
+#pragma unroll
+        for (int u = 0; u < AGAIN_TURNS; ++u) sum[u] = bound[u] = 0.0f;
+        if (g.pairs == 1) {                                        // all loads at once
+#pragma unroll
+            for (int u = 0; u < AGAIN_TURNS; ++u)
+                if (first + 256 * u + t < a.n) { sum[u] = g.values[first + 256 * u + t]; bound[u] = g.bounds[first + 256 * u + t]; }
+        } else {
+#pragma unroll
+            for (int u = 0; u < AGAIN_TURNS; ++u)
+                if (first + 256 * u + t < a.n) g.load(first + 256 * u + t, sum[u], bound[u]);
         }
+        bool any = false;
+#pragma unroll
+        for (int u = 0; u < AGAIN_TURNS; ++u) {
+            const bool stands = g.stands(sum[u], bound[u]);
+            if (blockIdx.x == 0 && stands && first + 256 * u + t < a.n) sqnorm[first + 256 * u + t] = sum[u];
+            those[u] = __ballot(!stands);
+            any |= !stands;
+        }
+        if (!__syncthreads_or(any)) continue;                      // (the last ones have been read, too)
+#pragma unroll
+        for (int u = 0; u < AGAIN_TURNS; ++u)
+            if (lane == 0) {
+                fallen[8 * u + 2 * wave] = (uint32_t)those[u];
+                fallen[8 * u + 2 * wave + 1] = (uint32_t)(those[u] >> 32);
+            }
         __syncthreads();
-        for (int w = 0; w < 8; ++w)
+        for (int w = 0; w < 8 * AGAIN_TURNS; ++w)
             for (uint32_t left = (uint32_t)__builtin_amdgcn_readfirstlane((int)fallen[w]); left; left &= left - 1) {
                 if (turn++ % at_once != mine) continue;
                 const int ex = first + 32 * w + __builtin_ctz(left), tiles_k = (features + AGAIN - 1) / AGAIN, tiles = (a.cout + AGAIN - 1) / AGAIN * tiles_k;
@@ -1083,7 +1100,7 @@ int ck_tiles(int v, int width) { return (v + width - 1) / width; }
 float ck_resolution(const Geo &g) { return std::max(0x1p-11f, (float)(g.cin + g.cout) * 0x1p-23f); }
 
 // Which of the two forms of norms: what they take, in microseconds a call.  bf16 (n, T, F, O: Gram form / contraction): 32, 64, 768, 768 15.0 / 9.9, with a
-// bias 15.1 / 9.8; 400, 64, 768, 768 21.0 / 50.9; 8, 128, 2048, 2048 22.5 / 14.3; 16, 64, 2048, 2048 18.9 / 17.4; 64, 16, 2048, 2048 21.2 / 43.4;
+// bias 15.1 / 9.8; 400, 64, 768, 768 20.2 / 50.9; 8, 128, 2048, 2048 22.5 / 14.3; 16, 64, 2048, 2048 18.9 / 17.4; 64, 16, 2048, 2048 21.2 / 43.4;
 // 8, 512, 2048, 2048 50.3 / 36.2; 16, 64, 4096, 4096 22.3 / 56.6; 16, 128, 4096, 4096 28.9 / 79.3; 16, 256, 4096, 4096 48.6 / 137.  fp32: 32, 64, 768, 768 21.6 / 14.8;
 // 16, 64, 2048, 2048 24.6 / 36.2; 55, 2, 1792, 576 20.3 / 24.8; 16, 256, 4096, 4096 90.4 / 396.  512 workgroups of either kind fill the chip.
 double gram_us(const Geo &g, double pairs, int splits, double chunks)
@@ -1219,8 +1236,12 @@ static dp_status launch_gram(const Geo &g, const CkPlan &p, CkDenseArgs a, bool 
     const GramSums sums = {values, bounds, pairs, (g.h + GT - 1) / GT, ck_resolution(g)};
     a.partials = reinterpret_cast<float *>(base + room.partials);
     const dim3 again((unsigned)(p.sharers * std::min(std::max(512 / p.sharers, 1), g.n)));
-    return g.bf16 ? launch_lds<ck_again_kernel<true>>(again, 256, 0, s, a, sums, p.sharers, arrived, sqnorm)
-                  : launch_lds<ck_again_kernel<false>>(again, 256, 0, s, a, sums, p.sharers, arrived, sqnorm);
+    // one example to a thread, or eight (16 x 64 tokens 4096 -> 4096: 22.4 us a call and 23.3; 400 x 64 768 -> 768 21.0 and 20.2; 65535 x 1
+    // 256 -> 256 1227 and 938)
+    if (g.n <= 256) return g.bf16 ? launch_lds<ck_again_kernel<true, 1>>(again, 256, 0, s, a, sums, p.sharers, arrived, sqnorm)
+                                  : launch_lds<ck_again_kernel<false, 1>>(again, 256, 0, s, a, sums, p.sharers, arrived, sqnorm);
+    return g.bf16 ? launch_lds<ck_again_kernel<true, 8>>(again, 256, 0, s, a, sums, p.sharers, arrived, sqnorm)
+                  : launch_lds<ck_again_kernel<false, 8>>(again, 256, 0, s, a, sums, p.sharers, arrived, sqnorm);
 }
 
 static dp_status launch_weighted(const Geo &g, CkDenseArgs a, float *out_w, float *out_b, void *ws, hipStream_t s)

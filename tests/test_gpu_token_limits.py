@@ -305,3 +305,25 @@ def test_recorded_norms_of_gradients_that_cancel(dtype):
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(eager, sq) and bool((sq > 0.0).all())
+
+
+@pytest.mark.parametrize("n,tokens", [(5003, 2), (2049, 6), (9000, 1)])
+def test_norms_of_many_examples_some_of_which_cancel(n, tokens):
+    """More examples than are looked at together."""
+    cin, cout = 256, 288
+    desc = layer(n, tokens, cin, cout)
+    gen = torch.Generator("cuda:0").manual_seed(n)
+    spread = 2.0 ** -(torch.arange(n, device="cuda:0") % 5 * 3.0)[:, None, None]
+    x = torch.randn((n, 1, cin), generator=gen, device="cuda:0") * 4.0 + spread * torch.randn((n, tokens, cin), generator=gen, device="cuda:0")
+    codes, scales, x = checkpoint(x.reshape(n * tokens, cin).to(torch.bfloat16))
+    dy = torch.randn((n, tokens, cout), generator=gen, device="cuda:0").to(torch.bfloat16)
+    if tokens > 1:
+        dy[:, 1::2] = -dy[:, 0::2]
+    got = squared_norms(desc, codes, scales, dy)
+    for i in range(0, n, 500):
+        g, v = dy[i:i + 500].double().transpose(1, 2).contiguous(), x.view(n, tokens, cin)[i:i + 500].contiguous()
+        w, off = g @ v, (tokens + 2) * U * (g.abs() @ v.abs())
+        want = (w ** 2).sum((1, 2))
+        far = (2 * w.abs() * off + off ** 2).sum((1, 2)) + 256 * U * want
+        assert bool(((got[i:i + 500] - want).abs() <= torch.maximum(far, want / 3)).all())
+        assert torch.equal(got[i:i + 500] > 0.0, want > 0.0)         # (two tokens that round to one and cancel leave nothing)
