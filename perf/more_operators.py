@@ -1,0 +1,421 @@
+"""The operators on either side of a token model's blocks -- the normalisation of tokens with per-example gradients of its scale and shift, and the
+log probabilities of tokens with their gradient -- as cases that can be timed and compared.
+
+Kinds of case ("op"):
+
+  "norm"      layer norm of every token over its features (or RMS norm: the mean taken as zero)
+  "norm_back" gradient of the tokens, and per example the gradients of scale and shift with their squared norm
+  "score"     log probabilities of given tokens under rows of logits, their entropies, the `top` most likely alternatives
+  "loss"      the same log probabilities with the gradient of their weighted sum, in one call
+  "entropy"   gradient of log probabilities and entropies, from the statistics that the call before left
+
+`own` False: the plain form, elementary torch operations.  `own` True: the calls of this repository's library.
+"""
+from __future__ import annotations
+
+import math
+
+import torch
+
+own = False
+
+DEVICE = "cuda:0"
+DTYPES = {"bf16": torch.bfloat16, "f32": torch.float32}
+EPS = 1e-5
+
+
+# ---- cases ----------------------------------------------------------------------------------------------------------
+
+def _norm(op, n, tokens, features, dtype="bf16", rms=False, shift=True, ragged=False, gap=0):
+    """n examples of `tokens` tokens; gap: elements between one token's features and the next one's; ragged: examples have lengths of their own."""
+    return dict(op=op, n=n, tokens=tokens, features=features, dtype=dtype, rms=rms, shift=shift and not rms, ragged=ragged, gap=gap)
+
+
+def _score(op, n, tokens, vocab, dtype="bf16", top=0, ragged=False, gap=0, scale=1.0):
+    """Logits [n, tokens, vocab], `gap` elements between one row and the next; scale: of the logits."""
+    return dict(op=op, n=n, tokens=tokens, vocab=vocab, dtype=dtype, top=top, ragged=ragged, gap=gap, scale=scale)
+
+
+def listed():
+    return [
+        # one token of each of a few sequences that are being answered: latency
+        dict(name="norm_single_tokens", **_norm("norm", 8, 1, 768)),
+        # the tokens of a whole micro-step
+        dict(name="norm_micro_step", **_norm("norm", 16, 2048, 2048)),
+        # fp32 rows of an odd width that lie in a wider tensor, examples of different lengths
+        dict(name="norm_odd_strided_f32", **_norm("norm", 6, 1000, 1003, "f32", ragged=True, gap=14)),
+        # short examples in a batch, as a classifier of sentences trains on
+        dict(name="norm_back_short_ragged", **_norm("norm_back", 32, 64, 768, ragged=True)),
+        # the backward pass of the micro-step
+        dict(name="norm_back_micro_step", **_norm("norm_back", 16, 2048, 2048)),
+        # a few long examples of wide tokens, fp32, without mean and shift
+        dict(name="norm_back_rms_f32", **_norm("norm_back", 3, 511, 5000, "f32", rms=True)),
+        # the next token of each sequence that is being answered, with the alternatives to it
+        dict(name="score_next_token", **_score("score", 8, 1, 131072, top=8, scale=0.7)),
+        # log probabilities and entropies of whole texts
+        dict(name="score_texts", **_score("score", 8, 512, 32768)),
+        # the same with alternatives, fp32 rows of an odd width in a wider tensor
+        dict(name="score_top_odd_f32", **_score("score", 4, 300, 50021, "f32", top=5, ragged=True, gap=3)),
+        # short examples over a small vocabulary
+        dict(name="loss_short_ragged", **_score("loss", 32, 64, 1000, ragged=True)),
+        # the loss of a micro-step and what the output layer's gradient is made of
+        dict(name="loss_micro_step", **_score("loss", 8, 512, 32768)),
+        # a policy's tokens with a bonus for entropy
+        dict(name="entropy_odd", **_score("entropy", 16, 100, 100003, scale=1.25)),
+    ]
+
+
+def _log_int(rng, lo, hi):
+    return max(lo, min(hi, int(round(lo * (hi / lo) ** rng.random()))))
+
+
+def _cost(case):
+    w = work(case)
+    return max(w["bytes"] / 5e12, w["flops"] / 1e14)
+
+
+def draw(rng):
+    while True:
+        op = rng.choice(("norm", "norm_back", "norm_back", "score", "score", "loss", "loss", "entropy"))
+        dtype = rng.choice(("bf16", "bf16", "f32"))
+        n, tokens, gap = _log_int(rng, 1, 64), _log_int(rng, 1, 2048), rng.choice((0, 0, rng.randint(1, 40)))
+        if op in ("norm", "norm_back"):
+            rms = rng.random() < 0.3
+            features = rng.choice((_log_int(rng, 16, 8192), 64 * _log_int(rng, 1, 128)))
+            case = _norm(op, n, tokens, features, dtype, rms, rng.random() < 0.8, rng.random() < 0.5, gap)
+        else:
+            vocab = rng.choice((_log_int(rng, 50, 131072), 64 * _log_int(rng, 1, 2048)))
+            if rng.random() < 0.3:
+                tokens = 1
+            top = rng.choice((0, 1, rng.randint(2, 32))) if op == "score" else 0
+            case = _score(op, n, tokens, vocab, dtype, top, rng.random() < 0.4, gap, rng.choice((1.0, 1.0, 0.7, 1.25)))
+        if _cost(case) <= max(_cost(c) for c in listed() if c["op"] == op):
+            return case
+
+
+# ---- inputs ---------------------------------------------------------------------------------------------------------
+
+def _lengths(gen, n, most, ragged):
+    """int32 lengths of 0 .. most (one example of full length, and from four on one of none), or None."""
+    if not ragged:
+        return None
+    v = torch.randint(1, most + 1, (n,), generator=gen, device=DEVICE, dtype=torch.int32)
+    v[n // 2] = most
+    if n >= 4:
+        v[n // 4] = 0
+    return v
+
+
+def _rows(values, gap, dtype):
+    """[n, tokens, width] values as rows of a tensor that is `gap` elements wider."""
+    n, tokens, width = values.shape
+    wide = torch.zeros((n, tokens, width + gap), dtype=dtype, device=DEVICE)
+    x = wide[..., :width]
+    x.copy_(values)
+    return x
+
+
+def prepare(case, seed):
+    gen = torch.Generator(device=DEVICE)
+    gen.manual_seed(seed)
+    randn = lambda *shape: torch.randn(shape, generator=gen, device=DEVICE)  # noqa: E731
+    dtype, n, tokens, state = DTYPES[case["dtype"]], case["n"], case["tokens"], dict(case=case)
+    state["lengths"] = _lengths(gen, n, tokens, case["ragged"])
+    if case["op"] in ("norm", "norm_back"):
+        features = case["features"]
+        # what layers see: tokens with a mean and a size of their own, a few features that are far larger in every token
+        loud = torch.where(torch.rand((features,), generator=gen, device=DEVICE) < 0.01, 20.0, 1.0)
+        x = randn(n, tokens, features).mul_(loud).add_(randn(n, tokens, 1)).mul_(torch.exp(randn(n, tokens, 1)))
+        state["x"] = _rows(x, case["gap"], dtype)
+        state["gamma"] = randn(features).mul_(0.2).add_(1.0)
+        state["beta"] = randn(features).mul_(0.1) if case["shift"] else None
+        if case["op"] == "norm_back":
+            state["dy"] = _rows(randn(n, tokens, features).mul_(0.01), case["gap"], dtype)
+        return state
+    vocab = case["vocab"]
+    # tokens that are common everywhere, and rows from nearly certain to nearly even
+    x = randn(n, tokens, vocab).mul_(torch.exp(randn(n, tokens, 1).mul_(0.5)).mul_(2.0)).add_(randn(vocab))
+    state["logits"] = _rows(x, case["gap"], dtype)
+    state["targets"] = torch.randint(0, vocab, (n, tokens), generator=gen, device=DEVICE, dtype=torch.int32)
+    if case["op"] != "score":
+        state["targets"][torch.rand((n, tokens), generator=gen, device=DEVICE) < 0.05] = -1      # tokens that are not scored
+        state["d_logprobs"] = randn(n, tokens) if case["op"] == "entropy" else torch.rand((n, tokens), generator=gen, device=DEVICE).sub_(1.0).div_(tokens)
+    if case["op"] == "entropy":
+        state["d_entropy"] = torch.rand((n, tokens), generator=gen, device=DEVICE).mul_(0.1)
+        z, there = _scaled(state)
+        top, log_sum, _, h = _statistics(z)
+        state["stats"] = torch.stack((top, log_sum), 2).contiguous()
+        state["entropy"] = torch.where(there, h, 0.0)
+    return state
+
+
+# ---- the plain forms ------------------------------------------------------------------------------------------------
+
+def _there(lengths, n, tokens):
+    """[n, tokens]: which tokens an example has."""
+    if lengths is None:
+        return torch.ones((n, tokens), dtype=torch.bool, device=DEVICE)
+    return torch.arange(tokens, device=DEVICE)[None, :] < lengths[:, None]
+
+
+def _normalised(case, x):
+    """(x - mean) / size in 32 bits, and 1 / size."""
+    x = x.float()
+    if not case["rms"]:
+        x = x - x.mean(2, keepdim=True)
+    r = 1.0 / torch.sqrt((x * x).mean(2, keepdim=True) + EPS)
+    return x * r, r
+
+
+def _plain_norm(state):
+    case, x = state["case"], state["x"]
+    y, _ = _normalised(case, x)
+    y = y * state["gamma"]
+    if case["shift"]:
+        y = y + state["beta"]
+    return torch.where(_there(state["lengths"], case["n"], case["tokens"])[:, :, None], y, 0.0).to(x.dtype)
+
+
+def _plain_norm_back(state):
+    case, x = state["case"], state["x"]
+    there = _there(state["lengths"], case["n"], case["tokens"])[:, :, None]
+    xhat, r = _normalised(case, x)
+    dy = torch.where(there, state["dy"].float(), 0.0)
+    g_w, g_b = (dy * xhat).sum(1), dy.sum(1) if case["shift"] else None
+    a = dy * state["gamma"]
+    dx = a - xhat * (a * xhat).mean(2, keepdim=True)
+    if not case["rms"]:
+        dx = dx - a.mean(2, keepdim=True)
+    sq = g_w.double().square().sum(1)
+    out = {"dx": (dx * r).to(x.dtype), "g_w": g_w}
+    if case["shift"]:
+        out["g_b"] = g_b
+        sq = sq + g_b.double().square().sum(1)
+    out["sqnorm"] = sq.float()
+    return out
+
+
+def _scaled(state):
+    case = state["case"]
+    return state["logits"].float() * case["scale"], _there(state["lengths"], case["n"], case["tokens"])
+
+
+def _statistics(z):
+    """Of rows of scaled logits: the largest, log of the sum of exp(z - largest), the log probabilities, the entropy."""
+    top = z.amax(2)
+    d = z - top[:, :, None]
+    e = torch.exp(d)
+    s = e.sum(2)
+    log_sum = torch.log(s)
+    return top, log_sum, d - log_sum[:, :, None], log_sum - (e * d).sum(2) / s
+
+
+def _scored(state, there):
+    """Which rows have a token that is scored, and that token."""
+    t = state["targets"].long()
+    return there & (t >= 0) & (t < state["case"]["vocab"]), t.clamp(0, state["case"]["vocab"] - 1)
+
+
+def _plain_score(state):
+    case = state["case"]
+    z, there = _scaled(state)
+    _, _, logp, h = _statistics(z)
+    scored, t = _scored(state, there)
+    out = {"logprobs": torch.where(scored, logp.gather(2, t[:, :, None])[:, :, 0], 0.0), "entropy": torch.where(there, h, 0.0)}
+    if case["top"]:
+        order = torch.sort(state["logits"], dim=2, descending=True, stable=True).indices[:, :, :case["top"]]
+        out["top_logprobs"] = torch.where(there[:, :, None], logp.gather(2, order), 0.0)
+        out["top_tokens"] = torch.where(there[:, :, None], order, -1).to(torch.int32)
+    return out
+
+
+def _plain_gradient(state):
+    case, dtype = state["case"], state["logits"].dtype
+    z, there = _scaled(state)
+    scored, t = _scored(state, there)
+    a = torch.where(scored, state["d_logprobs"], 0.0)
+    if case["op"] == "loss":
+        _, _, logp, _ = _statistics(z)
+    else:
+        logp = z - state["stats"][:, :, :1] - state["stats"][:, :, 1:]
+    p = torch.exp(logp)
+    d = -a[:, :, None] * p
+    if case["op"] == "entropy":
+        b = torch.where(there, state["d_entropy"], 0.0)
+        d = d - b[:, :, None] * p * (logp + state["entropy"][:, :, None])
+    d.scatter_add_(2, t[:, :, None], a[:, :, None])
+    out = {"dlogits": (torch.where(there[:, :, None], d, 0.0) * case["scale"]).to(dtype)}
+    if case["op"] == "loss":
+        out["logprobs"] = torch.where(scored, logp.gather(2, t[:, :, None])[:, :, 0], 0.0)
+    return out
+
+
+# ---- one pass -------------------------------------------------------------------------------------------------------
+
+def run(state):
+    if own:
+        return _run_own(state)
+    op = state["case"]["op"]
+    if op == "norm":
+        return _plain_norm(state)
+    if op == "norm_back":
+        return _plain_norm_back(state)
+    if op == "score":
+        return _plain_score(state)
+    return _plain_gradient(state)
+
+
+def _plan(state):
+    """What a program keeps from call to call: the descriptor, output buffers and the workspace."""
+    import paper_2109_12191_amd as dp
+    case, plan = state["case"], {}
+    dtype = dp.DP_BF16 if case["dtype"] == "bf16" else dp.DP_F32
+    n, tokens = case["n"], case["tokens"]
+    empty = lambda *shape, dtype=torch.float32: torch.empty(shape, dtype=dtype, device=DEVICE)  # noqa: E731
+    wide = lambda width: empty(n, tokens, width + case["gap"], dtype=DTYPES[case["dtype"]])[..., :width]  # noqa: E731
+    if case["op"] in ("norm", "norm_back"):
+        features = case["features"]
+        plan["desc"] = dp.NormDesc(in_dtype=dtype, n=n, tokens=tokens, features=features, rms=case["rms"], eps=EPS, row_stride=features + case["gap"])
+        plan["out"] = wide(features)
+        if case["op"] == "norm_back":
+            plan["stride"] = (features + 3) // 4 * 4                # rows of gradients begin at whole 16 bytes
+            plan["g_w"] = empty(n, plan["stride"])[:, :features]
+            plan["g_b"] = empty(n, plan["stride"])[:, :features] if case["shift"] else None
+            plan["sqnorm"] = empty(n)
+            plan["ws"] = empty(max(16, dp.dp_layer_norm_workspace_bytes(plan["desc"])), dtype=torch.uint8)
+        return plan
+    vocab = case["vocab"]
+    plan["desc"] = dp.LogprobDesc(in_dtype=dtype, n=n, tokens=tokens, vocab=vocab, top=case["top"], scale=case["scale"], row_stride=vocab + case["gap"])
+    plan["ws"] = empty(max(16, dp.dp_token_logprobs_workspace_bytes(plan["desc"])), dtype=torch.uint8)
+    plan["logprobs"] = empty(n, tokens)
+    if case["op"] == "score":
+        plan["entropy"] = empty(n, tokens)
+        plan["top_logprobs"] = empty(n, tokens, case["top"]) if case["top"] else None
+        plan["top_tokens"] = empty(n, tokens, case["top"], dtype=torch.int32) if case["top"] else None
+    else:
+        plan["out"] = wide(vocab)
+    return plan
+
+
+def _run_own(state):
+    import paper_2109_12191_amd as dp
+    if "plan" not in state:
+        state["plan"] = _plan(state)
+    case, plan = state["case"], state["plan"]
+    op, lengths = case["op"], state["lengths"]
+    if op == "norm":
+        dp.dp_layer_norm(plan["desc"], state["x"], state["gamma"], state["beta"], plan["out"], lengths=lengths)
+        return plan["out"]
+    if op == "norm_back":
+        dp.dp_layer_norm_backward(plan["desc"], state["x"], state["gamma"], state["dy"], plan["out"], plan["g_w"], plan["g_b"], plan["sqnorm"],
+                                  plan["ws"], lengths=lengths, g_stride=plan["stride"])
+        out = {"dx": plan["out"], "g_w": plan["g_w"], "sqnorm": plan["sqnorm"]}
+        if case["shift"]:
+            out["g_b"] = plan["g_b"]
+        return out
+    if op == "score":
+        dp.dp_token_logprobs(plan["desc"], state["logits"], state["targets"], plan["logprobs"], plan["entropy"], None, plan["top_logprobs"],
+                             plan["top_tokens"], plan["ws"], lengths=lengths)
+        out = {"logprobs": plan["logprobs"], "entropy": plan["entropy"]}
+        if case["top"]:
+            out["top_logprobs"], out["top_tokens"] = plan["top_logprobs"], plan["top_tokens"]
+        return out
+    if op == "loss":
+        dp.dp_token_logprobs_backward(plan["desc"], state["logits"], state["targets"], None, state["d_logprobs"], plan["out"], plan["ws"],
+                                      logprobs=plan["logprobs"], lengths=lengths)
+        return {"dlogits": plan["out"], "logprobs": plan["logprobs"]}
+    dp.dp_token_logprobs_backward(plan["desc"], state["logits"], state["targets"], state["stats"], state["d_logprobs"], plan["out"], plan["ws"],
+                                  entropy=state["entropy"], d_entropy=state["d_entropy"], lengths=lengths)
+    return {"dlogits": plan["out"]}
+
+
+# ---- what a pass cannot do without ----------------------------------------------------------------------------------
+
+def work(case):
+    """Bytes read and written once, and operations; lengths counted as full."""
+    size = 2 if case["dtype"] == "bf16" else 4
+    rows = case["n"] * case["tokens"]
+    if case["op"] in ("norm", "norm_back"):
+        f, affine = case["features"], 2 if case["shift"] else 1
+        if case["op"] == "norm":
+            return {"bytes": 2 * size * rows * f + 4 * affine * f, "flops": 8 * rows * f}
+        return {"bytes": 3 * size * rows * f + 4 * f + 4 * case["n"] * (affine * f + 1), "flops": 16 * rows * f}
+    v = case["vocab"]
+    if case["op"] == "score":
+        return {"bytes": size * rows * v + rows * (12 + 8 * case["top"]), "flops": 6 * rows * v}
+    return {"bytes": 2 * size * rows * v + rows * (12 if case["op"] == "loss" else 24), "flops": 8 * rows * v}
+
+
+# ---- the definitions in 64 bits -------------------------------------------------------------------------------------
+
+def exact(case, seed):
+    state = prepare(case, seed)
+    n, tokens = case["n"], case["tokens"]
+    lengths = [tokens] * n if state["lengths"] is None else state["lengths"].tolist()
+    each = [_exact_norms(state, i, lengths[i]) if case["op"] in ("norm", "norm_back") else _exact_rows(state, i, lengths[i]) for i in range(n)]
+    if case["op"] == "norm":
+        return torch.stack([e["y"] for e in each])
+    return {k: torch.stack([e[k] for e in each]) for k in each[0]}
+
+
+def _exact_norms(state, i, length):
+    case = state["case"]
+    tokens, features = case["tokens"], case["features"]
+    x, gamma = state["x"][i, :length].double(), state["gamma"].double()
+    mean = torch.zeros((length, 1), dtype=torch.float64, device=DEVICE) if case["rms"] else x.sum(1, keepdim=True) / features
+    size = (((x - mean) ** 2).sum(1, keepdim=True) / features + EPS).sqrt()
+    xhat = (x - mean) / size
+    whole = torch.zeros((tokens, features), dtype=torch.float64, device=DEVICE)
+    if case["op"] == "norm":
+        whole[:length] = xhat * gamma + (state["beta"].double() if case["shift"] else 0.0)
+        return {"y": whole}
+    dy = state["dy"][i, :length].double()
+    # the Jacobian of xhat applied to gamma dy: (I - 1 1^T / F - xhat xhat^T / F) / size
+    a = dy * gamma
+    along = (a * xhat).sum(1, keepdim=True) / features
+    level = torch.zeros_like(along) if case["rms"] else a.sum(1, keepdim=True) / features
+    whole[:length] = (a - level - xhat * along) / size
+    out = {"dx": whole, "g_w": (dy * xhat).sum(0)}
+    sq = (out["g_w"] ** 2).sum()
+    if case["shift"]:
+        out["g_b"] = dy.sum(0)
+        sq = sq + (out["g_b"] ** 2).sum()
+    out["sqnorm"] = sq
+    return out
+
+
+def _exact_rows(state, i, length):
+    case = state["case"]
+    tokens, vocab = case["tokens"], case["vocab"]
+    f64 = dict(dtype=torch.float64, device=DEVICE)
+    x = state["logits"][i, :length]
+    logp = torch.log_softmax(x.double() * case["scale"], 1)
+    target = state["targets"][i, :length].long()
+    scored = (target >= 0) & (target < vocab)
+    rows = torch.arange(length, device=DEVICE)
+    logprobs = torch.zeros(tokens, **f64)
+    logprobs[:length][scored] = logp[rows[scored], target[scored]]
+    entropy = -(logp.exp() * logp).sum(1)
+    if case["op"] == "score":
+        h = torch.zeros(tokens, **f64)
+        h[:length] = entropy
+        out = {"logprobs": logprobs, "entropy": h}
+        if case["top"]:
+            out["top_logprobs"] = torch.zeros((tokens, case["top"]), **f64)
+            out["top_tokens"] = torch.full((tokens, case["top"]), -1, dtype=torch.int32, device=DEVICE)
+            left = x.double()
+            for k in range(case["top"]):
+                best = (left == left.amax(1, keepdim=True)).int().argmax(1)          # the first of the largest
+                out["top_logprobs"][:length, k] = logp[rows, best]
+                out["top_tokens"][:length, k] = best.int()
+                left[rows, best] = -math.inf
+        return out
+    p = logp.exp()
+    a = torch.where(scored, state["d_logprobs"][i, :length].double(), 0.0)[:, None]
+    whole = torch.zeros((tokens, vocab), **f64)
+    g = -a * p
+    g[rows[scored], target[scored]] += a[scored, 0]
+    if case["op"] == "entropy":
+        g = g - state["d_entropy"][i, :length].double()[:, None] * p * (logp + entropy[:, None])
+    whole[:length] = g * case["scale"]
+    return {"dlogits": whole, "logprobs": logprobs} if case["op"] == "loss" else {"dlogits": whole}
