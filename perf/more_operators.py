@@ -143,8 +143,8 @@ def prepare(case, seed):
     if case["op"] == "entropy":
         state["d_entropy"] = torch.rand((n, tokens), generator=gen, device=DEVICE).mul_(0.1)
         z, there = _scaled(state)
-        top, log_sum, _, h = _statistics(z)
-        state["stats"] = torch.stack((top, log_sum), 2).contiguous()
+        _, log_sum, _, h = _statistics(z)
+        state["stats"] = torch.stack((state["logits"].float().amax(2), log_sum), 2).contiguous()         # (the largest logit as it is)
         state["entropy"] = torch.where(there, h, 0.0)
     return state
 
@@ -237,7 +237,7 @@ def _plain_gradient(state):
     if case["op"] == "loss":
         _, _, logp, _ = _statistics(z)
     else:
-        logp = z - state["stats"][:, :, :1] - state["stats"][:, :, 1:]
+        logp = (state["logits"].float() - state["stats"][:, :, :1]) * case["scale"] - state["stats"][:, :, 1:]
     p = torch.exp(logp)
     d = -a[:, :, None] * p
     if case["op"] == "entropy":
