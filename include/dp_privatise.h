@@ -499,6 +499,72 @@ dp_status dp_bias_softmax_backward(const dp_bias_desc *desc /*[host]*/, const vo
                                    const int32_t *key_lengths, void *dscores, float *g_table, size_t g_stride, float *sqnorm, void *ws,
                                    size_t ws_bytes, dp_stream stream);
 
+/* ---- Normalisation of tokens over their features, with per-example gradients of its scale and shift --------------------
+ *   y = gamma * xhat + beta,  xhat = (x - mean) / sqrt(mean((x - mean)^2) + eps),  means over the features of a token (RMS: mean(x) is taken as 0) */
+typedef struct dp_norm_desc {
+    int in_dtype;            /* dp_dtype of x, y and their gradients; gamma, beta and their gradients are fp32 */
+    int n, tokens, features; /* tensors are [n, tokens] rows of `features` values; each >= 1, features at most 2^20 */
+    int rms;
+    float eps;               /* finite, at least 1e-30 */
+    size_t row_stride;       /* elements from one row to the next, of every tensor of the call; 0: features */
+} dp_norm_desc;
+
+/* gamma, beta [device] [features], or NULL: ones, zeros.  x, y [device], aligned to their element; y may be x.
+ * lengths [device] [n] int32 tokens of each example (taken as 0 .. tokens), or NULL: all.  Rows of y beyond them are zeros, and what lies there
+ * in x is not used, whatever it is.  A row with a NaN or an infinity is NaN; one whose squared deviations add up beyond fp32's range is beta
+ * (deviations of 10^19 / sqrt(features) are safe).                                                                                */
+dp_status dp_layer_norm(const dp_norm_desc *desc /*[host]*/, const void *x, const float *gamma, const float *beta, const int32_t *lengths, void *y,
+                        dp_stream stream);
+
+/* Its backward pass, with H1 and H2 of gamma and beta; the statistics are worked out again from x:
+ *   dx = (a - mean(a) - xhat * mean(a * xhat)) / sqrt(mean((x - mean)^2) + eps),  a = gamma * dy           (RMS: without mean(a))
+ *   g_w[i] = sum_t dy * xhat,   g_b[i] = sum_t dy over the tokens that example i has;   sqnorm[i] = |g_w[i]|^2 + |g_b[i]|^2
+ * dx [device] in_dtype, zeros beyond the lengths; may be x or dy; NULL: not wanted (a model's first layer).
+ * g_w, g_b [device] fp32, example i's [features] at + i * g_stride, overwritten (g_stride 0: packed; else a multiple of 4, at least features),
+ * ready for dp_clip_accumulate; NULL: not wanted (g_b and sqnorm need g_w; without g_b the norm is g_w's).  sqnorm [device] [n] or NULL.
+ * ws: dp_layer_norm_workspace_bytes(desc).  Sums run in a fixed order: the same inputs give the same bits on every call.             */
+size_t dp_layer_norm_workspace_bytes(const dp_norm_desc *desc /*[host]*/);
+dp_status dp_layer_norm_backward(const dp_norm_desc *desc /*[host]*/, const void *x, const float *gamma, const void *dy, const int32_t *lengths,
+                                 void *dx, float *g_w, float *g_b, size_t g_stride, float *sqnorm, void *ws, size_t ws_bytes, dp_stream stream);
+
+/* ---- Log probabilities of tokens under rows of logits, and their gradient -----------------------------------------------
+ *   z = scale * logits,   logp_v = z_v - log(sum_u exp(z_u)),   p = exp(logp),   H = -sum_v p_v * logp_v                            */
+typedef struct dp_logprob_desc {
+    int in_dtype;            /* dp_dtype of logits and their gradient */
+    int n, tokens, vocab;    /* tensors are [n, tokens] rows of `vocab` values; each >= 1, vocab at most 2^24 */
+    int top;                 /* alternatives of a row, 0 .. 32 */
+    float scale;             /* finite, > 0 */
+    size_t row_stride;       /* elements from one row to the next, of logits and their gradient; 0: vocab */
+} dp_logprob_desc;
+
+/* logprobs     [device] [n, tokens]: logp of the row's target; 0 where the target is none of 0 .. vocab - 1.  NULL: not wanted
+ * entropy      [device] [n, tokens]: H.  NULL: not wanted
+ * stats        [device] [n, tokens, 2]: the largest logit m and log(sum exp(z - scale * m)), for dp_token_logprobs_backward.  NULL: not wanted
+ * top_logprobs, top_tokens [device] [n, tokens, top]: the `top` tokens of the largest logits, largest first, equal ones by their number, and their logp;
+ *              -1 and -inf where a row has fewer logits above -inf.  top_logprobs NULL: not wanted
+ * targets      [device] [n, tokens] int32; needed for logprobs.
+ * lengths      [device] [n] int32 tokens of each example (taken as 0 .. tokens), or NULL: all.  Rows beyond have logprob, entropy, stats and
+ *              top_logprobs 0 and top_tokens -1, and what lies there in logits is not used, whatever it is.
+ * A logit of -inf has p = 0 and logp = -inf.  A row of nothing else has logp = -inf, entropy 0, stats (0, inf) and no alternatives.  A row with a NaN or
+ * +inf has NaN for all of logprob, entropy, stats and top_logprobs, and top_tokens -1.
+ * logits [device] in_dtype, aligned to their element.  stats: aligned to 8 bytes.  ws: dp_token_logprobs_workspace_bytes(desc), which may be 0. */
+size_t dp_token_logprobs_workspace_bytes(const dp_logprob_desc *desc /*[host]*/);
+dp_status dp_token_logprobs(const dp_logprob_desc *desc /*[host]*/, const void *logits, const int32_t *targets, const int32_t *lengths,
+                            float *logprobs, float *entropy, float *stats, float *top_logprobs, int32_t *top_tokens, void *ws, size_t ws_bytes,
+                            dp_stream stream);
+
+/* Gradient of sum(d_logprobs * logprobs) + sum(d_entropy * entropy):
+ *   dlogits_v = scale * (d_logprobs * ([v is the target] - p_v) - d_entropy * p_v * (logp_v + H))
+ * d_logprobs, d_entropy [device] [n, tokens], or NULL: zeros (not both).  Rows without a target have no share of d_logprobs, whatever it is.
+ * stats, entropy [device] as dp_token_logprobs left them (entropy only for d_entropy); stats NULL: worked out in the same call -- a training step that
+ *              knows its tokens' weights beforehand needs this call alone.  A row of logits is then read once, up to 131072 bf16 or 65536 fp32.
+ * logprobs     [device] [n, tokens] or NULL: written as dp_token_logprobs does.
+ * dlogits      [device] in_dtype, zeros beyond the lengths and in rows of nothing but -inf, NaN in rows with a NaN or +inf; may be logits.
+ * desc->top has to be 0.  ws: dp_token_logprobs_workspace_bytes(desc).                                                           */
+dp_status dp_token_logprobs_backward(const dp_logprob_desc *desc /*[host]*/, const void *logits, const int32_t *targets, const int32_t *lengths,
+                                     const float *stats, const float *entropy, const float *d_logprobs, const float *d_entropy, float *logprobs,
+                                     void *dlogits, void *ws, size_t ws_bytes, dp_stream stream);
+
 /* The raw 32-bit Philox word behind each element of the stream above (diagnostic; lets a
  * test compare the integer stream bit for bit).  raw [device] [p] uint32.                      */
 dp_status dp_philox_raw(uint32_t *raw, size_t p, uint64_t seed, uint64_t step, uint32_t tensor_id,

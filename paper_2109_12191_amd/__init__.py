@@ -12,7 +12,9 @@ from .binding import (DP_BF16, DP_CONV2D, DP_DENSE, DP_F32, DP_GN_AFFINE, DP_NCH
                       dp_per_example_grad_partials, dp_per_example_grad_batch, dp_clip_accumulate_recompute_batch, LayerBatch, PartialTable, dp_per_example_grad, dp_per_example_grad_static, dp_static_scratch_bytes, dp_philox_raw, dp_profile_next_contraction, dp_version,
                       dp_batch_workspace_bytes, dp_weight_count, dp_workspace_bytes, lib_path, load_library, make_desc,
                       dp_checkpoint_pitch, dp_checkpoint_write, dp_checkpoint_read, dp_checkpoint_workspace_bytes, dp_checkpoint_example_grad, dp_checkpoint_clip_accumulate,
-                      BiasDesc, DP_QUERIES_AT_END, dp_bias_bucket, dp_bias_softmax, dp_bias_workspace_bytes, dp_bias_softmax_backward)
+                      BiasDesc, DP_QUERIES_AT_END, dp_bias_bucket, dp_bias_softmax, dp_bias_workspace_bytes, dp_bias_softmax_backward,
+                      NormDesc, dp_layer_norm, dp_layer_norm_workspace_bytes, dp_layer_norm_backward,
+                      LogprobDesc, dp_token_logprobs_workspace_bytes, dp_token_logprobs, dp_token_logprobs_backward)
 from .attention import PrivateAttention
 from .pipeline import PrivatiseStep
 
@@ -25,4 +27,6 @@ __all__ = [
     "dp_batch_workspace_bytes", "dp_workspace_bytes", "lib_path", "load_library", "make_desc", "PrivatiseStep", "PrivateAttention",
     "dp_checkpoint_pitch", "dp_checkpoint_write", "dp_checkpoint_read", "dp_checkpoint_workspace_bytes", "dp_checkpoint_example_grad", "dp_checkpoint_clip_accumulate",
     "BiasDesc", "DP_QUERIES_AT_END", "dp_bias_bucket", "dp_bias_softmax", "dp_bias_workspace_bytes", "dp_bias_softmax_backward",
+    "NormDesc", "dp_layer_norm", "dp_layer_norm_workspace_bytes", "dp_layer_norm_backward",
+    "LogprobDesc", "dp_token_logprobs_workspace_bytes", "dp_token_logprobs", "dp_token_logprobs_backward",
 ]

@@ -44,6 +44,18 @@ class BiasDesc(C.Structure):
                 ("query_offset", C.c_int), ("scale", C.c_float), ("row_stride", C.c_size_t)]
 
 
+class NormDesc(C.Structure):
+    """Mirror of dp_norm_desc."""
+    _fields_ = [("in_dtype", C.c_int), ("n", C.c_int), ("tokens", C.c_int), ("features", C.c_int), ("rms", C.c_int), ("eps", C.c_float),
+                ("row_stride", C.c_size_t)]
+
+
+class LogprobDesc(C.Structure):
+    """Mirror of dp_logprob_desc."""
+    _fields_ = [("in_dtype", C.c_int), ("n", C.c_int), ("tokens", C.c_int), ("vocab", C.c_int), ("top", C.c_int), ("scale", C.c_float),
+                ("row_stride", C.c_size_t)]
+
+
 def lib_path() -> str:
     return _LIB_PATH
 
@@ -58,7 +70,7 @@ def load_library():
                            "(or __graft_entry__.build()); there is no CPU fallback")
     lib = C.CDLL(_LIB_PATH)
     vp, sz, u64, u32, fl, it = C.c_void_p, C.c_size_t, C.c_uint64, C.c_uint32, C.c_float, C.c_int
-    dpp, dbp = C.POINTER(LayerDesc), C.POINTER(BiasDesc)
+    dpp, dbp, dnp, dlp = C.POINTER(LayerDesc), C.POINTER(BiasDesc), C.POINTER(NormDesc), C.POINTER(LogprobDesc)
     sigs = {
         "dp_group_clip_bounds": (it, [fl, it, vp, vp]),
         "dp_weight_count": (sz, [dpp]),
@@ -105,6 +117,12 @@ def load_library():
         "dp_bias_softmax": (it, [dbp, vp, vp, vp, vp, vp, vp]),
         "dp_bias_workspace_bytes": (sz, [dbp]),
         "dp_bias_softmax_backward": (it, [dbp, vp, vp, vp, vp, vp, vp, sz, vp, vp, sz, vp]),
+        "dp_layer_norm": (it, [dnp, vp, vp, vp, vp, vp, vp]),
+        "dp_layer_norm_workspace_bytes": (sz, [dnp]),
+        "dp_layer_norm_backward": (it, [dnp, vp, vp, vp, vp, vp, vp, vp, sz, vp, vp, sz, vp]),
+        "dp_token_logprobs_workspace_bytes": (sz, [dlp]),
+        "dp_token_logprobs": (it, [dlp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]),
+        "dp_token_logprobs_backward": (it, [dlp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]),
         "dp_profile_next_contraction": (it, [vp, vp]),
         "dp_last_error": (C.c_char_p, []),
         "dp_version": (C.c_char_p, []),
@@ -127,6 +145,8 @@ EXPORTED = ("dp_group_clip_bounds", "dp_weight_count", "dp_bias_count", "dp_work
             "dp_clip_factors", "dp_clip_accumulate", "dp_clip_accumulate_segments", "dp_clip_accumulate_recompute", "dp_add_noise_finalize", "dp_add_noise_finalize_update", "dp_add_example_noise",
             "dp_checkpoint_pitch", "dp_checkpoint_write", "dp_checkpoint_read", "dp_checkpoint_workspace_bytes", "dp_checkpoint_example_grad",
             "dp_checkpoint_clip_accumulate", "dp_bias_bucket", "dp_bias_softmax", "dp_bias_workspace_bytes", "dp_bias_softmax_backward",
+            "dp_layer_norm", "dp_layer_norm_workspace_bytes", "dp_layer_norm_backward",
+            "dp_token_logprobs_workspace_bytes", "dp_token_logprobs", "dp_token_logprobs_backward",
             "dp_add_noise_finalize_flat", "dp_philox_raw", "dp_profile_next_contraction", "dp_last_error", "dp_version")
 
 
@@ -538,3 +558,47 @@ def dp_bias_softmax_backward(desc: BiasDesc, probs, dprobs, dscores, g_table, sq
                                           _lengths(key_lengths, desc.n, "key_lengths"), _ptr(dscores),
                                                    _ptr(g_table), g_stride, _ptr(sqnorm), _ptr(ws),
                                                    _nbytes(ws) if ws_bytes is None else ws_bytes, _stream(stream)))
+
+
+# ---- normalisation of tokens over their features ---------------------------------------------------------------------
+
+def dp_layer_norm(desc: NormDesc, x, gamma, beta, y, lengths=None, stream=None):
+    """Layer norm (desc.rms: RMS norm) of every token of x [n, tokens, features] into y."""
+    _check(load_library().dp_layer_norm(C.byref(desc), _ptr(x), _ptr(gamma), _ptr(beta), _lengths(lengths, desc.n, "lengths"), _ptr(y), _stream(stream)))
+
+
+def dp_layer_norm_workspace_bytes(desc: NormDesc) -> int:
+    return int(load_library().dp_layer_norm_workspace_bytes(C.byref(desc)))
+
+
+def dp_layer_norm_backward(desc: NormDesc, x, gamma, dy, dx, g_w, g_b, sqnorm, ws, lengths=None, g_stride: int = 0,
+                           ws_bytes: Optional[int] = None, stream=None):
+    """Gradient of the tokens, and per example the gradients of gamma and beta and their squared norm."""
+    _check(load_library().dp_layer_norm_backward(C.byref(desc), _ptr(x), _ptr(gamma), _ptr(dy), _lengths(lengths, desc.n, "lengths"), _ptr(dx),
+                                                 _ptr(g_w), _ptr(g_b), g_stride, _ptr(sqnorm), _ptr(ws),
+                                                 _nbytes(ws) if ws_bytes is None else ws_bytes, _stream(stream)))
+
+
+# ---- log probabilities of tokens -------------------------------------------------------------------------------------
+
+def dp_token_logprobs_workspace_bytes(desc: LogprobDesc) -> int:
+    return int(load_library().dp_token_logprobs_workspace_bytes(C.byref(desc)))
+
+
+def dp_token_logprobs(desc: LogprobDesc, logits, targets, logprobs, entropy, stats, top_logprobs, top_tokens, ws, lengths=None,
+                      ws_bytes: Optional[int] = None, stream=None):
+    """Log probabilities of targets (int32 [n, tokens]) under rows of logits, entropies, statistics for the backward pass, the most likely tokens; any
+    of the results may be None."""
+    _check(load_library().dp_token_logprobs(C.byref(desc), _ptr(logits), _lengths(targets, desc.n * desc.tokens, "targets"),
+                                            _lengths(lengths, desc.n, "lengths"), _ptr(logprobs), _ptr(entropy), _ptr(stats), _ptr(top_logprobs),
+                                            _ptr(top_tokens), _ptr(ws), _nbytes(ws) if ws_bytes is None else ws_bytes, _stream(stream)))
+
+
+def dp_token_logprobs_backward(desc: LogprobDesc, logits, targets, stats, d_logprobs, dlogits, ws, entropy=None, d_entropy=None, logprobs=None,
+                               lengths=None, ws_bytes: Optional[int] = None, stream=None):
+    """Gradient of the logits from those of log probabilities and entropies; stats None: worked out in the same call, with the log probabilities
+    where there is a place for them."""
+    _check(load_library().dp_token_logprobs_backward(C.byref(desc), _ptr(logits), _lengths(targets, desc.n * desc.tokens, "targets"),
+                                                     _lengths(lengths, desc.n, "lengths"), _ptr(stats), _ptr(entropy), _ptr(d_logprobs),
+                                                     _ptr(d_entropy), _ptr(logprobs), _ptr(dlogits), _ptr(ws),
+                                                     _nbytes(ws) if ws_bytes is None else ws_bytes, _stream(stream)))

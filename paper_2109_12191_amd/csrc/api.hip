@@ -1236,4 +1236,136 @@ dp_status dp_bias_softmax_backward(const dp_bias_desc *desc, const void *probs, 
                                         static_cast<hipStream_t>(stream));
 }
 
+// ---- normalisation of tokens over their features ---------------------------------------------
+
+static dp_status make_norm_geo(const dp_norm_desc *d, NormGeo &g)
+{
+    if (!d) return fail(DP_ERR_INVALID_ARG, "descriptor is NULL");
+    if (d->in_dtype != DP_F32 && d->in_dtype != DP_BF16) return fail(DP_ERR_INVALID_ARG, "unknown input dtype %d", d->in_dtype);
+    if (d->n < 1 || d->tokens < 1 || d->features < 1)
+        return fail(DP_ERR_INVALID_ARG, "non-positive dimension (n %d tokens %d features %d)", d->n, d->tokens, d->features);
+    if (!std::isfinite(d->eps) || !(d->eps >= 1e-30f)) return fail(DP_ERR_INVALID_ARG, "eps must be finite and at least 1e-30");
+    if (d->row_stride && d->row_stride < (size_t)d->features) return fail(DP_ERR_INVALID_ARG, "row_stride smaller than the features");
+    g.bf16 = d->in_dtype == DP_BF16; g.n = d->n; g.tokens = d->tokens; g.features = d->features; g.rms = d->rms ? 1 : 0;
+    g.eps = d->eps;
+    g.row_stride = d->row_stride ? d->row_stride : (size_t)d->features;
+    if (d->features > (1 << 20)) return fail(DP_ERR_UNSUPPORTED, "more than 2^20 features");
+    if ((size_t)g.n * g.tokens >= ((size_t)1 << 31) || g.row_stride >= ((size_t)1 << 40)) return fail(DP_ERR_UNSUPPORTED, "2^31 rows or more");
+    return DP_OK;
+}
+
+dp_status dp_layer_norm(const dp_norm_desc *desc, const void *x, const float *gamma, const float *beta, const int32_t *lengths, void *y,
+                        dp_stream stream)
+{
+    NormGeo g;
+    DP_TRY(make_norm_geo(desc, g));
+    DP_TRY(check_rows(x, "x", desc->in_dtype));
+    DP_TRY(check_rows(y, "y", desc->in_dtype));
+    DP_TRY(check_ptr(gamma, "gamma", false, 4));
+    DP_TRY(check_ptr(beta, "beta", false, 4));
+    DP_TRY(check_ptr(lengths, "lengths", false, 4));
+    g_err[0] = 0;
+    return launch_norm(g, x, gamma, beta, lengths, y, static_cast<hipStream_t>(stream));
+}
+
+size_t dp_layer_norm_workspace_bytes(const dp_norm_desc *desc)
+{
+    NormGeo g;
+    return make_norm_geo(desc, g) == DP_OK ? norm_ws_bytes(g) : 0;
+}
+
+dp_status dp_layer_norm_backward(const dp_norm_desc *desc, const void *x, const float *gamma, const void *dy, const int32_t *lengths, void *dx,
+                                 float *g_w, float *g_b, size_t g_stride, float *sqnorm, void *ws, size_t ws_bytes, dp_stream stream)
+{
+    NormGeo g;
+    DP_TRY(make_norm_geo(desc, g));
+    DP_TRY(check_rows(x, "x", desc->in_dtype));
+    DP_TRY(check_rows(dy, "dy", desc->in_dtype));
+    DP_TRY(check_rows(dx, "dx", desc->in_dtype, false));
+    DP_TRY(check_ptr(gamma, "gamma", false, 4));
+    DP_TRY(check_ptr(lengths, "lengths", false, 4));
+    DP_TRY(check_ptr(g_w, "g_w", false));
+    DP_TRY(check_ptr(g_b, "g_b", false));
+    DP_TRY(check_ptr(sqnorm, "sqnorm", false, 4));
+    if (!dx && !g_w) return fail(DP_ERR_INVALID_ARG, "nothing to compute: dx and g_w are both NULL");
+    if (!g_w && (g_b || sqnorm)) return fail(DP_ERR_INVALID_ARG, "g_b or sqnorm given without g_w");
+    if (g_stride) {
+        if (g_stride % 4) return fail(DP_ERR_INVALID_ARG, "g_stride must be a multiple of 4");
+        if (g_stride < (size_t)g.features) return fail(DP_ERR_INVALID_ARG, "g_stride smaller than the features");
+    }
+    DP_TRY(check_room(norm_ws_bytes(g), ws, ws_bytes));
+    g_err[0] = 0;
+    return launch_norm_backward(g, x, gamma, dy, lengths, dx, g_w, g_b, g_stride ? g_stride : (size_t)g.features, sqnorm, ws,
+                                static_cast<hipStream_t>(stream));
+}
+
+// ---- log probabilities of tokens -------------------------------------------------------------
+
+static dp_status make_logprob_geo(const dp_logprob_desc *d, LogprobGeo &g)
+{
+    if (!d) return fail(DP_ERR_INVALID_ARG, "descriptor is NULL");
+    if (d->in_dtype != DP_F32 && d->in_dtype != DP_BF16) return fail(DP_ERR_INVALID_ARG, "unknown input dtype %d", d->in_dtype);
+    if (d->n < 1 || d->tokens < 1 || d->vocab < 1)
+        return fail(DP_ERR_INVALID_ARG, "non-positive dimension (n %d tokens %d vocab %d)", d->n, d->tokens, d->vocab);
+    if (!std::isfinite(d->scale) || !(d->scale > 0.0f)) return fail(DP_ERR_INVALID_ARG, "scale must be finite and > 0");
+    if (d->top < 0 || d->top > LOGPROB_TOP) return fail(DP_ERR_INVALID_ARG, "top = %d (need 0 .. %d)", d->top, LOGPROB_TOP);
+    if (d->row_stride && d->row_stride < (size_t)d->vocab) return fail(DP_ERR_INVALID_ARG, "row_stride smaller than the vocabulary");
+    if (d->vocab > (1 << 24)) return fail(DP_ERR_UNSUPPORTED, "more than 2^24 tokens in the vocabulary");
+    g.bf16 = d->in_dtype == DP_BF16; g.n = d->n; g.tokens = d->tokens; g.vocab = d->vocab; g.top = d->top; g.scale = d->scale;
+    g.row_stride = d->row_stride ? d->row_stride : (size_t)d->vocab;
+    if ((size_t)g.n * g.tokens >= ((size_t)1 << 31) || g.row_stride >= ((size_t)1 << 40)) return fail(DP_ERR_UNSUPPORTED, "2^31 rows or more");
+    return DP_OK;
+}
+
+size_t dp_token_logprobs_workspace_bytes(const dp_logprob_desc *desc)
+{
+    LogprobGeo g;
+    return make_logprob_geo(desc, g) == DP_OK ? logprob_ws_bytes(g) : 0;
+}
+
+dp_status dp_token_logprobs(const dp_logprob_desc *desc, const void *logits, const int32_t *targets, const int32_t *lengths, float *logprobs,
+                            float *entropy, float *stats, float *top_logprobs, int32_t *top_tokens, void *ws, size_t ws_bytes, dp_stream stream)
+{
+    LogprobGeo g;
+    DP_TRY(make_logprob_geo(desc, g));
+    DP_TRY(check_rows(logits, "logits", desc->in_dtype));
+    DP_TRY(check_ptr(targets, "targets", logprobs != nullptr, 4));
+    DP_TRY(check_ptr(lengths, "lengths", false, 4));
+    DP_TRY(check_ptr(logprobs, "logprobs", false, 4));
+    DP_TRY(check_ptr(entropy, "entropy", false, 4));
+    DP_TRY(check_ptr(stats, "stats", false, 8));
+    DP_TRY(check_ptr(top_logprobs, "top_logprobs", false, 4));
+    DP_TRY(check_ptr(top_tokens, "top_tokens", g.top > 0, 4));
+    if (g.top == 0 && (top_logprobs || top_tokens)) return fail(DP_ERR_INVALID_ARG, "places for alternatives given, but top is 0");
+    if (!logprobs && !entropy && !stats && !g.top) return fail(DP_ERR_INVALID_ARG, "nothing to compute: no place for a result");
+    DP_TRY(check_room(logprob_ws_bytes(g), ws, ws_bytes));
+    g_err[0] = 0;
+    return launch_logprobs(g, logits, targets, lengths, logprobs, entropy, stats, top_logprobs, top_tokens, ws, static_cast<hipStream_t>(stream));
+}
+
+dp_status dp_token_logprobs_backward(const dp_logprob_desc *desc, const void *logits, const int32_t *targets, const int32_t *lengths,
+                                     const float *stats, const float *entropy, const float *d_logprobs, const float *d_entropy, float *logprobs,
+                                     void *dlogits, void *ws, size_t ws_bytes, dp_stream stream)
+{
+    LogprobGeo g;
+    DP_TRY(make_logprob_geo(desc, g));
+    if (g.top) return fail(DP_ERR_INVALID_ARG, "top = %d: alternatives have no gradient", g.top);
+    DP_TRY(check_rows(logits, "logits", desc->in_dtype));
+    DP_TRY(check_rows(dlogits, "dlogits", desc->in_dtype));
+    DP_TRY(check_ptr(targets, "targets", d_logprobs || logprobs, 4));
+    DP_TRY(check_ptr(lengths, "lengths", false, 4));
+    DP_TRY(check_ptr(stats, "stats", false, 8));
+    DP_TRY(check_ptr(entropy, "entropy", false, 4));
+    DP_TRY(check_ptr(d_logprobs, "d_logprobs", false, 4));
+    DP_TRY(check_ptr(d_entropy, "d_entropy", false, 4));
+    DP_TRY(check_ptr(logprobs, "logprobs", false, 4));
+    if (!d_logprobs && !d_entropy) return fail(DP_ERR_INVALID_ARG, "nothing to compute: d_logprobs and d_entropy are both NULL");
+    if (d_entropy && stats && !entropy) return fail(DP_ERR_INVALID_ARG, "d_entropy with stats needs the entropies as well");
+    if (entropy && !stats) return fail(DP_ERR_INVALID_ARG, "entropy given without stats");
+    DP_TRY(check_room(logprob_ws_bytes(g), ws, ws_bytes));
+    g_err[0] = 0;
+    return launch_logprobs_backward(g, logits, targets, lengths, stats, entropy, d_logprobs, d_entropy, logprobs, dlogits, ws,
+                                    static_cast<hipStream_t>(stream));
+}
+
 }  // extern "C"

@@ -19,6 +19,7 @@
 // 16384 and by sixteen up to 32768 (backward: by four up to 8192); longer ones are read twice.  Bound by memory: 16 x 12 x 512 x 512 bf16
 // forward 44 us, 4.6 TB/s, backward 61, 4.9 (and 4 to join the tables); 4 x 8 x 1500 x 1500 fp32 backward, causal and ragged, 104.  Four
 // waves to a row of 1100 keys: 97 us, one wave 68.
+#include "lanes.h"
 #include "values.h"
 
 #include <algorithm>
@@ -71,27 +72,6 @@ struct RunWords {
     }
 };
 __device__ __forceinline__ int bias_word(const BiasArgs &a, int slot) { return (slot & 7) * a.plane + (slot >> 3); }
-
-// Sum and largest of a wave's values, in every lane, by data-parallel-primitive moves.
-__device__ __forceinline__ float wave_all_sum(float v)
-{
-    return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, wave_sum_last_lane(v)), 63));
-}
-__device__ __forceinline__ float wave_all_max(float v)
-{
-    auto step = [](float x, auto ctrl, auto rows) {              // lanes without a source keep their own value
-        const int bits = __builtin_bit_cast(int, x);
-        return fmaxf(x, __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(bits, bits, decltype(ctrl)::value, decltype(rows)::value, 0xf, false)));
-    };
-    typedef std::integral_constant<int, 0xf> all_rows;
-    v = step(v, std::integral_constant<int, 0x111>{}, all_rows{});
-    v = step(v, std::integral_constant<int, 0x112>{}, all_rows{});
-    v = step(v, std::integral_constant<int, 0x114>{}, all_rows{});
-    v = step(v, std::integral_constant<int, 0x118>{}, all_rows{});
-    v = step(v, std::integral_constant<int, 0x142>{}, std::integral_constant<int, 0xa>{});
-    v = step(v, std::integral_constant<int, 0x143>{}, std::integral_constant<int, 0xc>{});
-    return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), 63));
-}
 
 // What a workgroup works on.
 struct Rows {
@@ -472,25 +452,6 @@ __global__ void __launch_bounds__(256) bias_backward_kernel(const BiasArgs a)
 
 // ---- rows of at most 256 keys: TPR lanes of a wave to a row, 64 / TPR rows of a wave together, and eight rows of each of these in turn.  The
 // rows of a wave lie eight apart, so that the words of their runs have the shared part in common (RunWords).
-
-// Sum or largest of the TPR lanes of a row, in each of them.
-template <int TPR, bool MAX>
-__device__ __forceinline__ float lanes_reduce(float v)
-{
-    auto step = [](float x, auto ctrl) {
-        const float y = __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), decltype(ctrl)::value, 0xf, 0xf, true));
-        return MAX ? fmaxf(x, y) : x + y;
-    };
-    v = step(v, std::integral_constant<int, 0xB1>{});              // lane ^ 1
-    v = step(v, std::integral_constant<int, 0x4E>{});              // lane ^ 2
-    v = step(v, std::integral_constant<int, 0x141>{});             // the other four of eight
-    if constexpr (TPR >= 16) v = step(v, std::integral_constant<int, 0x140>{});    // the other eight of sixteen
-    if constexpr (TPR >= 32) {
-        const float y = __shfl_xor(v, 16, 64);
-        v = MAX ? fmaxf(v, y) : v + y;
-    }
-    return v;
-}
 
 // A workgroup's rows of a tensor, each lane with a run of a row of its own.  WORDS (as RowOf): buffer accesses, left out by an offset beyond the
 // buffer.  A run that a row ends in is loaded whole, with the next row's first values, and stored dword by dword.

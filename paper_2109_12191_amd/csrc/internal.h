@@ -235,6 +235,31 @@ dp_status launch_bias_softmax_backward(const BiasGeo &g, const void *probs, cons
                                        const int32_t *key_lengths, void *dscores, float *g_table, size_t g_stride, float *sqnorm, void *ws,
                                        hipStream_t s);
 
+// normalisation of tokens over their features, with per-example gradients of scale and shift (norm.hip)
+struct NormGeo {
+    int bf16, n, tokens, features, rms;
+    float eps;
+    size_t row_stride;
+};
+size_t norm_ws_bytes(const NormGeo &g);
+dp_status launch_norm(const NormGeo &g, const void *x, const float *gamma, const float *beta, const int32_t *lengths, void *y, hipStream_t s);
+dp_status launch_norm_backward(const NormGeo &g, const void *x, const float *gamma, const void *dy, const int32_t *lengths, void *dx, float *g_w,
+                               float *g_b, size_t g_stride, float *sqnorm, void *ws, hipStream_t s);
+
+// log probabilities of tokens, their entropies and alternatives, and their gradient (logprob.hip)
+constexpr int LOGPROB_TOP = 32;        // alternatives of a row, at most
+struct LogprobGeo {
+    int bf16, n, tokens, vocab, top;
+    float scale;
+    size_t row_stride;
+};
+size_t logprob_ws_bytes(const LogprobGeo &g);
+dp_status launch_logprobs(const LogprobGeo &g, const void *logits, const int32_t *targets, const int32_t *lengths, float *logprobs, float *entropy,
+                          float *stats, float *top_logprobs, int32_t *top_tokens, void *ws, hipStream_t s);
+dp_status launch_logprobs_backward(const LogprobGeo &g, const void *logits, const int32_t *targets, const int32_t *lengths, const float *stats,
+                                   const float *entropy, const float *d_logprobs, const float *d_entropy, float *logprobs, void *dlogits, void *ws,
+                                   hipStream_t s);
+
 // ---- device helpers --------------------------------------------------------------------
 #if defined(__HIP_DEVICE_COMPILE__) || defined(__HIPCC__)
 

@@ -1,0 +1,590 @@
+// Normalisation of tokens over their features, and its backward pass with the per-example gradients of scale and shift:
+//     xhat = (x - mean) r,  r = 1 / sqrt(mean((x - mean)^2) + eps),  y = gamma xhat + beta          (RMS: the mean is taken as zero)
+//     a = gamma dy,  dx = r (a - mean(a) - xhat mean(a xhat)),   g_w = sum_t dy xhat,  g_b = sum_t dy        (RMS: no mean(a))
+//
+// A row's values are held in registers between its sums and its results, 8 to a lane and run, by as many lanes as have one, so that memory sees
+// each value once.  The mean comes first; deviations from it are then summed with their squares, and what the mean's rounding left in
+// their sum is taken out again (a mean of 1000 deviations costs no digits of the variance).  The backward pass works the statistics out again
+// from x: two more sums of registers, nothing to keep from the forward pass.
+// Gradients of scale and shift: a lane keeps its columns' sums over the workgroup's rows in registers, workgroups leave theirs in the workspace,
+// and norm_join_kernel adds them up in order.
+#include "lanes.h"
+#include "token_rows.h"
+
+#include <algorithm>
+
+namespace dp {
+
+namespace {
+
+struct NormArgs {
+    const void *x, *dy;
+    void *out;
+    const float *gamma, *beta;
+    const int32_t *lengths;
+    float *partials;                 // backward: [n, blocks, 2, padded features]
+    float *stats;                    // of rows too long for registers: [n * tokens, 4]
+    int n, tokens, features, padded, rms;
+    float eps, inv_features;
+    size_t row_stride;
+    int rows, blocks;                // rows of a workgroup; workgroups of an example (backward)
+    unsigned first_block;            // workgroups of the launches before
+};
+
+// Sums of N values over the TPR threads of a row, in each of them.  Rows of several waves: every thread of the workgroup calls it, and `red`
+// has two places of 16 N words that are used in turn.
+template <int TPR, int N>
+__device__ __forceinline__ void row_sums(float (&v)[N], float *red, int &turn)
+{
+    if constexpr (TPR < 64) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] = lanes_reduce<TPR, false>(v[i]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] = wave_all_sum(v[i]);
+    }
+    if constexpr (TPR > 64) {
+        float *here = red + turn * 16 * 4;
+        turn ^= 1;
+        const int wave = threadIdx.x >> 6;
+        if ((threadIdx.x & 63) == 0)
+#pragma unroll
+            for (int i = 0; i < N; ++i) here[wave * N + i] = v[i];
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            v[i] = here[i];
+#pragma unroll
+            for (int w = 1; w < TPR / 64; ++w) v[i] += here[w * N + i];
+        }
+    }
+}
+
+// Values and what masks them: places after a row's last feature are zeros.
+template <bool BF16, int NV>
+__device__ __forceinline__ void masked(const Raw8<BF16> (&raw)[NV], int t, int step, int features, float (&v)[8 * NV])
+{
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+        float w[8];
+        raw[j].get(w);
+        const int left = features - 8 * (t + step * j);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[8 * j + i] = i < left ? w[i] : 0.0f;
+    }
+}
+
+// x becomes its deviations from the mean (but for the rounding of the mean, whose correction comes out of the next sums: add_up).
+template <int TPR, int NV>
+__device__ __forceinline__ void centre(const NormArgs &a, int t, float (&x)[8 * NV], float *red, int &turn)
+{
+    if (!a.rms) {
+        float s[1] = {0.0f};
+#pragma unroll
+        for (int i = 0; i < 8 * NV; ++i) s[0] += x[i];
+        row_sums<TPR, 1>(s, red, turn);
+        const float mean = s[0] * a.inv_features;
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            const int left = a.features - 8 * (t + TPR * j);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[8 * j + i] = i < left ? x[8 * j + i] - mean : 0.0f;
+        }
+    }
+}
+
+// gamma or beta of eight columns from k on; `none` where there is no such tensor
+__device__ __forceinline__ void columns8(const float *p, float none, int k, int features, float (&v)[8])
+{
+    if (p) {
+        load8f(p + (k < features ? k : 0), features - k, v);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = none;
+    }
+}
+template <int TPR, int NV>
+__device__ __forceinline__ void columns(const float *p, float none, int t, int features, float (&v)[8 * NV])
+{
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+        float w[8];
+        columns8(p, none, 8 * (t + TPR * j), features, w);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[8 * j + i] = w[i];
+    }
+}
+
+// Forward, rows of up to 8 TPR NV features; a workgroup's rows are consecutive ones of all examples.
+template <bool BF16, bool WORDS, int TPR, int NV>
+__global__ void __launch_bounds__(TPR > 256 ? TPR : 256) norm_kernel(const NormArgs a)
+{
+    __shared__ float red[2 * 16 * 4];
+    const int slots = TPR > 64 ? 1 : (int)blockDim.x / TPR;
+    const int slot = TPR > 64 ? 0 : TPR == 64 ? __builtin_amdgcn_readfirstlane((int)threadIdx.x / TPR) : (int)threadIdx.x / TPR;
+    const int t = (int)threadIdx.x % TPR;
+    const size_t first = (size_t)(a.first_block + blockIdx.x) * a.rows, all = (size_t)a.n * a.tokens;
+    const int rows = (int)min((size_t)a.rows, all - first);
+    const TokenRows<BF16, WORDS> in(a.x, first, rows, a.row_stride, a.features), out(a.out, first, rows, a.row_stride, a.features);
+    auto is_there = [&](int row) {
+        if (row >= rows) return false;
+        if (!a.lengths) return true;
+        const unsigned r = (unsigned)(first + row), ex = r / (unsigned)a.tokens;
+        return (int)(r - ex * (unsigned)a.tokens) < a.lengths[ex];
+    };
+    float gamma[8 * NV], beta[8 * NV];
+    columns<TPR, NV>(a.gamma, 1.0f, t, a.features, gamma);
+    columns<TPR, NV>(a.beta, 0.0f, t, a.features, beta);
+    Raw8<BF16> next[NV];
+    bool there = is_there(slot);
+#pragma unroll
+    for (int j = 0; j < NV; ++j) in.load(next[j], there, slot, 8 * (t + TPR * j));
+    int turn = 0;
+    for (int row0 = 0; row0 < rows; row0 += slots) {
+        const int row = row0 + slot;
+        float x[8 * NV];
+        masked<BF16, NV>(next, t, TPR, a.features, x);
+        const bool now = there;
+        there = is_there(row + slots);
+#pragma unroll
+        for (int j = 0; j < NV; ++j) in.load(next[j], there, row + slots, 8 * (t + TPR * j));
+        centre<TPR, NV>(a, t, x, red, turn);
+        float s[2] = {0.0f, 0.0f};
+#pragma unroll
+        for (int i = 0; i < 8 * NV; ++i) { s[0] += x[i]; s[1] = fmaf(x[i], x[i], s[1]); }
+        if (a.rms) s[0] = 0.0f;
+        row_sums<TPR, 2>(s, red, turn);
+        const float off = s[0] * a.inv_features, r = 1.0f / sqrtf(fmaf(-off, off, s[1] * a.inv_features) + a.eps);
+        if (row < rows) {
+#pragma unroll
+            for (int j = 0; j < NV; ++j) {
+                float y[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) y[i] = now ? fmaf((x[8 * j + i] - off) * r, gamma[8 * j + i], beta[8 * j + i]) : 0.0f;
+                out.store(row, 8 * (t + TPR * j), y);
+            }
+        }
+    }
+}
+
+// Backward, rows of up to 8 TPR NV features; a workgroup's rows are consecutive tokens of one example.
+template <bool BF16, bool WORDS, int TPR, int NV>
+__global__ void __launch_bounds__(TPR > 256 ? TPR : 256) norm_backward_kernel(const NormArgs a)
+{
+    __shared__ float red[2 * 16 * 4];
+    __shared__ float share[TPR > 64 ? 1 : 4 * 64 * 8];
+    const int slots = TPR > 64 ? 1 : (int)blockDim.x / TPR;
+    const int slot = TPR > 64 ? 0 : TPR == 64 ? __builtin_amdgcn_readfirstlane((int)threadIdx.x / TPR) : (int)threadIdx.x / TPR;
+    const int t = (int)threadIdx.x % TPR;
+    const unsigned block = a.first_block + blockIdx.x, ex = block / (unsigned)a.blocks;
+    const int token = (int)(block - ex * (unsigned)a.blocks) * a.rows, rows = min(a.rows, a.tokens - token);
+    const int length = min(a.lengths ? a.lengths[ex] - token : rows, rows);          // rows that are there (none if below zero)
+    const size_t first = (size_t)ex * a.tokens + token;
+    const TokenRows<BF16, WORDS> in(a.x, first, rows, a.row_stride, a.features), in2(a.dy, first, rows, a.row_stride, a.features),
+        out(a.out, first, rows, a.row_stride, a.features);
+    float gamma[8 * NV], sum_w[8 * NV], sum_b[8 * NV];
+    columns<TPR, NV>(a.gamma, 1.0f, t, a.features, gamma);
+#pragma unroll
+    for (int i = 0; i < 8 * NV; ++i) sum_w[i] = sum_b[i] = 0.0f;
+    Raw8<BF16> next[NV], next2[NV];
+    auto fetch = [&](int row) {
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            in.load(next[j], row < length, row, 8 * (t + TPR * j));
+            in2.load(next2[j], row < length, row, 8 * (t + TPR * j));
+        }
+    };
+    fetch(slot);
+    int turn = 0;
+    for (int row0 = 0; row0 < rows; row0 += slots) {
+        const int row = row0 + slot;
+        if (row0 < length) {
+            float x[8 * NV], d[8 * NV];
+            masked<BF16, NV>(next, t, TPR, a.features, x);
+            masked<BF16, NV>(next2, t, TPR, a.features, d);
+            fetch(row + slots);
+            centre<TPR, NV>(a, t, x, red, turn);
+            float s[4] = {0.0f, 0.0f, 0.0f, 0.0f};       // of deviations, their squares, a, and a times deviations
+#pragma unroll
+            for (int i = 0; i < 8 * NV; ++i) {
+                const float g = d[i] * gamma[i];
+                s[0] += x[i];
+                s[1] = fmaf(x[i], x[i], s[1]);
+                s[2] += g;
+                s[3] = fmaf(g, x[i], s[3]);
+            }
+            if (a.rms) s[0] = s[2] = 0.0f;
+            row_sums<TPR, 4>(s, red, turn);
+            const float off = s[0] * a.inv_features, r = 1.0f / sqrtf(fmaf(-off, off, s[1] * a.inv_features) + a.eps);
+            const float level = s[2] * a.inv_features, along = r * (s[3] - off * s[2]) * a.inv_features;
+            const bool there = row < length;
+#pragma unroll
+            for (int j = 0; j < NV; ++j) {
+                float g[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const float xhat = (x[8 * j + i] - off) * r, dy = d[8 * j + i];
+                    if (there) {                         // (an infinity of a row that is not there must not meet a zero)
+                        sum_w[8 * j + i] = fmaf(dy, xhat, sum_w[8 * j + i]);
+                        sum_b[8 * j + i] += dy;
+                    }
+                    g[i] = there ? r * fmaf(-xhat, along, fmaf(dy, gamma[8 * j + i], -level)) : 0.0f;
+                }
+                if (a.out && row < rows) out.store(row, 8 * (t + TPR * j), g);
+            }
+        } else if (a.out && row < rows) {
+            const float zeros[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+            for (int j = 0; j < NV; ++j) out.store(row, 8 * (t + TPR * j), zeros);
+        }
+    }
+    if (!a.partials) return;
+    float *part = a.partials + (size_t)block * 2 * a.padded;
+#pragma unroll
+    for (int which = 0; which < 2; ++which) {
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            float v[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                v[i] = which ? sum_b[8 * j + i] : sum_w[8 * j + i];
+                if constexpr (TPR < 64)
+#pragma unroll
+                    for (int off = TPR; off < 64; off <<= 1) v[i] += __shfl_xor(v[i], off, 64);
+            }
+            const int k = 8 * (t + TPR * j);
+            if constexpr (TPR <= 64) {                   // the waves' sums, in order
+                const int lane = (int)threadIdx.x & 63, wave = (int)threadIdx.x >> 6;
+                __syncthreads();
+                if (lane < TPR)
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) share[(wave * 8 + i) * 64 + t] = v[i];
+                __syncthreads();
+                if (wave == 0 && lane < TPR) {
+                    for (int w = 1; w < (int)blockDim.x / 64; ++w)
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) v[i] += share[(w * 8 + i) * 64 + t];
+                }
+                if (wave != 0 || lane >= TPR) continue;
+            }
+            if (k < a.padded) {
+                float4 *to = reinterpret_cast<float4 *>(part + which * a.padded + k);
+                to[0] = make_float4(v[0], v[1], v[2], v[3]);
+                to[1] = make_float4(v[4], v[5], v[6], v[7]);
+            }
+        }
+    }
+}
+
+// Rows too long for registers, a workgroup each, read three times.  Forward: all of it.  Backward: their statistics, and what dx needs.
+template <bool BF16, bool BACKWARD>
+__global__ void __launch_bounds__(1024) norm_long_kernel(const NormArgs a)
+{
+    __shared__ float red[2 * 16 * 4];
+    const size_t row = a.first_block + blockIdx.x;
+    const unsigned ex = (unsigned)row / (unsigned)a.tokens;
+    const bool there = !a.lengths || (int)((unsigned)row - ex * (unsigned)a.tokens) < a.lengths[ex];
+    typedef typename In<BF16>::type E;
+    const E *x = static_cast<const E *>(a.x) + row * a.row_stride;
+    const E *dy = BACKWARD ? static_cast<const E *>(a.dy) + row * a.row_stride : nullptr;
+    E *out = static_cast<E *>(a.out) + row * a.row_stride;
+    if (!there) {
+        const float zeros[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
+        if (!BACKWARD)
+            for (int k = 8 * (int)threadIdx.x; k < a.features; k += 8192) store8(out + k, a.features - k, zeros);
+        return;
+    }
+    int turn = 0;
+    float mean = 0.0f;
+    if (!a.rms) {
+        float s[1] = {0.0f};
+        for (int k = 8 * (int)threadIdx.x; k < a.features; k += 8192) {
+            Raw8<BF16> raw;
+            raw.load(x, (size_t)k, a.features - k);
+            float v[8];
+            raw.get(v);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) s[0] += v[i];
+        }
+        row_sums<1024, 1>(s, red, turn);
+        mean = s[0] * a.inv_features;
+    }
+    float s[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    for (int k = 8 * (int)threadIdx.x; k < a.features; k += 8192) {
+        Raw8<BF16> raw;
+        raw.load(x, (size_t)k, a.features - k);
+        float v[8], g[8];
+        raw.get(v);
+        if constexpr (BACKWARD) {
+            float gamma[8];
+            raw.load(dy, (size_t)k, a.features - k);
+            raw.get(g);
+            columns8(a.gamma, 1.0f, k, a.features, gamma);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) g[i] *= gamma[i];
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float dev = i < a.features - k ? v[i] - mean : 0.0f;
+            s[0] += dev;
+            s[1] = fmaf(dev, dev, s[1]);
+            if constexpr (BACKWARD) { s[2] += g[i]; s[3] = fmaf(g[i], dev, s[3]); }
+        }
+    }
+    if (a.rms) s[0] = s[2] = 0.0f;
+    row_sums<1024, 4>(s, red, turn);
+    const float off = s[0] * a.inv_features, r = 1.0f / sqrtf(fmaf(-off, off, s[1] * a.inv_features) + a.eps);
+    if constexpr (BACKWARD) {
+        // (the mean and its correction are kept apart: together they would be rounded to the mean's digits)
+        if (threadIdx.x == 0) {
+            *reinterpret_cast<float4 *>(a.stats + 4 * row) = make_float4(mean, off, r, r * (s[3] - off * s[2]) * a.inv_features);
+            a.stats[4 * (size_t)a.n * a.tokens + row] = s[2] * a.inv_features;
+        }
+        return;
+    }
+    for (int k = 8 * (int)threadIdx.x; k < a.features; k += 8192) {
+        Raw8<BF16> raw;
+        raw.load(x, (size_t)k, a.features - k);
+        float v[8], gamma[8], beta[8];
+        raw.get(v);
+        columns8(a.gamma, 1.0f, k, a.features, gamma);
+        columns8(a.beta, 0.0f, k, a.features, beta);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = fmaf((v[i] - mean - off) * r, gamma[i], beta[i]);
+        store8(out + k, a.features - k, v);
+    }
+}
+
+// Their backward pass by columns: a thread has eight, a workgroup 2048 of consecutive tokens of one example.
+template <bool BF16>
+__global__ void __launch_bounds__(256) norm_columns_kernel(const NormArgs a)
+{
+    typedef typename In<BF16>::type E;
+    const unsigned wide = (unsigned)(a.features + 2047) / 2048u, block = a.first_block + blockIdx.x, line = block / wide;
+    const unsigned ex = line / (unsigned)a.blocks;
+    const int token = (int)(line - ex * (unsigned)a.blocks) * a.rows, rows = min(a.rows, a.tokens - token);
+    const int length = min(a.lengths ? a.lengths[ex] - token : rows, rows);
+    const int k = (int)(block - line * wide) * 2048 + 8 * (int)threadIdx.x, count = a.features - k;
+    if (count <= 0) return;
+    float gamma[8], sum_w[8], sum_b[8];
+    columns8(a.gamma, 1.0f, k, a.features, gamma);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) sum_w[i] = sum_b[i] = 0.0f;
+    for (int t = 0; t < rows; ++t) {
+        const size_t row = (size_t)ex * a.tokens + token + t, at = row * a.row_stride + (size_t)k;
+        float out[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
+        if (t < length) {
+            const float4 st = *reinterpret_cast<const float4 *>(a.stats + 4 * row);
+            const float level = a.stats[4 * (size_t)a.n * a.tokens + row];
+            Raw8<BF16> raw, raw2;
+            raw.load(a.x, at, count);
+            raw2.load(a.dy, at, count);
+            float x[8], d[8];
+            raw.get(x);
+            raw2.get(d);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const float xhat = (x[i] - st.x - st.y) * st.z;
+                sum_w[i] = fmaf(d[i], xhat, sum_w[i]);
+                sum_b[i] += d[i];
+                out[i] = st.z * fmaf(-xhat, st.w, fmaf(d[i], gamma[i], -level));
+            }
+        }
+        if (a.out) store8(static_cast<E *>(a.out) + at, count, out);
+    }
+    if (!a.partials) return;
+    float4 *to = reinterpret_cast<float4 *>(a.partials + (size_t)line * 2 * a.padded + k);
+    to[0] = make_float4(sum_w[0], sum_w[1], sum_w[2], sum_w[3]);
+    to[1] = make_float4(sum_w[4], sum_w[5], sum_w[6], sum_w[7]);
+    to += a.padded / 4;
+    to[0] = make_float4(sum_b[0], sum_b[1], sum_b[2], sum_b[3]);
+    to[1] = make_float4(sum_b[4], sum_b[5], sum_b[6], sum_b[7]);
+}
+
+// Gradients of an example from its workgroups' sums, in order, and their squared norm: WHOLE, by a workgroup an example; else the
+// squares of 256 columns to a workgroup, which are added up by another launch.  A wave takes every sixteenth (fourth) sum of a column.
+struct NormJoinArgs {
+    const float *partials;
+    float *g_w, *g_b, *squares;      // [n, squares of an example]
+    size_t g_stride;
+    int blocks, features, padded, groups;
+    unsigned first_block;
+};
+template <bool WHOLE>
+__global__ void __launch_bounds__(WHOLE ? 1024 : 256) norm_join_kernel(const NormJoinArgs a)
+{
+    constexpr int WAVES = WHOLE ? 16 : 4;
+    __shared__ float4 share[WAVES][64];
+    const unsigned block = a.first_block + blockIdx.x, ex = WHOLE ? block : block / (unsigned)a.groups, group = WHOLE ? 0 : block - ex * (unsigned)a.groups;
+    const int lane = (int)threadIdx.x & 63, wave = (int)threadIdx.x >> 6, quads = (a.g_b ? 2 : 1) * a.padded / 4;
+    const float4 *from = reinterpret_cast<const float4 *>(a.partials + (size_t)ex * a.blocks * 2 * a.padded);
+    float ss = 0.0f;
+    for (int q0 = WHOLE ? 0 : 64 * (int)group; q0 < (WHOLE ? quads : min(quads, 64 * (int)group + 64)); q0 += 64) {
+        const int q = q0 + lane;
+        float4 s = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        if (q < quads)
+#pragma unroll 4
+            for (int b = wave; b < a.blocks; b += WAVES) {
+                const float4 v = from[(size_t)b * (a.padded / 2) + q];
+                s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
+            }
+        __syncthreads();
+        share[wave][lane] = s;
+        __syncthreads();
+        if (wave == 0 && q < quads) {
+#pragma unroll
+            for (int w = 1; w < WAVES; ++w) {
+                const float4 v = share[w][lane];
+                s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
+            }
+            const bool shift = q >= a.padded / 4;
+            const int k = 4 * (shift ? q - a.padded / 4 : q);
+            float *to = (shift ? a.g_b : a.g_w) + (size_t)ex * a.g_stride + k;
+            const float v[4] = {s.x, s.y, s.z, s.w};
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (k + i < a.features) { to[i] = v[i]; ss = fmaf(v[i], v[i], ss); }
+        }
+    }
+    if (wave == 0 && a.squares) {
+        ss = wave_all_sum(ss);
+        if (lane == 0) a.squares[block] = ss;
+    }
+}
+
+constexpr int NORM_HELD = 16384;       // features that a workgroup of sixteen waves holds in registers
+
+// Threads that share a row: as many as have a run of eight, a wave for up to 1024 features (forward 2048), four for up to 8192.
+int norm_lanes(int features, bool backward)
+{
+    if (features <= 64) return 8;
+    if (features <= 128) return 16;
+    if (features <= 256) return 32;
+    if (features <= (backward ? 1024 : 2048)) return 64;
+    return features <= 8192 ? 256 : backward ? 512 : 1024;
+}
+
+NormArgs norm_args(const NormGeo &g, bool backward)
+{
+    NormArgs a = {};
+    a.n = g.n; a.tokens = g.tokens; a.features = g.features; a.padded = (g.features + 7) & ~7; a.rms = g.rms;
+    a.eps = g.eps; a.inv_features = 1.0f / (float)g.features; a.row_stride = g.row_stride;
+    const long long all = (long long)g.n * g.tokens;
+    const int lanes = norm_lanes(g.features, backward), at_once = lanes > 64 ? 1 : 256 / lanes;
+    if (!backward) {
+        a.rows = (int)std::max(1ll, std::min(all / (2048ll * at_once), 64ll / at_once)) * at_once;
+    } else {
+        const long long each = std::max(1ll, std::min(all / (1024ll * at_once), 64ll));
+        a.rows = (int)std::min(each * at_once, (long long)(g.tokens + at_once - 1) / at_once * at_once);
+        a.blocks = (g.tokens + a.rows - 1) / a.rows;
+    }
+    if (backward && g.features > NORM_HELD) {
+        a.rows = std::min(g.tokens, 32);
+        a.blocks = (g.tokens + a.rows - 1) / a.rows;
+    }
+    return a;
+}
+
+template <bool BF16, bool WORDS>
+dp_status run_forward(const NormGeo &g, const NormArgs &a, hipStream_t s)
+{
+    const size_t all = (size_t)g.n * g.tokens, grid = (all + a.rows - 1) / a.rows;
+    if (g.features <= 64) return launch_blocks<norm_kernel<BF16, WORDS, 8, 1>>(grid, 256, 0, s, a);
+    if (g.features <= 128) return launch_blocks<norm_kernel<BF16, WORDS, 16, 1>>(grid, 256, 0, s, a);
+    if (g.features <= 256) return launch_blocks<norm_kernel<BF16, WORDS, 32, 1>>(grid, 256, 0, s, a);
+    if (g.features <= 512) return launch_blocks<norm_kernel<BF16, WORDS, 64, 1>>(grid, 256, 0, s, a);
+    if (g.features <= 1024) return launch_blocks<norm_kernel<BF16, WORDS, 64, 2>>(grid, 256, 0, s, a);
+    if (g.features <= 2048) return launch_blocks<norm_kernel<BF16, WORDS, 64, 4>>(grid, 256, 0, s, a);
+    if (g.features <= 4096) return launch_blocks<norm_kernel<BF16, WORDS, 256, 2>>(grid, 256, 0, s, a);
+    if (g.features <= 8192) return launch_blocks<norm_kernel<BF16, WORDS, 256, 4>>(grid, 256, 0, s, a);
+    return launch_blocks<norm_kernel<BF16, WORDS, 1024, 2>>(grid, 1024, 0, s, a);
+}
+
+template <bool BF16, bool WORDS>
+dp_status run_backward(const NormGeo &g, const NormArgs &a, hipStream_t s)
+{
+    const size_t grid = (size_t)g.n * a.blocks;
+    if (g.features <= 64) return launch_blocks<norm_backward_kernel<BF16, WORDS, 8, 1>>(grid, 256, 0, s, a);
+    if (g.features <= 128) return launch_blocks<norm_backward_kernel<BF16, WORDS, 16, 1>>(grid, 256, 0, s, a);
+    if (g.features <= 256) return launch_blocks<norm_backward_kernel<BF16, WORDS, 32, 1>>(grid, 256, 0, s, a);
+    if (g.features <= 512) return launch_blocks<norm_backward_kernel<BF16, WORDS, 64, 1>>(grid, 256, 0, s, a);
+    if (g.features <= 1024) return launch_blocks<norm_backward_kernel<BF16, WORDS, 64, 2>>(grid, 256, 0, s, a);
+    if (g.features <= 2048) return launch_blocks<norm_backward_kernel<BF16, WORDS, 256, 1>>(grid, 256, 0, s, a);
+    if (g.features <= 4096) return launch_blocks<norm_backward_kernel<BF16, WORDS, 256, 2>>(grid, 256, 0, s, a);
+    if (g.features <= 8192) return launch_blocks<norm_backward_kernel<BF16, WORDS, 256, 4>>(grid, 256, 0, s, a);
+    return launch_blocks<norm_backward_kernel<BF16, WORDS, 512, 4>>(grid, 512, 0, s, a);
+}
+
+template <bool BF16, bool BACKWARD>
+dp_status run_long(const NormGeo &g, const NormArgs &a, hipStream_t s)
+{
+    const size_t all = (size_t)g.n * g.tokens, wide = (size_t)(g.features + 2047) / 2048;
+    const dp_status st = launch_blocks<norm_long_kernel<BF16, BACKWARD>>(all, 1024, 0, s, a);
+    if (st != DP_OK || !BACKWARD) return st;
+    return launch_blocks<norm_columns_kernel<BF16>>((size_t)g.n * a.blocks * wide, 256, 0, s, a);
+}
+
+size_t round16(size_t b) { return (b + 15) & ~(size_t)15; }
+
+struct NormWs { size_t partials, squares, stats, total; int groups; };
+// Workspace: the workgroups' sums, the squares of groups of columns, statistics of long rows.
+NormWs norm_ws(const NormGeo &g, const NormArgs &a)
+{
+    NormWs w = {};
+    const size_t all = (size_t)g.n * g.tokens;
+    w.groups = (2 * a.padded / 4 + 63) / 64;
+    w.partials = round16((size_t)g.n * a.blocks * 2 * a.padded * 4);
+    w.squares = round16((size_t)g.n * w.groups * 4);
+    w.stats = g.features > NORM_HELD ? round16(all * 20) : 0;
+    w.total = w.partials + w.squares + w.stats;
+    return w;
+}
+
+}  // namespace
+
+size_t norm_ws_bytes(const NormGeo &g) { return norm_ws(g, norm_args(g, true)).total; }
+
+dp_status launch_norm(const NormGeo &g, const void *x, const float *gamma, const float *beta, const int32_t *lengths, void *y, hipStream_t s)
+{
+    NormArgs a = norm_args(g, false);
+    a.x = x; a.out = y; a.gamma = gamma; a.beta = beta; a.lengths = lengths;
+    if (g.features > NORM_HELD) return g.bf16 ? run_long<true, false>(g, a, s) : run_long<false, false>(g, a, s);
+    const bool words = token_rows_by_words(x, g.bf16, g.row_stride, a.rows) && token_rows_by_words(y, g.bf16, g.row_stride, a.rows);
+    if (!g.bf16) return words ? run_forward<false, true>(g, a, s) : run_forward<false, false>(g, a, s);
+    return words ? run_forward<true, true>(g, a, s) : run_forward<true, false>(g, a, s);
+}
+
+dp_status launch_norm_backward(const NormGeo &g, const void *x, const float *gamma, const void *dy, const int32_t *lengths, void *dx, float *g_w,
+                               float *g_b, size_t g_stride, float *sqnorm, void *ws, hipStream_t s)
+{
+    NormArgs a = norm_args(g, true);
+    const NormWs w = norm_ws(g, a);
+    char *room = static_cast<char *>(ws);
+    a.x = x; a.dy = dy; a.out = dx; a.gamma = gamma; a.lengths = lengths;
+    a.partials = g_w ? reinterpret_cast<float *>(room) : nullptr;
+    a.stats = reinterpret_cast<float *>(room + w.partials + w.squares);
+    dp_status st;
+    if (g.features > NORM_HELD) {
+        st = g.bf16 ? run_long<true, true>(g, a, s) : run_long<false, true>(g, a, s);
+    } else {
+        bool words = true;
+        for (const void *p : {x, dy, static_cast<const void *>(dx)}) words = words && token_rows_by_words(p, g.bf16, g.row_stride, a.rows);
+        if (!g.bf16) st = words ? run_backward<false, true>(g, a, s) : run_backward<false, false>(g, a, s);
+        else st = words ? run_backward<true, true>(g, a, s) : run_backward<true, false>(g, a, s);
+    }
+    if (st != DP_OK || !g_w) return st;
+    NormJoinArgs j = {};
+    j.partials = a.partials; j.g_w = g_w; j.g_b = g_b; j.g_stride = g_stride; j.blocks = a.blocks; j.features = g.features; j.padded = a.padded;
+    j.groups = ((g_b ? 2 : 1) * a.padded / 4 + 63) / 64;
+    // one workgroup an example where it has little to add up, or where there are as many as compute units
+    if (j.groups == 1 || g.n >= 256 || (size_t)a.blocks * 2 * a.padded <= 32768) {
+        j.squares = sqnorm;
+        return launch_blocks<norm_join_kernel<true>>((size_t)g.n, 1024, 0, s, j);
+    }
+    j.squares = sqnorm ? reinterpret_cast<float *>(room + w.partials) : nullptr;
+    st = launch_blocks<norm_join_kernel<false>>((size_t)g.n * j.groups, 256, 0, s, j);
+    if (st != DP_OK || !sqnorm) return st;
+    return launch_sum_partials(j.squares, g.n, j.groups, sqnorm, s);
+}
+
+}  // namespace dp
