@@ -564,6 +564,7 @@ __global__ void __launch_bounds__(TPR > 256 ? TPR : 256) logprob_held_kernel(con
     v.none();
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
+        if (j && row.index(j * TPR) >= row.count) break;     // (the same for all threads)
         float x[8];
         run_values<BF16, true>(raw[j], row.index(t + j * TPR), row.count, x);
 #pragma unroll
@@ -572,6 +573,7 @@ __global__ void __launch_bounds__(TPR > 256 ? TPR : 256) logprob_held_kernel(con
     }
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
+        if (j && row.index(j * TPR) >= row.count) break;
         float x[8];
         renew(raw[j]);
         run_values<BF16, true>(raw[j], row.index(t + j * TPR), row.count, x);
@@ -625,10 +627,15 @@ size_t partial_bytes(const LogprobGeo &g)
     return splits > 1 ? round16((size_t)g.n * g.tokens * splits * (4 + 2 * g.top) * 4) : 0;
 }
 
-// Most logits of a row that is held in registers.
-int held_logits(bool bf16) { return bf16 ? 131071 : 65536; }
-// Whether the gradient without statistics holds its rows: rows that fit, and enough of them.
-bool holds_rows(const LogprobGeo &g) { return g.vocab <= held_logits(g.bf16) && logprob_splits(g) == 1; }
+// Whether the gradient without statistics holds its rows in registers: rows that fit (with the place before them where they may begin inside a dword),
+// and enough of them.
+bool holds_rows(const LogprobGeo &g) { return g.vocab <= (g.bf16 ? 131071 : 65536) && logprob_splits(g) == 1; }
+// Places of a row's runs.
+int held_places(const LogprobArgs &a, bool bf16)
+{
+    const bool inside = bf16 && ((reinterpret_cast<uintptr_t>(a.logits) & 2) || (a.rows > 1 && a.row_stride % 2));
+    return a.vocab + (inside ? 1 : 0);
+}
 
 template <bool BF16>
 dp_status run_logprobs(const LogprobArgs &a, hipStream_t s)
@@ -661,14 +668,14 @@ template <bool BF16, bool ENTROPY>
 dp_status run_held(const LogprobArgs &a, hipStream_t s)
 {
     const size_t rows = (size_t)a.rows;
-    const int places = a.vocab + (BF16 ? 1 : 0);
+    const int places = held_places(a, BF16);
     if (places <= 512) return launch_blocks<logprob_held_kernel<BF16, 64, 1, ENTROPY>>((rows + 3) / 4, 256, 0, s, a);
     if (places <= 1024) return launch_blocks<logprob_held_kernel<BF16, 64, 2, ENTROPY>>((rows + 3) / 4, 256, 0, s, a);
     if (places <= 2048) return launch_blocks<logprob_held_kernel<BF16, 64, 4, ENTROPY>>((rows + 3) / 4, 256, 0, s, a);
     if (places <= 4096) return launch_blocks<logprob_held_kernel<BF16, 256, 2, ENTROPY>>(rows, 256, 0, s, a);
     if (places <= 8192) return launch_blocks<logprob_held_kernel<BF16, 256, 4, ENTROPY>>(rows, 256, 0, s, a);
     if (places <= 16384) return launch_blocks<logprob_held_kernel<BF16, 256, 8, ENTROPY>>(rows, 256, 0, s, a);
-    if (places <= 32768) return launch_blocks<logprob_held_kernel<BF16, 1024, 4, ENTROPY>>(rows, 1024, 0, s, a);
+    if (places <= 32768) return launch_blocks<logprob_held_kernel<BF16, 512, 8, ENTROPY>>(rows, 512, 0, s, a);
     if (!BF16 || places <= 65536) return launch_blocks<logprob_held_kernel<BF16, 1024, 8, ENTROPY>>(rows, 1024, 0, s, a);
     if constexpr (BF16) return launch_blocks<logprob_held_kernel<BF16, 1024, 16, ENTROPY>>(rows, 1024, 0, s, a);
 }

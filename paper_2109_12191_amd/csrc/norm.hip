@@ -23,6 +23,7 @@ struct NormArgs {
     const float *gamma, *beta;
     const int32_t *lengths;
     float *partials;                 // backward: [n, blocks, 2, padded features]
+    int shift;                       // backward: gradients of the shift are wanted
     float *stats;                    // of rows too long for registers: [n * tokens, 4]
     int n, tokens, features, padded, rms;
     float eps, inv_features;
@@ -60,35 +61,50 @@ __device__ __forceinline__ void row_sums(float (&v)[N], float *red, int &turn)
     }
 }
 
-// Values and what masks them: places after a row's last feature are zeros.
+// A thread's values of a row.  Runs beyond the row were loaded as zeros; in the run that the row ends in (there is one where its length is no multiple of
+// eight, the same for all rows) the places after it become zeros.
 template <bool BF16, int NV>
-__device__ __forceinline__ void masked(const Raw8<BF16> (&raw)[NV], int t, int step, int features, float (&v)[8 * NV])
+__device__ __forceinline__ void values(const Raw8<BF16> (&raw)[NV], int t, int step, int features, float (&v)[8 * NV])
 {
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
         float w[8];
         raw[j].get(w);
-        const int left = features - 8 * (t + step * j);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[8 * j + i] = i < left ? w[i] : 0.0f;
+        for (int i = 0; i < 8; ++i) v[8 * j + i] = w[i];
+    }
+    if (features & 7) {
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            const int left = features - 8 * (t + step * j);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[8 * j + i] = i < left ? v[8 * j + i] : 0.0f;
+        }
     }
 }
 
-// x becomes its deviations from the mean (but for the rounding of the mean, whose correction comes out of the next sums: add_up).
+// x becomes its deviations from the mean, zeros stay zeros beyond the row (but for the rounding of the mean, whose correction comes out of the next sums).
 template <int TPR, int NV>
 __device__ __forceinline__ void centre(const NormArgs &a, int t, float (&x)[8 * NV], float *red, int &turn)
 {
-    if (!a.rms) {
-        float s[1] = {0.0f};
+    if (a.rms) return;
+    float s[1] = {0.0f};
 #pragma unroll
-        for (int i = 0; i < 8 * NV; ++i) s[0] += x[i];
-        row_sums<TPR, 1>(s, red, turn);
-        const float mean = s[0] * a.inv_features;
+    for (int i = 0; i < 8 * NV; ++i) s[0] += x[i];
+    row_sums<TPR, 1>(s, red, turn);
+    const float mean = s[0] * a.inv_features;
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+        const float m = 8 * (t + TPR * j) < a.features ? mean : 0.0f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[8 * j + i] -= m;
+    }
+    if (a.features & 7) {
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
             const int left = a.features - 8 * (t + TPR * j);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) x[8 * j + i] = i < left ? x[8 * j + i] - mean : 0.0f;
+            for (int i = 0; i < 8; ++i) x[8 * j + i] = i < left ? x[8 * j + i] : 0.0f;
         }
     }
 }
@@ -143,7 +159,7 @@ __global__ void __launch_bounds__(TPR > 256 ? TPR : 256) norm_kernel(const NormA
     for (int row0 = 0; row0 < rows; row0 += slots) {
         const int row = row0 + slot;
         float x[8 * NV];
-        masked<BF16, NV>(next, t, TPR, a.features, x);
+        values<BF16, NV>(next, t, TPR, a.features, x);
         const bool now = there;
         there = is_there(row + slots);
 #pragma unroll
@@ -154,13 +170,13 @@ __global__ void __launch_bounds__(TPR > 256 ? TPR : 256) norm_kernel(const NormA
         for (int i = 0; i < 8 * NV; ++i) { s[0] += x[i]; s[1] = fmaf(x[i], x[i], s[1]); }
         if (a.rms) s[0] = 0.0f;
         row_sums<TPR, 2>(s, red, turn);
-        const float off = s[0] * a.inv_features, r = 1.0f / sqrtf(fmaf(-off, off, s[1] * a.inv_features) + a.eps);
+        const float off = s[0] * a.inv_features, r = 1.0f / sqrtf(fmaf(-off, off, s[1] * a.inv_features) + a.eps), shift = -off * r;
         if (row < rows) {
 #pragma unroll
             for (int j = 0; j < NV; ++j) {
                 float y[8];
 #pragma unroll
-                for (int i = 0; i < 8; ++i) y[i] = now ? fmaf((x[8 * j + i] - off) * r, gamma[8 * j + i], beta[8 * j + i]) : 0.0f;
+                for (int i = 0; i < 8; ++i) y[i] = now ? fmaf(fmaf(x[8 * j + i], r, shift), gamma[8 * j + i], beta[8 * j + i]) : 0.0f;
                 out.store(row, 8 * (t + TPR * j), y);
             }
         }
@@ -198,10 +214,10 @@ __global__ void __launch_bounds__(TPR > 256 ? TPR : 256) norm_backward_kernel(co
     int turn = 0;
     for (int row0 = 0; row0 < rows; row0 += slots) {
         const int row = row0 + slot;
-        if (row0 < length) {
+        if (TPR >= 64 ? row < length : row0 < length) {
             float x[8 * NV], d[8 * NV];
-            masked<BF16, NV>(next, t, TPR, a.features, x);
-            masked<BF16, NV>(next2, t, TPR, a.features, d);
+            values<BF16, NV>(next, t, TPR, a.features, x);
+            values<BF16, NV>(next2, t, TPR, a.features, d);
             fetch(row + slots);
             centre<TPR, NV>(a, t, x, red, turn);
             float s[4] = {0.0f, 0.0f, 0.0f, 0.0f};       // of deviations, their squares, a, and a times deviations
@@ -217,18 +233,18 @@ __global__ void __launch_bounds__(TPR > 256 ? TPR : 256) norm_backward_kernel(co
             row_sums<TPR, 4>(s, red, turn);
             const float off = s[0] * a.inv_features, r = 1.0f / sqrtf(fmaf(-off, off, s[1] * a.inv_features) + a.eps);
             const float level = s[2] * a.inv_features, along = r * (s[3] - off * s[2]) * a.inv_features;
-            const bool there = row < length;
+            const float shift = -off * r, slope = -r * along, base = -r * level;
+            const bool there = TPR >= 64 || row < length;
 #pragma unroll
             for (int j = 0; j < NV; ++j) {
                 float g[8];
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
-                    const float xhat = (x[8 * j + i] - off) * r, dy = d[8 * j + i];
-                    if (there) {                         // (an infinity of a row that is not there must not meet a zero)
-                        sum_w[8 * j + i] = fmaf(dy, xhat, sum_w[8 * j + i]);
-                        sum_b[8 * j + i] += dy;
-                    }
-                    g[i] = there ? r * fmaf(-xhat, along, fmaf(dy, gamma[8 * j + i], -level)) : 0.0f;
+                    const float xhat = fmaf(x[8 * j + i], r, shift), dy = d[8 * j + i];
+                    sum_w[8 * j + i] = fmaf(dy, xhat, sum_w[8 * j + i]);          // (of a row that is not there: x, dy and xhat are zeros)
+                    sum_b[8 * j + i] += dy;
+                    g[i] = fmaf(dy * gamma[8 * j + i], r, fmaf(xhat, slope, base));
+                    if (!there) g[i] = 0.0f;
                 }
                 if (a.out && row < rows) out.store(row, 8 * (t + TPR * j), g);
             }
@@ -242,6 +258,7 @@ __global__ void __launch_bounds__(TPR > 256 ? TPR : 256) norm_backward_kernel(co
     float *part = a.partials + (size_t)block * 2 * a.padded;
 #pragma unroll
     for (int which = 0; which < 2; ++which) {
+        if (which && !a.shift) break;
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
             float v[8];
@@ -396,64 +413,76 @@ __global__ void __launch_bounds__(256) norm_columns_kernel(const NormArgs a)
     float4 *to = reinterpret_cast<float4 *>(a.partials + (size_t)line * 2 * a.padded + k);
     to[0] = make_float4(sum_w[0], sum_w[1], sum_w[2], sum_w[3]);
     to[1] = make_float4(sum_w[4], sum_w[5], sum_w[6], sum_w[7]);
+    if (!a.shift) return;
     to += a.padded / 4;
     to[0] = make_float4(sum_b[0], sum_b[1], sum_b[2], sum_b[3]);
     to[1] = make_float4(sum_b[4], sum_b[5], sum_b[6], sum_b[7]);
 }
 
-// Gradients of an example from its workgroups' sums, in order, and their squared norm: WHOLE, by a workgroup an example; else the
-// squares of 256 columns to a workgroup, which are added up by another launch.  A wave takes every sixteenth (fourth) sum of a column.
+// Gradients of an example from its workgroups' sums, and their squares.  A workgroup has 4 QUADS columns (WHOLE: all of an example's, and the squared norm is
+// done); its THREADS / QUADS parts take ranges of the sums, which are added in order.  (A counter that tells a workgroup that it is an example's last, to
+// spare the launch that adds up the squares, takes longer than the launch: 59 us for 2048 workgroups, its fences empty caches.)
 struct NormJoinArgs {
     const float *partials;
-    float *g_w, *g_b, *squares;      // [n, squares of an example]
+    float *g_w, *g_b, *squares;      // squares: [n, groups]
     size_t g_stride;
     int blocks, features, padded, groups;
     unsigned first_block;
 };
-template <bool WHOLE>
-__global__ void __launch_bounds__(WHOLE ? 1024 : 256) norm_join_kernel(const NormJoinArgs a)
+template <int THREADS, int QUADS, bool WHOLE>
+__global__ void __launch_bounds__(THREADS) norm_join_kernel(const NormJoinArgs a)
 {
-    constexpr int WAVES = WHOLE ? 16 : 4;
-    __shared__ float4 share[WAVES][64];
-    const unsigned block = a.first_block + blockIdx.x, ex = WHOLE ? block : block / (unsigned)a.groups, group = WHOLE ? 0 : block - ex * (unsigned)a.groups;
-    const int lane = (int)threadIdx.x & 63, wave = (int)threadIdx.x >> 6, quads = (a.g_b ? 2 : 1) * a.padded / 4;
+    constexpr int PARTS = THREADS / QUADS;
+    __shared__ float4 share[PARTS > 1 ? PARTS : 1][PARTS > 1 ? QUADS : 1];
+    __shared__ float red[THREADS / 64];
+    const unsigned block = a.first_block + blockIdx.x, ex = block / (unsigned)a.groups, group = block - ex * (unsigned)a.groups;
+    const int part = (int)threadIdx.x / QUADS, column = (int)threadIdx.x % QUADS, quads = (a.g_b ? 2 : 1) * a.padded / 4;
     const float4 *from = reinterpret_cast<const float4 *>(a.partials + (size_t)ex * a.blocks * 2 * a.padded);
+    const int each = (a.blocks + PARTS - 1) / PARTS, end = min((part + 1) * each, a.blocks);
     float ss = 0.0f;
-    for (int q0 = WHOLE ? 0 : 64 * (int)group; q0 < (WHOLE ? quads : min(quads, 64 * (int)group + 64)); q0 += 64) {
-        const int q = q0 + lane;
+    for (int q0 = QUADS * (int)group; q0 < (WHOLE ? quads : min(quads, QUADS * ((int)group + 1))); q0 += QUADS) {
+        const int q = q0 + column;
         float4 s = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
         if (q < quads)
-#pragma unroll 4
-            for (int b = wave; b < a.blocks; b += WAVES) {
+#pragma unroll 8
+            for (int b = part * each; b < end; ++b) {
                 const float4 v = from[(size_t)b * (a.padded / 2) + q];
                 s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
             }
-        __syncthreads();
-        share[wave][lane] = s;
-        __syncthreads();
-        if (wave == 0 && q < quads) {
+        if constexpr (PARTS > 1) {
+            if (WHOLE) __syncthreads();
+            share[part][column] = s;
+            __syncthreads();
+        }
+        if (part == 0 && q < quads) {
 #pragma unroll
-            for (int w = 1; w < WAVES; ++w) {
-                const float4 v = share[w][lane];
+            for (int w = 1; w < PARTS; ++w) {
+                const float4 v = share[w][column];
                 s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
             }
             const bool shift = q >= a.padded / 4;
             const int k = 4 * (shift ? q - a.padded / 4 : q);
             float *to = (shift ? a.g_b : a.g_w) + (size_t)ex * a.g_stride + k;
             const float v[4] = {s.x, s.y, s.z, s.w};
+            if (k + 4 <= a.features) {
+                to[0] = v[0]; to[1] = v[1]; to[2] = v[2]; to[3] = v[3];
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-                if (k + i < a.features) { to[i] = v[i]; ss = fmaf(v[i], v[i], ss); }
+                for (int i = 0; i < 4; ++i) ss = fmaf(v[i], v[i], ss);
+            } else {
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (k + i < a.features) { to[i] = v[i]; ss = fmaf(v[i], v[i], ss); }
+            }
         }
     }
-    if (wave == 0 && a.squares) {
-        ss = wave_all_sum(ss);
-        if (lane == 0) a.squares[block] = ss;
-    }
+    if (!a.squares) return;
+    ss = block_sum<THREADS / 64>(ss, red);
+    if (threadIdx.x == 0) a.squares[block] = ss;
 }
 
 constexpr int NORM_HELD = 16384;       // features that a workgroup of sixteen waves holds in registers
 
+constexpr size_t JOIN_WHOLE = 16384;
 // Threads that share a row: as many as have a run of eight, a wave for up to 1024 features (forward 2048), four for up to 8192.
 int norm_lanes(int features, bool backward)
 {
@@ -461,7 +490,7 @@ int norm_lanes(int features, bool backward)
     if (features <= 128) return 16;
     if (features <= 256) return 32;
     if (features <= (backward ? 1024 : 2048)) return 64;
-    return features <= 8192 ? 256 : backward ? 512 : 1024;
+    return backward ? features <= 4096 ? 256 : 512 : features <= 8192 ? 256 : 1024;
 }
 
 NormArgs norm_args(const NormGeo &g, bool backward)
@@ -474,7 +503,10 @@ NormArgs norm_args(const NormGeo &g, bool backward)
     if (!backward) {
         a.rows = (int)std::max(1ll, std::min(all / (2048ll * at_once), 64ll / at_once)) * at_once;
     } else {
-        const long long each = std::max(1ll, std::min(all / (1024ll * at_once), 64ll));
+        // as few sums as there may be, at two workgroups to a compute unit; five of the kernel that holds the least (us, 512 workgroups and 1024: 64 x 200
+        // tokens of 4096 features 79 and 88, 32 x 500 of 768 23.6 and 27.4; but 16 x 2048 of 2048 98 and 96, 8 x 1000 of 2048 in fp32 53.7 and 51.1)
+        const long long workgroups = g.features > 1024 && g.features <= 2048 ? 1024 : 512;
+        const long long each = std::max(1ll, std::min((all + workgroups * at_once - 1) / (workgroups * at_once), 64ll));
         a.rows = (int)std::min(each * at_once, (long long)(g.tokens + at_once - 1) / at_once * at_once);
         a.blocks = (g.tokens + a.rows - 1) / a.rows;
     }
@@ -511,7 +543,7 @@ dp_status run_backward(const NormGeo &g, const NormArgs &a, hipStream_t s)
     if (g.features <= 1024) return launch_blocks<norm_backward_kernel<BF16, WORDS, 64, 2>>(grid, 256, 0, s, a);
     if (g.features <= 2048) return launch_blocks<norm_backward_kernel<BF16, WORDS, 256, 1>>(grid, 256, 0, s, a);
     if (g.features <= 4096) return launch_blocks<norm_backward_kernel<BF16, WORDS, 256, 2>>(grid, 256, 0, s, a);
-    if (g.features <= 8192) return launch_blocks<norm_backward_kernel<BF16, WORDS, 256, 4>>(grid, 256, 0, s, a);
+    if (g.features <= 8192) return launch_blocks<norm_backward_kernel<BF16, WORDS, 512, 2>>(grid, 512, 0, s, a);
     return launch_blocks<norm_backward_kernel<BF16, WORDS, 512, 4>>(grid, 512, 0, s, a);
 }
 
@@ -562,6 +594,7 @@ dp_status launch_norm_backward(const NormGeo &g, const void *x, const float *gam
     char *room = static_cast<char *>(ws);
     a.x = x; a.dy = dy; a.out = dx; a.gamma = gamma; a.lengths = lengths;
     a.partials = g_w ? reinterpret_cast<float *>(room) : nullptr;
+    a.shift = g_b != nullptr;
     a.stats = reinterpret_cast<float *>(room + w.partials + w.squares);
     dp_status st;
     if (g.features > NORM_HELD) {
@@ -575,14 +608,18 @@ dp_status launch_norm_backward(const NormGeo &g, const void *x, const float *gam
     if (st != DP_OK || !g_w) return st;
     NormJoinArgs j = {};
     j.partials = a.partials; j.g_w = g_w; j.g_b = g_b; j.g_stride = g_stride; j.blocks = a.blocks; j.features = g.features; j.padded = a.padded;
-    j.groups = ((g_b ? 2 : 1) * a.padded / 4 + 63) / 64;
     // one workgroup an example where it has little to add up, or where there are as many as compute units
-    if (j.groups == 1 || g.n >= 256 || (size_t)a.blocks * 2 * a.padded <= 32768) {
+    const int quads = (g_b ? 2 : 1) * a.padded / 4;
+    if (g.n >= 256 || (size_t)a.blocks * quads <= JOIN_WHOLE) {
+        j.groups = 1;
         j.squares = sqnorm;
-        return launch_blocks<norm_join_kernel<true>>((size_t)g.n, 1024, 0, s, j);
+        if (quads <= 128) return launch_blocks<norm_join_kernel<1024, 128, true>>((size_t)g.n, 1024, 0, s, j);
+        return launch_blocks<norm_join_kernel<1024, 512, true>>((size_t)g.n, 1024, 0, s, j);
     }
+    j.groups = (quads + 63) / 64;
     j.squares = sqnorm ? reinterpret_cast<float *>(room + w.partials) : nullptr;
-    st = launch_blocks<norm_join_kernel<false>>((size_t)g.n * j.groups, 256, 0, s, j);
+    st = (size_t)g.n * j.groups <= 512 ? launch_blocks<norm_join_kernel<1024, 64, false>>((size_t)g.n * j.groups, 1024, 0, s, j)
+                                       : launch_blocks<norm_join_kernel<256, 64, false>>((size_t)g.n * j.groups, 256, 0, s, j);
     if (st != DP_OK || !sqnorm) return st;
     return launch_sum_partials(j.squares, g.n, j.groups, sqnorm, s);
 }
