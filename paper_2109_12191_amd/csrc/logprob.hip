@@ -167,13 +167,12 @@ __device__ __forceinline__ void see(Seen &v, const float (&x)[U][8], float scale
         }
 }
 
-// Runs q0 + t, q0 + t + TPR .. below q1, of a row, by TPR threads.
+// Runs q0 + t, q0 + t + TPR .. below q1, of a row, by TPR threads.  `raw`: a thread's last four.
 template <bool BF16, int TPR>
-__device__ __forceinline__ void see_runs(Seen &v, const LogitRow<BF16> &row, int q0, int q1, int t, float scale, bool entropy)
+__device__ __forceinline__ void see_runs(Seen &v, const LogitRow<BF16> &row, int q0, int q1, int t, float scale, bool entropy, Raw8<BF16> (&raw)[4])
 {
     constexpr int U = 4;
     for (int q = q0; q < q1; q += U * TPR) {
-        Raw8<BF16> raw[U];
 #pragma unroll
         for (int u = 0; u < U; ++u) row.load(raw[u], q + t + u * TPR);
         float x[U][8];
@@ -233,11 +232,10 @@ __device__ __forceinline__ bool before(float x, int i, float y, int j) { return 
 
 constexpr int TOP_LIST = 1024;
 struct TopShared {
-    float most[256];
+    float bound[4];
     float list[TOP_LIST];
     int list_token[TOP_LIST];
     int threads[256];
-    float bound;
     int thread_count, list_count;
     float best[LOGPROB_TOP];
     int best_token[LOGPROB_TOP];
@@ -245,35 +243,68 @@ struct TopShared {
     int wave_token[4];
 };
 
+// The k-th largest of a wave's values (equal ones count one by one), in every lane.
+__device__ __forceinline__ float wave_kth(float v, int k)
+{
+    const int lane = (int)threadIdx.x & 63;
+    float m = wave_all_max(v);
+    for (; k > 1; --k) {
+        if (lane == __ffsll((long long)__ballot(v == m)) - 1) v = -INFINITY;
+        m = wave_all_max(v);
+    }
+    return m;
+}
+
 // The `top` largest logits of runs q0 .. q1 - 1 of a row, in order, into best / best_token (-inf and -1 beyond the last one above -inf).  `most`: the
-// largest logit of this thread's runs, q0 + thread + 256 j.  By a workgroup of 256; ends with a barrier.
-template <bool BF16>
-__device__ __forceinline__ void find_top(TopShared &sh, const LogitRow<BF16> &row, int q0, int q1, float most, int top)
+// largest logit of this thread's runs, q0 + thread + 256 j.  HELD: `raw` are those runs.  By a workgroup of 256; ends with a barrier.
+// The bound: of the waves whose threads all have a run (or the first), each holds a share of `top` logits that reach its share-th largest, so `top` reach the
+// lowest of these.
+template <bool BF16, bool HELD>
+__device__ __forceinline__ void find_top(TopShared &sh, const LogitRow<BF16> &row, int q0, int q1, float most, int top, const Raw8<BF16> (&raw)[4])
 {
     const int t = threadIdx.x, end = min(row.count, row.index(q1));
-    sh.most[t] = most;
+    const int waves = min(max((q1 - q0) >> 6, 1), 4);
+    if (t < 64 * waves) {
+        const float kth = wave_kth(most, (top + waves - 1) / waves);
+        if ((t & 63) == 0) sh.bound[t >> 6] = kth;
+    }
     if (t == 0) { sh.thread_count = 0; sh.list_count = 0; }
     if (t < LOGPROB_TOP) { sh.best[t] = -INFINITY; sh.best_token[t] = -1; }
     __syncthreads();
-    int rank = 0;
-    for (int u = 0; u < 256; u += 4) {
-        const float4 v = *reinterpret_cast<const float4 *>(sh.most + u);
-        rank += before(v.x, u, most, t) + before(v.y, u + 1, most, t) + before(v.z, u + 2, most, t) + before(v.w, u + 3, most, t);
-    }
-    if (rank == top - 1) sh.bound = most;
-    __syncthreads();
-    const float bound = sh.bound;
-    if (most >= bound) sh.threads[atomicAdd(&sh.thread_count, 1)] = t;
-    __syncthreads();
-    const int each = (q1 - q0 + 255) / 256 * 8, all = sh.thread_count * each;
-    for (int e = t; e < all; e += 256) {
-        const int which = e / each, in = e - which * each;
-        const int v = row.index(q0 + sh.threads[which] + 256 * (in >> 3)) + (in & 7);
-        if (v < 0 || v >= end) continue;
-        const float x = In<BF16>::ld(row.first + v);
-        if (x >= bound && x > -INFINITY) {
-            const int at = atomicAdd(&sh.list_count, 1);
-            if (at < TOP_LIST) { sh.list[at] = x; sh.list_token[at] = v; }
+    float bound = sh.bound[0];
+    for (int w = 1; w < waves; ++w) bound = fminf(bound, sh.bound[w]);
+    auto enter = [&](float x, int v) {
+        const int at = atomicAdd(&sh.list_count, 1);
+        if (at < TOP_LIST) { sh.list[at] = x; sh.list_token[at] = v; }
+    };
+    if constexpr (HELD) {
+        if (most >= bound)
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                const int v0 = row.index(q0 + t + 256 * u);
+                float x[8];
+                run_values<BF16, true>(raw[u], v0, end, x);
+                unsigned hits = 0;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) hits |= x[i] >= bound && x[i] > -INFINITY ? 1u << i : 0u;
+                for (; hits; hits &= hits - 1) {
+                    const int at = __ffs((int)hits) - 1;
+                    float y = x[0];
+#pragma unroll
+                    for (int i = 1; i < 8; ++i) y = at == i ? x[i] : y;
+                    enter(y, v0 + at);
+                }
+            }
+    } else {
+        if (most >= bound) sh.threads[atomicAdd(&sh.thread_count, 1)] = t;
+        __syncthreads();
+        const int each = (q1 - q0 + 255) / 256 * 8, all = sh.thread_count * each;
+        for (int e = t; e < all; e += 256) {
+            const int which = e / each, in = e - which * each;
+            const int v = row.index(q0 + sh.threads[which] + 256 * (in >> 3)) + (in & 7);
+            if (v < 0 || v >= end) continue;
+            const float x = In<BF16>::ld(row.first + v);
+            if (x >= bound && x > -INFINITY) enter(x, v);
         }
     }
     __syncthreads();
@@ -283,7 +314,8 @@ __device__ __forceinline__ void find_top(TopShared &sh, const LogitRow<BF16> &ro
             const float x = sh.list[c];
             const int v = sh.list_token[c];
             int place = 0;
-            for (int o = 0; o < count && place < top; ++o) place += before(sh.list[o], sh.list_token[o], x, v);
+#pragma unroll 8
+            for (int o = 0; o < count; ++o) place += before(sh.list[o], sh.list_token[o], x, v);
             if (place < top) { sh.best[place] = x; sh.best_token[place] = v; }
         }
     } else {
@@ -344,20 +376,97 @@ __global__ void __launch_bounds__(256) logprob_kernel(const LogprobArgs a)
     const LogitRow<BF16> row(a.logits, r * a.row_stride, a.vocab);
     Seen v;
     v.none();
-    see_runs<BF16, TPR>(v, row, 0, row.runs(), t, a.scale, a.entropy_out != nullptr);
+    Raw8<BF16> raw[4];
+    see_runs<BF16, TPR>(v, row, 0, row.runs(), t, a.scale, a.entropy_out != nullptr, raw);
     const float most = v.m;
     row_join<TPR>(v, a.scale, red);
     const RowResult res = row_result(v);
     if (t == 0) write_row<BF16>(a, row.first, r, res);
     if constexpr (TOP) {
         __shared__ TopShared sh;
-        find_top<BF16>(sh, row, 0, row.runs(), most, a.top);
+        find_top<BF16, false>(sh, row, 0, row.runs(), most, a.top, raw);
         if (t < a.top) write_top(a, r, t, sh.best[t], sh.best_token[t], res);
     }
 }
 
-// Rows that several workgroups share: each leaves what it has seen, and its largest logits.
-template <bool BF16, bool TOP>
+// Rows with alternatives, short enough for a wave to hold one: the largest logit is looked for `top` times, and taken out.  A lane knows the largest
+// of each of its runs, so a search is two reductions over the lanes and one run of eight (us, a workgroup a row and this, 8192 rows of 1000 logits with 8
+// alternatives 42 and 17, with 32 96 and 43; of 4000 logits, with twice the registers, 43 and 41, 68 and 92).
+template <bool BF16, int NV>
+__global__ void __launch_bounds__(256) logprob_wave_top_kernel(const LogprobArgs a)
+{
+    const int slot = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lane = (int)threadIdx.x & 63;
+    const size_t r = (size_t)(a.first_block + blockIdx.x) * 4 + slot;
+    if (r >= (size_t)a.rows) return;
+    if (!row_there(a, (unsigned)r)) {
+        if (lane == 0) write_absent(a, r);
+        return;
+    }
+    const LogitRow<BF16> row(a.logits, r * a.row_stride, a.vocab);
+    float x[NV][8], run_most[NV];
+    int run_at[NV];
+    auto most_of = [&](int j) {                          // of a run, the first of the largest
+        run_most[j] = x[j][0];
+        run_at[j] = 0;
+#pragma unroll
+        for (int i = 1; i < 8; ++i) {
+            const bool more = x[j][i] > run_most[j];
+            run_most[j] = more ? x[j][i] : run_most[j];
+            run_at[j] = more ? i : run_at[j];
+        }
+    };
+    {
+        Raw8<BF16> raw[NV];
+#pragma unroll
+        for (int j = 0; j < NV; ++j) row.load(raw[j], lane + 64 * j);
+#pragma unroll
+        for (int j = 0; j < NV; ++j) run_values<BF16, true>(raw[j], row.index(lane + 64 * j), row.count, x[j]);
+    }
+    Seen v;
+    v.none();
+    see<NV>(v, x, a.scale, a.entropy_out != nullptr);
+    wave_join(v, a.scale);
+    const RowResult res = row_result(v);
+    if (lane == 0) write_row<BF16>(a, row.first, r, res);
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[j][i] = x[j][i] == x[j][i] ? x[j][i] : -INFINITY;          // (rows with a NaN have no alternatives)
+        most_of(j);
+    }
+    float best = -INFINITY;
+    int best_token = -1;
+    for (int k = 0; k < a.top; ++k) {
+        float most = run_most[0];
+        int at = run_at[0], run = 0;
+#pragma unroll
+        for (int j = 1; j < NV; ++j) {
+            const bool more = run_most[j] > most;
+            most = more ? run_most[j] : most;
+            at = more ? run_at[j] : at;
+            run = more ? j : run;
+        }
+        const float all = wave_all_max(most);
+        if (!(all > -INFINITY)) break;
+        const int mine = row.index(lane + 64 * run) + at;
+        const int token = (int)-wave_all_max(most == all ? -(float)mine : -INFINITY);          // (below 2^24: a float exactly)
+        if (lane == k) { best = all; best_token = token; }
+        const int place = token + row.lead, taken = place >> 9;                                 // 64 runs of eight
+#pragma unroll
+        for (int j = 0; j < NV; ++j)
+            if (taken == j) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    if (lane == ((place >> 3) & 63) && (place & 7) == i) x[j][i] = -INFINITY;
+                most_of(j);
+            }
+    }
+    if (lane < a.top) write_top(a, r, lane, best, best_token, res);
+}
+
+// Rows that several workgroups share: each leaves what it has seen, and its largest logits.  A row's partial results: (m, s, t) of its workgroups, four
+// words each, then their largest logits, second largest and so on, then those logits' tokens.  TOP: 0, no alternatives; 1; 2, at most four runs a thread.
+template <bool BF16, int TOP>
 __global__ void __launch_bounds__(256) logprob_split_kernel(const LogprobArgs a)
 {
     __shared__ float red[12];
@@ -368,26 +477,28 @@ __global__ void __launch_bounds__(256) logprob_split_kernel(const LogprobArgs a)
     const int q0 = split * a.split_runs, q1 = min(q0 + a.split_runs, row.runs());
     Seen v;
     v.none();
-    see_runs<BF16, 256>(v, row, q0, q1, (int)threadIdx.x, a.scale, a.entropy_out != nullptr);
+    Raw8<BF16> raw[4];
+    see_runs<BF16, 256>(v, row, q0, q1, (int)threadIdx.x, a.scale, a.entropy_out != nullptr, raw);
     const float most = v.m;
     row_join<256>(v, a.scale, red);
-    float *part = a.partials + (size_t)block * (4 + 2 * a.top);
-    if (threadIdx.x == 0) *reinterpret_cast<float2 *>(part) = make_float2(v.m, v.s), part[2] = v.t;
+    float *part = a.partials + (size_t)r * a.splits * (4 + 2 * a.top);
+    if (threadIdx.x == 0) *reinterpret_cast<float4 *>(part + 4 * split) = make_float4(v.m, v.s, v.t, 0.0f);
     if constexpr (TOP) {
         __shared__ TopShared sh;
-        find_top<BF16>(sh, row, q0, q1, most, a.top);
+        find_top<BF16, TOP == 2>(sh, row, q0, q1, most, a.top, raw);
         if ((int)threadIdx.x < a.top) {
-            part[4 + threadIdx.x] = sh.best[threadIdx.x];
-            part[4 + a.top + threadIdx.x] = __int_as_float(sh.best_token[threadIdx.x]);
+            part += 4 * a.splits + (int)threadIdx.x * a.splits + split;
+            part[0] = sh.best[threadIdx.x];
+            part[a.top * a.splits] = __int_as_float(sh.best_token[threadIdx.x]);
         }
     }
 }
 
-// What the workgroups of a row have left, joined by a wave a row.  Alternatives: the workgroups' lists are in order, so the k-th largest of their first
-// entries, as many of each as make k or more together, is a bound as in find_top.
+// What the workgroups of a row have left, joined by a workgroup a row, from as many loads at once as there are.  Alternatives: the k-th largest of the
+// workgroups' first entries, as many of each as make 3 k together, is a bound as in find_top.
 constexpr int MOST_SPLITS = 64;
-template <bool BF16>
-__global__ void __launch_bounds__(64) logprob_join_kernel(const LogprobArgs a)
+template <bool BF16, bool TOP>
+__global__ void __launch_bounds__(256) logprob_join_kernel(const LogprobArgs a)
 {
     const size_t r = a.first_block + blockIdx.x;
     const int t = threadIdx.x;
@@ -395,46 +506,61 @@ __global__ void __launch_bounds__(64) logprob_join_kernel(const LogprobArgs a)
         if (t == 0) write_absent(a, r);
         return;
     }
-    const int words = 4 + 2 * a.top;
-    const float *part = a.partials + r * a.splits * words;
+    const float *part = a.partials + r * a.splits * (4 + 2 * a.top);
     Seen v;
     v.none();
-    if (t < a.splits) v = {part[t * words], part[t * words + 1], part[t * words + 2]};
+    const int lane = t & 63, all = a.top * a.splits;
+    if (lane < a.splits) {
+        const float4 p = *reinterpret_cast<const float4 *>(part + 4 * lane);
+        v = {p.x, p.y, p.z};
+    }
+    constexpr int MOST = MOST_SPLITS * LOGPROB_TOP / 256;
+    float x[MOST];
+    int token[MOST];
+    if constexpr (TOP)
+#pragma unroll
+        for (int i = 0; i < MOST; ++i) {
+            const int e = t + 256 * i;
+            x[i] = e < all ? part[4 * a.splits + e] : -INFINITY;
+            token[i] = e < all ? __float_as_int(part[4 * a.splits + all + e]) : -1;
+        }
     wave_join(v, a.scale);
     const RowResult res = row_result(v);
     if (t == 0) write_row<BF16>(a, static_cast<const typename In<BF16>::type *>(a.logits) + r * a.row_stride, r, res);
-    if (a.top == 0) return;
-    __shared__ float list[MOST_SPLITS * LOGPROB_TOP], bound;
-    __shared__ int list_token[MOST_SPLITS * LOGPROB_TOP], count;
-    const int each = (a.top + a.splits - 1) / a.splits, some = each * a.splits;
-    if (t == 0) { count = 0; bound = -FLT_MAX; }
-    for (int e = t; e < some; e += 64) {
-        const float *p = part + (e / each) * words + 4 + e % each;
-        list[e] = p[0];
-        list_token[e] = __float_as_int(p[a.top]);
-    }
-    __syncthreads();
-    for (int e = t; e < some; e += 64) {
-        int place = 0;
-        for (int o = 0; o < some; ++o) place += list[o] > list[e] || (list[o] == list[e] && o < e);
-        if (place == a.top - 1) bound = fmaxf(list[e], -FLT_MAX);
-    }
-    __syncthreads();
-    for (int e = t; e < a.splits * a.top; e += 64) {
-        const float *p = part + (e / a.top) * words + 4 + e % a.top;
-        if (p[0] >= bound) {
-            const int at = atomicAdd(&count, 1);
-            list[at] = p[0];
-            list_token[at] = __float_as_int(p[a.top]);
+    if constexpr (TOP) {
+        __shared__ float list[MOST_SPLITS * LOGPROB_TOP], bound;
+        __shared__ int list_token[MOST_SPLITS * LOGPROB_TOP], count;
+        const int some = min(a.top, (3 * a.top + a.splits - 1) / a.splits) * a.splits;      // at most 3 top + splits, below 256
+        if (t == 0) count = 0;
+        if (t < some) list[t] = x[0];
+        __syncthreads();
+        if (t < some) {
+            int place = 0;
+#pragma unroll 8
+            for (int o = 0; o < some; ++o) place += before(list[o], o, x[0], t);
+            if (place == a.top - 1) bound = fmaxf(x[0], -FLT_MAX);
         }
+        __syncthreads();
+        const float least = bound;
+#pragma unroll
+        for (int i = 0; i < MOST; ++i)
+            if (x[i] >= least) {
+                const int at = atomicAdd(&count, 1);
+                list[at] = x[i];
+                list_token[at] = token[i];
+            }
+        __syncthreads();
+        const int entries = count;
+        for (int e = t; e < entries; e += 256) {
+            const float y = list[e];
+            const int w = list_token[e];
+            int place = 0;
+#pragma unroll 8
+            for (int o = 0; o < entries; ++o) place += before(list[o], list_token[o], y, w);
+            if (place < a.top) write_top(a, r, place, y, w, res);
+        }
+        if (t >= entries && t < a.top) write_top(a, r, t, -INFINITY, -1, res);
     }
-    __syncthreads();
-    for (int e = t; e < count; e += 64) {
-        int place = 0;
-        for (int o = 0; o < count && place < a.top; ++o) place += before(list[o], list_token[o], list[e], list_token[e]);
-        if (place < a.top) write_top(a, r, place, list[e], list_token[e], res);
-    }
-    if (t >= count && t < a.top) write_top(a, r, t, -INFINITY, -1, res);
 }
 
 constexpr int NO_TARGET = -(1 << 30);
@@ -603,12 +729,14 @@ __global__ void __launch_bounds__(TPR > 256 ? TPR : 256) logprob_held_kernel(con
 
 size_t round16(size_t b) { return (b + 15) & ~(size_t)15; }
 
-// Workgroups that share a row: as many as make 1024 together, of 2048 logits or more each.
+// Workgroups that share a row: as many as make 1024 together, of 4096 logits or more each, where the launch that joins them pays (us, shared and not: 8 rows
+// of 20000 logits 6.2 and 5.6, of 40000 6.1 and 7.2, with 4 alternatives 12.3 and 11.3, of 60000 12.2 and 14.8; 100 rows of 40000 9.4 and 8.6, 150 of
+// 131072 15.5 and 23.4, 300 of 50000 14.6 and 13.2, of 131072 24.4 and 27.0).
 int logprob_splits(const LogprobGeo &g)
 {
     const long long rows = (long long)g.n * g.tokens;
-    if (rows >= 512 || g.vocab < 8192) return 1;
-    return (int)std::min<long long>({MOST_SPLITS, 1024 / rows, g.vocab / 2048});
+    if (rows >= 512 || g.vocab < 32768 + 128 * rows) return 1;
+    return (int)std::min<long long>({MOST_SPLITS, 1024 / rows, g.vocab / 4096});
 }
 
 LogprobArgs logprob_args(const LogprobGeo &g)
@@ -628,8 +756,9 @@ size_t partial_bytes(const LogprobGeo &g)
 }
 
 // Whether the gradient without statistics holds its rows in registers: rows that fit (with the place before them where they may begin inside a dword),
-// and enough of them.
-bool holds_rows(const LogprobGeo &g) { return g.vocab <= (g.bf16 ? 131071 : 65536) && logprob_splits(g) == 1; }
+// and enough of them (us, workgroups that share a row, then a pass over all, and held rows: 8 rows of 131000 bf16 logits 11 and 22, 64 of them 16 and 25,
+// 100 26 and 28, 200 40 and 34).
+bool holds_rows(const LogprobGeo &g) { return g.vocab <= (g.bf16 ? 131071 : 65536) && ((long long)g.n * g.tokens >= 128 || logprob_splits(g) == 1); }
 // Places of a row's runs.
 int held_places(const LogprobArgs &a, bool bf16)
 {
@@ -642,12 +771,19 @@ dp_status run_logprobs(const LogprobArgs &a, hipStream_t s)
 {
     const size_t rows = (size_t)a.rows;
     if (a.splits > 1) {
-        const dp_status st = a.top ? launch_blocks<logprob_split_kernel<BF16, true>>(rows * a.splits, 256, 0, s, a)
-                                   : launch_blocks<logprob_split_kernel<BF16, false>>(rows * a.splits, 256, 0, s, a);
+        const dp_status st = !a.top ? launch_blocks<logprob_split_kernel<BF16, 0>>(rows * a.splits, 256, 0, s, a)
+                             : a.split_runs > 1024 ? launch_blocks<logprob_split_kernel<BF16, 1>>(rows * a.splits, 256, 0, s, a)
+                                                   : launch_blocks<logprob_split_kernel<BF16, 2>>(rows * a.splits, 256, 0, s, a);
         if (st != DP_OK) return st;
-        return launch_blocks<logprob_join_kernel<BF16>>(rows, 64, 0, s, a);
+        return a.top ? launch_blocks<logprob_join_kernel<BF16, true>>(rows, 256, 0, s, a) : launch_blocks<logprob_join_kernel<BF16, false>>(rows, 256, 0, s, a);
     }
-    if (a.top) return launch_blocks<logprob_kernel<BF16, 256, true>>(rows, 256, 0, s, a);
+    if (a.top) {
+        const int places = held_places(a, BF16);
+        if (places <= 512) return launch_blocks<logprob_wave_top_kernel<BF16, 1>>((rows + 3) / 4, 256, 0, s, a);
+        if (places <= 1024) return launch_blocks<logprob_wave_top_kernel<BF16, 2>>((rows + 3) / 4, 256, 0, s, a);
+        if (places <= 2048) return launch_blocks<logprob_wave_top_kernel<BF16, 4>>((rows + 3) / 4, 256, 0, s, a);
+        return launch_blocks<logprob_kernel<BF16, 256, true>>(rows, 256, 0, s, a);
+    }
     if (a.vocab <= 4096) return launch_blocks<logprob_kernel<BF16, 64, false>>((rows + 3) / 4, 256, 0, s, a);
     return launch_blocks<logprob_kernel<BF16, 256, false>>(rows, 256, 0, s, a);
 }
