@@ -511,8 +511,8 @@ typedef struct dp_norm_desc {
 
 /* gamma, beta [device] [features], or NULL: ones, zeros.  x, y [device], aligned to their element; y may be x.
  * lengths [device] [n] int32 tokens of each example (taken as 0 .. tokens), or NULL: all.  Rows of y beyond them are zeros, and what lies there
- * in x is not used, whatever it is.  A row with a NaN or an infinity is NaN; one whose squared deviations add up beyond fp32's range is beta
- * (deviations of 10^19 / sqrt(features) are safe).                                                                                */
+ * in x is not used, whatever it is.  A row with a NaN or an infinity is NaN, and so is one whose sums leave fp32's range (squares of deviations that add
+ * up to less than 10^38 do not).                                                                                */
 dp_status dp_layer_norm(const dp_norm_desc *desc /*[host]*/, const void *x, const float *gamma, const float *beta, const int32_t *lengths, void *y,
                         dp_stream stream);
 
@@ -557,7 +557,8 @@ dp_status dp_token_logprobs(const dp_logprob_desc *desc /*[host]*/, const void *
  *   dlogits_v = scale * (d_logprobs * ([v is the target] - p_v) - d_entropy * p_v * (logp_v + H))
  * d_logprobs, d_entropy [device] [n, tokens], or NULL: zeros (not both).  Rows without a target have no share of d_logprobs, whatever it is.
  * stats, entropy [device] as dp_token_logprobs left them (entropy only for d_entropy); stats NULL: worked out in the same call -- a training step that
- *              knows its tokens' weights beforehand needs this call alone.  A row of logits is then read once, up to 131072 bf16 or 65536 fp32.
+ *              knows its tokens' weights beforehand needs this call alone.  Where there are rows enough, one of up to 131071 bf16
+ *              or 65536 fp32 logits is then read once.
  * logprobs     [device] [n, tokens] or NULL: written as dp_token_logprobs does.
  * dlogits      [device] in_dtype, zeros beyond the lengths and in rows of nothing but -inf, NaN in rows with a NaN or +inf; may be logits.
  * desc->top has to be 0.  ws: dp_token_logprobs_workspace_bytes(desc).                                                           */

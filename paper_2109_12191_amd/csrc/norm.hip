@@ -83,19 +83,13 @@ __device__ __forceinline__ void values(const Raw8<BF16> (&raw)[NV], int t, int s
     }
 }
 
-// x becomes its deviations from the mean, zeros stay zeros beyond the row (but for the rounding of the mean, whose correction comes out of the next sums).
+// A thread's values of a row become less by `by`; zeros stay zeros beyond the row.
 template <int TPR, int NV>
-__device__ __forceinline__ void centre(const NormArgs &a, int t, float (&x)[8 * NV], float *red, int &turn)
+__device__ __forceinline__ void lower(const NormArgs &a, int t, float (&x)[8 * NV], float by)
 {
-    if (a.rms) return;
-    float s[1] = {0.0f};
-#pragma unroll
-    for (int i = 0; i < 8 * NV; ++i) s[0] += x[i];
-    row_sums<TPR, 1>(s, red, turn);
-    const float mean = s[0] * a.inv_features;
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
-        const float m = 8 * (t + TPR * j) < a.features ? mean : 0.0f;
+        const float m = 8 * (t + TPR * j) < a.features ? by : 0.0f;
 #pragma unroll
         for (int i = 0; i < 8; ++i) x[8 * j + i] -= m;
     }
@@ -107,6 +101,30 @@ __device__ __forceinline__ void centre(const NormArgs &a, int t, float (&x)[8 * 
             for (int i = 0; i < 8; ++i) x[8 * j + i] = i < left ? x[8 * j + i] : 0.0f;
         }
     }
+}
+
+// x becomes its deviations from the mean (but for the rounding of the mean, whose correction comes out of the next sums).
+template <int TPR, int NV>
+__device__ __forceinline__ void centre(const NormArgs &a, int t, float (&x)[8 * NV], float *red, int &turn)
+{
+    if (a.rms) return;
+    float s[1] = {0.0f};
+#pragma unroll
+    for (int i = 0; i < 8 * NV; ++i) s[0] += x[i];
+    row_sums<TPR, 1>(s, red, turn);
+    lower<TPR, NV>(a, t, x, s[0] * a.inv_features);
+}
+
+// Whether what the mean's rounding left in the deviations, `off`, is much of them: a row of nearly one value, whose deviations are taken from their own
+// mean once more (each time is good for 2^-18 of the value before).
+constexpr int AGAIN = 3;
+__device__ __forceinline__ bool once_more(float off, float mean_square) { return off * off > mean_square * 0x1p-8f; }
+
+// 1 / sqrt(variance + eps), from deviations whose mean is `off`; NaN where their squares are no number below infinity.
+__device__ __forceinline__ float inverse_size(float off, float mean_square, float eps)
+{
+    const float v = fmaf(-off, off, mean_square);
+    return mean_square < INFINITY ? 1.0f / sqrtf((v < 0.0f ? 0.0f : v) + eps) : NAN;
 }
 
 // gamma or beta of eight columns from k on; `none` where there is no such tensor
@@ -165,12 +183,18 @@ __global__ void __launch_bounds__(TPR > 256 ? TPR : 256) norm_kernel(const NormA
 #pragma unroll
         for (int j = 0; j < NV; ++j) in.load(next[j], there, row + slots, 8 * (t + TPR * j));
         centre<TPR, NV>(a, t, x, red, turn);
-        float s[2] = {0.0f, 0.0f};
+        float s[2], off;
+        for (int again = 0;; ++again) {
+            s[0] = s[1] = 0.0f;
 #pragma unroll
-        for (int i = 0; i < 8 * NV; ++i) { s[0] += x[i]; s[1] = fmaf(x[i], x[i], s[1]); }
-        if (a.rms) s[0] = 0.0f;
-        row_sums<TPR, 2>(s, red, turn);
-        const float off = s[0] * a.inv_features, r = 1.0f / sqrtf(fmaf(-off, off, s[1] * a.inv_features) + a.eps), shift = -off * r;
+            for (int i = 0; i < 8 * NV; ++i) { s[0] += x[i]; s[1] = fmaf(x[i], x[i], s[1]); }
+            if (a.rms) s[0] = 0.0f;
+            row_sums<TPR, 2>(s, red, turn);
+            off = s[0] * a.inv_features;
+            if (again == AGAIN || !once_more(off, s[1] * a.inv_features)) break;
+            lower<TPR, NV>(a, t, x, off);
+        }
+        const float r = inverse_size(off, s[1] * a.inv_features, a.eps), shift = -off * r;
         if (row < rows) {
 #pragma unroll
             for (int j = 0; j < NV; ++j) {
@@ -220,18 +244,24 @@ __global__ void __launch_bounds__(TPR > 256 ? TPR : 256) norm_backward_kernel(co
             values<BF16, NV>(next2, t, TPR, a.features, d);
             fetch(row + slots);
             centre<TPR, NV>(a, t, x, red, turn);
-            float s[4] = {0.0f, 0.0f, 0.0f, 0.0f};       // of deviations, their squares, a, and a times deviations
+            float s[4], off;                             // of deviations, their squares, a, and a times deviations
+            for (int again = 0;; ++again) {
+                s[0] = s[1] = s[2] = s[3] = 0.0f;
 #pragma unroll
-            for (int i = 0; i < 8 * NV; ++i) {
-                const float g = d[i] * gamma[i];
-                s[0] += x[i];
-                s[1] = fmaf(x[i], x[i], s[1]);
-                s[2] += g;
-                s[3] = fmaf(g, x[i], s[3]);
+                for (int i = 0; i < 8 * NV; ++i) {
+                    const float g = d[i] * gamma[i];
+                    s[0] += x[i];
+                    s[1] = fmaf(x[i], x[i], s[1]);
+                    s[2] += g;
+                    s[3] = fmaf(g, x[i], s[3]);
+                }
+                if (a.rms) s[0] = s[2] = 0.0f;
+                row_sums<TPR, 4>(s, red, turn);
+                off = s[0] * a.inv_features;
+                if (again == AGAIN || !once_more(off, s[1] * a.inv_features)) break;
+                lower<TPR, NV>(a, t, x, off);
             }
-            if (a.rms) s[0] = s[2] = 0.0f;
-            row_sums<TPR, 4>(s, red, turn);
-            const float off = s[0] * a.inv_features, r = 1.0f / sqrtf(fmaf(-off, off, s[1] * a.inv_features) + a.eps);
+            const float r = inverse_size(off, s[1] * a.inv_features, a.eps);
             const float level = s[2] * a.inv_features, along = r * (s[3] - off * s[2]) * a.inv_features;
             const float shift = -off * r, slope = -r * along, base = -r * level;
             const bool there = TPR >= 64 || row < length;
@@ -326,35 +356,41 @@ __global__ void __launch_bounds__(1024) norm_long_kernel(const NormArgs a)
         row_sums<1024, 1>(s, red, turn);
         mean = s[0] * a.inv_features;
     }
-    float s[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-    for (int k = 8 * (int)threadIdx.x; k < a.features; k += 8192) {
-        Raw8<BF16> raw;
-        raw.load(x, (size_t)k, a.features - k);
-        float v[8], g[8];
-        raw.get(v);
-        if constexpr (BACKWARD) {
-            float gamma[8];
-            raw.load(dy, (size_t)k, a.features - k);
-            raw.get(g);
-            columns8(a.gamma, 1.0f, k, a.features, gamma);
+    float s[4], off, taken = 0.0f;                   // taken: what the deviations have been lowered by
+    for (int again = 0;; ++again) {
+        s[0] = s[1] = s[2] = s[3] = 0.0f;
+        for (int k = 8 * (int)threadIdx.x; k < a.features; k += 8192) {
+            Raw8<BF16> raw;
+            raw.load(x, (size_t)k, a.features - k);
+            float v[8], g[8];
+            raw.get(v);
+            if constexpr (BACKWARD) {
+                float gamma[8];
+                raw.load(dy, (size_t)k, a.features - k);
+                raw.get(g);
+                columns8(a.gamma, 1.0f, k, a.features, gamma);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) g[i] *= gamma[i];
-        }
+                for (int i = 0; i < 8; ++i) g[i] *= gamma[i];
+            }
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const float dev = i < a.features - k ? v[i] - mean : 0.0f;
-            s[0] += dev;
-            s[1] = fmaf(dev, dev, s[1]);
-            if constexpr (BACKWARD) { s[2] += g[i]; s[3] = fmaf(g[i], dev, s[3]); }
+            for (int i = 0; i < 8; ++i) {
+                const float dev = i < a.features - k ? v[i] - mean - taken : 0.0f;
+                s[0] += dev;
+                s[1] = fmaf(dev, dev, s[1]);
+                if constexpr (BACKWARD) { s[2] += g[i]; s[3] = fmaf(g[i], dev, s[3]); }
+            }
         }
+        if (a.rms) s[0] = s[2] = 0.0f;
+        row_sums<1024, 4>(s, red, turn);
+        off = s[0] * a.inv_features;
+        if (again == AGAIN || !once_more(off, s[1] * a.inv_features)) break;
+        taken += off;
     }
-    if (a.rms) s[0] = s[2] = 0.0f;
-    row_sums<1024, 4>(s, red, turn);
-    const float off = s[0] * a.inv_features, r = 1.0f / sqrtf(fmaf(-off, off, s[1] * a.inv_features) + a.eps);
+    const float r = inverse_size(off, s[1] * a.inv_features, a.eps);
     if constexpr (BACKWARD) {
         // (the mean and its correction are kept apart: together they would be rounded to the mean's digits)
         if (threadIdx.x == 0) {
-            *reinterpret_cast<float4 *>(a.stats + 4 * row) = make_float4(mean, off, r, r * (s[3] - off * s[2]) * a.inv_features);
+            *reinterpret_cast<float4 *>(a.stats + 4 * row) = make_float4(mean, taken + off, r, r * (s[3] - off * s[2]) * a.inv_features);
             a.stats[4 * (size_t)a.n * a.tokens + row] = s[2] * a.inv_features;
         }
         return;
@@ -367,7 +403,7 @@ __global__ void __launch_bounds__(1024) norm_long_kernel(const NormArgs a)
         columns8(a.gamma, 1.0f, k, a.features, gamma);
         columns8(a.beta, 0.0f, k, a.features, beta);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = fmaf((v[i] - mean - off) * r, gamma[i], beta[i]);
+        for (int i = 0; i < 8; ++i) v[i] = fmaf((v[i] - mean - taken - off) * r, gamma[i], beta[i]);
         store8(out + k, a.features - k, v);
     }
 }

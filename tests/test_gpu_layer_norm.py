@@ -328,3 +328,43 @@ def test_gradients_go_on_to_the_clipped_sum():
     # and the factor: half of the squared norm's error, a square root, a division
     off += 200 * U * torch.cat(((f * g_w).abs().sum(0), (f * g_b).abs().sum(0)))
     close(acc, want, off, "clipped sum")
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("features", [40, 100, 200, 500, 1000, 3001, 9000, 20000])
+def test_rows_of_one_value(features, dtype):
+    """Whatever the value: no deviation, y is beta and the scale's gradient zero.  A sum of equal values is off by 2^-18 of it at most, and so is its mean, whose
+    deviations are taken three times more: 2^-72 of 2^60, far below eps."""
+    x = torch.tensor([1e-30, 1.0, -777.7, 1e12, 1e18, 3e-8], device="cuda:0")[None, :, None].expand(2, 6, features).contiguous()
+    _, dy, gamma, beta = data(2, 6, features, 1)
+    x, dy = x.to(dtype), dy.to(dtype)
+    desc = desc_of(x)
+    ws = torch.empty(dp.dp_layer_norm_workspace_bytes(desc), dtype=torch.uint8, device="cuda:0")
+    y, dx, g_w, g_b = torch.empty_like(x), torch.empty_like(x), torch.empty((2, features), device="cuda:0"), torch.empty((2, features), device="cuda:0")
+    dp.dp_layer_norm(desc, x, gamma, beta, y)
+    assert bool(((y.double() - beta.double()).abs() <= HALF[dtype] * beta.double().abs() + 1e-4 * gamma.double().abs()).all())
+    if features % 4 == 0:
+        dp.dp_layer_norm_backward(desc, x, gamma, dy, dx, g_w, g_b, None, ws)
+        a = dy.double() * gamma.double()
+        want = (a - a.mean(2, keepdim=True)) / EPS ** 0.5
+        assert bool(((dx.double() - want).abs() <= HALF[dtype] * want.abs() + 1e-3 * (1.0 + a.abs().amax(2, keepdim=True)) / EPS ** 0.5).all())
+        assert bool((g_w.double().abs() <= 1e-4 * dy.double().abs().sum(1)).all())
+
+
+@pytest.mark.parametrize("rms", [0, 1])
+@pytest.mark.parametrize("features", [40, 200, 700, 1500, 6000, 18000])
+def test_rows_beyond_the_range_are_no_numbers(features, rms):
+    """An infinity or a NaN anywhere, or squares whose sum is beyond fp32: nothing of the row passes for a number, nor its example's norm."""
+    x, dy, gamma, beta = data(3, 3, features, 2)
+    x[0, 0, 7], x[0, 1, features - 1] = math.inf, math.nan
+    x[1, 2] *= 1e25
+    desc = desc_of(x, rms=rms)
+    ws = torch.empty(dp.dp_layer_norm_workspace_bytes(desc), dtype=torch.uint8, device="cuda:0")
+    y, dx, g_w, g_b, sq = torch.empty_like(x), torch.empty_like(x), torch.empty((3, features), device="cuda:0"), torch.empty((3, features), device="cuda:0"), torch.empty(3, device="cuda:0")
+    dp.dp_layer_norm(desc, x, gamma, beta, y)
+    dp.dp_layer_norm_backward(desc, x, gamma, dy, dx, g_w, g_b, sq, ws)
+    for t in (y, dx):
+        bad = t.isnan().all(2)
+        assert bad.tolist() == [[True, True, False], [False, False, True], [False, False, False]]
+        assert bool(t[~bad].isfinite().all())
+    assert sq.isnan().tolist() == [True, True, False]

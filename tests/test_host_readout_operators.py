@@ -120,6 +120,23 @@ def test_lengths_and_targets_have_to_be_int32_on_the_device(lib):
         _raises(INT, dp.dp_token_logprobs_backward, _logprob(), FAKE, bad, None, FAKE, FAKE, FAKE, stream=0)
 
 
+def test_tensors_have_to_be_what_the_descriptor_says(lib):
+    """Of its type, with room enough, on the device: calls take addresses."""
+    for bad in (torch.zeros(3, 5, 40), torch.zeros(3, 5, 40, dtype=torch.bfloat16), torch.zeros(3, 5, 40, dtype=torch.int16)):
+        for names in ("x", "y"):
+            _raises(INT, dp.dp_layer_norm, _norm(), bad if names == "x" else FAKE, None, None, bad if names == "y" else FAKE, stream=0)
+        for place in range(3):
+            t = [bad if i == place else FAKE for i in range(3)]
+            _raises(INT, dp.dp_layer_norm_backward, _norm(), t[0], None, t[1], t[2], FAKE, FAKE, FAKE, FAKE, ws_bytes=1 << 20, stream=0)
+        _raises(INT, dp.dp_token_logprobs, _logprob(), bad, FAKE, FAKE, None, None, None, None, FAKE, stream=0)
+        _raises(INT, dp.dp_token_logprobs_backward, _logprob(), FAKE, FAKE, None, FAKE, bad, FAKE, stream=0)
+    for bad in (torch.zeros(15), torch.zeros(15, dtype=torch.bfloat16), torch.zeros(15, dtype=torch.int32)):
+        _raises(INT, dp.dp_layer_norm, _norm(), FAKE, bad, None, FAKE, stream=0)
+        _raises(INT, dp.dp_token_logprobs, _logprob(), FAKE, FAKE, bad, None, None, None, None, FAKE, stream=0)
+        _raises(INT, dp.dp_token_logprobs, _logprob(), FAKE, FAKE, None, bad, None, None, None, FAKE, stream=0)
+        _raises(INT, dp.dp_token_logprobs_backward, _logprob(), FAKE, FAKE, None, bad, FAKE, FAKE, stream=0)
+
+
 def test_workspaces_of_every_size(lib):
     """Queries answer for the whole range, and grow with what they are for."""
     for features in (1, 7, 512, 1000, 8192, 16384, 16385, 1 << 20):
