@@ -461,25 +461,40 @@ def _lengths(t, n: int, what: str) -> Optional[int]:
     return t.data_ptr()
 
 
+_TYPES = ()                                       # torch's float32 and bfloat16 by dp_dtype, once a call has needed them
+
+
+def _types():
+    global _TYPES
+    import torch
+    _TYPES = (torch.float32, torch.bfloat16)
+    return _TYPES
+
+
+# (The order of what is asked, and no more of it, because a tensor takes 0.1 us to answer and the smallest calls take 4.)
 def _floats(t, n: int, what: str) -> Optional[int]:
     """Address of n fp32 numbers (or None)."""
     if t is None or type(t) is int:
         return t
-    import torch
-    if t.dtype is not torch.float32 or t.numel() < n or not t.is_contiguous() or not (t.is_cuda or t.is_pinned()):
+    if t.dtype is not (_TYPES or _types())[DP_F32] or t.nbytes < 4 * n or not t.is_contiguous() or not (t.is_cuda or t.is_pinned()):
         raise DpError(DP_ERR_INVALID_ARG, f"{what} must be {n} contiguous float32 on the device, not {t.dtype} {list(t.shape)} on {t.device}")
     return t.data_ptr()
 
 
-def _token_rows(t, desc, width: int, what: str) -> Optional[int]:
-    """Address of [n, tokens] rows of `width` values of the descriptor's type (or None)."""
+def _token_rows(t, desc, dtype: int, size: int, what: str) -> Optional[int]:
+    """Address of [n, tokens] rows of `size` bytes in all, of the descriptor's type (or None)."""
     if t is None or type(t) is int:
         return t
-    if t.element_size() != (2 if desc.in_dtype == DP_BF16 else 4) or not t.is_floating_point() or t.numel() < desc.n * desc.tokens * width or \
-            not (t.is_cuda or t.is_pinned()):
-        raise DpError(DP_ERR_INVALID_ARG, f"{what} must be {desc.n} x {desc.tokens} rows of {width} {'bfloat16' if desc.in_dtype == DP_BF16 else 'float32'} on the "
+    if t.nbytes < size or t.dtype is not (_TYPES or _types())[dtype] or not (t.is_cuda or t.is_pinned()):
+        raise DpError(DP_ERR_INVALID_ARG, f"{what} must be {desc.n} x {desc.tokens} rows of {'bfloat16' if dtype == DP_BF16 else 'float32'}, {size} bytes, on the "
                                           f"device, not {t.dtype} {list(t.shape)} on {t.device}")
     return t.data_ptr()
+
+
+def _row_bytes(desc, width: int):
+    """(type, bytes) of a call's tensors; an unknown type is the library's to refuse."""
+    dtype = 1 if desc.in_dtype == DP_BF16 else 0
+    return dtype, desc.n * desc.tokens * width * (2 if dtype else 4)
 
 
 # ---- 8-bit activation checkpoints ---------------------------------------------------------------------------------
@@ -586,8 +601,9 @@ def dp_bias_softmax_backward(desc: BiasDesc, probs, dprobs, dscores, g_table, sq
 def dp_layer_norm(desc: NormDesc, x, gamma, beta, y, lengths=None, stream=None):
     """Layer norm (desc.rms: RMS norm) of every token of x [n, tokens, features] into y."""
     f = desc.features
-    _check(load_library().dp_layer_norm(C.byref(desc), _token_rows(x, desc, f, "x"), _floats(gamma, f, "gamma"), _floats(beta, f, "beta"),
-                                        _lengths(lengths, desc.n, "lengths"), _token_rows(y, desc, f, "y"), _stream(stream)))
+    rows = _row_bytes(desc, f)
+    _check(load_library().dp_layer_norm(C.byref(desc), _token_rows(x, desc, *rows, "x"), _floats(gamma, f, "gamma"), _floats(beta, f, "beta"),
+                                        _lengths(lengths, desc.n, "lengths"), _token_rows(y, desc, *rows, "y"), _stream(stream)))
 
 
 def dp_layer_norm_workspace_bytes(desc: NormDesc) -> int:
@@ -598,8 +614,9 @@ def dp_layer_norm_backward(desc: NormDesc, x, gamma, dy, dx, g_w, g_b, sqnorm, w
                            ws_bytes: Optional[int] = None, stream=None):
     """Gradient of the tokens, and per example the gradients of gamma and beta and their squared norm."""
     f = desc.features
-    _check(load_library().dp_layer_norm_backward(C.byref(desc), _token_rows(x, desc, f, "x"), _floats(gamma, f, "gamma"), _token_rows(dy, desc, f, "dy"),
-                                                 _lengths(lengths, desc.n, "lengths"), _token_rows(dx, desc, f, "dx"), _ptr(g_w), _ptr(g_b), g_stride,
+    rows = _row_bytes(desc, f)
+    _check(load_library().dp_layer_norm_backward(C.byref(desc), _token_rows(x, desc, *rows, "x"), _floats(gamma, f, "gamma"), _token_rows(dy, desc, *rows, "dy"),
+                                                 _lengths(lengths, desc.n, "lengths"), _token_rows(dx, desc, *rows, "dx"), _ptr(g_w), _ptr(g_b), g_stride,
                                                  _floats(sqnorm, desc.n, "sqnorm"), _ptr(ws), _nbytes(ws) if ws_bytes is None else ws_bytes, _stream(stream)))
 
 
@@ -613,8 +630,8 @@ def dp_token_logprobs(desc: LogprobDesc, logits, targets, logprobs, entropy, sta
                       ws_bytes: Optional[int] = None, stream=None):
     """Log probabilities of targets (int32 [n, tokens]) under rows of logits, entropies, statistics for the backward pass, the most likely tokens; any
     of the results may be None."""
-    rows = desc.n * desc.tokens
-    _check(load_library().dp_token_logprobs(C.byref(desc), _token_rows(logits, desc, desc.vocab, "logits"), _lengths(targets, rows, "targets"),
+    rows, typed = desc.n * desc.tokens, _row_bytes(desc, desc.vocab)
+    _check(load_library().dp_token_logprobs(C.byref(desc), _token_rows(logits, desc, *typed, "logits"), _lengths(targets, rows, "targets"),
                                             _lengths(lengths, desc.n, "lengths"), _floats(logprobs, rows, "logprobs"), _floats(entropy, rows, "entropy"),
                                             _floats(stats, 2 * rows, "stats"), _floats(top_logprobs, rows * desc.top, "top_logprobs"),
                                             _lengths(top_tokens, rows * desc.top, "top_tokens"), _ptr(ws), _nbytes(ws) if ws_bytes is None else ws_bytes,
@@ -625,9 +642,9 @@ def dp_token_logprobs_backward(desc: LogprobDesc, logits, targets, stats, d_logp
                                lengths=None, ws_bytes: Optional[int] = None, stream=None):
     """Gradient of the logits from those of log probabilities and entropies; stats None: worked out in the same call, with the log probabilities
     where there is a place for them."""
-    rows = desc.n * desc.tokens
-    _check(load_library().dp_token_logprobs_backward(C.byref(desc), _token_rows(logits, desc, desc.vocab, "logits"), _lengths(targets, rows, "targets"),
+    rows, typed = desc.n * desc.tokens, _row_bytes(desc, desc.vocab)
+    _check(load_library().dp_token_logprobs_backward(C.byref(desc), _token_rows(logits, desc, *typed, "logits"), _lengths(targets, rows, "targets"),
                                                      _lengths(lengths, desc.n, "lengths"), _floats(stats, 2 * rows, "stats"), _floats(entropy, rows, "entropy"),
                                                      _floats(d_logprobs, rows, "d_logprobs"), _floats(d_entropy, rows, "d_entropy"),
-                                                     _floats(logprobs, rows, "logprobs"), _token_rows(dlogits, desc, desc.vocab, "dlogits"), _ptr(ws),
+                                                     _floats(logprobs, rows, "logprobs"), _token_rows(dlogits, desc, *typed, "dlogits"), _ptr(ws),
                                                      _nbytes(ws) if ws_bytes is None else ws_bytes, _stream(stream)))
