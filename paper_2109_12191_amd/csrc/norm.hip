@@ -541,8 +541,13 @@ NormArgs norm_args(const NormGeo &g, bool backward)
     } else {
         // as few sums as there may be, at two workgroups to a compute unit; five of the kernel that holds the least (us, 512 workgroups and 1024: 64 x 200
         // tokens of 4096 features 79 and 88, 32 x 500 of 768 23.6 and 27.4; but 16 x 2048 of 2048 98 and 96, 8 x 1000 of 2048 in fp32 53.7 and 51.1)
-        const long long workgroups = g.features > 1024 && g.features <= 2048 ? 1024 : 512;
-        const long long each = std::max(1ll, std::min((all + workgroups * at_once - 1) / (workgroups * at_once), 64ll));
+        const long long workgroups = g.features > 1024 && g.features <= 2048 && all * (g.bf16 ? 2 : 4) >= 32000 ? 1024 : 512;
+        long long each = std::max(1ll, std::min((all + workgroups * at_once - 1) / (workgroups * at_once), 64ll));
+        // at least a few rows where sums are wide or a few examples have them all, unless that leaves half the compute units idle (us: 3 x 511 tokens of
+        // 5000 features in fp32, three rows 35.4, four 33.2; 2 x 300 of 8000 two 27.5, four 22.0; 1 x 2000 of 300 four 13.0, eight 11.6; but 32 x 64 of 768
+        // four 10.4, eight 10.9)
+        const long long least = g.features > 2048 ? 4 : g.n < 8 ? 2 : 1;
+        if (all >= 128 * least * at_once) each = std::max(each, least);
         a.rows = (int)std::min(each * at_once, (long long)(g.tokens + at_once - 1) / at_once * at_once);
         a.blocks = (g.tokens + a.rows - 1) / a.rows;
     }
@@ -600,7 +605,7 @@ NormWs norm_ws(const NormGeo &g, const NormArgs &a)
 {
     NormWs w = {};
     const size_t all = (size_t)g.n * g.tokens;
-    w.groups = (2 * a.padded / 4 + 63) / 64;
+    w.groups = (2 * a.padded / 4 + 31) / 32;
     w.partials = round16((size_t)g.n * a.blocks * 2 * a.padded * 4);
     w.squares = round16((size_t)g.n * w.groups * 4);
     w.stats = g.features > NORM_HELD ? round16(all * 20) : 0;
@@ -652,10 +657,14 @@ dp_status launch_norm_backward(const NormGeo &g, const void *x, const float *gam
         if (quads <= 128) return launch_blocks<norm_join_kernel<1024, 128, true>>((size_t)g.n, 1024, 0, s, j);
         return launch_blocks<norm_join_kernel<1024, 512, true>>((size_t)g.n, 1024, 0, s, j);
     }
-    j.groups = (quads + 63) / 64;
+    // few groups: of fewer columns, and more parts (1 x 4000 tokens of 2048 features 40 and 27 us)
+    const bool narrow = (size_t)g.n * ((quads + 63) / 64) <= 64;
+    j.groups = narrow ? (quads + 31) / 32 : (quads + 63) / 64;
     j.squares = sqnorm ? reinterpret_cast<float *>(room + w.partials) : nullptr;
-    st = (size_t)g.n * j.groups <= 512 ? launch_blocks<norm_join_kernel<1024, 64, false>>((size_t)g.n * j.groups, 1024, 0, s, j)
-                                       : launch_blocks<norm_join_kernel<256, 64, false>>((size_t)g.n * j.groups, 256, 0, s, j);
+    const size_t grid = (size_t)g.n * j.groups;
+    if (narrow) st = launch_blocks<norm_join_kernel<1024, 32, false>>(grid, 1024, 0, s, j);
+    else if (grid <= 512) st = launch_blocks<norm_join_kernel<1024, 64, false>>(grid, 1024, 0, s, j);
+    else st = launch_blocks<norm_join_kernel<256, 64, false>>(grid, 256, 0, s, j);
     if (st != DP_OK || !sqnorm) return st;
     return launch_sum_partials(j.squares, g.n, j.groups, sqnorm, s);
 }
