@@ -12,8 +12,8 @@ An example's gradient is that of its checkpoint's values, for the norm and for t
 derivatives that a backward pass starts from are those of a sum over examples, not of a mean.
 
 logprobs' result carries a graph where its input requires a gradient: autograd's pass over it is `backward`, with the clipped sums of the parameters that
-belong to it, and gives the input's gradient.  Elsewhere `backward` is called, or `train` for both passes at once.  The block holds the values of one forward
-pass, for one such pass back.
+belong to it, and gives the input's gradient.  Elsewhere `backward` is called, or `train` for both passes at once, which is also what to record into a graph.  The
+block holds the values of one forward pass, for one such pass back, and the input itself, which has to stay as it is until then.
 """
 from __future__ import annotations
 

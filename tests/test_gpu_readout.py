@@ -187,3 +187,25 @@ def test_a_model_of_an_attention_block_and_the_readout():
         block.step(0)
         assert bool(block.theta.isfinite().all()) and not torch.equal(block.theta, before)
     assert bool((z[~there] == 0.0).all())
+
+
+def test_a_recorded_pass():
+    """Replays on new tokens, with eager passes of another block between them."""
+    x, targets, lengths, weights = data(3)
+    x, weights = torch.nan_to_num(x), torch.nan_to_num(weights)
+    recorded, eager = block_of(), block_of()
+    recorded.train(x, targets, weights, lengths)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        y, dx = recorded.train(x, targets, weights, lengths)
+    for seed in range(4):
+        new = data(20 + seed)
+        for old, fresh in zip((x, targets, lengths, weights), new):
+            old.copy_(torch.nan_to_num(fresh))
+        recorded.acc.zero_()
+        eager.acc.zero_()
+        graph.replay()
+        want = eager.train(x, targets, weights, lengths)
+        torch.cuda.synchronize()
+        assert torch.equal(y, want[0]) and torch.equal(dx, want[1]) and torch.equal(recorded.acc, eager.acc) and float(eager.acc.abs().max()) > 0.0
