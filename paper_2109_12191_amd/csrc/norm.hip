@@ -24,6 +24,8 @@ struct NormArgs {
     const int32_t *lengths;
     float *partials;                 // backward: [n, blocks, 2, padded features]
     int shift;                       // backward: gradients of the shift are wanted
+    float *g_w, *g_b, *sqnorm;       // backward, where an example has one workgroup: its results (else `partials`)
+    size_t g_stride;
     float *stats;                    // of rows too long for registers: [n * tokens, 4]
     int n, tokens, features, padded, rms;
     float eps, inv_features;
@@ -284,8 +286,8 @@ __global__ void __launch_bounds__(TPR > 256 ? TPR : 256) norm_backward_kernel(co
             for (int j = 0; j < NV; ++j) out.store(row, 8 * (t + TPR * j), zeros);
         }
     }
-    if (!a.partials) return;
-    float *part = a.partials + (size_t)block * 2 * a.padded;
+    if (!a.partials && !a.g_w) return;
+    float *part = a.partials + (size_t)block * 2 * a.padded, ss = 0.0f;
 #pragma unroll
     for (int which = 0; which < 2; ++which) {
         if (which && !a.shift) break;
@@ -314,13 +316,26 @@ __global__ void __launch_bounds__(TPR > 256 ? TPR : 256) norm_backward_kernel(co
                 }
                 if (wave != 0 || lane >= TPR) continue;
             }
-            if (k < a.padded) {
+            if (a.g_w) {
+                float *to = (which ? a.g_b : a.g_w) + (size_t)ex * a.g_stride + k;
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    if (k + i < a.features) { to[i] = v[i]; ss = fmaf(v[i], v[i], ss); }
+            } else if (k < a.padded) {
                 float4 *to = reinterpret_cast<float4 *>(part + which * a.padded + k);
                 to[0] = make_float4(v[0], v[1], v[2], v[3]);
                 to[1] = make_float4(v[4], v[5], v[6], v[7]);
             }
         }
     }
+    if (!a.g_w || !a.sqnorm) return;
+    if constexpr (TPR <= 64) {
+        if ((threadIdx.x >> 6) != 0) return;
+        ss = wave_all_sum(ss);
+    } else {
+        ss = block_sum<TPR / 64>(ss, red);
+    }
+    if (threadIdx.x == 0) a.sqnorm[ex] = ss;
 }
 
 // Rows too long for registers, a workgroup each, read three times.  Forward: all of it.  Backward: their statistics, and what dx needs.
@@ -517,8 +532,8 @@ __global__ void __launch_bounds__(THREADS) norm_join_kernel(const NormJoinArgs a
 }
 
 constexpr int NORM_HELD = 16384;       // features that a workgroup of sixteen waves holds in registers
+constexpr size_t JOIN_WHOLE = 16384;   // quads of sums that one workgroup adds up
 
-constexpr size_t JOIN_WHOLE = 16384;
 // Threads that share a row: as many as have a run of eight, a wave for up to 1024 features (forward 2048), four for up to 8192.
 int norm_lanes(int features, bool backward)
 {
@@ -548,6 +563,11 @@ NormArgs norm_args(const NormGeo &g, bool backward)
         // four 10.4, eight 10.9)
         const long long least = g.features > 2048 ? 4 : g.n < 8 ? 2 : 1;
         if (all >= 128 * least * at_once) each = std::max(each, least);
+        // Examples that one workgroup is soon done with have one, and need no launch to join its sums (us, joined and not: 1000 x 3 tokens of 100 features 12.0
+        // and 4.6, 300 x 10 of 768 14.0 and 10.2, 150 x 5 of 768 9.3 and 7.2, 300 x 20 of 4096 in fp32 88.7 and 85.0; but 150 x 40 of 768 15.1 and 16.8, 8 x 16 of 768 8.1 and 9.1, 300 x 60 of
+        // 2048 62 and 92).
+        const long long turns = (g.tokens + at_once - 1) / at_once;
+        if (turns <= (g.n >= 256 ? 20 : 3)) each = turns;
         a.rows = (int)std::min(each * at_once, (long long)(g.tokens + at_once - 1) / at_once * at_once);
         a.blocks = (g.tokens + a.rows - 1) / a.rows;
     }
@@ -639,6 +659,8 @@ dp_status launch_norm_backward(const NormGeo &g, const void *x, const float *gam
     a.partials = g_w ? reinterpret_cast<float *>(room) : nullptr;
     a.shift = g_b != nullptr;
     a.stats = reinterpret_cast<float *>(room + w.partials + w.squares);
+    const bool direct = g_w && a.blocks == 1 && g.features <= NORM_HELD;
+    if (direct) { a.partials = nullptr; a.g_w = g_w; a.g_b = g_b; a.g_stride = g_stride; a.sqnorm = sqnorm; }
     dp_status st;
     if (g.features > NORM_HELD) {
         st = g.bf16 ? run_long<true, true>(g, a, s) : run_long<false, true>(g, a, s);
@@ -648,7 +670,7 @@ dp_status launch_norm_backward(const NormGeo &g, const void *x, const float *gam
         if (!g.bf16) st = words ? run_backward<false, true>(g, a, s) : run_backward<false, false>(g, a, s);
         else st = words ? run_backward<true, true>(g, a, s) : run_backward<true, false>(g, a, s);
     }
-    if (st != DP_OK || !g_w) return st;
+    if (st != DP_OK || !g_w || direct) return st;
     NormJoinArgs j = {};
     j.partials = a.partials; j.g_w = g_w; j.g_b = g_b; j.g_stride = g_stride; j.blocks = a.blocks; j.features = g.features; j.padded = a.padded;
     // one workgroup an example where it has little to add up, or where there are as many as compute units
