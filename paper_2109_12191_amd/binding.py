@@ -481,6 +481,15 @@ def _floats(t, n: int, what: str) -> Optional[int]:
     return t.data_ptr()
 
 
+def _gradient_rows(t, n: int, width: int, what: str) -> Optional[int]:
+    """Address of n examples' fp32 gradients, rows of `width` at least (or None)."""
+    if t is None or type(t) is int:
+        return t
+    if t.dtype is not (_TYPES or _types())[DP_F32] or t.nbytes < 4 * n * width or not (t.is_cuda or t.is_pinned()):
+        raise DpError(DP_ERR_INVALID_ARG, f"{what} must be {n} rows of {width} float32 on the device, not {t.dtype} {list(t.shape)} on {t.device}")
+    return t.data_ptr()
+
+
 def _token_rows(t, desc, dtype: int, size: int, what: str) -> Optional[int]:
     """Address of [n, tokens] rows of `size` bytes in all, of the descriptor's type (or None)."""
     if t is None or type(t) is int:
@@ -616,8 +625,8 @@ def dp_layer_norm_backward(desc: NormDesc, x, gamma, dy, dx, g_w, g_b, sqnorm, w
     f = desc.features
     rows = _row_bytes(desc, f)
     _check(load_library().dp_layer_norm_backward(C.byref(desc), _token_rows(x, desc, *rows, "x"), _floats(gamma, f, "gamma"), _token_rows(dy, desc, *rows, "dy"),
-                                                 _lengths(lengths, desc.n, "lengths"), _token_rows(dx, desc, *rows, "dx"), _ptr(g_w), _ptr(g_b), g_stride,
-                                                 _floats(sqnorm, desc.n, "sqnorm"), _ptr(ws), _nbytes(ws) if ws_bytes is None else ws_bytes, _stream(stream)))
+                                                 _lengths(lengths, desc.n, "lengths"), _token_rows(dx, desc, *rows, "dx"), _gradient_rows(g_w, desc.n, f, "g_w"),
+                                                 _gradient_rows(g_b, desc.n, f, "g_b"), g_stride, _floats(sqnorm, desc.n, "sqnorm"), _ptr(ws), _nbytes(ws) if ws_bytes is None else ws_bytes, _stream(stream)))
 
 
 # ---- log probabilities of tokens -------------------------------------------------------------------------------------

@@ -2,12 +2,13 @@
 //     xhat = (x - mean) r,  r = 1 / sqrt(mean((x - mean)^2) + eps),  y = gamma xhat + beta          (RMS: the mean is taken as zero)
 //     a = gamma dy,  dx = r (a - mean(a) - xhat mean(a xhat)),   g_w = sum_t dy xhat,  g_b = sum_t dy        (RMS: no mean(a))
 //
-// Bound by memory: 32768 tokens of 2048 bf16 features forward 52 us, 5.2 TB/s, backward 88, 4.8 (and 10 to join sums and add up squares).  A row's values are
-// held in registers between its sums and its results, 8 to a lane and run, by as many lanes as have one, so that memory sees each value once.  The mean comes first; deviations from it are then summed with their squares, and what the mean's rounding left in
-// their sum is taken out again (a mean of 1000 deviations costs no digits of the variance).  The backward pass works the statistics out again
-// from x: two more sums of registers, nothing to keep from the forward pass.
+// Bound by memory: 32768 tokens of 2048 bf16 features forward 52 us, 5.2 TB/s, backward 88, 4.8 (and 10 to join sums and add up squares).  A row's
+// values are held in registers between its sums and its results, 8 to a lane and run, by as many lanes as have one, so that memory sees each value
+// once.  The mean comes first; deviations from it are then summed with their squares, and what the mean's rounding left in their sum is taken out again
+// (a mean of 1000 deviations costs no digits of the variance).  The backward pass works the statistics out again from x: two more sums of registers,
+// nothing to keep from the forward pass.
 // Gradients of scale and shift: a lane keeps its columns' sums over the workgroup's rows in registers, workgroups leave theirs in the workspace,
-// and norm_join_kernel adds them up in order.
+// and norm_join_kernel adds them up in order; where an example has one workgroup, it writes the results itself.
 #include "lanes.h"
 #include "token_rows.h"
 
@@ -571,9 +572,9 @@ NormArgs norm_args(const NormGeo &g, bool backward)
         // four 10.4, eight 10.9)
         const long long least = g.features > 2048 ? 4 : g.n < 8 ? 2 : 1;
         if (all >= 128 * least * at_once) each = std::max(each, least);
-        // Examples that one workgroup is soon done with have one, and need no launch to join its sums (us, joined and not: 1000 x 3 tokens of 100 features 12.0
-        // and 4.6, 300 x 10 of 768 14.0 and 10.2, 150 x 5 of 768 9.3 and 7.2, 300 x 20 of 4096 in fp32 88.7 and 85.0; but 150 x 40 of 768 15.1 and 16.8, 8 x 16 of 768 8.1 and 9.1, 300 x 60 of
-        // 2048 62 and 92).
+        // Examples that one workgroup is soon done with have one, and need no launch to join its sums (us, joined and not: 1000 x 3 tokens of 100
+        // features 12.0 and 4.6, 300 x 10 of 768 14.0 and 10.2, 150 x 5 of 768 9.3 and 7.2, 300 x 20 of 4096 in fp32 88.7 and 85.0; but 150 x 40 of 768
+        // 15.1 and 16.8, 8 x 16 of 768 8.1 and 9.1, 300 x 60 of 2048 62 and 92).
         const long long turns = (g.tokens + at_once - 1) / at_once;
         if (turns <= (g.n >= 256 ? 20 : 3)) each = turns;
         a.rows = (int)std::min(each * at_once, (long long)(g.tokens + at_once - 1) / at_once * at_once);

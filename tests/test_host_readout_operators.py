@@ -130,6 +130,10 @@ def test_tensors_have_to_be_what_the_descriptor_says(lib):
             _raises(INT, dp.dp_layer_norm_backward, _norm(), t[0], None, t[1], t[2], FAKE, FAKE, FAKE, FAKE, ws_bytes=1 << 20, stream=0)
         _raises(INT, dp.dp_token_logprobs, _logprob(), bad, FAKE, FAKE, None, None, None, None, FAKE, stream=0)
         _raises(INT, dp.dp_token_logprobs_backward, _logprob(), FAKE, FAKE, None, FAKE, bad, FAKE, stream=0)
+    for bad in (torch.zeros(3, 40), torch.zeros(3, 40, dtype=torch.bfloat16), torch.zeros(2, 40)):
+        for place in range(2):
+            g = [bad if i == place else FAKE for i in range(2)]
+            _raises(INT, dp.dp_layer_norm_backward, _norm(), FAKE, None, FAKE, FAKE, *g, FAKE, FAKE, ws_bytes=1 << 20, stream=0)
     for bad in (torch.zeros(15), torch.zeros(15, dtype=torch.bfloat16), torch.zeros(15, dtype=torch.int32)):
         _raises(INT, dp.dp_layer_norm, _norm(), FAKE, bad, None, FAKE, stream=0)
         _raises(INT, dp.dp_token_logprobs, _logprob(), FAKE, FAKE, bad, None, None, None, None, FAKE, stream=0)
