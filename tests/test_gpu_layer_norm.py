@@ -368,3 +368,33 @@ def test_rows_beyond_the_range_are_no_numbers(features, rms):
         assert bad.tolist() == [[True, True, False], [False, False, True], [False, False, False]]
         assert bool(t[~bad].isfinite().all())
     assert sq.isnan().tolist() == [True, True, False]
+
+
+@pytest.mark.parametrize("features,tokens,stride", [(1000, 1100, 1 << 22), (1001, 1100, (1 << 22) + 1), (4096, 1100000, 4096), (20000, 230000, 20000)], ids=str)
+def test_offsets_beyond_2_to_the_32(features, tokens, stride):
+    """The last tokens of tensors of 4.5 billion places against the same tokens by themselves: rows far apart, and many of them."""
+    torch.cuda.empty_cache()
+    if torch.cuda.mem_get_info()[0] < 32 * 2 ** 30:
+        pytest.skip("32 GiB of device memory are not free")
+    last = 64
+    values, grads, gamma, beta = data(1, last, features, 3)
+    buffers = [torch.zeros(tokens * stride, dtype=torch.bfloat16, device="cuda:0") for _ in range(2)]
+    x, dy = (torch.as_strided(b, (1, tokens, features), (tokens * stride, stride, 1)) for b in buffers)
+    x[:, -last:], dy[:, -last:] = values, grads
+
+    def run(x, dy):
+        desc = desc_of(x)
+        ws = torch.empty(dp.dp_layer_norm_workspace_bytes(desc), dtype=torch.uint8, device="cuda:0")
+        n, tokens, features = x.shape
+        wide = (features + 3) // 4 * 4
+        g_w, g_b, sq = torch.empty((1, wide), device="cuda:0"), torch.empty((1, wide), device="cuda:0"), torch.empty(1, device="cuda:0")
+        dp.dp_layer_norm_backward(desc, x, gamma, dy, dy, g_w, g_b, sq, ws, g_stride=wide)
+        dp.dp_layer_norm(desc, x, gamma, beta, x)
+        return x[:, -last:].clone(), dy[:, -last:].clone(), g_w[:, :features], g_b[:, :features], sq
+    alone = run(x[:, -last:].clone(), dy[:, -last:].clone())
+    whole = run(x, dy)
+    for a, b in zip(whole[:2], alone[:2]):
+        assert bool(((a.double() - b.double()).abs() <= 2.0 ** -7 * b.double().abs() + 2.0 ** -9).all())      # (held by other numbers of threads)
+    # the tokens before them are zeros, with gradients of zeros: the sums are the same numbers in another order
+    for a, b in zip(whole[2:], alone[2:]):
+        assert bool(((a - b).abs() <= 200 * U * last * b.abs().amax()).all())
