@@ -225,8 +225,32 @@ __global__ void __launch_bounds__(TPR > 256 ? TPR : 256) norm_backward_kernel(co
     const size_t first = (size_t)ex * a.tokens + token;
     const TokenRows<BF16, WORDS> in(a.x, first, rows, a.row_stride, a.features), in2(a.dy, first, rows, a.row_stride, a.features),
         out(a.out, first, rows, a.row_stride, a.features);
-    float gamma[8 * NV], sum_w[8 * NV], sum_b[8 * NV];
-    columns<TPR, NV>(a.gamma, 1.0f, t, a.features, gamma);
+    // The scale of a thread's columns: in registers, or where those leave a compute unit room for one workgroup of eight waves only, in LDS (us, LDS and
+    // registers: 300 x 20 tokens of 6000 features 74 and 88, 32 x 300 90 and 93; but in the kernel of four waves 64 x 200 of 4096 80.9 and 79.6).
+    constexpr bool LDS = TPR == 512 && NV == 2;
+    float gamma[LDS ? 1 : 8 * NV], sum_w[8 * NV], sum_b[8 * NV];
+    __shared__ float4 scales[LDS ? NV * 2 : 1][LDS ? TPR : 1];
+    if constexpr (LDS) {
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            float v[8];
+            columns8(a.gamma, 1.0f, 8 * (t + TPR * j), a.features, v);
+            scales[2 * j][t] = make_float4(v[0], v[1], v[2], v[3]);
+            scales[2 * j + 1][t] = make_float4(v[4], v[5], v[6], v[7]);
+        }
+    } else {
+        columns<TPR, NV>(a.gamma, 1.0f, t, a.features, gamma);
+    }
+    auto scale_of = [&](int j, float (&v)[8]) {          // (a thread reads what it wrote)
+        if constexpr (LDS) {
+            const float4 lo = scales[2 * j][t], hi = scales[2 * j + 1][t];
+            v[0] = lo.x; v[1] = lo.y; v[2] = lo.z; v[3] = lo.w;
+            v[4] = hi.x; v[5] = hi.y; v[6] = hi.z; v[7] = hi.w;
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = gamma[8 * j + i];
+        }
+    };
 #pragma unroll
     for (int i = 0; i < 8 * NV; ++i) sum_w[i] = sum_b[i] = 0.0f;
     Raw8<BF16> next[NV], next2[NV];
@@ -251,12 +275,17 @@ __global__ void __launch_bounds__(TPR > 256 ? TPR : 256) norm_backward_kernel(co
             for (int again = 0;; ++again) {
                 s[0] = s[1] = s[2] = s[3] = 0.0f;
 #pragma unroll
-                for (int i = 0; i < 8 * NV; ++i) {
-                    const float g = d[i] * gamma[i];
-                    s[0] += x[i];
-                    s[1] = fmaf(x[i], x[i], s[1]);
-                    s[2] += g;
-                    s[3] = fmaf(g, x[i], s[3]);
+                for (int j = 0; j < NV; ++j) {
+                    float scale[8];
+                    scale_of(j, scale);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        const float dev = x[8 * j + i], g = d[8 * j + i] * scale[i];
+                        s[0] += dev;
+                        s[1] = fmaf(dev, dev, s[1]);
+                        s[2] += g;
+                        s[3] = fmaf(g, dev, s[3]);
+                    }
                 }
                 if (a.rms) s[0] = s[2] = 0.0f;
                 row_sums<TPR, 4>(s, red, turn);
@@ -270,13 +299,14 @@ __global__ void __launch_bounds__(TPR > 256 ? TPR : 256) norm_backward_kernel(co
             const bool there = TPR >= 64 || row < length;
 #pragma unroll
             for (int j = 0; j < NV; ++j) {
-                float g[8];
+                float g[8], scale[8];
+                scale_of(j, scale);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
                     const float xhat = fmaf(x[8 * j + i], r, shift), dy = d[8 * j + i];
                     sum_w[8 * j + i] = fmaf(dy, xhat, sum_w[8 * j + i]);          // (of a row that is not there: x, dy and xhat are zeros)
                     sum_b[8 * j + i] += dy;
-                    g[i] = fmaf(dy * gamma[8 * j + i], r, fmaf(xhat, slope, base));
+                    g[i] = fmaf(dy * scale[i], r, fmaf(xhat, slope, base));
                     if (!there) g[i] = 0.0f;
                 }
                 if (a.out && row < rows) out.store(row, 8 * (t + TPR * j), g);
