@@ -684,7 +684,8 @@ dp_status launch_norm(const NormGeo &g, const void *x, const float *gamma, const
     NormArgs a = norm_args(g, false);
     a.x = x; a.out = y; a.gamma = gamma; a.beta = beta; a.lengths = lengths;
     if (g.features > NORM_HELD) return g.bf16 ? run_long<true, false>(g, a, s) : run_long<false, false>(g, a, s);
-    const bool words = token_rows_by_words(x, g.bf16, g.row_stride, a.rows) && token_rows_by_words(y, g.bf16, g.row_stride, a.rows);
+    const size_t all = (size_t)g.n * g.tokens;
+    const bool words = token_rows_by_words(x, g.bf16, g.row_stride, all, a.rows) && token_rows_by_words(y, g.bf16, g.row_stride, all, a.rows);
     if (!g.bf16) return words ? run_forward<false, true>(g, a, s) : run_forward<false, false>(g, a, s);
     return words ? run_forward<true, true>(g, a, s) : run_forward<true, false>(g, a, s);
 }
@@ -706,7 +707,7 @@ dp_status launch_norm_backward(const NormGeo &g, const void *x, const float *gam
         st = g.bf16 ? run_long<true, true>(g, a, s) : run_long<false, true>(g, a, s);
     } else {
         bool words = true;
-        for (const void *p : {x, dy, static_cast<const void *>(dx)}) words = words && token_rows_by_words(p, g.bf16, g.row_stride, a.rows);
+        for (const void *p : {x, dy, static_cast<const void *>(dx)}) words = words && token_rows_by_words(p, g.bf16, g.row_stride, (size_t)g.n * g.tokens, a.rows);
         if (!g.bf16) st = words ? run_backward<false, true>(g, a, s) : run_backward<false, false>(g, a, s);
         else st = words ? run_backward<true, true>(g, a, s) : run_backward<true, false>(g, a, s);
     }

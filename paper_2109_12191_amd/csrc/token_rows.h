@@ -1,20 +1,12 @@
 // A workgroup's rows of a tensor of tokens, in runs of eight consecutive values from any multiple of eight on.  gfx950 only.
 #pragma once
 
+#include "token_words.h"
 #include "values.h"
 
 namespace dp {
 
 typedef uint32_t u32x4_v __attribute__((ext_vector_type(4)));
-
-// Whether the rows of a call can be read by whole dwords from one buffer per workgroup: bf16 rows have to begin at whole dwords, and what a
-// workgroup's `rows` rows span has to be below 2^31 bytes.
-inline bool token_rows_by_words(const void *p, bool bf16, size_t stride, size_t rows)
-{
-    const size_t size = bf16 ? 2 : 4;
-    if (bf16 && ((reinterpret_cast<uintptr_t>(p) & 3) || (rows > 1 && stride % 2))) return false;
-    return rows * stride <= ((size_t)1 << 30) / size;
-}
 
 // Rows `first` .. `first + rows - 1` of a tensor, `width` values each.  WORDS: 16-byte buffer accesses, left out by an offset beyond the buffer;
 // a run that a row ends in is loaded whole, with what follows it in memory (zeros after the last row, but for the other half of a last dword),

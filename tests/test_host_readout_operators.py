@@ -2,6 +2,7 @@
 could be launched, and their pure-host queries."""
 import math
 import os
+import subprocess
 
 import pytest
 import torch
@@ -152,3 +153,11 @@ def test_workspaces_of_every_size(lib):
             plain, top = (dp.dp_token_logprobs_workspace_bytes(_logprob(tokens=tokens, vocab=vocab, top=k)) for k in (0, 32))
             assert plain % 16 == 0 and top % 16 == 0
             assert plain > 0 or tokens == 1000 or vocab < 65536
+
+
+def test_rows_are_taken_by_words_only_where_every_workgroup_begins_at_one(tmp_path):
+    here, exe = os.path.dirname(os.path.abspath(__file__)), str(tmp_path / "token_words")
+    subprocess.run(["g++", "-std=c++17", "-O1", "-I" + os.path.join(here, "..", "paper_2109_12191_amd", "csrc"), os.path.join(here, "token_words.cpp"), "-o", exe],
+                   check=True)
+    run = subprocess.run([exe], capture_output=True, text=True)
+    assert run.returncode == 0, run.stdout
