@@ -35,6 +35,12 @@ struct NormArgs {
     unsigned first_block;            // workgroups of the launches before
 };
 
+// Of the `rows` rows from token `token` of example `ex` on, those that it has (none if below zero; a length may be any number).
+__device__ __forceinline__ int rows_there(const NormArgs &a, unsigned ex, int token, int rows)
+{
+    return a.lengths ? min(max(a.lengths[ex], 0) - token, rows) : rows;
+}
+
 // Sums of N values over the TPR threads of a row, in each of them.  Rows of several waves: every thread of the workgroup calls it, and `red`
 // has two places of 16 N words that are used in turn.
 template <int TPR, int N>
@@ -221,7 +227,7 @@ __global__ void __launch_bounds__(TPR > 256 ? TPR : 256) norm_backward_kernel(co
     const int t = (int)threadIdx.x % TPR;
     const unsigned block = a.first_block + blockIdx.x, ex = block / (unsigned)a.blocks;
     const int token = (int)(block - ex * (unsigned)a.blocks) * a.rows, rows = min(a.rows, a.tokens - token);
-    const int length = min(a.lengths ? a.lengths[ex] - token : rows, rows);          // rows that are there (none if below zero)
+    const int length = rows_there(a, ex, token, rows);
     const size_t first = (size_t)ex * a.tokens + token;
     const TokenRows<BF16, WORDS> in(a.x, first, rows, a.row_stride, a.features), in2(a.dy, first, rows, a.row_stride, a.features),
         out(a.out, first, rows, a.row_stride, a.features);
@@ -462,7 +468,7 @@ __global__ void __launch_bounds__(256) norm_columns_kernel(const NormArgs a)
     const unsigned wide = (unsigned)(a.features + 2047) / 2048u, block = a.first_block + blockIdx.x, line = block / wide;
     const unsigned ex = line / (unsigned)a.blocks;
     const int token = (int)(line - ex * (unsigned)a.blocks) * a.rows, rows = min(a.rows, a.tokens - token);
-    const int length = min(a.lengths ? a.lengths[ex] - token : rows, rows);
+    const int length = rows_there(a, ex, token, rows);
     const int k = (int)(block - line * wide) * 2048 + 8 * (int)threadIdx.x, count = a.features - k;
     if (count <= 0) return;
     float gamma[8], sum_w[8], sum_b[8];

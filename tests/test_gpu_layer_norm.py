@@ -172,6 +172,16 @@ def test_many_tokens_and_many_examples(n, tokens, features, dtype):
     check_backward(x, dy, dtype, gamma, lengths)
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("tokens,features", [(300, 48), (300, 700), (300, 1500), (300, 5000), (40, 9000), (70, 18000)], ids=str)
+def test_lengths_may_be_any_numbers(tokens, features, dtype):
+    """Far below zero and far beyond the tokens: taken as none and all, by every workgroup of an example."""
+    x, dy, gamma, beta = data(6, tokens, features, tokens)
+    lengths = torch.tensor([-2 ** 31, 2 ** 31 - 1, -2 ** 31 + 5, tokens + 1, -1, 17], dtype=torch.int32, device="cuda:0")
+    check_forward(x, dtype, gamma, beta, lengths)
+    check_backward(x, dy, dtype, gamma, lengths)
+
+
 def test_gradients_of_the_tokens_alone():
     """dx not wanted: gradients of scale and shift as with it."""
     x, dy, gamma, _ = data(4, 33, 500, 1)
