@@ -28,7 +28,7 @@ struct LogprobArgs {
     const float *stats, *entropy, *d_logprobs, *d_entropy;
     float *logprobs_out, *entropy_out, *stats_out, *top_logprobs;
     int32_t *top_tokens;
-    float *partials;                 // of rows that several workgroups share: [rows, splits, 4 + 2 top]
+    float *partials;                 // of rows that several workgroups share: [rows, part_words]
     int n, tokens, vocab, top;
     float scale;
     size_t row_stride;
@@ -36,6 +36,9 @@ struct LogprobArgs {
     int rows;                        // rows of the call
     unsigned first_block;            // workgroups of the launches before
 };
+
+// Words of a row's partial results, whole 16 bytes: they are written and read by those.
+__host__ __device__ constexpr size_t part_words(int splits, int top) { return ((size_t)splits * (4 + 2 * top) + 3) & ~(size_t)3; }
 
 // e^x, x at most 0
 __device__ __forceinline__ float exp_of(float x) { return __builtin_amdgcn_exp2f(x * 1.44269504088896340736f); }
@@ -482,7 +485,7 @@ __global__ void __launch_bounds__(256) logprob_split_kernel(const LogprobArgs a)
     see_runs<BF16, 256>(v, row, q0, q1, (int)threadIdx.x, a.scale, a.entropy_out != nullptr, raw);
     const float most = v.m;
     row_join<256>(v, a.scale, red);
-    float *part = a.partials + (size_t)r * a.splits * (4 + 2 * a.top);
+    float *part = a.partials + (size_t)r * part_words(a.splits, a.top);
     if (threadIdx.x == 0) *reinterpret_cast<float4 *>(part + 4 * split) = make_float4(v.m, v.s, v.t, 0.0f);
     if constexpr (TOP) {
         __shared__ TopShared sh;
@@ -507,7 +510,7 @@ __global__ void __launch_bounds__(256) logprob_join_kernel(const LogprobArgs a)
         if (t == 0) write_absent(a, r);
         return;
     }
-    const float *part = a.partials + r * a.splits * (4 + 2 * a.top);
+    const float *part = a.partials + r * part_words(a.splits, a.top);
     Seen v;
     v.none();
     const int lane = t & 63, all = a.top * a.splits;
@@ -753,7 +756,7 @@ LogprobArgs logprob_args(const LogprobGeo &g)
 size_t partial_bytes(const LogprobGeo &g)
 {
     const int splits = logprob_splits(g);
-    return splits > 1 ? round16((size_t)g.n * g.tokens * splits * (4 + 2 * g.top) * 4) : 0;
+    return splits > 1 ? (size_t)g.n * g.tokens * part_words(splits, g.top) * 4 : 0;
 }
 
 // Whether the gradient without statistics holds its rows in registers: rows that fit (with the place before them where they may begin inside a dword),

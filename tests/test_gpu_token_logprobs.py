@@ -426,3 +426,14 @@ def test_more_rows_than_a_launch_has_room_for():
         assert bool(((dx[part, 0] - want).abs() <= 1e-4 * (1 + r * a.abs().amax(1, keepdim=True))).all())
         s = (g_w[part].double() ** 2 + g_b[part].double() ** 2).sum(1)
         assert bool(((sq[part] - s).abs() <= 1e-5 * s).all())
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("n,vocab,top", [(3, 36864, 1), (5, 36864, 3), (7, 45060, 5), (2, 53251, 31)], ids=str)
+def test_odd_numbers_of_workgroups_and_alternatives(n, vocab, top, dtype):
+    """Rows that 9, 11 and 13 workgroups share, with odd numbers of alternatives."""
+    gen = torch.Generator("cuda:0").manual_seed(vocab + top)
+    values = torch.randn((n, 1, vocab), generator=gen, device="cuda:0") * 3.0
+    targets = torch.randint(0, vocab, (n, 1), generator=gen, device="cuda:0", dtype=torch.int32)
+    check_scores(values, dtype, targets, top=top)
+    check_scores(values, dtype, targets, top=top, lengths=torch.tensor([1, 0, 1, 1, 0, 1, 1][:n], dtype=torch.int32, device="cuda:0"))

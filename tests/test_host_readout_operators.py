@@ -161,3 +161,16 @@ def test_rows_are_taken_by_words_only_where_every_workgroup_begins_at_one(tmp_pa
                    check=True)
     run = subprocess.run([exe], capture_output=True, text=True)
     assert run.returncode == 0, run.stdout
+
+
+def test_partial_results_of_shared_rows_begin_at_whole_16_bytes(lib):
+    """They are stored and loaded by 16 bytes, so each row's room is a whole number of them, odd counts of workgroups and alternatives among them."""
+    shared = 0
+    for rows in (1, 2, 3, 5, 7, 100):
+        for vocab in (33281, 36864, 45056, 60000, 131072):
+            for top in range(33):
+                need = dp.dp_token_logprobs_workspace_bytes(_logprob(n=rows, tokens=1, vocab=vocab, top=top))
+                shared += need > 0
+                if top:                                      # (without, a gradient's statistics are in there too)
+                    assert need % (16 * rows) == 0, (rows, vocab, top, need)
+    assert shared > 500
