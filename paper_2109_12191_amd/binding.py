@@ -490,20 +490,45 @@ def _gradient_rows(t, n: int, width: int, what: str) -> Optional[int]:
     return t.data_ptr()
 
 
-def _token_rows(t, desc, dtype: int, size: int, what: str) -> Optional[int]:
-    """Address of [n, tokens] rows of `size` bytes in all, of the descriptor's type (or None)."""
+def _row_layout(desc, width: int):
+    """Of a call's rows: type, their number, values, elements from one to the next, bytes of all values, and the shape and strides of a tensor of n, tokens and
+    width where there is something between rows.  What is unknown is the library's to refuse."""
+    dtype, n, tokens, spacing = 1 if desc.in_dtype == DP_BF16 else 0, desc.n, desc.tokens, desc.row_stride or width
+    rows = n * tokens
+    return dtype, rows, width, spacing, rows * width * (2 if dtype else 4), None if spacing == width else ((n, tokens, width), (tokens * spacing, spacing, 1))
+
+
+def _has_rows(t, rows: int, width: int, spacing: int) -> bool:
+    """Whether a tensor's leading dimensions are `rows` rows or more, one every `spacing` elements, its trailing ones `width` values or more of each.  One
+    dimension alone is taken as memory."""
+    shape, strides = t.shape, t.stride()
+    dims = [(size, stride) for size, stride in zip(reversed(shape), reversed(strides)) if size != 1]          # (the stride of a dimension of one means nothing)
+    if len(dims) == 1 and dims[0][1] == 1:
+        return dims[0][0] >= (rows - 1) * spacing + width
+    row, at = 1, 0
+    while at < len(dims) and dims[at][1] == row and (row < width or row * dims[at][0] <= spacing):
+        row *= dims[at][0]
+        at += 1
+    if row < width:
+        return False
+    found = 1
+    while found < rows and at < len(dims) and dims[at][1] == spacing * found and row <= spacing:
+        found *= dims[at][0]
+        at += 1
+    return found >= rows
+
+
+def _token_rows(t, layout, what: str) -> Optional[int]:
+    """Address of [n, tokens] rows, of the descriptor's type and where it says they are (or None)."""
     if t is None or type(t) is int:
         return t
-    if t.nbytes < size or t.dtype is not (_TYPES or _types())[dtype] or not (t.is_cuda or t.is_pinned()):
-        raise DpError(DP_ERR_INVALID_ARG, f"{what} must be {desc.n} x {desc.tokens} rows of {'bfloat16' if dtype == DP_BF16 else 'float32'}, {size} bytes, on the "
-                                          f"device, not {t.dtype} {list(t.shape)} on {t.device}")
+    dtype, rows, width, spacing, size, gaps = layout
+    kind = (_TYPES or _types())[dtype]
+    plain = t.nbytes == size and t.is_contiguous() if gaps is None else t.shape == gaps[0] and t.stride() == gaps[1]
+    if t.dtype is not kind or not (plain or _has_rows(t, rows, width, spacing)) or not (t.is_cuda or t.is_pinned()):
+        raise DpError(DP_ERR_INVALID_ARG, f"{what} must be {rows} rows of {width} {kind} on the device, one every {spacing}, not {t.dtype} {list(t.shape)} of "
+                                          f"strides {list(t.stride())} on {t.device}")
     return t.data_ptr()
-
-
-def _row_bytes(desc, width: int):
-    """(type, bytes) of a call's tensors; an unknown type is the library's to refuse."""
-    dtype = 1 if desc.in_dtype == DP_BF16 else 0
-    return dtype, desc.n * desc.tokens * width * (2 if dtype else 4)
 
 
 # ---- 8-bit activation checkpoints ---------------------------------------------------------------------------------
@@ -610,9 +635,9 @@ def dp_bias_softmax_backward(desc: BiasDesc, probs, dprobs, dscores, g_table, sq
 def dp_layer_norm(desc: NormDesc, x, gamma, beta, y, lengths=None, stream=None):
     """Layer norm (desc.rms: RMS norm) of every token of x [n, tokens, features] into y."""
     f = desc.features
-    rows = _row_bytes(desc, f)
-    _check(load_library().dp_layer_norm(C.byref(desc), _token_rows(x, desc, *rows, "x"), _floats(gamma, f, "gamma"), _floats(beta, f, "beta"),
-                                        _lengths(lengths, desc.n, "lengths"), _token_rows(y, desc, *rows, "y"), _stream(stream)))
+    rows = _row_layout(desc, f)
+    _check(load_library().dp_layer_norm(C.byref(desc), _token_rows(x, rows, "x"), _floats(gamma, f, "gamma"), _floats(beta, f, "beta"),
+                                        _lengths(lengths, desc.n, "lengths"), _token_rows(y, rows, "y"), _stream(stream)))
 
 
 def dp_layer_norm_workspace_bytes(desc: NormDesc) -> int:
@@ -623,9 +648,9 @@ def dp_layer_norm_backward(desc: NormDesc, x, gamma, dy, dx, g_w, g_b, sqnorm, w
                            ws_bytes: Optional[int] = None, stream=None):
     """Gradient of the tokens, and per example the gradients of gamma and beta and their squared norm."""
     f = desc.features
-    rows = _row_bytes(desc, f)
-    _check(load_library().dp_layer_norm_backward(C.byref(desc), _token_rows(x, desc, *rows, "x"), _floats(gamma, f, "gamma"), _token_rows(dy, desc, *rows, "dy"),
-                                                 _lengths(lengths, desc.n, "lengths"), _token_rows(dx, desc, *rows, "dx"), _gradient_rows(g_w, desc.n, f, "g_w"),
+    rows = _row_layout(desc, f)
+    _check(load_library().dp_layer_norm_backward(C.byref(desc), _token_rows(x, rows, "x"), _floats(gamma, f, "gamma"), _token_rows(dy, rows, "dy"),
+                                                 _lengths(lengths, desc.n, "lengths"), _token_rows(dx, rows, "dx"), _gradient_rows(g_w, desc.n, f, "g_w"),
                                                  _gradient_rows(g_b, desc.n, f, "g_b"), g_stride, _floats(sqnorm, desc.n, "sqnorm"), _ptr(ws), _nbytes(ws) if ws_bytes is None else ws_bytes, _stream(stream)))
 
 
@@ -639,8 +664,8 @@ def dp_token_logprobs(desc: LogprobDesc, logits, targets, logprobs, entropy, sta
                       ws_bytes: Optional[int] = None, stream=None):
     """Log probabilities of targets (int32 [n, tokens]) under rows of logits, entropies, statistics for the backward pass, the most likely tokens; any
     of the results may be None."""
-    rows, typed = desc.n * desc.tokens, _row_bytes(desc, desc.vocab)
-    _check(load_library().dp_token_logprobs(C.byref(desc), _token_rows(logits, desc, *typed, "logits"), _lengths(targets, rows, "targets"),
+    rows, layout = desc.n * desc.tokens, _row_layout(desc, desc.vocab)
+    _check(load_library().dp_token_logprobs(C.byref(desc), _token_rows(logits, layout, "logits"), _lengths(targets, rows, "targets"),
                                             _lengths(lengths, desc.n, "lengths"), _floats(logprobs, rows, "logprobs"), _floats(entropy, rows, "entropy"),
                                             _floats(stats, 2 * rows, "stats"), _floats(top_logprobs, rows * desc.top, "top_logprobs"),
                                             _lengths(top_tokens, rows * desc.top, "top_tokens"), _ptr(ws), _nbytes(ws) if ws_bytes is None else ws_bytes,
@@ -651,9 +676,9 @@ def dp_token_logprobs_backward(desc: LogprobDesc, logits, targets, stats, d_logp
                                lengths=None, ws_bytes: Optional[int] = None, stream=None):
     """Gradient of the logits from those of log probabilities and entropies; stats None: worked out in the same call, with the log probabilities
     where there is a place for them."""
-    rows, typed = desc.n * desc.tokens, _row_bytes(desc, desc.vocab)
-    _check(load_library().dp_token_logprobs_backward(C.byref(desc), _token_rows(logits, desc, *typed, "logits"), _lengths(targets, rows, "targets"),
+    rows, layout = desc.n * desc.tokens, _row_layout(desc, desc.vocab)
+    _check(load_library().dp_token_logprobs_backward(C.byref(desc), _token_rows(logits, layout, "logits"), _lengths(targets, rows, "targets"),
                                                      _lengths(lengths, desc.n, "lengths"), _floats(stats, 2 * rows, "stats"), _floats(entropy, rows, "entropy"),
                                                      _floats(d_logprobs, rows, "d_logprobs"), _floats(d_entropy, rows, "d_entropy"),
-                                                     _floats(logprobs, rows, "logprobs"), _token_rows(dlogits, desc, *typed, "dlogits"), _ptr(ws),
+                                                     _floats(logprobs, rows, "logprobs"), _token_rows(dlogits, layout, "dlogits"), _ptr(ws),
                                                      _nbytes(ws) if ws_bytes is None else ws_bytes, _stream(stream)))
