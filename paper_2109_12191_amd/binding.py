@@ -481,12 +481,15 @@ def _floats(t, n: int, what: str) -> Optional[int]:
     return t.data_ptr()
 
 
-def _gradient_rows(t, n: int, width: int, what: str) -> Optional[int]:
-    """Address of n examples' fp32 gradients, rows of `width` at least (or None)."""
+def _gradient_rows(t, n: int, width: int, spacing: int, what: str) -> Optional[int]:
+    """Address of n examples' fp32 gradients of `width` values, one every `spacing` (or None)."""
     if t is None or type(t) is int:
         return t
-    if t.dtype is not (_TYPES or _types())[DP_F32] or t.nbytes < 4 * n * width or not (t.is_cuda or t.is_pinned()):
-        raise DpError(DP_ERR_INVALID_ARG, f"{what} must be {n} rows of {width} float32 on the device, not {t.dtype} {list(t.shape)} on {t.device}")
+    shape = t.shape
+    plain = t.stride() == (spacing, 1) and shape[0] >= n and shape[1] >= width
+    if t.dtype is not (_TYPES or _types())[DP_F32] or not (plain or _has_rows(t, n, width, spacing)) or not (t.is_cuda or t.is_pinned()):
+        raise DpError(DP_ERR_INVALID_ARG, f"{what} must be {n} rows of {width} float32 on the device, one every {spacing}, not {t.dtype} {list(shape)} of strides "
+                                          f"{list(t.stride())} on {t.device}")
     return t.data_ptr()
 
 
@@ -648,10 +651,10 @@ def dp_layer_norm_backward(desc: NormDesc, x, gamma, dy, dx, g_w, g_b, sqnorm, w
                            ws_bytes: Optional[int] = None, stream=None):
     """Gradient of the tokens, and per example the gradients of gamma and beta and their squared norm."""
     f = desc.features
-    rows = _row_layout(desc, f)
+    rows, spacing = _row_layout(desc, f), g_stride or f
     _check(load_library().dp_layer_norm_backward(C.byref(desc), _token_rows(x, rows, "x"), _floats(gamma, f, "gamma"), _token_rows(dy, rows, "dy"),
-                                                 _lengths(lengths, desc.n, "lengths"), _token_rows(dx, rows, "dx"), _gradient_rows(g_w, desc.n, f, "g_w"),
-                                                 _gradient_rows(g_b, desc.n, f, "g_b"), g_stride, _floats(sqnorm, desc.n, "sqnorm"), _ptr(ws), _nbytes(ws) if ws_bytes is None else ws_bytes, _stream(stream)))
+                                                 _lengths(lengths, desc.n, "lengths"), _token_rows(dx, rows, "dx"), _gradient_rows(g_w, desc.n, f, spacing, "g_w"),
+                                                 _gradient_rows(g_b, desc.n, f, spacing, "g_b"), g_stride, _floats(sqnorm, desc.n, "sqnorm"), _ptr(ws), _nbytes(ws) if ws_bytes is None else ws_bytes, _stream(stream)))
 
 
 # ---- log probabilities of tokens -------------------------------------------------------------------------------------

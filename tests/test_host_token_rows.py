@@ -132,3 +132,66 @@ def test_rows_of_one_value(library):
         for call, place in calls_with(t, row_stride, features=1):
             call()
             assert library.calls[-1][1][place] == t.data_ptr()
+
+
+def gradient_calls(t, g_stride, n=N):
+    def call(g_w, g_b):
+        dp.dp_layer_norm_backward(norm(n=n), P, None, P, P, g_w, g_b, P, P, g_stride=g_stride, ws_bytes=1 << 20, stream=0)
+    return [(lambda: call(t, P), 6), (lambda: call(P, t), 7)]
+
+
+def grads(*shape):
+    return make(*shape, dtype=torch.float32)
+
+
+GOOD_GRADIENTS = {
+    "packed": lambda: (grads(N, WIDTH), 0),
+    "packed, said so": lambda: (grads(N, WIDTH), WIDTH),
+    "with room behind each": lambda: (grads(N, WIDTH + 8), WIDTH + 8),
+    "left columns": lambda: (grads(N, 2 * WIDTH)[:, :WIDTH], 2 * WIDTH),
+    "right columns": lambda: (grads(N, 2 * WIDTH)[:, WIDTH:], 2 * WIDTH),
+    "of more examples": lambda: (grads(N + 1, WIDTH), 0),
+    "memory": lambda: (grads(N * WIDTH), 0),
+    "memory with gaps": lambda: (grads((N - 1) * 64 + WIDTH), 64),
+    "one of two for each example": lambda: (grads(N, 2, WIDTH)[:, 1], 2 * WIDTH),
+    "scale and shift of each example": lambda: (grads(N, 2, WIDTH), 2 * WIDTH),
+}
+
+
+@pytest.mark.parametrize("case", GOOD_GRADIENTS)
+def test_gradients_where_g_stride_says(library, case):
+    t, g_stride = GOOD_GRADIENTS[case]()
+    for call, place in gradient_calls(t, g_stride):
+        call()
+        assert library.calls[-1][1][place] == t.data_ptr()
+
+
+BAD_GRADIENTS = {
+    "packed, said to have room behind each": lambda: (grads(N, WIDTH), WIDTH + 8),
+    "right columns, said to be left ones": lambda: (grads(N, WIDTH + 8)[:, 12:], WIDTH + 8),
+    "with room behind each, said to be packed": lambda: (grads(N, WIDTH + 8), 0),
+    "memory that ends in the last row": lambda: (grads((N - 1) * 64 + WIDTH - 1), 64),
+    "one example for all": lambda: (grads(1, WIDTH).expand(N, WIDTH), 0),
+    "features first": lambda: (grads(WIDTH, N).t(), 0),
+    "fewer examples": lambda: (grads(N - 1, 2 * WIDTH), 2 * WIDTH),
+    "one value": lambda: (grads(), 0),
+    "another type": lambda: (make(N, WIDTH), 0),
+}
+
+
+@pytest.mark.parametrize("case", BAD_GRADIENTS)
+def test_gradients_elsewhere_are_refused(library, case):
+    t, g_stride = BAD_GRADIENTS[case]()
+    for call, _ in gradient_calls(t, g_stride):
+        with pytest.raises(dp.DpError) as raised:
+            call()
+        assert raised.value.status == B.DP_ERR_INVALID_ARG
+    assert not library.calls
+
+
+def test_a_single_example_has_no_spacing(library):
+    for t in (grads(1, WIDTH), grads(WIDTH), grads(2, WIDTH)[1:]):
+        for g_stride in (0, WIDTH, WIDTH + 64):
+            for call, place in gradient_calls(t, g_stride, n=1):
+                call()
+                assert library.calls[-1][1][place] == t.data_ptr()
