@@ -44,12 +44,18 @@ class _Recorded(torch.autograd.Function):
 class PrivateAttention:
     """Weights [q; k; v] (three of [width, width], one after the other), the output's [width, width] and the bias table [buckets, heads], fp32 in
     one vector `theta`; activations are bf16.  Tokens beyond an example's length (int32 `lengths`, None: all there) count for nothing,
-    but the activations and gradients there have to be finite."""
+    but the activations and gradients there have to be finite.
+
+    The noise of a tensor is a function of seed, step and its number, from first_tensor on: blocks of one model and one seed need numbers of their own (the next block's
+    first_tensor is this one's next_tensor), or two tensors get the same noise, which a difference takes out again."""
 
     def __init__(self, n: int, tokens: int, width: int, heads: int, clip_c: float, sigma: float, total_batch: int, lr: float = 0.0, momentum: float = 0.0,
-                 seed: int = 0, buckets: int = 32, max_distance: int = 128, bidirectional: bool = True, causal: bool = False, device: str = "cuda"):
+                 seed: int = 0, buckets: int = 32, max_distance: int = 128, bidirectional: bool = True, causal: bool = False, device: str = "cuda",
+                 first_tensor: int = 0):
         if width % heads or width // heads % 2:
             raise ValueError(f"{width} features cannot be shared by {heads} heads")
+        if not 0 <= first_tensor < (1 << 32) - 5:
+            raise ValueError(f"first_tensor {first_tensor} and those behind it are not numbers of 32 bits")
         self.n, self.tokens, self.width, self.heads, self.head = n, tokens, width, heads, width // heads
         self.clip_c, self.sigma, self.total_batch, self.lr, self.momentum, self.seed = clip_c, sigma, total_batch, lr, momentum, seed
         self.buckets, self.device = buckets, device
@@ -59,7 +65,8 @@ class PrivateAttention:
             begins.append(begins[-1] + (size + 3) // 4 * 4)
         f32 = dict(dtype=torch.float32, device=device)
         self.theta, self.acc, self.velocity = torch.zeros(begins[-1], **f32), torch.zeros(begins[-1], **f32), torch.zeros(begins[-1], **f32)
-        self.tensors = B.TensorTable(begins[:-1], sizes, range(5))
+        self.tensors = B.TensorTable(begins[:-1], sizes, range(first_tensor, first_tensor + 5))
+        self.next_tensor = first_tensor + 5               # the first number that is none of this block's
         view = lambda flat: [flat[b:b + s].view(*shape) for b, s, shape in zip(begins, sizes, [(width, width)] * 4 + [(buckets, heads)])]
         self.weights, self.sums = view(self.theta), view(self.acc)
         gen = torch.Generator(device=device).manual_seed(seed)

@@ -22,6 +22,9 @@ import torch
 from . import binding as B
 
 
+FIRST_TENSOR = 1 << 16               # a model's last block: behind the tensors of the blocks before it, which count theirs from zero
+
+
 class _Recorded(torch.autograd.Function):
     """A forward pass that autograd knows of as a whole."""
 
@@ -42,10 +45,16 @@ class _Recorded(torch.autograd.Function):
 class PrivateReadout:
     """Scale [width] and shift [width] of the normalisation (rms: no shift, no mean) and the projection [vocab, width], fp32 in one vector `theta`;
     activations and logits are bf16, log probabilities fp32.  Tokens beyond an example's length (int32 `lengths`, None: all there) count for nothing,
-    whatever they hold; tokens whose target is none of 0 .. vocab - 1 are not scored."""
+    whatever they hold; tokens whose target is none of 0 .. vocab - 1 are not scored.
+
+    The noise of a tensor is a function of seed, step and its number, from first_tensor on: blocks of one model and one seed need numbers of their own, or two tensors get
+    the same noise, which a difference takes out again.  A read-out's own begin far behind those of the blocks before it; a model of several gives each its first_tensor."""
 
     def __init__(self, n: int, tokens: int, width: int, vocab: int, clip_c: float, sigma: float, total_batch: int, lr: float = 0.0, momentum: float = 0.0,
-                 seed: int = 0, rms: bool = False, eps: float = 1e-5, scale: float = 1.0, device: str = "cuda"):
+                 seed: int = 0, rms: bool = False, eps: float = 1e-5, scale: float = 1.0, device: str = "cuda",
+                 first_tensor: int = FIRST_TENSOR):
+        if not 0 <= first_tensor < (1 << 32) - 3:
+            raise ValueError(f"first_tensor {first_tensor} and those behind it are not numbers of 32 bits")
         self.n, self.tokens, self.width, self.vocab, self.rms = n, tokens, width, vocab, rms
         self.clip_c, self.sigma, self.total_batch, self.lr, self.momentum, self.seed = clip_c, sigma, total_batch, lr, momentum, seed
         self.device = device
@@ -56,7 +65,8 @@ class PrivateReadout:
         f32 = dict(dtype=torch.float32, device=device)
         self.theta, self.acc, self.velocity = torch.zeros(total, **f32), torch.zeros(total, **f32), torch.zeros(total, **f32)
         sizes = [s[0] if len(s) == 1 else s[0] * s[1] for s in shapes]
-        self.tensors = B.TensorTable(begins, sizes, range(len(begins)))
+        self.tensors = B.TensorTable(begins, sizes, range(first_tensor, first_tensor + len(begins)))
+        self.next_tensor = first_tensor + len(begins)     # the first number that is none of this block's
         view = lambda flat: [flat[b:b + size].view(*shape) for b, size, shape in zip(begins, sizes, shapes)]  # noqa: E731
         self.weights, self.sums = view(self.theta), view(self.acc)
         self.weights[0].fill_(1.0)

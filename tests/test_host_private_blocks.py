@@ -1,0 +1,59 @@
+"""CPU-only checks of the private blocks' optimiser step: which noise their tensors get."""
+import numpy as np
+import pytest
+import torch
+
+import oracle
+import paper_2109_12191_amd as dp
+from paper_2109_12191_amd import binding as B
+
+N, TOKENS, WIDTH, VOCAB = 2, 3, 64, 100
+
+
+def attention(**more):
+    return dp.PrivateAttention(N, TOKENS, WIDTH, 4, **{**dict(clip_c=1.0, sigma=1.0, total_batch=N, device="cpu"), **more})
+
+
+def readout(**more):
+    return dp.PrivateReadout(N, TOKENS, WIDTH, VOCAB, **{**dict(clip_c=1.0, sigma=1.0, total_batch=N, device="cpu"), **more})
+
+
+@pytest.fixture
+def noise(monkeypatch):
+    """What blocks ask for in a step: a list of (tensor ids, sigma, bound, examples, seed, step)."""
+    asked = []
+
+    def stand_in(acc, out, table, sigma, clip_total, total_batch, seed, step=0, **more):
+        asked.append((list(table.tensor_id), sigma, clip_total, total_batch, seed, step))
+    monkeypatch.setattr(B, "dp_add_noise_finalize_flat", stand_in)
+    return asked
+
+
+@pytest.mark.parametrize("rms", [False, True])
+def test_blocks_of_a_model_have_noise_of_their_own(noise, rms):
+    """As they are made without another word: an attention block, a second one behind it, a read-out."""
+    first = attention()
+    blocks = [first, attention(first_tensor=first.next_tensor), readout(rms=rms)]
+    for block in blocks:
+        block.step(7)
+    ids = [(seed, step, i) for table, _, _, _, seed, step in noise for i in table]
+    assert len(ids) == 5 + 5 + (2 if rms else 3) == len(set(ids))
+    z = np.stack([oracle.noise_normal(seed, step, i, 256) for seed, step, i in ids])
+    # 256 independent normals: a product of two has a mean of 0 +- 1/16, and 0.4 is beyond six times that
+    corr = z @ z.T / 256
+    assert (np.abs(corr - np.diag(np.diag(corr))) < 0.4).all()
+
+
+def test_numbers_of_tensors_are_the_callers_to_choose(noise):
+    a, r = attention(first_tensor=12), readout(first_tensor=30)
+    a.step(0)
+    r.step(0)
+    assert noise[0][0] == [12, 13, 14, 15, 16] and a.next_tensor == 17
+    assert noise[1][0] == [30, 31, 32] and r.next_tensor == 33
+    b = attention()
+    b.step(0)
+    assert noise[2][0] == [0, 1, 2, 3, 4]                # as ever
+    for bad in (-1, (1 << 32) - 1, 1 << 40):
+        for make in (attention, readout):
+            with pytest.raises(ValueError, match="first_tensor"):
+                make(first_tensor=bad)
