@@ -47,16 +47,23 @@ class PrivateAttention:
     but the activations and gradients there have to be finite.
 
     The noise of a tensor is a function of seed, step and its number, from first_tensor on: blocks of one model and one seed need numbers of their own (the next block's
-    first_tensor is this one's next_tensor), or two tensors get the same noise, which a difference takes out again."""
+    first_tensor is this one's next_tensor), or two tensors get the same noise, which a difference takes out again.
+
+    clip_c bounds what an example adds to this block.  A model of several blocks releases all their updates, so an example's part in what is released is bounded by the square
+    root of the sum of the blocks' clip_c squared (dp_group_clip_bounds shares a bound out): that is every block's clip_total, which its noise has sigma times of.  None:
+    the block is the whole model."""
 
     def __init__(self, n: int, tokens: int, width: int, heads: int, clip_c: float, sigma: float, total_batch: int, lr: float = 0.0, momentum: float = 0.0,
                  seed: int = 0, buckets: int = 32, max_distance: int = 128, bidirectional: bool = True, causal: bool = False, device: str = "cuda",
-                 first_tensor: int = 0):
+                 first_tensor: int = 0, clip_total: float | None = None):
         if width % heads or width // heads % 2:
             raise ValueError(f"{width} features cannot be shared by {heads} heads")
         if not 0 <= first_tensor < (1 << 32) - 5:
             raise ValueError(f"first_tensor {first_tensor} and those behind it are not numbers of 32 bits")
         self.n, self.tokens, self.width, self.heads, self.head = n, tokens, width, heads, width // heads
+        if clip_total is not None and not clip_total >= clip_c * (1.0 - 2.0 ** -23):          # (bounds are fp32 to the library)
+            raise ValueError(f"clip_total {clip_total} does not cover this block's own clip_c {clip_c}")
+        self.clip_total = clip_total
         self.clip_c, self.sigma, self.total_batch, self.lr, self.momentum, self.seed = clip_c, sigma, total_batch, lr, momentum, seed
         self.buckets, self.device = buckets, device
         sizes = [width * width] * 4 + [buckets * heads]
@@ -172,7 +179,8 @@ class PrivateAttention:
 
     def step(self, index: int):
         """The optimiser step after total_batch examples: noise, mean, update; the next one's sums begin at zero."""
-        B.dp_add_noise_finalize_flat(self.acc, None, self.tensors, self.sigma, self.clip_c, self.total_batch, self.seed, index, theta=self.theta,
+        bound = self.clip_c if self.clip_total is None else self.clip_total
+        B.dp_add_noise_finalize_flat(self.acc, None, self.tensors, self.sigma, bound, self.total_batch, self.seed, index, theta=self.theta,
                                      velocity=self.velocity, lr=self.lr, momentum=self.momentum)
         self.acc.zero_()
         self._round()

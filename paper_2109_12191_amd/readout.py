@@ -48,14 +48,21 @@ class PrivateReadout:
     whatever they hold; tokens whose target is none of 0 .. vocab - 1 are not scored.
 
     The noise of a tensor is a function of seed, step and its number, from first_tensor on: blocks of one model and one seed need numbers of their own, or two tensors get
-    the same noise, which a difference takes out again.  A read-out's own begin far behind those of the blocks before it; a model of several gives each its first_tensor."""
+    the same noise, which a difference takes out again.  A read-out's own begin far behind those of the blocks before it; a model of several gives each its first_tensor.
+
+    clip_c bounds what an example adds to this block.  A model of several blocks releases all their updates, so an example's part in what is released is bounded by the square
+    root of the sum of the blocks' clip_c squared (dp_group_clip_bounds shares a bound out): that is every block's clip_total, which its noise has sigma times of.  None:
+    the block is the whole model."""
 
     def __init__(self, n: int, tokens: int, width: int, vocab: int, clip_c: float, sigma: float, total_batch: int, lr: float = 0.0, momentum: float = 0.0,
                  seed: int = 0, rms: bool = False, eps: float = 1e-5, scale: float = 1.0, device: str = "cuda",
-                 first_tensor: int = FIRST_TENSOR):
+                 first_tensor: int = FIRST_TENSOR, clip_total: float | None = None):
         if not 0 <= first_tensor < (1 << 32) - 3:
             raise ValueError(f"first_tensor {first_tensor} and those behind it are not numbers of 32 bits")
         self.n, self.tokens, self.width, self.vocab, self.rms = n, tokens, width, vocab, rms
+        if clip_total is not None and not clip_total >= clip_c * (1.0 - 2.0 ** -23):          # (bounds are fp32 to the library)
+            raise ValueError(f"clip_total {clip_total} does not cover this block's own clip_c {clip_c}")
+        self.clip_total = clip_total
         self.clip_c, self.sigma, self.total_batch, self.lr, self.momentum, self.seed = clip_c, sigma, total_batch, lr, momentum, seed
         self.device = device
         affine = (width + 3) // 4 * 4
@@ -182,7 +189,8 @@ class PrivateReadout:
 
     def step(self, index: int):
         """The optimiser step after total_batch examples: noise, mean, update; the next one's sums begin at zero."""
-        B.dp_add_noise_finalize_flat(self.acc, None, self.tensors, self.sigma, self.clip_c, self.total_batch, self.seed, index, theta=self.theta,
+        bound = self.clip_c if self.clip_total is None else self.clip_total
+        B.dp_add_noise_finalize_flat(self.acc, None, self.tensors, self.sigma, bound, self.total_batch, self.seed, index, theta=self.theta,
                                      velocity=self.velocity, lr=self.lr, momentum=self.momentum)
         self.acc.zero_()
         self._round()

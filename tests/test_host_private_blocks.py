@@ -57,3 +57,18 @@ def test_numbers_of_tensors_are_the_callers_to_choose(noise):
         for make in (attention, readout):
             with pytest.raises(ValueError, match="first_tensor"):
                 make(first_tensor=bad)
+
+
+def test_the_noise_covers_the_whole_model(noise):
+    """Blocks that clip their own parts of an example's gradient: each gets the noise of the bound on the whole of it."""
+    (each, _), whole = B.dp_group_clip_bounds(0.7, 2)
+    for block in (attention(clip_c=each, clip_total=whole), readout(clip_c=each, clip_total=whole)):
+        block.step(1)
+    assert [asked[2] for asked in noise] == [whole, whole] and whole == pytest.approx(0.7) and each == pytest.approx(0.7 / 2 ** 0.5)
+    for make in (attention, readout):
+        make(clip_c=0.7, clip_total=B.dp_group_clip_bounds(0.7, 1)[1])          # one block's whole, of fp32
+        make(clip_c=0.5).step(1)
+        assert noise[-1][2] == 0.5                       # alone: as ever
+        for bad in (0.4999, float("nan")):
+            with pytest.raises(ValueError, match="clip_total"):
+                make(clip_c=0.5, clip_total=bad)
