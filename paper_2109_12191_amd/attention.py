@@ -13,7 +13,8 @@ An example's gradient is that of its checkpoints' values, for the norm and for t
 not matter to the bound: no more than clip_c of an example gets into the sum, to within the norms' own rounding (dp_checkpoint_example_grad).
 
 forward's result carries a graph where its input requires a gradient: autograd's pass over it is `backward`, with the clipped sums of the weights that
-belong to it, and gives the input's gradient.  Elsewhere `backward` is called.  The block holds the values of one forward pass, for one such pass back.
+belong to it, and gives the input's gradient.  Elsewhere `backward` is called.  The block holds the values of one forward pass, its lengths among
+them, for one such pass back.
 
 examples/private_attention.py trains one on synthetic data.
 """
@@ -128,7 +129,7 @@ class PrivateAttention:
 
     def _forward(self, x, lengths):
         self.passes += 1
-        self.lengths = lengths
+        self.lengths = None if lengths is None else lengths.clone()
         B.dp_checkpoint_write(x, *self.inputs)
         self.q, self.k, self.v = (self._heads(part) for part in (x @ self.qkv_weight.t()).chunk(3, dim=-1))
         scores = self.q @ self.k.transpose(2, 3).contiguous()

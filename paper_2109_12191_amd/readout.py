@@ -13,7 +13,8 @@ derivatives that a backward pass starts from are those of a sum over examples, n
 
 logprobs' result carries a graph where its input requires a gradient: autograd's pass over it is `backward`, with the clipped sums of the parameters that
 belong to it, and gives the input's gradient.  Elsewhere `backward` is called, or `train` for both passes at once, which is also what to record into a graph.  The
-block holds the values of one forward pass, for one such pass back, and the input itself, which has to stay as it is until then.
+block holds the values of one forward pass, its targets and lengths among them, for one such pass back, and the input itself, which has to stay as it is until
+then.
 """
 from __future__ import annotations
 
@@ -128,7 +129,7 @@ class PrivateReadout:
 
     def _logprobs(self, x, targets, lengths):
         self.passes += 1
-        self.x, self.targets, self.lengths = x.detach(), targets, lengths
+        self.x, self.targets, self.lengths = x.detach(), targets.clone(), None if lengths is None else lengths.clone()
         self.logits = self._logits(x, lengths)
         f32 = dict(dtype=torch.float32, device=self.theta.device)
         result, self.stats = torch.empty((self.n, self.tokens), **f32), torch.empty((self.n, self.tokens, 2), **f32)
