@@ -14,7 +14,7 @@ derivatives that a backward pass starts from are those of a sum over examples, n
 logprobs' result carries a graph where its input requires a gradient: autograd's pass over it is `backward`, with the clipped sums of the parameters that
 belong to it, and gives the input's gradient.  Elsewhere `backward` is called, or `train` for both passes at once, which is also what to record into a graph.  The
 block holds the values of one forward pass, its targets and lengths among them, for one such pass back, and the input itself, which has to stay as it is until
-then.
+then (autograd's pass refuses one that was written to).
 """
 from __future__ import annotations
 
@@ -33,6 +33,7 @@ class _Recorded(torch.autograd.Function):
     def forward(ctx, x, block, targets, lengths):
         y = block._logprobs(x, targets, lengths)
         ctx.block, ctx.passes = block, block.passes
+        ctx.save_for_backward(x)
         return y
 
     @staticmethod
@@ -40,6 +41,7 @@ class _Recorded(torch.autograd.Function):
     def backward(ctx, d_logprobs):
         if ctx.block.passes != ctx.passes:
             raise RuntimeError("the block no longer holds this forward pass: there was another one, or a pass back over it")
+        ctx.saved_tensors                                  # (raises where x was written to)
         return ctx.block.backward(d_logprobs), None, None, None
 
 

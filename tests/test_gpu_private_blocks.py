@@ -55,3 +55,17 @@ def test_a_pass_back_is_over_the_targets_and_lengths_of_its_forward_pass(which, 
     kept, filled = passes(False), passes(True)
     assert float(kept[0].abs().max()) > 0.0 and float(kept[1].abs().max()) > 0.0
     assert torch.equal(kept[0], filled[0]) and torch.equal(kept[1], filled[1])
+
+
+def test_an_input_that_was_written_to_is_refused():
+    """The read-out holds its input as it is, without a copy: autograd's pass back says so."""
+    n, tokens, width, vocab = 2, 5, 64, 100
+    block = dp.PrivateReadout(n, tokens, width, vocab, clip_c=0.5, sigma=0.0, total_batch=n, device="cuda:0")
+    leaf = torch.randn((n, tokens, width), device="cuda:0").to(torch.bfloat16).requires_grad_()
+    x = leaf * 1.0
+    y = block.logprobs(x, torch.zeros((n, tokens), dtype=torch.int32, device="cuda:0"))
+    with torch.no_grad():
+        x.add_(1.0)
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        y.sum().backward()
+    assert float(block.acc.abs().max()) == 0.0
