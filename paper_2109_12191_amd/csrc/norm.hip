@@ -571,7 +571,7 @@ __global__ void __launch_bounds__(THREADS) norm_join_kernel(const NormJoinArgs a
 constexpr int NORM_HELD = 16384;       // features that a workgroup of sixteen waves holds in registers
 constexpr size_t JOIN_WHOLE = 16384;   // quads of sums that one workgroup adds up
 
-// Threads that share a row: as many as have a run of eight, a wave for up to 1024 features (forward 2048), four for up to 8192.
+// Threads that share a row: as many as have a run of eight, a wave for up to 1024 features (forward 2048), four for up to 4096 (forward 8192); then eight (forward sixteen).
 int norm_lanes(int features, bool backward)
 {
     if (features <= 64) return 8;

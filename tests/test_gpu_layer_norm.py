@@ -408,3 +408,21 @@ def test_offsets_beyond_2_to_the_32(features, tokens, stride):
     # the tokens before them are zeros, with gradients of zeros: the sums are the same numbers in another order
     for a, b in zip(whole[2:], alone[2:]):
         assert bool(((a - b).abs() <= 200 * U * last * b.abs().amax()).all())
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("features", [41, 129, 300, 513, 1025, 1500, 2047, 3001, 6001, 12001, 17001])
+def test_gradients_of_rows_of_one_value(features, dtype):
+    """Widths of every backward kernel, no multiples of four among them, packed gradients: bounds as of test_rows_of_one_value."""
+    x = torch.tensor([1e-30, 1.0, -777.7, 1e12, 1e18, 3e-8], device="cuda:0")[None, :, None].expand(2, 6, features).contiguous().to(dtype)
+    _, dy, gamma, _ = data(2, 6, features, 1)
+    dy = dy.to(dtype)
+    desc = desc_of(x)
+    ws = torch.empty(dp.dp_layer_norm_workspace_bytes(desc), dtype=torch.uint8, device="cuda:0")
+    dx, g_w, g_b = torch.empty_like(x), torch.empty((2, features), device="cuda:0"), torch.empty((2, features), device="cuda:0")
+    dp.dp_layer_norm_backward(desc, x, gamma, dy, dx, g_w, g_b, None, ws)
+    a = dy.double() * gamma.double()
+    want = (a - a.mean(2, keepdim=True)) / EPS ** 0.5
+    assert bool(((dx.double() - want).abs() <= HALF[dtype] * want.abs() + 1e-3 * (1.0 + a.abs().amax(2, keepdim=True)) / EPS ** 0.5).all())
+    assert bool((g_w.double().abs() <= 1e-4 * dy.double().abs().sum(1)).all())
+    close(g_b, dy.double().sum(1), (x.shape[1] + 32) * U * dy.double().abs().sum(1), "g_b")
