@@ -511,8 +511,8 @@ typedef struct dp_norm_desc {
 
 /* gamma, beta [device] [features], or NULL: ones, zeros.  x, y [device], aligned to their element; y may be x.
  * lengths [device] [n] int32 tokens of each example (taken as 0 .. tokens), or NULL: all.  Rows of y beyond them are zeros, and what lies there
- * in x is not used, whatever it is.  A row with a NaN or an infinity is NaN, and so is one whose sums leave fp32's range (squares of deviations that add
- * up to less than 10^38 do not).                                                                                */
+ * in x is not used, whatever it is.  A row with a NaN or an infinity is NaN, and so is one whose sums leave fp32's range (those of values below 10^18 whose
+ * squares of deviations, RMS: whose squares, add up to less than 10^38 do not).                                 */
 dp_status dp_layer_norm(const dp_norm_desc *desc /*[host]*/, const void *x, const float *gamma, const float *beta, const int32_t *lengths, void *y,
                         dp_stream stream);
 
@@ -545,7 +545,7 @@ typedef struct dp_logprob_desc {
  * targets      [device] [n, tokens] int32; needed for logprobs.
  * lengths      [device] [n] int32 tokens of each example (taken as 0 .. tokens), or NULL: all.  Rows beyond have logprob, entropy, stats and
  *              top_logprobs 0 and top_tokens -1, and what lies there in logits is not used, whatever it is.
- * A logit of -inf has p = 0 and logp = -inf.  A row of nothing else has logp = -inf, entropy 0, stats (0, inf) and no alternatives.  A row with a NaN or
+ * A logit of -inf has p = 0 and logp = -inf, and so has one that is below the row's largest by more than fp32 holds.  A row of nothing else has logp = -inf, entropy 0, stats (0, inf) and no alternatives.  A row with a NaN or
  * +inf has NaN for all of logprob, entropy, stats and top_logprobs, and top_tokens -1.
  * logits [device] in_dtype, aligned to their element.  stats: aligned to 8 bytes.  ws: dp_token_logprobs_workspace_bytes(desc), which may be 0. */
 size_t dp_token_logprobs_workspace_bytes(const dp_logprob_desc *desc /*[host]*/);

@@ -40,7 +40,8 @@ struct LogprobArgs {
 // Words of a row's partial results, whole 16 bytes: they are written and read by those.
 __host__ __device__ constexpr size_t part_words(int splits, int top) { return ((size_t)splits * (4 + 2 * top) + 3) & ~(size_t)3; }
 
-// e^x, x at most 0
+// e^x, x at most 0: the hardware's 2^x of a product rounded to 32 bits, off by a share |x| 2^-24 and an ulp or two.  In a row's sum, whose largest term is 1, that
+// is |x| e^x 2^-24 of a term, less than half of 2^-24; a derivative p is off by the share |logp| 2^-24.  Splitting the product would cost two operations a logit.
 __device__ __forceinline__ float exp_of(float x) { return __builtin_amdgcn_exp2f(x * 1.44269504088896340736f); }
 
 // What has been seen of a row: the largest logit, and over all the sums of exp(scale (x - largest)) and of that times its exponent.  No logit above -inf: s is 0.

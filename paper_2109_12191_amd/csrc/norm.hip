@@ -610,7 +610,7 @@ NormArgs norm_args(const NormGeo &g, bool backward)
         if (all >= 128 * least * at_once) each = std::max(each, least);
         // Examples that one workgroup is soon done with have one, and need no launch to join its sums (us, joined and not: 1000 x 3 tokens of 100
         // features 12.0 and 4.6, 300 x 10 of 768 14.0 and 10.2, 150 x 5 of 768 9.3 and 7.2, 300 x 20 of 4096 in fp32 88.7 and 85.0; but 150 x 40 of 768
-        // 15.1 and 16.8, 8 x 16 of 768 8.1 and 9.1, 300 x 60 of 2048 62 and 92).
+        // 15.1 and 16.8, 8 x 16 of 768 8.1 and 9.1, 300 x 60 of 2048 62 and 92; nothing was measured between 150 and 300 examples).
         const long long turns = (g.tokens + at_once - 1) / at_once;
         if (turns <= (g.n >= 256 ? 20 : 3)) each = turns;
         a.rows = (int)std::min(each * at_once, (long long)(g.tokens + at_once - 1) / at_once * at_once);
