@@ -545,8 +545,9 @@ typedef struct dp_logprob_desc {
  * targets      [device] [n, tokens] int32; needed for logprobs.
  * lengths      [device] [n] int32 tokens of each example (taken as 0 .. tokens), or NULL: all.  Rows beyond have logprob, entropy, stats and
  *              top_logprobs 0 and top_tokens -1, and what lies there in logits is not used, whatever it is.
- * A logit of -inf has p = 0 and logp = -inf, and so has one that is below the row's largest by more than fp32 holds.  A row of nothing else has logp = -inf, entropy 0, stats (0, inf) and no alternatives.  A row with a NaN or
- * +inf has NaN for all of logprob, entropy, stats and top_logprobs, and top_tokens -1.
+ * A logit of -inf has p = 0 and logp = -inf, and so has one that is below the row's largest by more than fp32 holds.  A row of nothing but -inf has
+ * logp = -inf, entropy 0, stats (0, inf) and no alternatives.  A row with a NaN or +inf has NaN for all of logprob, entropy, stats and top_logprobs, and
+ * top_tokens -1.
  * logits [device] in_dtype, aligned to their element.  stats: aligned to 8 bytes.  ws: dp_token_logprobs_workspace_bytes(desc), which may be 0. */
 size_t dp_token_logprobs_workspace_bytes(const dp_logprob_desc *desc /*[host]*/);
 dp_status dp_token_logprobs(const dp_logprob_desc *desc /*[host]*/, const void *logits, const int32_t *targets, const int32_t *lengths,
